@@ -95,7 +95,7 @@ typedef enum {
                            (the comparison baseline of Section 4): W <- (1 - lr wd) W
                            - lr rho sqrt(max(m, n)) U, no equilibration. Every entry must
                            be MEQ_KIND_HIDDEN (that baseline updates the others with
-                           AdamW, which this library does not provide). */
+                           AdamW: a meq_adamw state of their own). */
 } meq_update_rule;
 
 /* Parameter type, selecting the branch of Algorithm 1 applied to it. */
@@ -185,9 +185,10 @@ meq_status meq_sync(meq_state* st);
 meq_status meq_free(meq_state* st);
 
 /* Human-readable text of the last error of st; with st NULL, of the last
- * failed call made without a state (meq_init_state[_kinds],
- * meq_state_bytes[_kinds], meq_ns_cv_trajectory, meq_row_col_stats_noalloc).
- * Valid until the next such call. */
+ * failed call that this thread made without a state (meq_init_state[_kinds],
+ * meq_state_bytes[_kinds], meq_ns_cv_trajectory, meq_row_col_stats_noalloc,
+ * meq_adamw_init, meq_adamw_state_bytes, the loss calls).
+ * Valid until its next such call. */
 const char* meq_last_error(const meq_state* st);
 const char* meq_status_string(meq_status s);
 
@@ -328,6 +329,90 @@ meq_status meq_debug_wait_selftest(meq_state* st, float timeout_ms);
 meq_status meq_row_col_stats_noalloc(const float* U, int64_t rows, int64_t cols, float eps,
                                      float tie_atol, float* r, float* c, double* gammas,
                                      int* direction, void* cuda_stream);
+
+/* ---- AdamW over many tensors ----------------------------------------------
+ * AdamW for what MeqMuon does not step (embedding, head, norm weights under
+ * the comparison rule of Eq. (6)) or for a whole model. For every element of
+ * entry i at step t, with g' = s g:
+ *
+ *   m <- beta1 m + (1 - beta1) g'         v <- beta2 v + (1 - beta2) g'^2
+ *   p <- (1 - lr wd decay_i) p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * in fp32, whatever the types of p and g (16-bit gradients are widened, a bf16
+ * parameter is rounded to nearest once, at the end). One launch per 256
+ * entries; no host synchronisation and no copy, so a step can be captured into
+ * a CUDA graph (the scalars and pointers of the call are then fixed).
+ *
+ * The moments are fp32, or 8-bit codes with one fp32 scale per 256 consecutive
+ * elements for each of m and r = sqrt(v), the largest |m| and r among them:
+ * m = S_m sign(q) (q / 127)^2 with q in -127..127, r = S_r (q / 255)^2 with q in
+ * 0..255, rounded to the nearest code (r > 0 never to 0). The update of a step
+ * uses the moments as computed, before they are rounded. A block with a
+ * non-finite moment has a NaN scale; one whose largest value is below 2^-126 is
+ * held as zero. Entries are independent: what an entry becomes does not depend
+ * on the others of the list. Each entry's moments start at a multiple of 256
+ * elements of the state's arrays, in the order of the list.
+ *
+ * Pointers need the alignment of their element type only; 16-byte aligned
+ * fp32 tensors (8-byte aligned 16-bit ones) move in wide accesses. */
+typedef enum { MEQ_F32 = 0, MEQ_BF16 = 1, MEQ_F16 = 2 } meq_dtype;
+
+typedef struct {
+  double beta1, beta2; /* 0.9, 0.999; in [0, 1) */
+  double eps;          /* 1e-8; > 0 */
+  int state_bits;      /* 32 (default) or 8 */
+  int param_type;      /* MEQ_F32 (default) or MEQ_BF16 */
+  int grad_type;       /* a meq_dtype; default MEQ_F32 */
+} meq_adamw_options;
+
+typedef struct meq_adamw meq_adamw; /* opaque */
+
+void meq_adamw_default_options(meq_adamw_options* opt);
+/* Bytes of the moments (with their scales) and of everything else the state
+ * would allocate, computed on the host. Either output may be NULL. */
+meq_status meq_adamw_state_bytes(const meq_shape* shapes, int n, const meq_adamw_options* opt,
+                                 size_t* persistent_bytes, size_t* workspace_bytes);
+/* State for n entries on the current device, moments and step count zero.
+ * decay[i] >= 0 multiplies the weight decay of entry i (NULL: 1 for all; 0 for
+ * norm weights and biases); opt may be NULL. Shapes have meq_init_state's
+ * limits; only their element counts matter. */
+meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, const meq_adamw_options* opt,
+                          void* cuda_stream, meq_adamw** out);
+/* out[0] = the Euclidean norm of all gradients together, out[1] = the
+ * coefficient that brings it to at most max_norm (1 if it is there; NaN if the
+ * norm is not finite in fp32). out: device, two floats. max_norm > 0, may be
+ * infinite. Sums of squares: fp32 per thread, then double, in a fixed order. */
+meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float max_norm, float* out, void* cuda_stream);
+/* One step. params (updated in place) and grads: device, contiguous, of the
+ * state's types. copies: NULL, or per entry a device bf16 tensor of its size
+ * that receives the updated parameter rounded to nearest. grad_scale: NULL
+ * (s = 1), or a device float s: a clipping coefficient (out + 1 of
+ * meq_adamw_grad_norm), the inverse of a loss scale, or both. If s is not
+ * finite the step is skipped on the device: parameters, moments and step count
+ * stay as they are, and meq_adamw_sync says so. */
+meq_status meq_adamw_step(void* const* params, const void* const* grads, void* const* copies, meq_adamw* st, float lr,
+                          float weight_decay, const float* grad_scale, void* cuda_stream);
+/* The state's own arrays (device), valid until meq_adamw_free, to checkpoint
+ * and resume exactly: m and v (fp32), or the codes of m (int8) and r (uint8)
+ * with their scales (else NULL); *elements = their length, entries padded to
+ * multiples of 256 (scales: a 256th of it). The padding holds zeros and has to.
+ * Any output may be NULL. */
+meq_status meq_adamw_state_ptrs(meq_adamw* st, void** m, void** v, float** m_scale, float** v_scale, int64_t* elements);
+/* The values of m and v, whichever way they are held, into device fp32 arrays
+ * of *elements each, laid out as the state's (16-byte aligned; either may be
+ * NULL). */
+meq_status meq_adamw_read_values(meq_adamw* st, float* m, float* v, void* cuda_stream);
+/* Number of steps done (synchronises the state's last stream), and its
+ * overwriting, to resume. Skipped steps do not count. */
+meq_status meq_adamw_steps(meq_adamw* st, int64_t* steps);
+meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps);
+/* Wait for the state's work; then MEQ_ERR_NONFINITE if since the last sync a
+ * step was skipped or left a non-finite moment (meq_adamw_last_error names the
+ * entry; such a step is not skipped). Each report clears the condition. */
+meq_status meq_adamw_sync(meq_adamw* st);
+/* Releases the state (synchronises its last stream first). NULL is a no-op. */
+meq_status meq_adamw_free(meq_adamw* st);
+const char* meq_adamw_last_error(const meq_adamw* st);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,804 @@
+// AdamW over many tensors at once, and the norm of their gradients.
+//
+// For every element of every entry, at step t (g' = s g with the caller's
+// coefficient s):
+//
+//   m <- b1 m + (1 - b1) g'          v <- b2 v + (1 - b2) g'^2
+//   p <- (1 - lr wd d) p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// One pass: 28 bytes per element with everything in fp32 (p, m, v read and
+// written, g read), so HBM bounds it. A launch covers up to kMaxEntries
+// entries, whose pointers travel in the kernel's arguments (no copy to the
+// device before a step), and a block 2048 consecutive elements of one entry: a
+// warp takes 256 of them as two groups of 128, so that every load and store of
+// a warp is one run of 512 bytes (fp32), and all loads are issued before the
+// first is used.
+//
+// 8-bit states: 256 elements, one warp's share, have an fp32 scale each for m
+// and for r = sqrt(v), the largest |m| and r of the block, and a code per
+// element:
+//
+//   m = S_m sign(q) (q / 127)^2, |q| <= 127       r = S_r (q / 255)^2, 0 <= q <= 255
+//
+// A quadratic code spends its steps near zero, where most of a block lies, and
+// r is coded instead of v because its range is half as wide (in logarithm) and
+// because the update divides by r. Both are rounded to the nearest code; an r
+// above zero keeps a code of at least one, since the update would otherwise be
+// divided by eps alone. The update itself uses the step's m and r as computed,
+// before that rounding. Every operation up to the codes is one IEEE rounding
+// (no contraction), so the codes do not depend on how a compiler fuses them.
+#include <cfloat>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "../../include/meq.h"
+#include "meq_elementwise.cuh"
+
+using namespace meq;
+
+namespace {
+
+constexpr int kBlock = 256;               // elements per scale and per warp
+constexpr int kAdamThreads = 256;
+constexpr int kAdamChunk = kBlock * kAdamThreads / 32;  // elements per block
+constexpr int kMaxEntries = 256;          // pointers of one launch: 6 KB of its arguments
+constexpr int kNormBlocksPerSm = 8;
+constexpr int kSkipped = 0x7fffffff;      // value of AdamClock::nonfinite: a step was skipped
+
+struct AdamEntry {
+  int64_t numel;
+  int64_t off;     // first element in the state's arrays, a multiple of kBlock
+  int64_t chunk0;  // first chunk
+  float decay;
+  int32_t pad;
+};
+
+// What the next step needs of the number of steps so far; the last block of a
+// step moves it on, so a step that is skipped on the device does not count.
+struct AdamClock {
+  double b1t, b2t;          // b1^t, b2^t of the next step
+  float inv_bc1;            // 1 / (1 - b1^t)
+  float inv_sqrt_bc2;       // 1 / sqrt(1 - b2^t)
+  long long steps;          // steps done
+  unsigned int ticket;      // blocks of this step that are done (0 between steps)
+  unsigned int norm_ticket; // the same for the norm
+  int nonfinite;            // 0, 1 + entry with a non-finite moment, or kSkipped
+  int pad;
+};
+
+__host__ __device__ inline void set_clock(AdamClock* c, double b1t, double b2t, long long steps) {
+  c->b1t = b1t, c->b2t = b2t, c->steps = steps;
+  c->inv_bc1 = static_cast<float>(1.0 / (1.0 - b1t));
+  c->inv_sqrt_bc2 = static_cast<float>(1.0 / sqrt(1.0 - b2t));
+}
+
+struct AdamArgs {
+  const AdamEntry* entries;
+  const int32_t* chunk_entry;
+  AdamClock* clock;
+  void* m;              // fp32, or int8 codes
+  void* v;              // fp32, or uint8 codes of sqrt(v)
+  float* m_scale;       // 8-bit states: one per block
+  float* r_scale;
+  const float* grad_scale;
+  double beta1, beta2;
+  float b1, one_minus_b1, b2, one_minus_b2, eps, lr, wd;
+  int32_t entry0, last;  // first entry of this launch; 1: the step's last launch
+  int64_t chunk0;        // first chunk of this launch
+  void* params[kMaxEntries];
+  const void* grads[kMaxEntries];
+  void* copies[kMaxEntries];
+};
+
+struct NormArgs {
+  const AdamEntry* entries;
+  const int32_t* chunk_entry;
+  AdamClock* clock;
+  double* partials;
+  float* out;
+  float max_norm;
+  int32_t entry0, last, part0, parts;  // first partial of this launch; partials of all launches
+  int64_t chunk0, chunks;
+  const void* grads[kMaxEntries];
+};
+
+// Four consecutive elements as fp32: one load where they are aligned and all
+// there, else one per element (those beyond n as zero).
+template <typename T>
+struct Quad;
+template <>
+struct Quad<float> {
+  static __device__ __forceinline__ void load(const float* p, float* x) {
+    const float4 q = __ldcs(reinterpret_cast<const float4*>(p));
+    x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* x) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+  }
+};
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+__device__ __forceinline__ void from_f(float x, float* p) { *p = x; }
+__device__ __forceinline__ void from_f(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void from_f(float x, __half* p) { *p = __float2half_rn(x); }
+template <typename T>
+struct Quad {
+  static __device__ __forceinline__ void load(const T* p, float* x) {
+    const uint2 q = __ldcs(reinterpret_cast<const uint2*>(p));
+    T h[4];
+    memcpy(h, &q, 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = to_f(h[i]);
+  }
+  static __device__ __forceinline__ void store(T* p, const float* x) {
+    T h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from_f(x[i], &h[i]);
+    uint2 q;
+    memcpy(&q, h, 8);
+    __stcs(reinterpret_cast<uint2*>(p), q);
+  }
+};
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, int64_t n, bool vec, float* x) {
+  if (vec) {
+    Quad<T>::load(p, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < n ? to_f(p[i]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int64_t n, bool vec, const float* x) {
+  if (vec) {
+    Quad<T>::store(p, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) from_f(x[i], p + i);
+  }
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+
+// scale (code / most)^2 with the code's sign
+__device__ __forceinline__ float decode(float code, float inv_most, float scale) {
+  const float t = __fmul_rn(code, inv_most);
+  return __fmul_rn(__fmul_rn(t, fabsf(t)), scale);
+}
+__device__ __forceinline__ float encode(float x, float inv_scale, float most) {
+  return rintf(__fmul_rn(most, __fsqrt_rn(__fmul_rn(fabsf(x), inv_scale))));
+}
+// The scale of a block whose largest magnitude is top, and its reciprocal. A
+// block of denormals is taken as zero: the reciprocal would overflow.
+__device__ __forceinline__ float block_scale(float top, float* inv) {
+  const bool some = top >= FLT_MIN;
+  *inv = some ? __frcp_rn(top) : 0.f;
+  return some ? top : 0.f;
+}
+__device__ __forceinline__ void decode_m4(uint32_t w, float scale, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = decode(static_cast<float>(static_cast<int8_t>(w >> (8 * i))), 1.0f / 127.0f, scale);
+}
+__device__ __forceinline__ void decode_r4(uint32_t w, float scale, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = decode(static_cast<float>((w >> (8 * i)) & 255u), 1.0f / 255.0f, scale);
+}
+
+template <typename P, typename G, int kBits>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs a) {
+  pdl_allow_dependents();
+  const int64_t chunk = a.chunk0 + blockIdx.x;
+  const int ei = a.chunk_entry[chunk];
+  const AdamEntry E = a.entries[ei];
+  const int lane = threadIdx.x & 31;
+  const int64_t base = (chunk - E.chunk0) * kAdamChunk + (threadIdx.x >> 5) * kBlock;  // the warp's block of E
+  P* p = static_cast<P*>(a.params[ei - a.entry0]);
+  const G* g = static_cast<const G*>(a.grads[ei - a.entry0]);
+  __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(a.copies[ei - a.entry0]);
+  pdl_wait_predecessor();
+  float gs = 1.f;
+  if (a.grad_scale) {
+    gs = *a.grad_scale;
+    if (!(fabsf(gs) <= FLT_MAX)) {  // every block sees it: nothing changes, the step does not count
+      if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(&a.clock->nonfinite, 0, kSkipped);
+      return;
+    }
+  }
+  const float step = __fmul_rn(a.lr, a.clock->inv_bc1);
+  const float rbc2 = a.clock->inv_sqrt_bc2;
+  const float keep = 1.f - a.lr * a.wd * E.decay;
+  if (base < E.numel) {
+    const bool full = base + kBlock <= E.numel;
+    const bool pvec = full && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(P) - 1)) == 0;
+    const bool gvec = full && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
+    const bool cvec = full && (reinterpret_cast<uintptr_t>(copy) & 7u) == 0;
+    float pv[8], gv[8], m[8], r[8];  // two groups of four, 128 apart; r holds v until its root is taken
+    const int64_t at = base + 4 * lane;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      load4(g + at + 128 * j, E.numel - at - 128 * j, gvec, gv + 4 * j);
+      load4(p + at + 128 * j, E.numel - at - 128 * j, pvec, pv + 4 * j);
+    }
+    const int64_t so = E.off + at;  // the state's arrays are padded to whole blocks
+    const int64_t sb = (E.off + base) / kBlock;
+    if (kBits == 32) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Quad<float>::load(static_cast<const float*>(a.m) + so + 128 * j, m + 4 * j);
+        Quad<float>::load(static_cast<const float*>(a.v) + so + 128 * j, r + 4 * j);
+      }
+    } else {
+      const float ms = a.m_scale[sb], rs = a.r_scale[sb];
+      uint32_t mc[2], rc[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        mc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(a.m) + so + 128 * j));
+        rc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + so + 128 * j));
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        decode_m4(mc[j], ms, m + 4 * j);
+        decode_r4(rc[j], rs, r + 4 * j);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = __fmul_rn(r[i], r[i]);
+    }
+    bool bad = false;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __fmul_rn(gv[i], gs);
+      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(x, a.one_minus_b1));
+      v[i] = __fadd_rn(__fmul_rn(r[i], a.b2), __fmul_rn(__fmul_rn(x, x), a.one_minus_b2));
+      r[i] = __fsqrt_rn(v[i]);
+      const float u = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(r[i], rbc2), a.eps));
+      pv[i] = __fadd_rn(__fmul_rn(pv[i], keep), -__fmul_rn(u, step));
+      bad = bad || !(fabsf(m[i]) <= FLT_MAX) || !(r[i] <= FLT_MAX);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      store4(p + at + 128 * j, E.numel - at - 128 * j, pvec, pv + 4 * j);
+      if (copy) store4(copy + at + 128 * j, E.numel - at - 128 * j, cvec, pv + 4 * j);
+    }
+    if (kBits == 32) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Quad<float>::store(static_cast<float*>(a.m) + so + 128 * j, m + 4 * j);
+        Quad<float>::store(static_cast<float*>(a.v) + so + 128 * j, v + 4 * j);
+      }
+    } else {
+      float mt = 0.f, rt = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mt = fmaxf(mt, fabsf(m[i])), rt = fmaxf(rt, r[i]);
+      float mi, ri;
+      float ms = block_scale(warp_max(mt), &mi), rs = block_scale(warp_max(rt), &ri);
+      if (__any_sync(0xffffffffu, bad)) ms = rs = __int_as_float(0x7fc00000);  // no code says NaN: the block's scale does
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t mc = 0, rc = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = m[4 * j + i], y = r[4 * j + i];
+          const int q = static_cast<int>(encode(x, mi, 127.f));
+          mc |= (static_cast<uint32_t>(x < 0.f ? -q : q) & 255u) << (8 * i);
+          float k = encode(y, ri, 255.f);
+          if (y > 0.f) k = fmaxf(k, 1.f);
+          rc |= (static_cast<uint32_t>(static_cast<int>(k)) & 255u) << (8 * i);
+        }
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<int8_t*>(a.m) + so + 128 * j), mc);
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + so + 128 * j), rc);
+      }
+      if (lane == 0) a.m_scale[sb] = ms, a.r_scale[sb] = rs;
+    }
+    if (bad) atomicCAS(&a.clock->nonfinite, 0, ei + 1);
+  }
+  if (a.last) {
+    __syncthreads();  // every thread of this block has read the clock
+    if (threadIdx.x == 0 && atomicInc(&a.clock->ticket, gridDim.x - 1) == gridDim.x - 1)
+      set_clock(a.clock, a.clock->b1t * a.beta1, a.clock->b2t * a.beta2, a.clock->steps + 1);
+  }
+}
+
+// Sum over the block, in double, in a fixed order; thread 0 has it.
+__device__ __forceinline__ double block_sum(double x, double* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+  __syncthreads();
+  double s = 0.0;
+  if (threadIdx.x == 0)
+    for (int i = 0; i < kAdamThreads / 32; ++i) s += sh[i];
+  return s;
+}
+
+// out[0] = sqrt(sum g^2), out[1] = the coefficient that brings it to at most
+// max_norm. Bound by the one read of the gradients. A thread adds the squares
+// of its share in fp32 (eight sums side by side), the rest is added in double;
+// the blocks' sums lie in `partials` and the last block to finish adds them up,
+// in an order that does not depend on which block that is.
+template <typename G>
+__global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ double sh[kAdamThreads / 32];
+  __shared__ bool final_block;
+  const int lane = threadIdx.x & 31;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int64_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    const int64_t chunk = a.chunk0 + c;
+    const int ei = a.chunk_entry[chunk];
+    const int64_t numel = a.entries[ei].numel;
+    const int64_t base = (chunk - a.entries[ei].chunk0) * kAdamChunk + (threadIdx.x >> 5) * kBlock;
+    if (base >= numel) continue;
+    const G* g = static_cast<const G*>(a.grads[ei - a.entry0]);
+    const bool vec = base + kBlock <= numel && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
+    const int64_t at = base + 4 * lane;
+    float x[8];
+    load4(g + at, numel - at, vec, x);
+    load4(g + at + 128, numel - at - 128, vec, x + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
+  }
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t += static_cast<double>(acc[i]);
+  const double s = block_sum(t, sh);
+  if (threadIdx.x == 0) {
+    a.partials[a.part0 + blockIdx.x] = s;
+    __threadfence();
+    final_block = a.last && atomicInc(&a.clock->norm_ticket, gridDim.x - 1) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!final_block) return;
+  __threadfence();
+  double all = 0.0;
+  for (int i = threadIdx.x; i < a.parts; i += kAdamThreads) all += __ldcg(a.partials + i);
+  __syncthreads();  // sh is free again
+  all = block_sum(all, sh);
+  if (threadIdx.x == 0) {
+    const float norm = static_cast<float>(sqrt(all));
+    a.out[0] = norm;
+    a.out[1] = !(norm <= FLT_MAX) ? __int_as_float(0x7fc00000) : norm > a.max_norm ? __fdiv_rn(a.max_norm, norm) : 1.f;
+  }
+}
+
+// The values that the 8-bit states stand for.
+__global__ void __launch_bounds__(kAdamThreads) adamw_values_kernel(const uint32_t* __restrict__ m_code,
+                                                                    const uint32_t* __restrict__ r_code,
+                                                                    const float* __restrict__ m_scale,
+                                                                    const float* __restrict__ r_scale, int64_t quads,
+                                                                    float* __restrict__ m, float* __restrict__ v) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kAdamThreads + threadIdx.x;
+  if (i >= quads) return;
+  const int64_t b = i / (kBlock / 4);
+  float x[4];
+  if (m) {
+    decode_m4(__ldcs(m_code + i), m_scale[b], x);
+    __stcs(reinterpret_cast<float4*>(m) + i, make_float4(x[0], x[1], x[2], x[3]));
+  }
+  if (v) {
+    decode_r4(__ldcs(r_code + i), r_scale[b], x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(x[k], x[k]);
+    __stcs(reinterpret_cast<float4*>(v) + i, make_float4(x[0], x[1], x[2], x[3]));
+  }
+}
+
+// One launch's share of the entries.
+struct Part {
+  int entry0, entries;
+  int64_t chunk0, chunks;
+  int norm_blocks, part0;
+};
+
+size_t dtype_bytes(int t) { return t == MEQ_F32 ? 4 : 2; }
+
+}  // namespace
+
+struct meq_adamw {
+  int n = 0;
+  std::vector<AdamEntry> entries;
+  std::vector<Part> parts;
+  meq_adamw_options opt{};
+  int64_t elements = 0;  // of the padded state arrays
+  int device = 0, total_parts = 0;
+  char* arena = nullptr;
+  void *d_m = nullptr, *d_v = nullptr;
+  float *d_ms = nullptr, *d_rs = nullptr;
+  AdamEntry* d_entries = nullptr;
+  int32_t* d_chunk_entry = nullptr;
+  AdamClock* d_clock = nullptr;
+  double* d_partials = nullptr;
+  cudaStream_t last_stream = nullptr;
+  std::string last_error;
+};
+
+namespace {
+
+meq_status fail(meq_adamw* st, meq_status s, const std::string& msg) {
+  if (st) st->last_error = msg;
+  else meq::set_global_error(msg);
+  return s;
+}
+meq_status cuda_fail(meq_adamw* st, cudaError_t e, const char* what) {
+  return fail(st, MEQ_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+
+// No C++ exception leaves a C entry.
+template <typename F>
+meq_status guarded(meq_adamw* st, F f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    if (st) st->last_error.clear();
+    return MEQ_ERR_OOM;
+  } catch (...) {
+    return MEQ_ERR_INVALID_ARG;
+  }
+}
+
+bool valid_adamw_options(const meq_adamw_options& o, std::string* why) {
+  auto beta = [](double b) { return b >= 0.0 && b < 1.0; };
+  if (!beta(o.beta1) || !beta(o.beta2)) { *why = "beta1 and beta2 must be in [0, 1)"; return false; }
+  if (!(static_cast<float>(o.eps) > 0.f) || !std::isfinite(static_cast<float>(o.eps))) { *why = "eps must be positive and finite in fp32"; return false; }
+  if (o.state_bits != 32 && o.state_bits != 8) { *why = "state_bits must be 32 or 8"; return false; }
+  if (o.param_type != MEQ_F32 && o.param_type != MEQ_BF16) { *why = "param_type must be MEQ_F32 or MEQ_BF16"; return false; }
+  if (o.grad_type != MEQ_F32 && o.grad_type != MEQ_BF16 && o.grad_type != MEQ_F16) { *why = "grad_type must be a meq_dtype"; return false; }
+  return true;
+}
+
+int64_t pad_block(int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; }
+
+// Entries, launches and the arena's layout; host only.
+struct Plan {
+  int64_t elements = 0, chunks = 0, persistent = 0, total = 0;
+  int64_t o_m = 0, o_v = 0, o_ms = 0, o_rs = 0, o_entries = 0, o_chunks = 0, o_clock = 0, o_partials = 0;
+  int total_parts = 0;
+  std::vector<AdamEntry> entries;
+  std::vector<Part> parts;
+};
+Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_adamw_options& o, int sms) {
+  Plan P;
+  P.entries.resize(n);
+  for (int i = 0; i < n; ++i) {
+    AdamEntry& E = P.entries[i];
+    E.numel = shapes[i].rows * shapes[i].cols;
+    E.off = P.elements;
+    E.chunk0 = P.chunks;
+    E.decay = decay ? decay[i] : 1.f;
+    E.pad = 0;
+    P.elements += pad_block(E.numel);
+    P.chunks += (E.numel + kAdamChunk - 1) / kAdamChunk;
+  }
+  for (int i = 0; i < n; i += kMaxEntries) {
+    Part p{};
+    p.entry0 = i;
+    p.entries = n - i < kMaxEntries ? n - i : kMaxEntries;
+    p.chunk0 = P.entries[i].chunk0;
+    p.chunks = (i + p.entries < n ? P.entries[i + p.entries].chunk0 : P.chunks) - p.chunk0;
+    const int64_t most = static_cast<int64_t>(sms) * kNormBlocksPerSm;
+    p.norm_blocks = static_cast<int>(p.chunks < most ? p.chunks : most);
+    p.part0 = P.total_parts;
+    P.total_parts += p.norm_blocks;
+    P.parts.push_back(p);
+  }
+  auto add = [&](int64_t bytes) {
+    const int64_t off = P.total;
+    P.total += (bytes + 255) / 256 * 256;
+    return off;
+  };
+  const int64_t each = o.state_bits / 8, scales = o.state_bits == 8 ? P.elements / kBlock * 4 : 0;
+  P.o_m = add(P.elements * each);
+  P.o_v = add(P.elements * each);
+  P.o_ms = add(scales);
+  P.o_rs = add(scales);
+  P.o_entries = add(static_cast<int64_t>(n) * sizeof(AdamEntry));
+  P.o_chunks = add(P.chunks * 4);
+  P.o_clock = add(sizeof(AdamClock));
+  P.o_partials = add(static_cast<int64_t>(P.total_parts) * 8);
+  P.persistent = 2 * (P.elements * each + scales);
+  return P;
+}
+
+bool check_plan(const Plan& P, std::string* why) {
+  for (const Part& p : P.parts)
+    if (p.chunks > 0x7fffffff) { *why = "too many elements in 256 consecutive entries for one launch"; return false; }
+  if (P.chunks > 0x7fffffff) { *why = "more than 2^42 elements in one state"; return false; }
+  return true;
+}
+
+meq_status check_call(meq_adamw* st, const void* const* ptrs, size_t align, const char* what) {
+  if (!ptrs) return fail(st, MEQ_ERR_INVALID_ARG, std::string(what) + " must be non-NULL");
+  for (int i = 0; i < st->n; ++i) {
+    if (!ptrs[i]) return fail(st, MEQ_ERR_INVALID_ARG, std::string("NULL ") + what + " pointer at " + std::to_string(i));
+    if (reinterpret_cast<uintptr_t>(ptrs[i]) % align)
+      return fail(st, MEQ_ERR_INVALID_ARG, std::string(what) + " pointer " + std::to_string(i) + " is not aligned to its type");
+  }
+  return MEQ_OK;
+}
+
+meq_status check_device(meq_adamw* st) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return cuda_fail(st, e, "cudaGetDevice");
+  if (dev != st->device)
+    return fail(st, MEQ_ERR_INVALID_ARG, "the state is on device " + std::to_string(st->device) + ", the current device is " + std::to_string(dev));
+  return MEQ_OK;
+}
+
+template <typename P, typename G>
+cudaError_t launch_adamw(int bits, const AdamArgs& a, unsigned grid, cudaStream_t s) {
+  if (bits == 32) return launch_pdl(adamw_kernel<P, G, 32>, dim3(grid), dim3(kAdamThreads), 0, s, 1, a);
+  return launch_pdl(adamw_kernel<P, G, 8>, dim3(grid), dim3(kAdamThreads), 0, s, 1, a);
+}
+template <typename P>
+cudaError_t launch_adamw(const meq_adamw_options& o, const AdamArgs& a, unsigned grid, cudaStream_t s) {
+  if (o.grad_type == MEQ_F32) return launch_adamw<P, float>(o.state_bits, a, grid, s);
+  if (o.grad_type == MEQ_BF16) return launch_adamw<P, __nv_bfloat16>(o.state_bits, a, grid, s);
+  return launch_adamw<P, __half>(o.state_bits, a, grid, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+void meq_adamw_default_options(meq_adamw_options* opt) {
+  if (!opt) return;
+  std::memset(opt, 0, sizeof(*opt));
+  opt->beta1 = 0.9, opt->beta2 = 0.999, opt->eps = 1e-8;
+  opt->state_bits = 32;
+  opt->param_type = MEQ_F32, opt->grad_type = MEQ_F32;
+}
+
+meq_status meq_adamw_state_bytes(const meq_shape* shapes, int n, const meq_adamw_options* opt, size_t* persistent_bytes,
+                                 size_t* workspace_bytes) {
+  return guarded(nullptr, [&]() -> meq_status {
+    meq_adamw_options o;
+    if (opt) o = *opt; else meq_adamw_default_options(&o);
+    std::string why;
+    if (!meq::valid_shapes(shapes, n, &why) || !valid_adamw_options(o, &why)) return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
+    const Plan P = make_plan(shapes, nullptr, n, o, 152);
+    if (!check_plan(P, &why)) return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
+    if (persistent_bytes) *persistent_bytes = static_cast<size_t>(P.persistent);
+    if (workspace_bytes) *workspace_bytes = static_cast<size_t>(P.total - P.persistent);
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, const meq_adamw_options* opt,
+                          void* cuda_stream, meq_adamw** out) {
+  if (!out) return fail(nullptr, MEQ_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  return guarded(nullptr, [&]() -> meq_status {
+    meq_adamw_options o;
+    if (opt) o = *opt; else meq_adamw_default_options(&o);
+    std::string why;
+    if (!meq::valid_shapes(shapes, n, &why) || !valid_adamw_options(o, &why)) return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
+    for (int i = 0; decay && i < n; ++i)
+      if (!(decay[i] >= 0.f) || !std::isfinite(decay[i]))
+        return fail(nullptr, MEQ_ERR_INVALID_ARG, "decay of entry " + std::to_string(i) + " must be finite and >= 0");
+    int dev = 0, sms = 0;
+    meq_status ms = meq::check_sm103(&dev, &sms);
+    if (ms != MEQ_OK) return ms;
+    Plan P = make_plan(shapes, decay, n, o, sms);
+    if (!check_plan(P, &why)) return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
+    std::vector<int32_t> chunk_entry(static_cast<size_t>(P.chunks));
+    for (int i = 0; i < n; ++i) {
+      const int64_t end = i + 1 < n ? P.entries[i + 1].chunk0 : P.chunks;
+      for (int64_t c = P.entries[i].chunk0; c < end; ++c) chunk_entry[static_cast<size_t>(c)] = i;
+    }
+    AdamClock clock;
+    std::memset(&clock, 0, sizeof(clock));
+    set_clock(&clock, o.beta1, o.beta2, 0);
+
+    struct Owner {  // of the state until it is handed out
+      meq_adamw* st;
+      ~Owner() {
+        if (!st) return;
+        if (st->arena) cudaFree(st->arena);
+        delete st;
+      }
+    } own{new meq_adamw()};
+    meq_adamw* st = own.st;
+    st->n = n, st->opt = o, st->device = dev;
+    st->elements = P.elements, st->total_parts = P.total_parts;
+    cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&st->arena), static_cast<size_t>(P.total));
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      st->arena = nullptr;
+      return fail(nullptr, MEQ_ERR_OOM, "cudaMalloc of " + std::to_string(P.total) + " bytes failed");
+    }
+    char* A = st->arena;
+    st->d_m = A + P.o_m, st->d_v = A + P.o_v;
+    st->d_ms = reinterpret_cast<float*>(A + P.o_ms), st->d_rs = reinterpret_cast<float*>(A + P.o_rs);
+    st->d_entries = reinterpret_cast<AdamEntry*>(A + P.o_entries);
+    st->d_chunk_entry = reinterpret_cast<int32_t*>(A + P.o_chunks);
+    st->d_clock = reinterpret_cast<AdamClock*>(A + P.o_clock);
+    st->d_partials = reinterpret_cast<double*>(A + P.o_partials);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    e = cudaMemsetAsync(A, 0, static_cast<size_t>(P.total), s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_entries, P.entries.data(), sizeof(AdamEntry) * n, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_chunk_entry, chunk_entry.data(), 4 * chunk_entry.size(), cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_clock, &clock, sizeof(clock), cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_CUDA, std::string("initialising the AdamW state failed: ") + cudaGetErrorString(e));
+    st->entries = std::move(P.entries);
+    st->parts = std::move(P.parts);
+    st->last_stream = s;
+    own.st = nullptr;
+    *out = st;
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float max_norm, float* out, void* cuda_stream) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    meq_status ms = check_call(st, grads, dtype_bytes(st->opt.grad_type), "grads");
+    if (ms != MEQ_OK) return ms;
+    if (!out || reinterpret_cast<uintptr_t>(out) % 4) return fail(st, MEQ_ERR_INVALID_ARG, "out must be a device pointer to two floats");
+    if (!(max_norm > 0.f)) return fail(st, MEQ_ERR_INVALID_ARG, "max_norm must be > 0");
+    ms = check_device(st);
+    if (ms != MEQ_OK) return ms;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    NormArgs a;
+    a.entries = st->d_entries, a.chunk_entry = st->d_chunk_entry, a.clock = st->d_clock, a.partials = st->d_partials;
+    a.out = out, a.max_norm = max_norm, a.parts = st->total_parts;
+    for (size_t k = 0; k < st->parts.size(); ++k) {
+      const Part& p = st->parts[k];
+      a.entry0 = p.entry0, a.chunk0 = p.chunk0, a.chunks = p.chunks, a.part0 = p.part0;
+      a.last = k + 1 == st->parts.size() ? 1 : 0;
+      for (int i = 0; i < p.entries; ++i) a.grads[i] = grads[p.entry0 + i];
+      const dim3 grid(static_cast<unsigned>(p.norm_blocks)), block(kAdamThreads);
+      cudaError_t e = st->opt.grad_type == MEQ_F32    ? launch_pdl(grad_norm_kernel<float>, grid, block, 0, s, 1, a)
+                      : st->opt.grad_type == MEQ_BF16 ? launch_pdl(grad_norm_kernel<__nv_bfloat16>, grid, block, 0, s, 1, a)
+                                                      : launch_pdl(grad_norm_kernel<__half>, grid, block, 0, s, 1, a);
+      if (e != cudaSuccess) return cuda_fail(st, e, "gradient norm launch");
+    }
+    st->last_stream = s;
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_step(void* const* params, const void* const* grads, void* const* copies, meq_adamw* st, float lr,
+                          float weight_decay, const float* grad_scale, void* cuda_stream) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    meq_status ms = check_call(st, const_cast<const void* const*>(params), dtype_bytes(st->opt.param_type), "params");
+    if (ms == MEQ_OK) ms = check_call(st, grads, dtype_bytes(st->opt.grad_type), "grads");
+    if (ms == MEQ_OK && copies) ms = check_call(st, const_cast<const void* const*>(copies), 2, "copies");
+    if (ms != MEQ_OK) return ms;
+    if (!std::isfinite(lr) || !std::isfinite(weight_decay)) return fail(st, MEQ_ERR_INVALID_ARG, "lr and weight_decay must be finite");
+    if (reinterpret_cast<uintptr_t>(grad_scale) % 4) return fail(st, MEQ_ERR_INVALID_ARG, "grad_scale is not aligned to its type");
+    ms = check_device(st);
+    if (ms != MEQ_OK) return ms;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    AdamArgs a;
+    a.entries = st->d_entries, a.chunk_entry = st->d_chunk_entry, a.clock = st->d_clock;
+    a.m = st->d_m, a.v = st->d_v, a.m_scale = st->d_ms, a.r_scale = st->d_rs, a.grad_scale = grad_scale;
+    a.beta1 = st->opt.beta1, a.beta2 = st->opt.beta2;
+    a.b1 = static_cast<float>(a.beta1), a.one_minus_b1 = static_cast<float>(1.0 - a.beta1);
+    a.b2 = static_cast<float>(a.beta2), a.one_minus_b2 = static_cast<float>(1.0 - a.beta2);
+    a.eps = static_cast<float>(st->opt.eps), a.lr = lr, a.wd = weight_decay;
+    for (size_t k = 0; k < st->parts.size(); ++k) {
+      const Part& p = st->parts[k];
+      a.entry0 = p.entry0, a.chunk0 = p.chunk0;
+      a.last = k + 1 == st->parts.size() ? 1 : 0;
+      for (int i = 0; i < p.entries; ++i) {
+        a.params[i] = params[p.entry0 + i];
+        a.grads[i] = grads[p.entry0 + i];
+        a.copies[i] = copies ? copies[p.entry0 + i] : nullptr;
+      }
+      const unsigned grid = static_cast<unsigned>(p.chunks);
+      cudaError_t e = st->opt.param_type == MEQ_F32 ? launch_adamw<float>(st->opt, a, grid, s)
+                                                    : launch_adamw<__nv_bfloat16>(st->opt, a, grid, s);
+      if (e != cudaSuccess) return cuda_fail(st, e, "AdamW launch");
+    }
+    st->last_stream = s;
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_state_ptrs(meq_adamw* st, void** m, void** v, float** m_scale, float** v_scale, int64_t* elements) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  const bool scales = st->opt.state_bits == 8;
+  if (m) *m = st->d_m;
+  if (v) *v = st->d_v;
+  if (m_scale) *m_scale = scales ? st->d_ms : nullptr;
+  if (v_scale) *v_scale = scales ? st->d_rs : nullptr;
+  if (elements) *elements = st->elements;
+  return MEQ_OK;
+}
+
+meq_status meq_adamw_read_values(meq_adamw* st, float* m, float* v, void* cuda_stream) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    if ((reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(v)) % 16)
+      return fail(st, MEQ_ERR_INVALID_ARG, "m and v must be 16-byte aligned");
+    meq_status ms = check_device(st);
+    if (ms != MEQ_OK) return ms;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = cudaSuccess;
+    if (st->opt.state_bits == 32) {
+      const size_t bytes = static_cast<size_t>(st->elements) * 4;
+      if (m) e = cudaMemcpyAsync(m, st->d_m, bytes, cudaMemcpyDeviceToDevice, s);
+      if (e == cudaSuccess && v) e = cudaMemcpyAsync(v, st->d_v, bytes, cudaMemcpyDeviceToDevice, s);
+    } else if (m || v) {
+      const int64_t quads = st->elements / 4, blocks = (quads + kAdamThreads - 1) / kAdamThreads;
+      e = launch_pdl(adamw_values_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kAdamThreads), 0, s, 1,
+                     static_cast<const uint32_t*>(st->d_m), static_cast<const uint32_t*>(st->d_v),
+                     static_cast<const float*>(st->d_ms), static_cast<const float*>(st->d_rs), quads, m, v);
+    }
+    if (e != cudaSuccess) return cuda_fail(st, e, "reading the AdamW state");
+    st->last_stream = s;
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_steps(meq_adamw* st, int64_t* steps) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    if (!steps) return fail(st, MEQ_ERR_INVALID_ARG, "steps is NULL");
+    AdamClock c;
+    cudaError_t e = cudaStreamSynchronize(st->last_stream);
+    if (e == cudaSuccess) e = cudaMemcpy(&c, st->d_clock, sizeof(c), cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return cuda_fail(st, e, "reading the step count");
+    *steps = c.steps;
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    if (steps < 0) return fail(st, MEQ_ERR_INVALID_ARG, "steps must be >= 0");
+    AdamClock c;
+    std::memset(&c, 0, sizeof(c));
+    set_clock(&c, std::pow(st->opt.beta1, static_cast<double>(steps) + 1.0),
+              std::pow(st->opt.beta2, static_cast<double>(steps) + 1.0), steps);
+    cudaError_t e = cudaStreamSynchronize(st->last_stream);
+    if (e == cudaSuccess) e = cudaMemcpy(st->d_clock, &c, offsetof(AdamClock, ticket), cudaMemcpyHostToDevice);
+    if (e != cudaSuccess) return cuda_fail(st, e, "writing the step count");
+    return MEQ_OK;
+  });
+}
+
+meq_status meq_adamw_sync(meq_adamw* st) {
+  if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
+  return guarded(st, [&]() -> meq_status {
+    cudaError_t e = cudaStreamSynchronize(st->last_stream);
+    if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamSynchronize");
+    int bad = 0;
+    e = cudaMemcpy(&bad, &st->d_clock->nonfinite, sizeof(int), cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return cuda_fail(st, e, "reading the non-finite flag");
+    if (bad == 0) return MEQ_OK;
+    const int zero = 0;
+    e = cudaMemcpy(&st->d_clock->nonfinite, &zero, sizeof(int), cudaMemcpyHostToDevice);
+    if (e != cudaSuccess) return cuda_fail(st, e, "clearing the non-finite flag");
+    if (bad == kSkipped) return fail(st, MEQ_ERR_NONFINITE, "a step was skipped: its gradient coefficient was not finite");
+    return fail(st, MEQ_ERR_NONFINITE, "non-finite moment (gradient, or a previous non-finite step) in entry " + std::to_string(bad - 1));
+  });
+}
+
+meq_status meq_adamw_free(meq_adamw* st) {
+  if (!st) return MEQ_OK;
+  cudaStreamSynchronize(st->last_stream);
+  if (st->arena) cudaFree(st->arena);
+  delete st;
+  return MEQ_OK;
+}
+
+const char* meq_adamw_last_error(const meq_adamw* st) { return st ? st->last_error.c_str() : meq_last_error(nullptr); }
+
+}  // extern "C"

@@ -42,7 +42,8 @@ constexpr int64_t kAlignBytes = 1024;
 
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-std::string g_init_error;  // last meq_init_state failure text
+// Text of the calling thread's last failed call made without a state: the loss calls may come from several threads.
+thread_local std::string g_init_error;
 
 struct Group {
   int64_t s = 0, l = 0, lp = 0, sp = 0, count = 0;
@@ -208,7 +209,11 @@ bool valid_kinds(const meq_shape* shapes, const int* kinds, int n, int rule, std
   return true;
 }
 
-bool valid_shapes(const meq_shape* shapes, int n, std::string* why) {
+float pow2_round(double x) { return static_cast<float>(std::ldexp(1.0, static_cast<int>(std::lround(std::log2(std::max(x, 1.0)))))); }
+
+}  // namespace
+
+bool meq::valid_shapes(const meq_shape* shapes, int n, std::string* why) {
   if (n <= 0) { *why = "n must be positive"; return false; }
   if (!shapes) { *why = "shapes is NULL"; return false; }
   for (int i = 0; i < n; ++i) {
@@ -223,7 +228,21 @@ bool valid_shapes(const meq_shape* shapes, int n, std::string* why) {
   return true;
 }
 
-float pow2_round(double x) { return static_cast<float>(std::ldexp(1.0, static_cast<int>(std::lround(std::log2(std::max(x, 1.0)))))); }
+meq_status meq::check_sm103(int* device, int* num_sms) {
+  cudaError_t e = cudaGetDevice(device);
+  if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_UNSUPPORTED, std::string("no CUDA device: ") + cudaGetErrorString(e));
+  int major = 0, minor = 0;
+  e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, *device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, *device);
+  if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_CUDA, std::string("cudaDeviceGetAttribute: ") + cudaGetErrorString(e));
+  if (major != 10 || minor != 3)
+    return fail(nullptr, MEQ_ERR_UNSUPPORTED,
+                "this library is built for sm_103a (GB300); device is sm_" + std::to_string(major) + std::to_string(minor));
+  return MEQ_OK;
+}
+
+namespace {
 
 // Rows per block of the one-pass form over a remaining 2D parameter of m rows:
 // at least kColSlab (the partial sums are sized for that), and as many more as
@@ -707,18 +726,11 @@ static meq_status init_state(const meq_shape* shapes, const int* kinds, int n, c
   if (!valid_shapes(shapes, n, &why) || !valid_options(o, &why) || !valid_kinds(shapes, kinds, n, o.update_rule, &why))
     return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
 
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_UNSUPPORTED, std::string("no CUDA device: ") + cudaGetErrorString(e));
-  int major = 0, minor = 0, smem_optin = 0, num_sms = 0;
-  e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, dev);
+  int dev = 0, smem_optin = 0, num_sms = 0;
+  const meq_status supported = meq::check_sm103(&dev, &num_sms);
+  if (supported != MEQ_OK) return supported;
+  cudaError_t e = cudaDeviceGetAttribute(&smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
   if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_CUDA, std::string("cudaDeviceGetAttribute: ") + cudaGetErrorString(e));
-  if (major != 10 || minor != 3)
-    return fail(nullptr, MEQ_ERR_UNSUPPORTED,
-                "this library is built for sm_103a (GB300); device is sm_" + std::to_string(major) + std::to_string(minor));
   if (smem_optin < ns_gemm_smem_bytes(o.ns_cta_pair ? 2 : 1))
     return fail(nullptr, MEQ_ERR_UNSUPPORTED, "not enough opt-in shared memory per block");
   if (!get_encode()) return fail(nullptr, MEQ_ERR_UNSUPPORTED, "cuTensorMapEncodeTiled is not available from the driver");

@@ -10,6 +10,8 @@
 #include <string>
 #include <utility>
 
+#include "../../include/meq.h"
+
 namespace meq {
 
 // ------------------------------------------------------------ error codes
@@ -191,5 +193,10 @@ cudaError_t launch_row_col_stats(const float* U, int64_t rows, int64_t cols, flo
 
 // Error text of the last failed call made without a state (meq_last_error(NULL)).
 void set_global_error(const std::string& msg);
+
+// The shape limits every state shares, and the current device if it is an
+// sm_103 one (else the status, with its text for meq_last_error(NULL)).
+bool valid_shapes(const meq_shape* shapes, int n, std::string* why);
+meq_status check_sm103(int* device, int* num_sms);
 
 }  // namespace meq

@@ -47,6 +47,17 @@ class MeqOptions(ctypes.Structure):
     ]
 
 
+class MeqAdamWOptions(ctypes.Structure):
+    _fields_ = [
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("state_bits", ctypes.c_int),
+        ("param_type", ctypes.c_int),
+        ("grad_type", ctypes.c_int),
+    ]
+
+
 EXPORTED = [
     "meq_default_options", "meq_state_bytes", "meq_init_state", "meq_step", "meq_sync", "meq_free",
     "meq_last_error", "meq_status_string", "meq_read_momentum", "meq_write_momentum",
@@ -57,9 +68,13 @@ EXPORTED = [
     "meq_check_canaries", "meq_canary_count", "meq_debug_corrupt_canary",
     "meq_step_prepare", "meq_step_apply", "meq_read_update", "meq_ns_flops_per_step",
     "meq_ns_gemm_tile_columns",
+    "meq_adamw_default_options", "meq_adamw_state_bytes", "meq_adamw_init", "meq_adamw_grad_norm", "meq_adamw_step",
+    "meq_adamw_state_ptrs", "meq_adamw_read_values", "meq_adamw_steps", "meq_adamw_set_steps", "meq_adamw_sync",
+    "meq_adamw_free", "meq_adamw_last_error",
 ]
 HIDDEN, REMAINING_2D, VECTOR = 0, 1, 2  # meq_kind
 RULE_MEQMUON, RULE_MUON = 0, 1          # meq_update_rule
+DTYPES = {"float32": 0, "bfloat16": 1, "float16": 2}  # meq_dtype
 
 
 def _load():
@@ -133,6 +148,32 @@ def _load():
     lib.meq_canary_count.restype = I
     lib.meq_debug_corrupt_canary.argtypes = [P, I]
     lib.meq_debug_corrupt_canary.restype = I
+    S, PP, I64 = ctypes.c_size_t, ctypes.POINTER(P), ctypes.c_int64
+    lib.meq_adamw_default_options.argtypes = [ctypes.POINTER(MeqAdamWOptions)]
+    lib.meq_adamw_default_options.restype = None
+    lib.meq_adamw_state_bytes.argtypes = [ctypes.POINTER(MeqShape), I, ctypes.POINTER(MeqAdamWOptions), ctypes.POINTER(S),
+                                          ctypes.POINTER(S)]
+    lib.meq_adamw_state_bytes.restype = I
+    lib.meq_adamw_init.argtypes = [ctypes.POINTER(MeqShape), P, I, ctypes.POINTER(MeqAdamWOptions), P, PP]
+    lib.meq_adamw_init.restype = I
+    lib.meq_adamw_grad_norm.argtypes = [P, P, F, P, P]
+    lib.meq_adamw_grad_norm.restype = I
+    lib.meq_adamw_step.argtypes = [P, P, P, P, F, F, P, P]
+    lib.meq_adamw_step.restype = I
+    lib.meq_adamw_state_ptrs.argtypes = [P, PP, PP, PP, PP, ctypes.POINTER(I64)]
+    lib.meq_adamw_state_ptrs.restype = I
+    lib.meq_adamw_read_values.argtypes = [P, P, P, P]
+    lib.meq_adamw_read_values.restype = I
+    lib.meq_adamw_steps.argtypes = [P, ctypes.POINTER(I64)]
+    lib.meq_adamw_steps.restype = I
+    lib.meq_adamw_set_steps.argtypes = [P, I64]
+    lib.meq_adamw_set_steps.restype = I
+    lib.meq_adamw_sync.argtypes = [P]
+    lib.meq_adamw_sync.restype = I
+    lib.meq_adamw_free.argtypes = [P]
+    lib.meq_adamw_free.restype = I
+    lib.meq_adamw_last_error.argtypes = [P]
+    lib.meq_adamw_last_error.restype = ctypes.c_char_p
     return lib
 
 
@@ -233,6 +274,16 @@ def _stream_handle(stream):
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _empty(size, dtype_name, device, stream):
+    """An uninitialised CUDA tensor whose memory belongs to the stream that the call runs on."""
+    import torch
+
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):  # None: the current stream
+        return torch.empty(size, dtype=getattr(torch, dtype_name), device=f"cuda:{device}")
 
 
 class MeqMuon:
@@ -394,6 +445,163 @@ class MeqMuon:
     def close(self):
         if self._st:
             lib.meq_free(self._st)
+            self._st = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------------- AdamW
+def _adamw_options(o, param_dtype, grad_dtype):
+    for what, name in (("param_dtype", param_dtype), ("grad_dtype", grad_dtype)):
+        if name not in DTYPES:
+            raise ValueError(f"{what} must be one of {sorted(DTYPES)}")
+    opts = MeqAdamWOptions()
+    lib.meq_adamw_default_options(ctypes.byref(opts))
+    for k, v in o.items():
+        if not hasattr(opts, k):
+            raise KeyError(k)
+        setattr(opts, k, v)
+    opts.param_type, opts.grad_type = DTYPES[param_dtype], DTYPES[grad_dtype]
+    return opts
+
+
+def adamw_state_bytes(shapes, param_dtype="float32", grad_dtype="float32", **opts):
+    """(persistent, workspace) bytes of an AdamW state, computed on the host (meq_adamw_state_bytes)."""
+    p, w = ctypes.c_size_t(), ctypes.c_size_t()
+    o = _adamw_options(opts, param_dtype, grad_dtype)
+    s = lib.meq_adamw_state_bytes(_shape_array(shapes), len(shapes), ctypes.byref(o), ctypes.byref(p), ctypes.byref(w))
+    if s != MEQ_OK:
+        raise MeqError(s, lib.meq_adamw_last_error(None).decode())
+    return p.value, w.value
+
+
+class _DeviceArray:
+    """Device memory of a state as torch.as_tensor takes it; keeps its owner alive."""
+
+    def __init__(self, owner, ptr, shape, typestr):
+        self._owner = owner
+        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": shape, "typestr": typestr, "version": 2}
+
+
+class AdamW:
+    """AdamW over a fixed list of parameters (rows, cols), with moments in 32
+    or 8 bits (meq_adamw_init). decay: a factor of the weight decay per entry
+    (default 1); options beta1, beta2, eps, state_bits."""
+
+    BLOCK = 256  # each entry's moments start at a multiple of this many elements
+
+    def __init__(self, shapes, stream=None, decay=None, param_dtype="float32", grad_dtype="float32", **opts):
+        import torch
+
+        self.shapes = [(int(r), int(c)) for r, c in shapes]
+        n = len(self.shapes)
+        if decay is not None and len(decay) != n:
+            raise ValueError("one decay factor per shape")
+        self._opts = _adamw_options(opts, param_dtype, grad_dtype)
+        self._param_dtype, self._grad_dtype = getattr(torch, param_dtype), getattr(torch, grad_dtype)
+        self._numels = [r * c for r, c in self.shapes]
+        self._device = torch.cuda.current_device()
+        self._st = ctypes.c_void_p()
+        d = None if decay is None else (ctypes.c_float * n)(*[float(x) for x in decay])
+        s = lib.meq_adamw_init(_shape_array(self.shapes), d, n, ctypes.byref(self._opts), _stream_handle(stream),
+                               ctypes.byref(self._st))
+        if s != MEQ_OK:
+            raise MeqError(s, lib.meq_adamw_last_error(None).decode())
+        self.offsets, at = [], 0  # first element of each entry in the state's arrays
+        for k in self._numels:
+            self.offsets.append(at)
+            at += -(-k // self.BLOCK) * self.BLOCK
+        self._ptrs = ctypes.c_void_p * n
+
+    def _check(self, s):
+        if s != MEQ_OK:
+            raise MeqError(s, lib.meq_adamw_last_error(self._st).decode())
+
+    def _pointers(self, ts, dtype, what):
+        if len(ts) != len(self._numels):
+            raise ValueError(f"{what} must have one tensor per entry")
+        for i, (t, k) in enumerate(zip(ts, self._numels)):
+            if not (t.dtype is dtype and t.is_cuda and t.numel() == k and t.is_contiguous() and t.get_device() == self._device):
+                _require_cuda(t, str(dtype)[6:], k, f"{what}[{i}]", self._device)
+        return self._ptrs(*[t.data_ptr() for t in ts])
+
+    def grad_norm(self, grads, max_norm=float("inf"), out=None, stream=None):
+        """(norm, clipping coefficient) of the gradients as a CUDA tensor of two floats, without a host sync."""
+        if out is None:
+            out = _empty(2, "float32", self._device, stream)
+        else:
+            _require_cuda(out, "float32", 2, "out", self._device)
+        self._check(lib.meq_adamw_grad_norm(self._pointers(grads, self._grad_dtype, "grads"), self._st, float(max_norm),
+                                            ctypes.c_void_p(out.data_ptr()), _stream_handle(stream)))
+        return out
+
+    def step(self, params, grads, lr, weight_decay=0.0, grad_scale=None, copies=None, stream=None):
+        """One step on lists of contiguous CUDA tensors (params updated in place).
+        grad_scale: a CUDA float32 tensor of one element that multiplies the
+        gradients (not finite: the step is skipped); copies: bf16 tensors that
+        receive the updated parameters."""
+        if grad_scale is not None:
+            _require_cuda(grad_scale, "float32", 1, "grad_scale", self._device)
+        c = None
+        if copies is not None:
+            import torch
+
+            c = self._pointers(copies, torch.bfloat16, "copies")
+        self._check(lib.meq_adamw_step(self._pointers(params, self._param_dtype, "params"),
+                                       self._pointers(grads, self._grad_dtype, "grads"), c, self._st, float(lr),
+                                       float(weight_decay),
+                                       None if grad_scale is None else ctypes.c_void_p(grad_scale.data_ptr()),
+                                       _stream_handle(stream)))
+
+    def state(self):
+        """The state's own arrays as CUDA tensors: m and v, or m_code, r_code and
+        their scales per 256 elements (meq_adamw_state_ptrs); copy them to
+        checkpoint and copy into them to resume."""
+        import torch
+
+        p = [ctypes.c_void_p() for _ in range(4)]
+        n = ctypes.c_int64()
+        self._check(lib.meq_adamw_state_ptrs(self._st, *[ctypes.byref(x) for x in p], ctypes.byref(n)))
+        k = n.value
+        if self._opts.state_bits == 32:
+            named = [("m", p[0], k, "<f4"), ("v", p[1], k, "<f4")]
+        else:
+            named = [("m_code", p[0], k, "|i1"), ("r_code", p[1], k, "|u1"), ("m_scale", p[2], k // self.BLOCK, "<f4"),
+                     ("r_scale", p[3], k // self.BLOCK, "<f4")]
+        return {name: torch.as_tensor(_DeviceArray(self, ptr.value, (size,), ts), device=f"cuda:{self._device}")
+                for name, ptr, size, ts in named}
+
+    def read_values(self, m=None, v=None, stream=None):
+        """(m, v) as fp32 CUDA tensors laid out as the state's arrays (entry i at offsets[i])."""
+        k = self.offsets[-1] + -(-self._numels[-1] // self.BLOCK) * self.BLOCK
+        m = _empty(k, "float32", self._device, stream) if m is None else m
+        v = _empty(k, "float32", self._device, stream) if v is None else v
+        _require_cuda(m, "float32", k, "m", self._device)
+        _require_cuda(v, "float32", k, "v", self._device)
+        self._check(lib.meq_adamw_read_values(self._st, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()),
+                                              _stream_handle(stream)))
+        return m, v
+
+    @property
+    def steps(self):
+        """Steps done, skipped ones not counted (waits for them)."""
+        n = ctypes.c_int64()
+        self._check(lib.meq_adamw_steps(self._st, ctypes.byref(n)))
+        return n.value
+
+    def set_steps(self, steps):
+        self._check(lib.meq_adamw_set_steps(self._st, int(steps)))
+
+    def sync(self):
+        self._check(lib.meq_adamw_sync(self._st))
+
+    def close(self):
+        if self._st:
+            lib.meq_adamw_free(self._st)
             self._st = ctypes.c_void_p()
 
     def __del__(self):
