@@ -414,6 +414,75 @@ meq_status meq_adamw_sync(meq_adamw* st);
 meq_status meq_adamw_free(meq_adamw* st);
 const char* meq_adamw_last_error(const meq_adamw* st);
 
+/* ---- losses on token log-probabilities --------------------------------------
+ * The losses of fine-tuning with a policy or with preferences, from logits z
+ * (rows x cols, one row per token) and one target token t_i per row:
+ *
+ *   logp_i = z_{i,t_i} - log sum_j exp(z_ij)
+ *   dL/dz_ij = c_i ([j = t_i] - softmax_j(z_i)),  c_i = grad_scale dL/dlogp_i
+ *
+ * logits: device, of meq_dtype `type`, consecutive columns, rows `ld` elements
+ *   apart (ld >= cols; rows may start at any element). -inf masks a token; a
+ *   row with a NaN or +inf, or with -inf alone, gives NaN.
+ * targets: device int64. A negative target marks a row that is not scored: its
+ *   logits are not read, its logp is 0, its gradient zero. A target >= cols
+ *   gives NaN. In the losses a weight of 0 leaves a row out in the same way.
+ * grad: NULL, or device memory of the logits' type for dL/dz, rows ld_grad
+ *   elements apart, every row written, rounded to nearest once. It may be the
+ *   logits themselves (same pointer, ld_grad = ld), else it must not overlap
+ *   them. Fastest where grad and logits lie at the same offset within 16 bytes
+ *   in every row.
+ * grad_scale: NULL (1), or a device float that multiplies the gradient: the
+ *   incoming gradient of the loss, a loss scale.
+ * work: device scratch of meq_loss_work_floats floats, 16-byte aligned, free
+ *   again when the enqueued kernels have run.
+ * Softmax statistics and all scalars are fp32, sums over rows double, all in
+ * fixed orders: results repeat bit for bit. Nothing is allocated, and the
+ * calls may come from several threads. rows may be 0. Limits: rows <= 2^27,
+ * cols <= 2^28. */
+
+/* logp (rows floats) and, if lse is not NULL, log sum_j exp(z_ij) (0 for rows
+ * that are not scored). */
+meq_status meq_token_logprobs(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
+                              float* logp, float* lse, void* cuda_stream);
+
+/* Floats of `work` for a loss over rows tokens and (meq_preference_loss) pairs
+ * pairs (0: meq_policy_loss). Host only. */
+int64_t meq_loss_work_floats(int64_t rows, int64_t pairs);
+
+/* The clipped policy loss with a KL term. With r = exp(logp - old_logp),
+ * A = advantages, d = ref_logp - logp:
+ *
+ *   L = sum_i w_i (s_i + kl_coef k_i)
+ *   s = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A),  k = exp(d) - d - 1
+ *
+ * weights: w (NULL: 1 for all), e.g. the answer's mask over its length.
+ * ref_logp is read where kl_coef > 0 only. old_logp, advantages, weights,
+ * ref_logp: device, rows floats. sums: device, 4 floats: L, sum w s, sum w k,
+ * and the weight of the rows whose ratio is clipped. logp: device, rows
+ * floats, out. clip_low in 0..1; clip_high, kl_coef >= 0. */
+meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
+                           const float* old_logp, const float* advantages, const float* weights, const float* ref_logp,
+                           float clip_low, float clip_high, float kl_coef, float* sums, float* logp, void* grad,
+                           int64_t ld_grad, const float* grad_scale, float* work, void* cuda_stream);
+
+/* The paired preference loss: rows starts[2j] .. starts[2j+1] - 1 are the
+ * preferred answer of pair j, starts[2j+1] .. starts[2j+2] - 1 the other.
+ *
+ *   x_j = beta (sum_preferred w (logp - ref_logp) - sum_other w (logp - ref_logp))
+ *   L = mean_j (-(1 - e) log sigma(x_j) - e log sigma(-x_j)),  e = label_smoothing
+ *
+ * starts: device, 2 pairs + 1 int64, not decreasing, within 0..rows (an answer
+ * may be empty; a pair whose starts are not so gives NaN and no gradient).
+ * ref_logp per token, as meq_token_logprobs gives it, keeps the small
+ * differences that a sum over an answer would round off. Rows in no answer get
+ * a zero gradient. loss: device float; margins: device, pairs floats, the x_j.
+ * pairs in 1..2^27, beta > 0, label_smoothing in 0..1. */
+meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
+                               const int64_t* starts, int64_t pairs, const float* ref_logp, const float* weights, float beta,
+                               float label_smoothing, float* loss, float* margins, float* logp, void* grad, int64_t ld_grad,
+                               const float* grad_scale, float* work, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,6 +6,7 @@ importing this module raises.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -71,6 +72,7 @@ EXPORTED = [
     "meq_adamw_default_options", "meq_adamw_state_bytes", "meq_adamw_init", "meq_adamw_grad_norm", "meq_adamw_step",
     "meq_adamw_state_ptrs", "meq_adamw_read_values", "meq_adamw_steps", "meq_adamw_set_steps", "meq_adamw_sync",
     "meq_adamw_free", "meq_adamw_last_error",
+    "meq_token_logprobs", "meq_loss_work_floats", "meq_policy_loss", "meq_preference_loss",
 ]
 HIDDEN, REMAINING_2D, VECTOR = 0, 1, 2  # meq_kind
 RULE_MEQMUON, RULE_MUON = 0, 1          # meq_update_rule
@@ -174,6 +176,14 @@ def _load():
     lib.meq_adamw_free.restype = I
     lib.meq_adamw_last_error.argtypes = [P]
     lib.meq_adamw_last_error.restype = ctypes.c_char_p
+    lib.meq_token_logprobs.argtypes = [P, I, I64, I64, I64, P, P, P, P]
+    lib.meq_token_logprobs.restype = I
+    lib.meq_loss_work_floats.argtypes = [I64, I64]
+    lib.meq_loss_work_floats.restype = I64
+    lib.meq_policy_loss.argtypes = [P, I, I64, I64, I64, P, P, P, P, P, F, F, F, P, P, P, I64, P, P, P]
+    lib.meq_policy_loss.restype = I
+    lib.meq_preference_loss.argtypes = [P, I, I64, I64, I64, P, P, I64, P, P, F, F, P, P, P, P, I64, P, P, P]
+    lib.meq_preference_loss.restype = I
     return lib
 
 
@@ -280,9 +290,11 @@ def _empty(size, dtype_name, device, stream):
     """An uninitialised CUDA tensor whose memory belongs to the stream that the call runs on."""
     import torch
 
+    if stream is None:
+        return torch.empty(size, dtype=getattr(torch, dtype_name), device=f"cuda:{device}")
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
-    with torch.cuda.stream(stream):  # None: the current stream
+    with torch.cuda.stream(stream):
         return torch.empty(size, dtype=getattr(torch, dtype_name), device=f"cuda:{device}")
 
 
@@ -609,3 +621,118 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+# --------------------------------------------------------------------- losses
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logp lse")
+PolicyLoss = collections.namedtuple("PolicyLoss", "loss sums logp grad")
+PreferenceLoss = collections.namedtuple("PreferenceLoss", "loss margins logp grad")
+
+
+def _logits_args(logits, what="logits"):
+    """(dtype name, rows, cols, row stride) of a CUDA matrix whose columns are consecutive."""
+    name = str(logits.dtype)[6:]
+    if not logits.is_cuda or name not in DTYPES or logits.dim() != 2:
+        raise ValueError(f"{what} must be a CUDA matrix of one of {sorted(DTYPES)}")
+    rows, cols = logits.shape
+    if cols < 1 or (cols > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < cols):
+        raise ValueError(f"{what} must have consecutive columns in rows that do not overlap")
+    return name, rows, cols, max(logits.stride(0), cols)
+
+
+def _vector(t, dtype_name, n, device, what):
+    """The device pointer of a contiguous CUDA vector, or None."""
+    if t is None:
+        return None
+    _require_cuda(t, dtype_name, n, what, device)
+    return t.data_ptr()
+
+
+def _grad_for(logits, grad, stream):
+    """The gradient's tensor: None, the given one, or (True) a new one whose rows
+    lie in their 16 bytes as the logits' do."""
+    if grad is None or grad is False:
+        return None, 0
+    name, rows, cols, ld = _logits_args(logits)
+    if grad is True:
+        n = 16 // logits.element_size()
+        lead, ldg = logits.data_ptr() % 16 // logits.element_size(), cols + (ld - cols) % n
+        flat = _empty(rows * ldg + n, name, logits.device.index, stream)
+        return flat.as_strided((rows, cols), (ldg, 1), lead), ldg
+    if grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.device != logits.device:
+        raise ValueError("grad must have the logits' shape, type and device")
+    return grad, _logits_args(grad, "grad")[3]
+
+
+def _current_device(t, what):
+    import torch
+
+    device = t.device.index
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{what} is on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return device
+
+
+def _check_loss(s):
+    if s != MEQ_OK:
+        raise MeqError(s, lib.meq_last_error(None).decode())
+
+
+def token_logprobs(logits, targets, stream=None):
+    """Log-probabilities of the target tokens and the rows' log-sum-exp
+    (meq_token_logprobs). logits: CUDA matrix, fp32, bf16 or fp16, one row per
+    token; targets: int64, negative where a row is not scored."""
+    name, rows, cols, ld = _logits_args(logits)
+    device = _current_device(logits, "logits")
+    t = _vector(targets, "int64", rows, device, "targets")
+    out = _empty((2, rows), "float32", device, stream)
+    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, out.data_ptr(),
+                                       out.data_ptr() + 4 * rows, _stream_handle(stream)))
+    return TokenLogprobs(out[0], out[1])
+
+
+def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
+                grad=None, grad_scale=None, stream=None):
+    """The clipped policy loss with a KL term and, if asked for, the gradient of
+    the logits (meq_policy_loss). grad: True for a new tensor, or the tensor to
+    write (it may be logits). sums holds the loss, its surrogate and KL parts
+    and the clipped weight; loss is its first entry."""
+    name, rows, cols, ld = _logits_args(logits)
+    device = _current_device(logits, "logits")
+    vectors = [_vector(t, "float32", rows, device, what) for t, what in
+               ((old_logp, "old_logp"), (advantages, "advantages"), (weights, "weights"), (ref_logp, "ref_logp"))]
+    t = _vector(targets, "int64", rows, device, "targets")
+    scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
+    grad, ldg = _grad_for(logits, grad, stream)
+    work = _empty(lib.meq_loss_work_floats(rows, 0) + rows + 4, "float32", device, stream)
+    sums, logp = work[-4:], work[-4 - rows:-4] if rows else work[:0]
+    _check_loss(lib.meq_policy_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, *vectors, float(clip_low),
+                                    float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(),
+                                    None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
+                                    _stream_handle(stream)))
+    return PolicyLoss(sums[0], sums, logp, grad)
+
+
+def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, label_smoothing=0.0, grad=None, grad_scale=None,
+                    stream=None):
+    """The paired preference loss and, if asked for, the gradient of the logits
+    (meq_preference_loss). starts: int64 CUDA vector of 2 pairs + 1 row offsets,
+    preferred and other answer in turn; grad as in policy_loss."""
+    name, rows, cols, ld = _logits_args(logits)
+    device = _current_device(logits, "logits")
+    if starts.numel() < 3 or starts.numel() % 2 == 0:
+        raise ValueError("starts must hold 2 pairs + 1 offsets")
+    pairs = starts.numel() // 2
+    st = _vector(starts, "int64", 2 * pairs + 1, device, "starts")
+    vectors = [_vector(t, "float32", rows, device, what) for t, what in ((ref_logp, "ref_logp"), (weights, "weights"))]
+    t = _vector(targets, "int64", rows, device, "targets")
+    scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
+    grad, ldg = _grad_for(logits, grad, stream)
+    n = lib.meq_loss_work_floats(rows, pairs)
+    work = _empty(n + rows + pairs + 1, "float32", device, stream)
+    logp, margins, loss = work[n:n + rows], work[n + rows:n + rows + pairs], work[n + rows + pairs]
+    _check_loss(lib.meq_preference_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, st, pairs, *vectors, float(beta),
+                                        float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(),
+                                        None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
+                                        _stream_handle(stream)))
+    return PreferenceLoss(loss, margins, logp, grad)
