@@ -381,7 +381,7 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
 /* out[0] = the Euclidean norm of all gradients together, out[1] = the
  * coefficient that brings it to at most max_norm (1 if it is there; NaN if the
  * norm is not finite in fp32). out: device, two floats. max_norm > 0, may be
- * infinite. Sums of squares: fp32 per thread, then double, in a fixed order. */
+ * infinite. Sums of squares: fp32 per thread, then compensated, in a fixed order. */
 meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float max_norm, float* out, void* cuda_stream);
 /* One step. params (updated in place) and grads: device, contiguous, of the
  * state's types. copies: NULL, or per entry a device bf16 tensor of its size
@@ -436,8 +436,8 @@ const char* meq_adamw_last_error(const meq_adamw* st);
  *   incoming gradient of the loss, a loss scale.
  * work: device scratch of meq_loss_work_floats floats, 16-byte aligned, free
  *   again when the enqueued kernels have run.
- * Softmax statistics and all scalars are fp32, sums over rows double, all in
- * fixed orders: results repeat bit for bit. Nothing is allocated, and the
+ * Softmax statistics and all scalars are fp32, sums over rows compensated, all
+ * in fixed orders: results repeat bit for bit. Nothing is allocated, and the
  * calls may come from several threads. rows may be 0. Limits: rows <= 2^27,
  * cols <= 2^28. */
 

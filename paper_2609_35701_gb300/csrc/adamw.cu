@@ -70,9 +70,10 @@ struct AdamClock {
 };
 
 __host__ __device__ inline void set_clock(AdamClock* c, double b1t, double b2t, long long steps) {
+  // only the differences need double, whose division and root are slow on this GPU
   c->b1t = b1t, c->b2t = b2t, c->steps = steps;
-  c->inv_bc1 = static_cast<float>(1.0 / (1.0 - b1t));
-  c->inv_sqrt_bc2 = static_cast<float>(1.0 / sqrt(1.0 - b2t));
+  c->inv_bc1 = 1.f / static_cast<float>(1.0 - b1t);
+  c->inv_sqrt_bc2 = 1.f / sqrtf(static_cast<float>(1.0 - b2t));
 }
 
 struct AdamArgs {
@@ -97,7 +98,7 @@ struct NormArgs {
   const AdamEntry* entries;
   const int32_t* chunk_entry;
   AdamClock* clock;
-  double* partials;
+  float* partials;
   float* out;
   float max_norm;
   int32_t entry0, last, part0, parts;  // first partial of this launch; partials of all launches
@@ -308,28 +309,16 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   }
 }
 
-// Sum over the block, in double, in a fixed order; thread 0 has it.
-__device__ __forceinline__ double block_sum(double x, double* sh) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double s = 0.0;
-  if (threadIdx.x == 0)
-    for (int i = 0; i < kAdamThreads / 32; ++i) s += sh[i];
-  return s;
-}
-
 // out[0] = sqrt(sum g^2), out[1] = the coefficient that brings it to at most
 // max_norm. Bound by the one read of the gradients. A thread adds the squares
-// of its share in fp32 (eight sums side by side), the rest is added in double;
-// the blocks' sums lie in `partials` and the last block to finish adds them up,
+// of its share in fp32 (eight sums side by side), the rest is added as
+// WideSum; the blocks' sums lie in `partials` and the last block to finish adds them up,
 // in an order that does not depend on which block that is.
 template <typename G>
 __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_constant__ NormArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ double sh[kAdamThreads / 32];
+  __shared__ WideSum sh[2][kAdamThreads / 32];
   __shared__ bool final_block;
   const int lane = threadIdx.x & 31;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -348,10 +337,10 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
   }
-  double t = 0.0;
+  WideSum t;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) t += static_cast<double>(acc[i]);
-  const double s = block_sum(t, sh);
+  for (int i = 0; i < 8; ++i) t.add(acc[i]);
+  const float s = block_total(t, sh[0]);
   if (threadIdx.x == 0) {
     a.partials[a.part0 + blockIdx.x] = s;
     __threadfence();
@@ -360,12 +349,11 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   __syncthreads();
   if (!final_block) return;
   __threadfence();
-  double all = 0.0;
-  for (int i = threadIdx.x; i < a.parts; i += kAdamThreads) all += __ldcg(a.partials + i);
-  __syncthreads();  // sh is free again
-  all = block_sum(all, sh);
+  WideSum all;
+  for (int i = threadIdx.x; i < a.parts; i += kAdamThreads) all.add(__ldcg(a.partials + i));
+  const float total = block_total(all, sh[1]);
   if (threadIdx.x == 0) {
-    const float norm = static_cast<float>(sqrt(all));
+    const float norm = __fsqrt_rn(total);
     a.out[0] = norm;
     a.out[1] = !(norm <= FLT_MAX) ? __int_as_float(0x7fc00000) : norm > a.max_norm ? __fdiv_rn(a.max_norm, norm) : 1.f;
   }
@@ -419,7 +407,7 @@ struct meq_adamw {
   AdamEntry* d_entries = nullptr;
   int32_t* d_chunk_entry = nullptr;
   AdamClock* d_clock = nullptr;
-  double* d_partials = nullptr;
+  float* d_partials = nullptr;
   cudaStream_t last_stream = nullptr;
   std::string last_error;
 };
@@ -506,7 +494,7 @@ Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_ada
   P.o_entries = add(static_cast<int64_t>(n) * sizeof(AdamEntry));
   P.o_chunks = add(P.chunks * 4);
   P.o_clock = add(sizeof(AdamClock));
-  P.o_partials = add(static_cast<int64_t>(P.total_parts) * 8);
+  P.o_partials = add(static_cast<int64_t>(P.total_parts) * 4);
   P.persistent = 2 * (P.elements * each + scales);
   return P;
 }
@@ -625,7 +613,7 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
     st->d_entries = reinterpret_cast<AdamEntry*>(A + P.o_entries);
     st->d_chunk_entry = reinterpret_cast<int32_t*>(A + P.o_chunks);
     st->d_clock = reinterpret_cast<AdamClock*>(A + P.o_clock);
-    st->d_partials = reinterpret_cast<double*>(A + P.o_partials);
+    st->d_partials = reinterpret_cast<float*>(A + P.o_partials);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     e = cudaMemsetAsync(A, 0, static_cast<size_t>(P.total), s);
     if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_entries, P.entries.data(), sizeof(AdamEntry) * n, cudaMemcpyHostToDevice, s);

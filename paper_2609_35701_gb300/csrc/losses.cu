@@ -34,12 +34,13 @@ using namespace meq;
 namespace {
 
 constexpr int kPieces = 8;          // 16-byte pieces per thread
+constexpr int kChunkPieces = 32 * kPieces;  // of a warp
 constexpr int kMaxCluster = 8;
 constexpr int kRowThreads = 512;    // most threads of a CTA before the cluster grows
 constexpr int kRowThreadsMax = 1024;
 constexpr int kGradThreads = 256;
 constexpr int kGradPieces = 4;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950216293335f;  // and kLog2eLo
 
 struct RowArgs {
   const void* logits;
@@ -62,11 +63,47 @@ struct RowArgs {
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// exp(x - m); m is finite or the result is NaN (0 for x = -inf where m is a stand-in)
-__device__ __forceinline__ float exp_diff(float x, float m) { return exp2_approx((x - m) * kLog2e); }
+// Two fp32 operations in one instruction, each rounded as a single one is.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)), "l"(*reinterpret_cast<uint64_t*>(&c)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return *reinterpret_cast<float2*>(&d);
+}
+// exp(a - b) for the few joins of statistics (0 for a = -inf and any finite b)
+__device__ __forceinline__ float exp_diff(float a, float b) { return exp2_approx((a - b) * kLog2e); }
+
+// exp(x - m) as 2^(x log2e - c) with c = m log2e rounded: one multiply-add per
+// element (its product is not rounded, so no x overflows it), and the rounding
+// of c undone once, by the factor `fix`. m: finite, at most kFar in magnitude,
+// where c is off by less than 0.1. log2e in two parts: the first alone is off
+// by 1.3e-8 of itself, which would bias a sum by as much per unit of m - x; a
+// single element can do without the second part (fix_hi).
+constexpr float kLog2eLo = 1.9259629911266175e-8f;
+constexpr float kFar = 1e6f;
+struct ExpBase {
+  float c, fix, fix_hi;
+  __device__ __forceinline__ explicit ExpBase(float m) {
+    c = m * kLog2e;
+    const float off = fmaf(m, kLog2e, -c);
+    fix = exp2_approx(-fmaf(m, kLog2eLo, off));
+    fix_hi = exp2_approx(-off);
+  }
+};
 
 template <typename T>
 struct Elem;  // 16-bit and 32-bit logits
@@ -74,11 +111,12 @@ template <>
 struct Elem<float> {
   static constexpr int N = 4;
   static constexpr uint32_t kNegInf = 0xFF800000u;
-  static __device__ __forceinline__ void unpack(uint4 q, float* x) {
-    x[0] = __uint_as_float(q.x), x[1] = __uint_as_float(q.y), x[2] = __uint_as_float(q.z), x[3] = __uint_as_float(q.w);
+  static __device__ __forceinline__ void unpack(uint4 q, float2* x) {
+    x[0] = make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
+    x[1] = make_float2(__uint_as_float(q.z), __uint_as_float(q.w));
   }
-  static __device__ __forceinline__ uint4 pack(const float* x) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  static __device__ __forceinline__ uint4 pack(const float2* x) {
+    return make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
   }
   static __device__ __forceinline__ float get(const float* p) { return *p; }
   using Max = float;  // running maximum of the elements of pieces
@@ -88,24 +126,22 @@ struct Elem<float> {
   static __device__ __forceinline__ Max none() { return -INFINITY; }
   static __device__ __forceinline__ float value(Max m) { return m; }
   using Bits = uint32_t;
+  static __device__ __forceinline__ float make(float x) { return x; }
 };
 template <>
 struct Elem<__nv_bfloat16> {
   static constexpr int N = 8;
   static constexpr uint32_t kNegInf = 0xFF80FF80u;
-  static __device__ __forceinline__ void unpack(uint4 q, float* x) {
+  static __device__ __forceinline__ void unpack(uint4 q, float2* x) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
-  static __device__ __forceinline__ uint4 pack(const float* x) {
+  static __device__ __forceinline__ uint4 pack(const float2* x) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[i].x, x[i].y);
       w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -122,24 +158,22 @@ struct Elem<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
   using Bits = uint16_t;
+  static __device__ __forceinline__ __nv_bfloat16 make(float x) { return __float2bfloat16_rn(x); }
 };
 template <>
 struct Elem<__half> {
   static constexpr int N = 8;
   static constexpr uint32_t kNegInf = 0xFC00FC00u;
-  static __device__ __forceinline__ void unpack(uint4 q, float* x) {
+  static __device__ __forceinline__ void unpack(uint4 q, float2* x) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      x[2 * i] = f.x, x[2 * i + 1] = f.y;
-    }
+    for (int i = 0; i < 4; ++i) x[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
   }
-  static __device__ __forceinline__ uint4 pack(const float* x) {
+  static __device__ __forceinline__ uint4 pack(const float2* x) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      const __half2 h = __floats2half2_rn(x[i].x, x[i].y);
       w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -156,6 +190,7 @@ struct Elem<__half> {
   }
   static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
   using Bits = uint16_t;
+  static __device__ __forceinline__ __half make(float x) { return __float2half_rn(x); }
 };
 
 // The 128 bits of a piece moved by one element towards its end or its start,
@@ -187,14 +222,18 @@ __device__ __forceinline__ uint32_t pop_front(uint4& q, T) {
 
 // A row cut at the 16-byte boundaries of its address: piece k holds elements
 // k N - lead .. k N - lead + N - 1 of the row, as far as they exist. Pieces
-// `begin` .. `end` - 1 exist whole; at most the first and the last do not.
+// `begin` .. `end` - 1 exist whole; at most the first and the last do not. A
+// warp takes chunks of 32 P consecutive pieces, lane l pieces l, l + 32, .. of
+// it: of a chunk that exists whole every access has a fixed distance from the
+// lane's first, and only the row's first and last chunk look at their pieces
+// one by one.
 template <typename T>
 struct Row {
   static constexpr int N = Elem<T>::N;
   using Bits = typename Elem<T>::Bits;
-  const T* p;   // element 0
+  const T* p;  // element 0
   int cols;
-  int lead;     // elements of the first 16 bytes that precede the row
+  int lead;    // elements of the first 16 bytes that precede the row
   int pieces, begin, end;
   __device__ __forceinline__ Row(const void* base, int64_t row, int64_t ld, int64_t cols_)
       : p(static_cast<const T*>(base) + row * ld), cols(static_cast<int>(cols_)) {
@@ -203,29 +242,81 @@ struct Row {
     begin = lead > 0 ? 1 : 0;
     end = (cols + lead) / N;
   }
-  __device__ __forceinline__ bool whole(int k) const { return k >= begin && k < end; }
-  __device__ __forceinline__ uint4 load(int k) const {
-    if (whole(k)) return __ldcs(reinterpret_cast<const uint4*>(p + (k * N - lead)));
-    uint4 q = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
-    if (k < pieces) {
-      const Bits* b = reinterpret_cast<const Bits*>(p);
-#pragma unroll 1
-      for (int i = k * N - lead + N - 1; i >= k * N - lead; --i)
-        push_front(q, i >= 0 && i < cols ? b[i] : static_cast<Bits>(Elem<T>::kNegInf), T());
+  // A piece that does not exist whole, element by element.
+  __device__ __forceinline__ uint4 load_part(int k) const {
+    const Bits* b = reinterpret_cast<const Bits*>(p);
+    uint4 q = none();
+#pragma unroll
+    for (int e = N - 1; e >= 0; --e) {
+      const int i = k * N - lead + e;
+      push_front(q, i >= 0 && i < cols ? b[i] : static_cast<Bits>(Elem<T>::kNegInf), T());
     }
     return q;
   }
-  // Piece k (< pieces) of the gradient's row g; `same`: g has the same offset in its 16 bytes as p.
-  __device__ __forceinline__ void store(T* g, bool same, int k, uint4 q) const {
-    if (same && whole(k)) {
-      __stcs(reinterpret_cast<uint4*>(g + (k * N - lead)), q);
-      return;
-    }
+  __device__ __forceinline__ void store_part(T* g, int k, uint4 q) const {
     Bits* b = reinterpret_cast<Bits*>(g);
 #pragma unroll 1
     for (int i = k * N - lead; i < k * N - lead + N; ++i) {
       const uint32_t bits = pop_front(q, T());
       if (i >= 0 && i < cols) b[i] = static_cast<Bits>(bits);
+    }
+  }
+  static __device__ __forceinline__ uint4 none() {
+    return make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
+  }
+  // Whether the row's last piece is a part, and this lane's (as its piece last_of / 32).
+  template <int P>
+  __device__ __forceinline__ bool last_part(int k0, int* last_of) const {
+    *last_of = pieces - 1 - k0;
+    return pieces > end && pieces > begin && *last_of >= 0 && *last_of < 32 * P && *last_of % 32 == 0;
+  }
+  // Pieces k0 + 32 j of the chunk that starts at piece `first` (-inf where there is none); k0 = first + lane.
+  template <int P>
+  __device__ __forceinline__ void load(int first, int k0, uint4 (&q)[P]) const {
+    const uint4* s = reinterpret_cast<const uint4*>(p + (k0 * N - lead));
+    if (first >= begin && first + 32 * P <= end) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) q[j] = __ldcs(s + 32 * j);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const int k = k0 + 32 * j;
+      q[j] = none();
+      if (k >= begin && k < end) q[j] = __ldcs(s + 32 * j);
+    }
+    if (k0 < begin) q[0] = load_part(0);
+    int last;
+    if (last_part<P>(k0, &last)) {
+      const uint4 x = load_part(pieces - 1);
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+        if (32 * j == last) q[j] = x;
+    }
+  }
+  // f(x) of each piece x = q[j] into the gradient's row g. `same`: g has the same offset in its 16 bytes as p.
+  template <int P, typename F>
+  __device__ __forceinline__ void store(T* g, bool same, int first, int k0, const uint4 (&q)[P], F f) const {
+    uint4* d = reinterpret_cast<uint4*>(g + (k0 * N - lead));
+    if (same && first >= begin && first + 32 * P <= end) {
+#pragma unroll
+      for (int j = 0; j < P; ++j) __stcs(d + 32 * j, f(q[j]));
+    } else if (same) {
+      int last;
+      const bool part = last_part<P>(k0, &last);
+      uint4 x = q[0];
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const int k = k0 + 32 * j;
+        if (k >= begin && k < end) __stcs(d + 32 * j, f(q[j]));
+        if (32 * j == last) x = q[j];
+      }
+      if (k0 < begin) store_part(g, 0, f(q[0]));
+      if (part) store_part(g, pieces - 1, f(x));
+    } else {
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+        if (k0 + 32 * j < pieces) store_part(g, k0 + 32 * j, f(q[j]));
     }
   }
 };
@@ -234,26 +325,57 @@ __device__ __forceinline__ bool same_offset(const void* a, const void* b) {
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// Pieces k0, k0 + step, .. < k1 of a gradient row set to zero.
-template <typename T>
-__device__ __forceinline__ void zero_pieces(const Row<T>& r, T* g, bool same, int k0, int k1, int step) {
-  for (int k = k0; k < k1; k += step) r.store(g, same, k, make_uint4(0u, 0u, 0u, 0u));
-}
-// c ([j = target] - exp(z_j - top) / sum) of one piece, neg = -c / sum
-template <typename T>
-__device__ __forceinline__ void grad_piece(const Row<T>& r, T* g, bool same, int k, uint4 q, float top, float neg, float c,
-                                           int64_t target) {
-  float x[Elem<T>::N];
-  Elem<T>::unpack(q, x);
-#pragma unroll
-  for (int e = 0; e < Elem<T>::N; ++e) x[e] = exp_diff(x[e], top) * neg;
-  const int off = static_cast<int>(target) + r.lead - k * Elem<T>::N;  // target < cols where c is finite and not 0
-  if (off >= 0 && off < Elem<T>::N) {
-#pragma unroll
-    for (int e = 0; e < Elem<T>::N; ++e)
-      if (e == off) x[e] += c;
+// What turns logits into gradients: c ([j = target] - exp(z_j - top) / sum).
+struct GradScale {
+  float c, base, neg;  // neg = -c / sum with the base's fix
+  bool far;            // |top| above kFar (masks of a type's lowest value, all of a row's): exp(z - top) step by step
+  float top;
+  __device__ __forceinline__ GradScale(float c_, float top_, float sum) : c(c_), top(top_) {
+    far = !(fabsf(top_) <= kFar);
+    const ExpBase b(far ? 0.f : top_);
+    base = b.c;
+    neg = -c_ / sum * b.fix_hi;
   }
-  r.store(g, same, k, Elem<T>::pack(x));
+  // of tokens that are not the target
+  template <bool kFarTop>
+  __device__ __forceinline__ float2 other(float2 x) const {
+    if (kFarTop) return make_float2(exp_diff(x.x, top) * neg, exp_diff(x.y, top) * neg);
+    x = fma2(x, make_float2(kLog2e, kLog2e), make_float2(-base, -base));
+    return mul2(make_float2(exp2_approx(x.x), exp2_approx(x.y)), make_float2(neg, neg));
+  }
+};
+// Whether this lane holds the target's piece (no lane does for kNoToken).
+constexpr int kNoToken = -(1 << 30);
+template <typename T, int P>
+__device__ __forceinline__ bool holds(const Row<T>& r, int k0, int target) {
+  const unsigned at = static_cast<unsigned>((target + r.lead) / Elem<T>::N - k0);
+  return at < 32u * P && at % 32u == 0u;
+}
+// The gradient of a chunk. The target's token is written once more, by the
+// thread that has just written its piece (and alone needs zt).
+template <bool kFarTop, typename T, int P>
+__device__ __forceinline__ void store_grad_of(const Row<T>& r, T* g, bool same, int first, int k0, const uint4 (&q)[P],
+                                              const GradScale& s, int target, float zt) {
+  constexpr int H = Elem<T>::N / 2;
+  r.template store<P>(g, same, first, k0, q, [&](uint4 piece) {
+    float2 x[H];
+    Elem<T>::unpack(piece, x);
+#pragma unroll
+    for (int e = 0; e < H; ++e) x[e] = s.template other<kFarTop>(x[e]);
+    return Elem<T>::pack(x);
+  });
+  if (holds<T, P>(r, k0, target)) g[target] = Elem<T>::make(s.template other<kFarTop>(make_float2(zt, zt)).x + s.c);
+}
+template <typename T, int P>
+__device__ __forceinline__ void store_grad(const Row<T>& r, T* g, bool same, int first, int k0, const uint4 (&q)[P],
+                                           const GradScale& s, int target, float zt) {
+  if (s.far) store_grad_of<true>(r, g, same, first, k0, q, s, target, zt);
+  else store_grad_of<false>(r, g, same, first, k0, q, s, target, zt);
+}
+template <typename T, int P>
+__device__ __forceinline__ void store_zeros(const Row<T>& r, T* g, bool same, int first, int k0) {
+  const uint4 q[P] = {};
+  r.template store<P>(g, same, first, k0, q, [](uint4 piece) { return piece; });
 }
 
 // Running maximum and sum of exponentials relative to it.
@@ -293,11 +415,13 @@ __device__ __forceinline__ MaxSum row_join(MaxSum w, RowShared& sh, uint32_t ran
   __syncthreads();
   MaxSum t{-INFINITY, 0.f};
   if (lane < warps) t = sh.warp[lane];
+  float m = t.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    MaxSum b{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o)};
-    t = join(t, b);
-  }
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  t.s *= exp_diff(t.m, finite_or_zero(m));
+  t.m = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
   if (ctas == 1) return t;
   // every CTA of the cluster has begun (the wait of the arrive at the kernel's start)
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -316,7 +440,7 @@ __device__ __forceinline__ MaxSum row_join(MaxSum w, RowShared& sh, uint32_t ran
 
 // max and sum of exponentials over a warp's pieces, for all its lanes
 template <typename T>
-__device__ __forceinline__ MaxSum warp_stats(const uint4* q) {
+__device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[kPieces]) {
   MaxSum w;
   typename Elem<T>::Max top = Elem<T>::none();
 #pragma unroll
@@ -325,16 +449,33 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4* q) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   w.m = m;
-  const float base = finite_or_zero(m);
-  float s[2] = {0.f, 0.f};
+  constexpr int H = Elem<T>::N / 2;
+  float2 s = make_float2(0.f, 0.f);
+  if (fabsf(m) <= kFar || m == -INFINITY) {
+    const ExpBase b(finite_or_zero(m));
 #pragma unroll
-  for (int j = 0; j < kPieces; ++j) {
-    float x[Elem<T>::N];
-    Elem<T>::unpack(q[j], x);
+    for (int j = 0; j < kPieces; ++j) {
+      float2 x[H];
+      Elem<T>::unpack(q[j], x);
 #pragma unroll
-    for (int e = 0; e < Elem<T>::N; ++e) s[e & 1] += exp_diff(x[e], base);
+      for (int e = 0; e < H; ++e) {
+        const float2 y = fma2(x[e], make_float2(kLog2e, kLog2e), make_float2(-b.c, -b.c));
+        const float2 z = fma2(x[e], make_float2(kLog2eLo, kLog2eLo), y);
+        s = add2(s, make_float2(exp2_approx(z.x), exp2_approx(z.y)));
+      }
+    }
+    w.s = (s.x + s.y) * b.fix;
+  } else {
+    // far from zero (+inf gives NaN)
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      float2 x[H];
+      Elem<T>::unpack(q[j], x);
+#pragma unroll
+      for (int e = 0; e < H; ++e) s = add2(s, make_float2(exp_diff(x[e].x, m), exp_diff(x[e].y, m)));
+    }
+    w.s = s.x + s.y;
   }
-  w.s = s[0] + s[1];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) w.s += __shfl_xor_sync(0xffffffffu, w.s, o);
   return w;
@@ -379,40 +520,37 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
   const int64_t target = a.targets[row];
   float w = 1.f;
   if (a.weights) w = a.weights[row];
-  const int threads = static_cast<int>(blockDim.x), tid = static_cast<int>(threadIdx.x);
+  const int warps = static_cast<int>(blockDim.x >> 5);
+  const int first = (static_cast<int>(rank) * warps + static_cast<int>(threadIdx.x >> 5)) * kChunkPieces;  // the warp's chunk
+  const int k0 = first + static_cast<int>(threadIdx.x & 31);
   T* g = nullptr;
   if (kPolicy && a.grad) g = static_cast<T*>(a.grad) + row * a.ld_grad;
   const bool same = same_offset(r.p, g);
-  const bool first = rank == 0 && tid == 0;
+  const bool leader = rank == 0 && threadIdx.x == 0;
   if (target < 0 || w == 0.f) {  // not scored: the logits are not read
-    if (first) {
+    if (leader) {
       a.logp[row] = 0.f;
       if (a.lse) a.lse[row] = 0.f;
       if (a.stat) a.stat[row] = make_float2(0.f, 1.f);
       if (a.coef) a.coef[row] = 0.f;
       if (kPolicy) a.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    if (kPolicy && g) {
-      const int span = kPieces * threads, k0 = static_cast<int>(rank) * span;
-      zero_pieces(r, g, same, k0 + tid, min(r.pieces, k0 + span), threads);
-    }
+    if (kPolicy && g) store_zeros<T, kPieces>(r, g, same, first, k0);
     if (ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     return;
   }
   // beyond the row: no such token, everything that depends on it is NaN
-  const float zt = target < a.cols ? Elem<T>::get(r.p + target) : __int_as_float(0x7fc00000);
+  const int token = target < a.cols ? static_cast<int>(target) : kNoToken;
+  const float zt = token != kNoToken ? Elem<T>::get(r.p + token) : __int_as_float(0x7fc00000);
   uint4 q[kPieces];
   MaxSum ws{-INFINITY, 0.f};
-  const int k0 = static_cast<int>(rank) * kPieces * threads + tid;
   if (kPolicy) {
-#pragma unroll
-    for (int j = 0; j < kPieces; ++j) q[j] = r.load(k0 + j * threads);
+    r.load(first, k0, q);
     ws = warp_stats<T>(q);
   } else {
-    const int step = static_cast<int>(ctas) * kPieces * threads;
-    for (int k = k0; k - tid < r.pieces; k += step) {  // the same rounds for all threads of the CTA
-#pragma unroll
-      for (int j = 0; j < kPieces; ++j) q[j] = r.load(k + j * threads);
+    const int step = static_cast<int>(ctas) * warps * kChunkPieces;
+    for (int k = 0; first + k < r.pieces; k += step) {
+      r.load(first + k, k0 + k, q);
       ws = join(ws, warp_stats<T>(q));
     }
   }
@@ -420,7 +558,7 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
   const float logs = logf(all.s);
   const float logp = (zt - all.m) - logs;
   if (!kPolicy) {
-    if (first) {
+    if (leader) {
       a.logp[row] = logp;
       if (a.lse) a.lse[row] = all.m + logs;
       if (a.stat) a.stat[row] = make_float2(all.m, all.s);
@@ -429,22 +567,17 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
     return;
   }
   const TokenLoss t = policy_token(logp, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
-  if (first) {
+  if (leader) {
     a.logp[row] = logp;
     a.terms[row] = make_float4(w * (t.surrogate + a.kl * t.k3), w * t.surrogate, w * t.k3, w * t.clipped);
   }
   if (!g) return;
   const float c = w * t.slope * (a.grad_scale ? *a.grad_scale : 1.f);
   if (c == 0.f) {
-    zero_pieces(r, g, same, k0, min(r.pieces, k0 - tid + kPieces * threads), threads);
+    store_zeros<T, kPieces>(r, g, same, first, k0);
     return;
   }
-  const float neg = -c / all.s;
-#pragma unroll
-  for (int j = 0; j < kPieces; ++j) {
-    const int k = k0 + j * threads;
-    if (k < r.pieces) grad_piece(r, g, same, k, q[j], all.m, neg, c, target);
-  }
+  store_grad(r, g, same, first, k0, q, GradScale(c, all.m, all.s), token, zt);
 }
 
 // The policy terms and coefficients of rows whose statistics are known.
@@ -471,38 +604,24 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, int
   for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
     const int64_t row = a.rows - 1 - b / tiles;
     const Row<T> r(a.logits, row, a.ld, a.cols);
-    const int k0 = static_cast<int>(b % tiles) * kGradPieces * kGradThreads + static_cast<int>(threadIdx.x);
+    const int first = (static_cast<int>(b % tiles) * (kGradThreads / 32) + static_cast<int>(threadIdx.x >> 5)) * 32 * kGradPieces;
+    const int k0 = first + static_cast<int>(threadIdx.x & 31);
     T* g = static_cast<T*>(a.grad) + row * a.ld_grad;
     const bool same = same_offset(r.p, g);
     const float c = a.coef[row];
     if (c == 0.f) {
-      zero_pieces(r, g, same, k0, min(r.pieces, k0 + kGradPieces * kGradThreads), kGradThreads);
+      store_zeros<T, kGradPieces>(r, g, same, first, k0);
       continue;
     }
     const float2 stat = a.stat[row];
-    const float neg = -c / stat.y;
     const int64_t target = a.targets[row];
     uint4 q[kGradPieces];
-#pragma unroll
-    for (int j = 0; j < kGradPieces; ++j) q[j] = r.load(k0 + j * kGradThreads);
-#pragma unroll
-    for (int j = 0; j < kGradPieces; ++j) {
-      const int k = k0 + j * kGradThreads;
-      if (k < r.pieces) grad_piece(r, g, same, k, q[j], stat.x, neg, c, target);
-    }
+    r.load(first, k0, q);
+    const int token = target < a.cols ? static_cast<int>(target) : kNoToken;
+    // read by the thread that will write it, since the gradient may lie in the logits' place
+    const float zt = holds<T, kGradPieces>(r, k0, token) ? Elem<T>::get(r.p + token) : 0.f;
+    store_grad(r, g, same, first, k0, q, GradScale(c, stat.x, stat.y), token, zt);
   }
-}
-
-// Fixed-order block sum in double, for every thread.
-__device__ __forceinline__ double block_total(double x, double* sh) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  __syncthreads();  // sh may hold an earlier sum
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double s = 0.0;
-  for (int i = 0; i < static_cast<int>(blockDim.x >> 5); ++i) s += sh[i];
-  return s;
 }
 
 // One block per pair: the weighted sums of logp - ref over the two answers,
@@ -512,21 +631,21 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const RowArgs a, const i
                                                         float* __restrict__ pair_loss) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ double sh[kThreads / 32];
+  __shared__ WideSum sh[kThreads / 32];
   const int64_t j = blockIdx.x;
   const int64_t s0 = starts[2 * j], s1 = starts[2 * j + 1], s2 = starts[2 * j + 2];
   if (!(0 <= s0 && s0 <= s1 && s1 <= s2 && s2 <= a.rows)) {  // no such answers: NaN, and no gradient
     if (threadIdx.x == 0) margins[j] = pair_loss[j] = __int_as_float(0x7fc00000);
     return;
   }
-  double d = 0.0;
+  WideSum d;
   for (int64_t i = s0 + threadIdx.x; i < s2; i += kThreads) {
     const float w = a.weights ? a.weights[i] : 1.f;
     if (a.targets[i] < 0 || w == 0.f) continue;
-    const double x = static_cast<double>(w) * (static_cast<double>(a.logp[i]) - static_cast<double>(a.ref_logp[i]));
-    d += i < s1 ? x : -x;
+    const float x = w * (a.logp[i] - a.ref_logp[i]);
+    d.add(i < s1 ? x : -x);
   }
-  const float x = static_cast<float>(static_cast<double>(beta) * block_total(d, sh));
+  const float x = beta * block_total(d, sh);
   // -log sigma(y) = max(-y, 0) + log(1 + exp(-|y|))
   const float e = expf(-fabsf(x)), tail = log1pf(e);
   const float sigma = x >= 0.f ? 1.f / (1.f + e) : e / (1.f + e);
@@ -546,16 +665,15 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const RowArgs a, const i
   }
 }
 
-// sums[k] = sum of terms[i * K + k] over n rows, in double and in a fixed order.
+// sums[k] = sum of terms[i * K + k] over n rows, in a fixed order.
+constexpr int kSumThreads = 512;
 template <int K>
-__global__ void __launch_bounds__(1024) sum_kernel(const float* __restrict__ terms, int64_t n, float* __restrict__ sums) {
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const float* __restrict__ terms, int64_t n, float* __restrict__ sums) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ double sh[32];
-  double s[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k) s[k] = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) {
+  __shared__ WideSum sh[K][kSumThreads / 32];
+  WideSum s[K];
+  for (int64_t i = threadIdx.x; i < n; i += kSumThreads) {
     float x[K];
     if (K == 4) {
       const float4 q = reinterpret_cast<const float4*>(terms)[i];
@@ -564,12 +682,12 @@ __global__ void __launch_bounds__(1024) sum_kernel(const float* __restrict__ ter
       x[0] = terms[i];
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) s[k] += static_cast<double>(x[k]);
+    for (int k = 0; k < K; ++k) s[k].add(x[k]);
   }
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const double t = block_total(s[k], sh);
-    if (threadIdx.x == 0) sums[k] = static_cast<float>(t);
+    const float t = block_total(s[k], sh[k]);
+    if (threadIdx.x == 0) sums[k] = t;
   }
 }
 
@@ -729,7 +847,7 @@ meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t c
         }
       }
     }
-    e = launch_pdl(sum_kernel<4>, dim3(1), dim3(1024), 0, st, 1, static_cast<const float*>(work), rows, sums);
+    e = launch_pdl(sum_kernel<4>, dim3(1), dim3(kSumThreads), 0, st, 1, static_cast<const float*>(work), rows, sums);
     return launch_status(e, "meq_policy_loss", "sum launch");
   });
 }
@@ -768,7 +886,7 @@ meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64
       e = launch_grad(a, type, st);
       if (e != cudaSuccess) return launch_status(e, "meq_preference_loss", "gradient launch");
     }
-    e = launch_pdl(sum_kernel<1>, dim3(1), dim3(1024), 0, st, 1, static_cast<const float*>(pair_loss), pairs, loss);
+    e = launch_pdl(sum_kernel<1>, dim3(1), dim3(kSumThreads), 0, st, 1, static_cast<const float*>(pair_loss), pairs, loss);
     return launch_status(e, "meq_preference_loss", "sum launch");
   });
 }
