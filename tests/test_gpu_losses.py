@@ -110,8 +110,11 @@ CLIP_LOW, CLIP_HIGH = 0.2, 0.28
 
 
 def _policy_inputs(z, t, g, kl):
-    n = z.shape[0]
-    logp, _, _ = _rows64(z, t)
+    return _policy_inputs_at(_rows64(z, t)[0], g, kl)
+
+
+def _policy_inputs_at(logp, g, kl):
+    n = len(logp)
     d = 0.3 * torch.randn(n, generator=g).double().numpy()
     for edge in (1 - CLIP_LOW, 1 + CLIP_HIGH):  # no ratio where rounding decides whether it is clipped
         d = np.where(np.abs(np.exp(d) - edge) < 1e-3, d + 5e-3, d)
@@ -177,6 +180,52 @@ def test_policy_loss(meq, dtype, kl, rows, cols, pad, shift):
 def test_policy_loss_of_rows_that_no_cluster_holds(meq, dtype, rows, cols, pad, shift):
     z, t, g = _tokens(rows, cols, dtype, 3, pad, shift)
     _check_policy(meq, z, t, g, 0.05, dtype, True)
+
+
+# many long rows: one CTA per row, then clusters of 2, 4 and 8, aligned and not
+STREAMED = [("bf16", 700, 20011, 0, 0), ("bf16", 310, 32000, 0, 0), ("fp16", 330, 57345, 1, 3), ("fp32", 320, 28672, 0, 0),
+            ("fp32", 307, 50001, 2, 1), ("bf16", 310, 60001, 5, 0), ("bf16", 305, 151936, 0, 0), ("fp16", 305, 200003, 0, 1),
+            ("fp32", 304, 151936, 64, 0), ("fp32", 304, 262147, 0, 3), ("bf16", 304, 800003, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype,rows,cols,pad,shift", STREAMED)
+@pytest.mark.parametrize("scored", [1.0, 0.6, 0.01])
+def test_many_long_rows(meq, dtype, rows, cols, pad, shift, scored):
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    z = _matrix(rows, cols, dtype, pad, shift)
+    z.copy_(3.0 * torch.randn(rows, cols, generator=g, device="cuda"))
+    t = torch.randint(0, cols, (rows,), generator=g, device="cuda")
+    t[:4] = torch.tensor([0, cols - 1, 1, cols // 2], device="cuda")
+    skip = torch.rand(rows, generator=g, device="cuda") >= scored
+    skip[0] = False
+    keep = torch.where(skip, -100, t)
+    logp64, dist = torch.zeros(rows, dtype=torch.float64, device="cuda"), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 64):
+        x = z[i:i + 64].double()
+        zt = x.gather(1, t[i:i + 64, None])[:, 0]
+        logp64[i:i + 64], dist[i:i + 64] = zt - torch.logsumexp(x, 1), (zt - x.amax(1)).abs()
+    logp, dist = _np(logp64), _np(dist)
+    tol = _tol(logp, dist)
+    on = ~_np(skip).astype(bool)
+    r = meq.token_logprobs(z, keep)
+    assert (np.abs(_np(r.logp) - logp) <= tol)[on].all() and not _np(r.logp)[~on].any()
+    old, adv, w, ref = _policy_inputs_at(logp, torch.Generator().manual_seed(1), 0.05)
+    r = meq.policy_loss(z, keep, old, adv, w, ref, CLIP_LOW, CLIP_HIGH, 0.05, grad=True)
+    on &= _np(w) != 0
+    assert (np.abs(_np(r.logp) - logp) <= tol)[on].all() and not _np(r.logp)[~on].any()
+    _, c, size = _policy64(logp, _np(old), _np(adv), np.where(on, _np(w), 0), _np(ref), 0.05)
+    c, dc = torch.tensor(c).cuda(), torch.tensor(size * (2 * tol + 2.0 ** -20)).cuda()
+    for i in range(0, rows, 64):
+        p = torch.softmax(z[i:i + 64].double(), 1)
+        want = -c[i:i + 64, None] * p
+        hit = torch.zeros_like(p).scatter_(1, t[i:i + 64, None], 1.0)
+        want += c[i:i + 64, None] * hit
+        bound = c[i:i + 64, None].abs() * p * 2.0 ** -17 + dc[i:i + 64, None] * (p + hit) + LEAST[dtype]
+        bound += HALF_ULP[dtype] * (want.abs() + bound)
+        assert ((r.grad[i:i + 64].double() - want).abs() <= bound).all(), i
+    assert not r.grad[torch.tensor(~on).cuda()].any()
+    again = meq.policy_loss(z, keep, old, adv, w, ref, CLIP_LOW, CLIP_HIGH, 0.05, grad=z)  # in place
+    assert torch.equal(again.grad, r.grad) and torch.equal(again.sums, r.sums)
 
 
 @pytest.mark.parametrize("cols,pad,gpad,gshift", [(1001, 0, 0, 1), (1001, 0, 1, 0), (1000, 8, 0, 3), (4099, 1, 6, 0)])
