@@ -216,15 +216,32 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const RowArgs a)
   a.terms[row] = terms;
 }
 
-// Gradient of the logits from each row's statistics and coefficient, the last rows first.
+// out = sum of n terms, in a fixed order, by one block.
+struct Total {
+  const float* terms;
+  int64_t n;
+  float* out;  // NULL: nothing to do
+  __device__ __forceinline__ void write(WideSum* sh) const {
+    WideSum s;
+    for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s.add(terms[i]);
+    const float t = block_total(s, sh);
+    if (threadIdx.x == 0) *out = t;
+  }
+};
+
+// Gradient of the logits from each row's statistics and coefficient, the last
+// rows first (x, the part of a row, runs faster than y, the row).
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, int tiles, int64_t blocks) {
+__global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, const Total total) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-    const int64_t row = a.rows - 1 - b / tiles;
+  if (total.out && blockIdx.x == 0 && blockIdx.y == 0) {
+    __shared__ WideSum sh[kGradThreads / 32];
+    total.write(sh);
+  }
+  for (int64_t row = a.rows - 1 - blockIdx.y; row >= 0; row -= gridDim.y) {
     const Row<T> r(a.logits, row, a.ld, a.cols);
-    const int first = (static_cast<int>(b % tiles) * (kGradThreads / 32) + static_cast<int>(threadIdx.x >> 5)) * 32 * kGradPieces;
+    const int first = (static_cast<int>(blockIdx.x) * (kGradThreads / 32) + static_cast<int>(threadIdx.x >> 5)) * 32 * kGradPieces;
     const int k0 = first + static_cast<int>(threadIdx.x & 31);
     T* g = static_cast<T*>(a.grad) + row * a.ld_grad;
     const bool same = same_offset(r.p, g);
@@ -285,27 +302,25 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const RowArgs a, const i
   }
 }
 
-// sums[k] = sum of terms[i * K + k] over n rows, in a fixed order.
 constexpr int kSumThreads = 512;
-template <int K>
-__global__ void __launch_bounds__(kSumThreads) sum_kernel(const float* __restrict__ terms, int64_t n, float* __restrict__ sums) {
+__global__ void __launch_bounds__(kSumThreads) total_kernel(const Total total) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ WideSum sh[K][kSumThreads / 32];
-  WideSum s[K];
-  for (int64_t i = threadIdx.x; i < n; i += kSumThreads) {
-    float x[K];
-    if (K == 4) {
-      const float4 q = reinterpret_cast<const float4*>(terms)[i];
-      x[0] = q.x, x[1 % K] = q.y, x[2 % K] = q.z, x[3 % K] = q.w;
-    } else {
-      x[0] = terms[i];
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) s[k].add(x[k]);
+  __shared__ WideSum sh[kSumThreads / 32];
+  total.write(sh);
+}
+// The four sums of the policy loss over the rows' terms, each in a fixed order.
+__global__ void __launch_bounds__(kSumThreads) policy_sums_kernel(const float4* __restrict__ terms, int64_t rows, float* __restrict__ sums) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ WideSum sh[4][kSumThreads / 32];
+  WideSum s[4];
+  for (int64_t i = threadIdx.x; i < rows; i += kSumThreads) {
+    const float4 q = terms[i];
+    s[0].add(q.x), s[1].add(q.y), s[2].add(q.z), s[3].add(q.w);
   }
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
+  for (int k = 0; k < 4; ++k) {
     const float t = block_total(s[k], sh[k]);
     if (threadIdx.x == 0) sums[k] = t;
   }
@@ -361,15 +376,13 @@ cudaError_t launch_rows_of(const RowArgs& a, int type, const RowShape& s, cudaSt
   return launch_pdl(row_kernel<__half, kPolicy>, grid, block, 0, st, s.ctas, a);
 }
 
-cudaError_t launch_grad(const RowArgs& a, int type, cudaStream_t st) {
+cudaError_t launch_grad(const RowArgs& a, const Total& total, int type, cudaStream_t st) {
   const int n = 16 / elem_bytes(type);
   const int64_t pieces = (a.cols + 2 * n - 2) / n, per = kGradPieces * kGradThreads;
-  const int tiles = static_cast<int>((pieces + per - 1) / per);
-  const int64_t blocks = a.rows * tiles;
-  const dim3 grid(static_cast<unsigned>(blocks < 0x40000000 ? blocks : 0x40000000)), block(kGradThreads);
-  if (type == MEQ_F32) return launch_pdl(grad_kernel<float>, grid, block, 0, st, 1, a, tiles, blocks);
-  if (type == MEQ_BF16) return launch_pdl(grad_kernel<__nv_bfloat16>, grid, block, 0, st, 1, a, tiles, blocks);
-  return launch_pdl(grad_kernel<__half>, grid, block, 0, st, 1, a, tiles, blocks);
+  const dim3 grid(static_cast<unsigned>((pieces + per - 1) / per), static_cast<unsigned>(a.rows < 65535 ? a.rows : 65535)), block(kGradThreads);
+  if (type == MEQ_F32) return launch_pdl(grad_kernel<float>, grid, block, 0, st, 1, a, total);
+  if (type == MEQ_BF16) return launch_pdl(grad_kernel<__nv_bfloat16>, grid, block, 0, st, 1, a, total);
+  return launch_pdl(grad_kernel<__half>, grid, block, 0, st, 1, a, total);
 }
 
 int device_sms(cudaError_t* e) {
@@ -463,12 +476,12 @@ meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t c
         e = launch_pdl(policy_terms_kernel, dim3(static_cast<unsigned>((rows + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, 1, a);
         if (e != cudaSuccess) return launch_status(e, "meq_policy_loss", "terms launch");
         if (grad) {
-          e = launch_grad(a, type, st);
+          e = launch_grad(a, Total{}, type, st);
           if (e != cudaSuccess) return launch_status(e, "meq_policy_loss", "gradient launch");
         }
       }
     }
-    e = launch_pdl(sum_kernel<4>, dim3(1), dim3(kSumThreads), 0, st, 1, static_cast<const float*>(work), rows, sums);
+    e = launch_pdl(policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, 1, reinterpret_cast<const float4*>(work), rows, sums);
     return launch_status(e, "meq_policy_loss", "sum launch");
   });
 }
@@ -503,12 +516,10 @@ meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64
     e = launch_pdl(pair_kernel, dim3(static_cast<unsigned>(pairs)), dim3(kThreads), 0, st, 1, a, starts, beta, label_smoothing,
                    static_cast<float>(1.0 / static_cast<double>(pairs)), margins, pair_loss);
     if (e != cudaSuccess) return launch_status(e, "meq_preference_loss", "pair launch");
-    if (grad && rows > 0) {
-      e = launch_grad(a, type, st);
-      if (e != cudaSuccess) return launch_status(e, "meq_preference_loss", "gradient launch");
-    }
-    e = launch_pdl(sum_kernel<1>, dim3(1), dim3(kSumThreads), 0, st, 1, static_cast<const float*>(pair_loss), pairs, loss);
-    return launch_status(e, "meq_preference_loss", "sum launch");
+    const Total total{pair_loss, pairs, loss};
+    if (grad && rows > 0)
+      return launch_status(launch_grad(a, total, type, st), "meq_preference_loss", "gradient launch");
+    return launch_status(launch_pdl(total_kernel, dim3(1), dim3(kSumThreads), 0, st, 1, total), "meq_preference_loss", "sum launch");
   });
 }
 

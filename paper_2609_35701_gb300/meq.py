@@ -6,8 +6,10 @@ importing this module raises.
 """
 from __future__ import annotations
 
+import array
 import collections
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -280,7 +282,8 @@ def _require_cuda(t, dtype_name, numel, what, device=None):
 def _stream_handle(stream):
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        # the raw handle: torch.cuda.current_stream() builds a Stream object, which takes longer than a launch
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -491,6 +494,9 @@ def adamw_state_bytes(shapes, param_dtype="float32", grad_dtype="float32", **opt
     return p.value, w.value
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 class _DeviceArray:
     """Device memory of a state as torch.as_tensor takes it; keeps its owner alive."""
 
@@ -527,19 +533,24 @@ class AdamW:
         for k in self._numels:
             self.offsets.append(at)
             at += -(-k // self.BLOCK) * self.BLOCK
-        self._ptrs = ctypes.c_void_p * n
 
     def _check(self, s):
         if s != MEQ_OK:
             raise MeqError(s, lib.meq_adamw_last_error(self._st).decode())
 
     def _pointers(self, ts, dtype, what):
-        if len(ts) != len(self._numels):
+        """An array of the tensors' pointers. The checks go over the list a property at a time, which
+        takes a third of the time that a loop over the tensors does."""
+        import torch
+
+        T, n = torch.Tensor, len(ts)
+        if n != len(self._numels):
             raise ValueError(f"{what} must have one tensor per entry")
-        for i, (t, k) in enumerate(zip(ts, self._numels)):
-            if not (t.dtype is dtype and t.is_cuda and t.numel() == k and t.is_contiguous() and t.get_device() == self._device):
+        if not (list(map(T.numel, ts)) == self._numels and all(map(T.is_contiguous, ts)) and
+                set(map(_dtype_of, ts)) == {dtype} and set(map(T.get_device, ts)) == {self._device}):
+            for i, (t, k) in enumerate(zip(ts, self._numels)):
                 _require_cuda(t, str(dtype)[6:], k, f"{what}[{i}]", self._device)
-        return self._ptrs(*[t.data_ptr() for t in ts])
+        return array.array("Q", map(T.data_ptr, ts))
 
     def grad_norm(self, grads, max_norm=float("inf"), out=None, stream=None):
         """(norm, clipping coefficient) of the gradients as a CUDA tensor of two floats, without a host sync."""
@@ -547,8 +558,9 @@ class AdamW:
             out = _empty(2, "float32", self._device, stream)
         else:
             _require_cuda(out, "float32", 2, "out", self._device)
-        self._check(lib.meq_adamw_grad_norm(self._pointers(grads, self._grad_dtype, "grads"), self._st, float(max_norm),
-                                            ctypes.c_void_p(out.data_ptr()), _stream_handle(stream)))
+        g = self._pointers(grads, self._grad_dtype, "grads")
+        self._check(lib.meq_adamw_grad_norm(g.buffer_info()[0], self._st, float(max_norm), out.data_ptr(),
+                                            _stream_handle(stream)))
         return out
 
     def step(self, params, grads, lr, weight_decay=0.0, grad_scale=None, copies=None, stream=None):
@@ -558,16 +570,16 @@ class AdamW:
         receive the updated parameters."""
         if grad_scale is not None:
             _require_cuda(grad_scale, "float32", 1, "grad_scale", self._device)
+        p = self._pointers(params, self._param_dtype, "params")
+        g = self._pointers(grads, self._grad_dtype, "grads")
         c = None
         if copies is not None:
             import torch
 
             c = self._pointers(copies, torch.bfloat16, "copies")
-        self._check(lib.meq_adamw_step(self._pointers(params, self._param_dtype, "params"),
-                                       self._pointers(grads, self._grad_dtype, "grads"), c, self._st, float(lr),
-                                       float(weight_decay),
-                                       None if grad_scale is None else ctypes.c_void_p(grad_scale.data_ptr()),
-                                       _stream_handle(stream)))
+        self._check(lib.meq_adamw_step(p.buffer_info()[0], g.buffer_info()[0], None if c is None else c.buffer_info()[0],
+                                       self._st, float(lr), float(weight_decay),
+                                       None if grad_scale is None else grad_scale.data_ptr(), _stream_handle(stream)))
 
     def state(self):
         """The state's own arrays as CUDA tensors: m and v, or m_code, r_code and
@@ -625,8 +637,17 @@ class AdamW:
 
 # --------------------------------------------------------------------- losses
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logp lse")
-PolicyLoss = collections.namedtuple("PolicyLoss", "loss sums logp grad")
 PreferenceLoss = collections.namedtuple("PreferenceLoss", "loss margins logp grad")
+
+
+class PolicyLoss(collections.namedtuple("PolicyLoss", "sums logp grad")):
+    """sums: the loss, its surrogate and KL parts, the clipped weight."""
+
+    __slots__ = ()
+
+    @property
+    def loss(self):
+        return self.sums[0]
 
 
 def _logits_args(logits, what="logits"):
@@ -635,16 +656,20 @@ def _logits_args(logits, what="logits"):
     if not logits.is_cuda or name not in DTYPES or logits.dim() != 2:
         raise ValueError(f"{what} must be a CUDA matrix of one of {sorted(DTYPES)}")
     rows, cols = logits.shape
-    if cols < 1 or (cols > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < cols):
+    ld, step = logits.stride()
+    if cols < 1 or (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{what} must have consecutive columns in rows that do not overlap")
-    return name, rows, cols, max(logits.stride(0), cols)
+    return name, rows, cols, max(ld, cols)
 
 
 def _vector(t, dtype_name, n, device, what):
     """The device pointer of a contiguous CUDA vector, or None."""
     if t is None:
         return None
-    _require_cuda(t, dtype_name, n, what, device)
+    import torch
+
+    if not (t.dtype is getattr(torch, dtype_name) and t.get_device() == device and t.numel() == n and t.is_contiguous()):
+        _require_cuda(t, dtype_name, n, what, device)
     return t.data_ptr()
 
 
@@ -667,7 +692,7 @@ def _grad_for(logits, grad, stream):
 def _current_device(t, what):
     import torch
 
-    device = t.device.index
+    device = t.get_device()
     if device != torch.cuda.current_device():
         raise ValueError(f"{what} is on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
     return device
@@ -685,10 +710,10 @@ def token_logprobs(logits, targets, stream=None):
     name, rows, cols, ld = _logits_args(logits)
     device = _current_device(logits, "logits")
     t = _vector(targets, "int64", rows, device, "targets")
-    out = _empty((2, rows), "float32", device, stream)
-    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, out.data_ptr(),
-                                       out.data_ptr() + 4 * rows, _stream_handle(stream)))
-    return TokenLogprobs(out[0], out[1])
+    logp, lse = _empty(rows, "float32", device, stream), _empty(rows, "float32", device, stream)
+    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, logp.data_ptr(), lse.data_ptr(),
+                                       _stream_handle(stream)))
+    return TokenLogprobs(logp, lse)
 
 
 def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
@@ -696,7 +721,7 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
     """The clipped policy loss with a KL term and, if asked for, the gradient of
     the logits (meq_policy_loss). grad: True for a new tensor, or the tensor to
     write (it may be logits). sums holds the loss, its surrogate and KL parts
-    and the clipped weight; loss is its first entry."""
+    and the clipped weight; loss is the first of them."""
     name, rows, cols, ld = _logits_args(logits)
     device = _current_device(logits, "logits")
     vectors = [_vector(t, "float32", rows, device, what) for t, what in
@@ -704,13 +729,13 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
     t = _vector(targets, "int64", rows, device, "targets")
     scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
     grad, ldg = _grad_for(logits, grad, stream)
-    work = _empty(lib.meq_loss_work_floats(rows, 0) + rows + 4, "float32", device, stream)
-    sums, logp = work[-4:], work[-4 - rows:-4] if rows else work[:0]
+    work = _empty(lib.meq_loss_work_floats(rows, 0), "float32", device, stream)
+    sums, logp = _empty(4, "float32", device, stream), _empty(rows, "float32", device, stream)
     _check_loss(lib.meq_policy_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, *vectors, float(clip_low),
                                     float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(),
                                     None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
                                     _stream_handle(stream)))
-    return PolicyLoss(sums[0], sums, logp, grad)
+    return PolicyLoss(sums, logp, grad)
 
 
 def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, label_smoothing=0.0, grad=None, grad_scale=None,
@@ -728,9 +753,8 @@ def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, l
     t = _vector(targets, "int64", rows, device, "targets")
     scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
     grad, ldg = _grad_for(logits, grad, stream)
-    n = lib.meq_loss_work_floats(rows, pairs)
-    work = _empty(n + rows + pairs + 1, "float32", device, stream)
-    logp, margins, loss = work[n:n + rows], work[n + rows:n + rows + pairs], work[n + rows + pairs]
+    work = _empty(lib.meq_loss_work_floats(rows, pairs), "float32", device, stream)
+    logp, margins, loss = (_empty(n, "float32", device, stream) for n in (rows, pairs, ()))
     _check_loss(lib.meq_preference_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, st, pairs, *vectors, float(beta),
                                         float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(),
                                         None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
