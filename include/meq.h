@@ -359,7 +359,7 @@ typedef enum { MEQ_F32 = 0, MEQ_BF16 = 1, MEQ_F16 = 2 } meq_dtype;
 
 typedef struct {
   double beta1, beta2; /* 0.9, 0.999; in [0, 1) */
-  double eps;          /* 1e-8; > 0 */
+  double eps;          /* 1e-8; >= 2^-126 */
   int state_bits;      /* 32 (default) or 8 */
   int param_type;      /* MEQ_F32 (default) or MEQ_BF16 */
   int grad_type;       /* a meq_dtype; default MEQ_F32 */

@@ -87,6 +87,7 @@ struct AdamArgs {
   const float* grad_scale;
   double beta1, beta2;
   float b1, one_minus_b1, b2, one_minus_b2, eps, lr, wd;
+  float one;             // 1: see sum2
   int32_t entry0, last;  // first entry of this launch; 1: the step's last launch
   int64_t chunk0;        // first chunk of this launch
   void* params[kMaxEntries];
@@ -125,7 +126,6 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
 __device__ __forceinline__ void from_f(float x, float* p) { *p = x; }
 __device__ __forceinline__ void from_f(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
-__device__ __forceinline__ void from_f(float x, __half* p) { *p = __float2half_rn(x); }
 template <typename T>
 struct Quad {
   static __device__ __forceinline__ void load(const T* p, float* x) {
@@ -164,19 +164,55 @@ __device__ __forceinline__ void store4(T* p, int64_t n, bool vec, const float* x
   }
 }
 
+// The larger magnitude or NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  for (int o = 16; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
-
-// scale (code / most)^2 with the code's sign
-__device__ __forceinline__ float decode(float code, float inv_most, float scale) {
-  const float t = __fmul_rn(code, inv_most);
-  return __fmul_rn(__fmul_rn(t, fabsf(t)), scale);
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-__device__ __forceinline__ float encode(float x, float inv_scale, float most) {
-  return rintf(__fmul_rn(most, __fsqrt_rn(__fmul_rn(fabsf(x), inv_scale))));
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
+
+// a + b rounded once. An addition of two products would be contracted into a
+// multiply-add (which add.rn.f32x2 does not keep the assembler from doing); one
+// factor that is only known to the launch does.
+__device__ __forceinline__ float2 sum2(float2 a, float2 b, float one) { return fma2(a, splat(one), b); }
+
+// A byte as fp32: put below the exponent of 2^23, which is taken off again.
+__device__ __forceinline__ float2 two_bytes(uint32_t w, int i) {
+  const float2 x = make_float2(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + i)),
+                               __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7541 + i)));
+  return x;
+}
+// Four codes and a scale: scale (code / most)^2, with the code's sign for m.
+__device__ __forceinline__ void decode_m4(uint32_t w, float scale, float2* x) {
+  w ^= 0x80808080u;  // code + 128
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 t = mul2(add2(two_bytes(w, 2 * i), splat(-8388608.f - 128.f)), splat(1.0f / 127.0f));
+    x[i] = mul2(make_float2(__fmul_rn(t.x, fabsf(t.x)), __fmul_rn(t.y, fabsf(t.y))), splat(scale));
+  }
+}
+__device__ __forceinline__ void decode_r4(uint32_t w, float scale, float2* x) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 t = mul2(add2(two_bytes(w, 2 * i), splat(-8388608.f)), splat(1.0f / 255.0f));
+    x[i] = mul2(mul2(t, t), splat(scale));
+  }
 }
 // The scale of a block whose largest magnitude is top, and its reciprocal. A
 // block of denormals is taken as zero: the reciprocal would overflow.
@@ -185,14 +221,32 @@ __device__ __forceinline__ float block_scale(float top, float* inv) {
   *inv = some ? __frcp_rn(top) : 0.f;
   return some ? top : 0.f;
 }
-__device__ __forceinline__ void decode_m4(uint32_t w, float scale, float* x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = decode(static_cast<float>(static_cast<int8_t>(w >> (8 * i))), 1.0f / 127.0f, scale);
+// The code of x >= 0 before its rounding, most sqrt(x / scale), every operation
+// rounded once.
+__device__ __forceinline__ float code_exact(float x, float inv, float most) {
+  return __fmul_rn(most, __fsqrt_rn(__fmul_rn(x, inv)));
 }
-__device__ __forceinline__ void decode_r4(uint32_t w, float scale, float* x) {
+// kRound + y holds rint(y) in its low byte, in two's complement.
+constexpr float kRound = 12582912.f;  // 1.5 2^23
+// Codes y of four elements, rounded and packed. The codes have been formed with
+// approximate roots; *worst is the largest distance from a whole number among
+// them, so that the caller can see whether one lies too near a half to trust.
+__device__ __forceinline__ uint32_t pack_codes(const float2* y, float* worst) {
+  float2 z[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = decode(static_cast<float>((w >> (8 * i)) & 255u), 1.0f / 255.0f, scale);
+  for (int i = 0; i < 2; ++i) {
+    z[i] = add2(y[i], splat(kRound));
+    const float2 off = fma2(add2(z[i], splat(-kRound)), splat(-1.f), y[i]);
+    *worst = fmaxf(*worst, fmaxf(fabsf(off.x), fabsf(off.y)));
+  }
+  const uint32_t lo = __byte_perm(__float_as_uint(z[0].x), __float_as_uint(z[0].y), 0x0040);
+  const uint32_t hi = __byte_perm(__float_as_uint(z[1].x), __float_as_uint(z[1].y), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
 }
+// sqrt.approx is within 2^-23, relative; with the roundings beside it and those
+// of the exact formula that is 127 * 3.0e-7 for m and, with r's own root, 255 *
+// 4.2e-7 for r.
+constexpr float kNearM = 0.5f - 6e-5f, kNearR = 0.5f - 1.6e-4f;
 
 template <typename P, typename G, int kBits>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs a) {
@@ -222,8 +276,8 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     const bool pvec = full && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(P) - 1)) == 0;
     const bool gvec = full && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
     const bool cvec = full && (reinterpret_cast<uintptr_t>(copy) & 7u) == 0;
-    float pv[8], gv[8], m[8], r[8];  // two groups of four, 128 apart; r holds v until its root is taken
     const int64_t at = base + 4 * lane;
+    float pv[8], gv[8];  // two groups of four, 128 apart
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       load4(g + at + 128 * j, E.numel - at - 128 * j, gvec, gv + 4 * j);
@@ -231,11 +285,29 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     }
     const int64_t so = E.off + at;  // the state's arrays are padded to whole blocks
     const int64_t sb = (E.off + base) / kBlock;
+    bool bad;
     if (kBits == 32) {
+      float m[8], v[8];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         Quad<float>::load(static_cast<const float*>(a.m) + so + 128 * j, m + 4 * j);
-        Quad<float>::load(static_cast<const float*>(a.v) + so + 128 * j, r + 4 * j);
+        Quad<float>::load(static_cast<const float*>(a.v) + so + 128 * j, v + 4 * j);
+      }
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = gv[i] * gs;
+        m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(x, a.one_minus_b1));
+        v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(x, x), a.one_minus_b2));
+        const float u = __fdiv_rn(m[i], fmaf(__fsqrt_rn(v[i]), rbc2, a.eps));
+        pv[i] = fmaf(pv[i], keep, -(u * step));
+        top = max_nan(top, max_nan(fabsf(m[i]), v[i]));
+      }
+      bad = !(top <= FLT_MAX);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Quad<float>::store(static_cast<float*>(a.m) + so + 128 * j, m + 4 * j);
+        Quad<float>::store(static_cast<float*>(a.v) + so + 128 * j, v + 4 * j);
       }
     } else {
       const float ms = a.m_scale[sb], rs = a.r_scale[sb];
@@ -245,60 +317,86 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         mc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(a.m) + so + 128 * j));
         rc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + so + 128 * j));
       }
+      float2 m[4], v[4], r[4];
+      float mt = 0.f, vt = 0.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        decode_m4(mc[j], ms, m + 4 * j);
-        decode_r4(rc[j], rs, r + 4 * j);
+        decode_m4(mc[j], ms, m + 2 * j);
+        decode_r4(rc[j], rs, v + 2 * j);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = __fmul_rn(r[i], r[i]);
-    }
-    bool bad = false;
-    float v[8];
+      for (int i = 0; i < 4; ++i) {
+        const float2 x = mul2(make_float2(gv[2 * i], gv[2 * i + 1]), splat(gs));
+        m[i] = sum2(mul2(m[i], splat(a.b1)), mul2(x, splat(a.one_minus_b1)), a.one);
+        v[i] = sum2(mul2(mul2(v[i], v[i]), splat(a.b2)), mul2(mul2(x, x), splat(a.one_minus_b2)), a.one);
+        mt = max_nan(mt, max_nan(fabsf(m[i].x), fabsf(m[i].y)));
+        vt = max_nan(vt, max_nan(v[i].x, v[i].y));
+        r[i] = make_float2(sqrt_approx(v[i].x), sqrt_approx(v[i].y));
+        const float2 d = fma2(r[i], splat(rbc2), splat(a.eps));
+        const float2 u = mul2(mul2(m[i], make_float2(rcp_approx(d.x), rcp_approx(d.y))), splat(-step));
+        const float2 q = fma2(make_float2(pv[2 * i], pv[2 * i + 1]), splat(keep), u);
+        pv[2 * i] = q.x, pv[2 * i + 1] = q.y;
+      }
+      mt = warp_max(mt), vt = warp_max(vt);
+      bad = !(mt <= FLT_MAX) || !(vt <= FLT_MAX);
+      float mi, ri;
+      float ms_new = block_scale(mt, &mi), rs_new = block_scale(__fsqrt_rn(vt), &ri);
+      if (bad) ms_new = rs_new = __int_as_float(0x7fc00000);  // no code says NaN: the block's scale does
+      float worst_m = 0.f, worst_r = 0.f;
+      float2 y[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = __fmul_rn(gv[i], gs);
-      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(x, a.one_minus_b1));
-      v[i] = __fadd_rn(__fmul_rn(r[i], a.b2), __fmul_rn(__fmul_rn(x, x), a.one_minus_b2));
-      r[i] = __fsqrt_rn(v[i]);
-      const float u = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(r[i], rbc2), a.eps));
-      pv[i] = __fadd_rn(__fmul_rn(pv[i], keep), -__fmul_rn(u, step));
-      bad = bad || !(fabsf(m[i]) <= FLT_MAX) || !(r[i] <= FLT_MAX);
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 s = mul2(m[2 * j + i], splat(mi));
+          const float2 k = mul2(make_float2(sqrt_approx(fabsf(s.x)), sqrt_approx(fabsf(s.y))), splat(127.f));
+          y[i] = make_float2(copysignf(k.x, s.x), copysignf(k.y, s.y));
+        }
+        mc[j] = pack_codes(y, &worst_m);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 s = mul2(r[2 * j + i], splat(ri));
+          const float2 k = mul2(make_float2(sqrt_approx(s.x), sqrt_approx(s.y)), splat(255.f));
+          // above zero, at least one
+          y[i] = make_float2(fmaxf(k.x, __saturatef(k.x * 1e38f)), fmaxf(k.y, __saturatef(k.y * 1e38f)));
+        }
+        rc[j] = pack_codes(y, &worst_r);
+      }
+      float unused = 0.f;
+      if (worst_m > kNearM) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float2 s = m[2 * j + i];
+            y[i] = make_float2(copysignf(code_exact(fabsf(s.x), mi, 127.f), s.x), copysignf(code_exact(fabsf(s.y), mi, 127.f), s.y));
+          }
+          mc[j] = pack_codes(y, &unused);
+        }
+      }
+      if (worst_r > kNearR) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float2 s = v[2 * j + i];
+            const float kx = code_exact(__fsqrt_rn(s.x), ri, 255.f), ky = code_exact(__fsqrt_rn(s.y), ri, 255.f);
+            y[i] = make_float2(fmaxf(kx, __saturatef(kx * 1e38f)), fmaxf(ky, __saturatef(ky * 1e38f)));
+          }
+          rc[j] = pack_codes(y, &unused);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<int8_t*>(a.m) + so + 128 * j), mc[j]);
+        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + so + 128 * j), rc[j]);
+      }
+      if (lane == 0) a.m_scale[sb] = ms_new, a.r_scale[sb] = rs_new;
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       store4(p + at + 128 * j, E.numel - at - 128 * j, pvec, pv + 4 * j);
       if (copy) store4(copy + at + 128 * j, E.numel - at - 128 * j, cvec, pv + 4 * j);
-    }
-    if (kBits == 32) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        Quad<float>::store(static_cast<float*>(a.m) + so + 128 * j, m + 4 * j);
-        Quad<float>::store(static_cast<float*>(a.v) + so + 128 * j, v + 4 * j);
-      }
-    } else {
-      float mt = 0.f, rt = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) mt = fmaxf(mt, fabsf(m[i])), rt = fmaxf(rt, r[i]);
-      float mi, ri;
-      float ms = block_scale(warp_max(mt), &mi), rs = block_scale(warp_max(rt), &ri);
-      if (__any_sync(0xffffffffu, bad)) ms = rs = __int_as_float(0x7fc00000);  // no code says NaN: the block's scale does
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t mc = 0, rc = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = m[4 * j + i], y = r[4 * j + i];
-          const int q = static_cast<int>(encode(x, mi, 127.f));
-          mc |= (static_cast<uint32_t>(x < 0.f ? -q : q) & 255u) << (8 * i);
-          float k = encode(y, ri, 255.f);
-          if (y > 0.f) k = fmaxf(k, 1.f);
-          rc |= (static_cast<uint32_t>(static_cast<int>(k)) & 255u) << (8 * i);
-        }
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<int8_t*>(a.m) + so + 128 * j), mc);
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + so + 128 * j), rc);
-      }
-      if (lane == 0) a.m_scale[sb] = ms, a.r_scale[sb] = rs;
     }
     if (bad) atomicCAS(&a.clock->nonfinite, 0, ei + 1);
   }
@@ -370,16 +468,15 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_values_kernel(const uint32
   const int64_t i = static_cast<int64_t>(blockIdx.x) * kAdamThreads + threadIdx.x;
   if (i >= quads) return;
   const int64_t b = i / (kBlock / 4);
-  float x[4];
+  float2 x[2];
   if (m) {
     decode_m4(__ldcs(m_code + i), m_scale[b], x);
-    __stcs(reinterpret_cast<float4*>(m) + i, make_float4(x[0], x[1], x[2], x[3]));
+    __stcs(reinterpret_cast<float4*>(m) + i, make_float4(x[0].x, x[0].y, x[1].x, x[1].y));
   }
   if (v) {
     decode_r4(__ldcs(r_code + i), r_scale[b], x);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = __fmul_rn(x[k], x[k]);
-    __stcs(reinterpret_cast<float4*>(v) + i, make_float4(x[0], x[1], x[2], x[3]));
+    x[0] = mul2(x[0], x[0]), x[1] = mul2(x[1], x[1]);
+    __stcs(reinterpret_cast<float4*>(v) + i, make_float4(x[0].x, x[0].y, x[1].x, x[1].y));
   }
 }
 
@@ -439,7 +536,7 @@ meq_status guarded(meq_adamw* st, F f) {
 bool valid_adamw_options(const meq_adamw_options& o, std::string* why) {
   auto beta = [](double b) { return b >= 0.0 && b < 1.0; };
   if (!beta(o.beta1) || !beta(o.beta2)) { *why = "beta1 and beta2 must be in [0, 1)"; return false; }
-  if (!(static_cast<float>(o.eps) > 0.f) || !std::isfinite(static_cast<float>(o.eps))) { *why = "eps must be positive and finite in fp32"; return false; }
+  if (!(static_cast<float>(o.eps) >= FLT_MIN) || !std::isfinite(static_cast<float>(o.eps))) { *why = "eps must be a positive normal number in fp32"; return false; }
   if (o.state_bits != 32 && o.state_bits != 8) { *why = "state_bits must be 32 or 8"; return false; }
   if (o.param_type != MEQ_F32 && o.param_type != MEQ_BF16) { *why = "param_type must be MEQ_F32 or MEQ_BF16"; return false; }
   if (o.grad_type != MEQ_F32 && o.grad_type != MEQ_BF16 && o.grad_type != MEQ_F16) { *why = "grad_type must be a meq_dtype"; return false; }
@@ -678,7 +775,7 @@ meq_status meq_adamw_step(void* const* params, const void* const* grads, void* c
     a.beta1 = st->opt.beta1, a.beta2 = st->opt.beta2;
     a.b1 = static_cast<float>(a.beta1), a.one_minus_b1 = static_cast<float>(1.0 - a.beta1);
     a.b2 = static_cast<float>(a.beta2), a.one_minus_b2 = static_cast<float>(1.0 - a.beta2);
-    a.eps = static_cast<float>(st->opt.eps), a.lr = lr, a.wd = weight_decay;
+    a.eps = static_cast<float>(st->opt.eps), a.lr = lr, a.wd = weight_decay, a.one = 1.f;
     for (size_t k = 0; k < st->parts.size(); ++k) {
       const Part& p = st->parts[k];
       a.entry0 = p.entry0, a.chunk0 = p.chunk0;

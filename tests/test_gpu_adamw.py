@@ -180,6 +180,37 @@ def test_8bit_codes_are_those_of_the_formula(meq):
     opt.close()
 
 
+@pytest.mark.parametrize("seed", [1, 2])
+def test_8bit_codes_over_many_values(meq, seed):
+    """Four million codes of each kind, over twelve orders of magnitude and three steps, bit for bit those of
+    the formula in fp32, each operation rounded: no approximate root, no contracted sum decides a code."""
+    n = 1 << 22
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    opt = meq.AdamW([(1024, n // 1024)], beta1=B1, beta2=B2, eps=EPS, state_bits=8)
+    size = 10.0 ** (12 * torch.rand(n // 256, generator=g, device="cuda") - 9).repeat_interleave(256)
+    scale = torch.tensor([0.37], device="cuda")
+    m, r = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    for _ in range(3):
+        x = torch.randn(n, generator=g, device="cuda") * size * torch.exp(2.0 * torch.randn(n, generator=g, device="cuda"))
+        opt.step([torch.zeros(1024, n // 1024, device="cuda")], [x.view(1024, -1)], 1e-3, grad_scale=scale)
+        x = x * scale
+        st, held = opt.state(), []
+        m = m * B1 + x * (1.0 - B1)
+        r = torch.sqrt((r * r) * B2 + (x * x) * (1.0 - B2))
+        for y, most, code, scales in ((m, 127.0, "m_code", "m_scale"), (r, 255.0, "r_code", "r_scale")):
+            b = y.view(-1, 256)
+            top = b.abs().amax(1)
+            q = torch.round(most * torch.sqrt(b.abs() * (1.0 / top)[:, None]))
+            q = q * torch.sign(b) if most == 127.0 else torch.where(b > 0, q.clamp(min=1.0), q)
+            assert torch.equal(st[scales], top) and torch.equal(st[code].float(), q.view(-1))
+            t = q * (1.0 / most)
+            held.append(((t * t.abs()) * top[:, None]).view(-1))
+        m, r = held
+    got_m, got_v = opt.read_values()
+    assert torch.equal(got_m, m) and torch.equal(got_v, r * r)
+    opt.close()
+
+
 def test_copies_and_clipping(meq):
     shapes = [(50, 300), (1, 300), (7, 11)]
     opt = meq.AdamW(shapes, beta1=B1, beta2=B2, eps=EPS)
