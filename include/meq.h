@@ -353,8 +353,8 @@ meq_status meq_row_col_stats_noalloc(const float* U, int64_t rows, int64_t cols,
  * on the others of the list. Each entry's moments start at a multiple of 256
  * elements of the state's arrays, in the order of the list.
  *
- * Pointers need the alignment of their element type only; 16-byte aligned
- * fp32 tensors (8-byte aligned 16-bit ones) move in wide accesses. */
+ * Pointers need the alignment of their element type only; entries whose
+ * tensors are all 16-byte aligned move in wide accesses. */
 typedef enum { MEQ_F32 = 0, MEQ_BF16 = 1, MEQ_F16 = 2 } meq_dtype;
 
 typedef struct {

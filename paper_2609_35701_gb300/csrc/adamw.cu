@@ -43,15 +43,31 @@ namespace {
 
 constexpr int kBlock = 256;               // elements per scale and per warp
 constexpr int kAdamThreads = 256;
-constexpr int kAdamChunk = kBlock * kAdamThreads / 32;  // elements per block
+// Thread blocks of a step. With 8-bit states a block is one warp: its warps are
+// kept busy by computing, get apart, and would wait for each other's ends.
+template <int kBits>
+struct Step {
+  static constexpr int kWarps = kBits == 8 ? 1 : 8;
+  static constexpr int kThreads = 32 * kWarps, kPerSm = kBits == 8 ? 24 : 4;
+  static constexpr int kTile = kBlock * kWarps;  // elements that a thread block takes at once: one kBlock per warp
+  static constexpr int kMinChunk = kTile, kMaxChunk = kBits == 8 ? 4096 : 16384;  // elements that it takes in turn
+};
 constexpr int kMaxEntries = 256;          // pointers of one launch: 6 KB of its arguments
-constexpr int kNormBlocksPerSm = 8;
+constexpr int kNormBlocksPerSm = 6;
+constexpr int kNormUnit = 2048;           // most elements of a warp's turn in the norm
 constexpr int kSkipped = 0x7fffffff;      // value of AdamClock::nonfinite: a step was skipped
 
-struct AdamEntry {
+struct AdamEntry {  // host
   int64_t numel;
   int64_t off;     // first element in the state's arrays, a multiple of kBlock
   int64_t chunk0;  // first chunk
+  float decay;
+};
+struct __align__(16) Chunk {
+  int64_t first;   // element of its entry that it starts at
+  int64_t off;     // the same in the state's arrays
+  int32_t left;    // elements of the entry in it
+  int32_t entry;
   float decay;
   int32_t pad;
 };
@@ -77,8 +93,7 @@ __host__ __device__ inline void set_clock(AdamClock* c, double b1t, double b2t, 
 }
 
 struct AdamArgs {
-  const AdamEntry* entries;
-  const int32_t* chunk_entry;
+  const Chunk* chunks_of;  // of the state
   AdamClock* clock;
   void* m;              // fp32, or int8 codes
   void* v;              // fp32, or uint8 codes of sqrt(v)
@@ -96,93 +111,145 @@ struct AdamArgs {
 };
 
 struct NormArgs {
-  const AdamEntry* entries;
-  const int32_t* chunk_entry;
+  const Chunk* chunks_of;  // of the state
   AdamClock* clock;
   float* partials;
   float* out;
   float max_norm;
   int32_t entry0, last, part0, parts;  // first partial of this launch; partials of all launches
+  int32_t shift, unit;                 // a warp takes `unit` elements at a time, 1 << shift of them per chunk
   int64_t chunk0, chunks;
   const void* grads[kMaxEntries];
 };
 
-// Four consecutive elements as fp32: one load where they are aligned and all
-// there, else one per element (those beyond n as zero).
-template <typename T>
-struct Quad;
-template <>
-struct Quad<float> {
-  static __device__ __forceinline__ void load(const float* p, float* x) {
-    const float4 q = __ldcs(reinterpret_cast<const float4*>(p));
-    x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float* x) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
-  }
-};
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-__device__ __forceinline__ void from_f(float x, float* p) { *p = x; }
 __device__ __forceinline__ void from_f(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
-template <typename T>
-struct Quad {
-  static __device__ __forceinline__ void load(const T* p, float* x) {
-    const uint2 q = __ldcs(reinterpret_cast<const uint2*>(p));
-    T h[4];
-    memcpy(h, &q, 8);
+// Two 16-bit elements as fp32, and back.
+__device__ __forceinline__ float2 wide(uint32_t w, __nv_bfloat16) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ float2 wide(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t narrow(float x, float y, __nv_bfloat16) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Groups of four elements of a lane, kGap apart, as fp32: in wide accesses where
+// they are aligned and all there (kVec), else one by one (those beyond n as
+// zero). Two groups that are neighbours go as one access of 16-bit elements.
+template <int kGap, bool kVec>
+__device__ __forceinline__ void load8(const float* p, int n, float* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = to_f(h[i]);
-  }
-  static __device__ __forceinline__ void store(T* p, const float* x) {
-    T h[4];
+  for (int j = 0; j < 2; ++j) {
+    if (kVec) {
+      const float4 q = __ldcs(reinterpret_cast<const float4*>(p + kGap * j));
+      x[4 * j] = q.x, x[4 * j + 1] = q.y, x[4 * j + 2] = q.z, x[4 * j + 3] = q.w;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) from_f(x[i], &h[i]);
-    uint2 q;
-    memcpy(&q, h, 8);
-    __stcs(reinterpret_cast<uint2*>(p), q);
+      for (int i = 0; i < 4; ++i) x[4 * j + i] = kGap * j + i < n ? p[kGap * j + i] : 0.f;
+    }
   }
-};
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, int64_t n, bool vec, float* x) {
-  if (vec) {
-    Quad<T>::load(p, x);
+}
+template <int kGap, bool kVec, typename T>
+__device__ __forceinline__ void load8(const T* p, int n, float* x) {
+  if (kVec) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint2 q = __ldcs(reinterpret_cast<const uint2*>(p + kGap * j));
+      w[2 * j] = q.x, w[2 * j + 1] = q.y;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = wide(w[i], T());
+      x[2 * i] = v.x, x[2 * i + 1] = v.y;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i < n ? to_f(p[i]) : 0.f;
+    for (int i = 0; i < 8; ++i) {
+      const int at = kGap * (i / 4) + i % 4;
+      x[i] = at < n ? to_f(p[at]) : 0.f;
+    }
+  }
+}
+template <int kGap, bool kVec>
+__device__ __forceinline__ void store8(float* p, int n, const float* x) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    if (kVec) {
+      __stcs(reinterpret_cast<float4*>(p + kGap * j), make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (kGap * j + i < n) p[kGap * j + i] = x[4 * j + i];
+    }
+  }
+}
+template <int kGap, bool kVec, typename T>
+__device__ __forceinline__ void store8(T* p, int n, const float* x) {
+  if (kVec) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = narrow(x[2 * i], x[2 * i + 1], T());
+    if (kGap == 4) {
+      __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+      __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+      __stcs(reinterpret_cast<uint2*>(p + kGap), make_uint2(w[2], w[3]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = kGap * (i / 4) + i % 4;
+      if (at < n) from_f(x[i], p + at);
+    }
+  }
+}
+// Eight neighbouring elements in shared memory.
+__device__ __forceinline__ void near8(const float* p, float* x) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float4 q = reinterpret_cast<const float4*>(p)[j];
+    x[4 * j] = q.x, x[4 * j + 1] = q.y, x[4 * j + 2] = q.z, x[4 * j + 3] = q.w;
   }
 }
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int64_t n, bool vec, const float* x) {
-  if (vec) {
-    Quad<T>::store(p, x);
-  } else {
+__device__ __forceinline__ void near8(const T* p, float* x) {
+  const uint4 q = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) from_f(x[i], p + i);
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = wide(w[i], T());
+    x[2 * i] = v.x, x[2 * i + 1] = v.y;
   }
 }
 
-// The larger magnitude or NaN.
-__device__ __forceinline__ float max_nan(float a, float b) {
+// The largest magnitude, or NaN if one is NaN.
+__device__ __forceinline__ float max_mag(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
+__device__ __forceinline__ float warp_max_mag(float x) {
+  float r;
+  asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
 }
 __device__ __forceinline__ float sqrt_approx(float x) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rsqrt_approx(float x) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
@@ -214,16 +281,13 @@ __device__ __forceinline__ void decode_r4(uint32_t w, float scale, float2* x) {
     x[i] = mul2(mul2(t, t), splat(scale));
   }
 }
-// The scale of a block whose largest magnitude is top, and its reciprocal. A
-// block of denormals is taken as zero: the reciprocal would overflow.
-__device__ __forceinline__ float block_scale(float top, float* inv) {
-  const bool some = top >= FLT_MIN;
-  *inv = some ? __frcp_rn(top) : 0.f;
-  return some ? top : 0.f;
-}
-// The code of x >= 0 before its rounding, most sqrt(x / scale), every operation
-// rounded once.
-__device__ __forceinline__ float code_exact(float x, float inv, float most) {
+// A block whose largest magnitude is a denormal is held as zero, codes and
+// scale: its reciprocal would overflow.
+__device__ __forceinline__ float block_scale(float top) { return top >= FLT_MIN ? top : 0.f; }
+// The code of x >= 0 before its rounding, most sqrt(x (1 / scale)), every
+// operation rounded once.
+__device__ __forceinline__ float code_exact(float x, float scale, float most) {
+  const float inv = scale > 0.f ? __frcp_rn(scale) : 0.f;
   return __fmul_rn(most, __fsqrt_rn(__fmul_rn(x, inv)));
 }
 // kRound + y holds rint(y) in its low byte, in two's complement.
@@ -237,174 +301,272 @@ __device__ __forceinline__ uint32_t pack_codes(const float2* y, float* worst) {
   for (int i = 0; i < 2; ++i) {
     z[i] = add2(y[i], splat(kRound));
     const float2 off = fma2(add2(z[i], splat(-kRound)), splat(-1.f), y[i]);
-    *worst = fmaxf(*worst, fmaxf(fabsf(off.x), fabsf(off.y)));
+    *worst = max_mag(*worst, off.x, off.y);
   }
   const uint32_t lo = __byte_perm(__float_as_uint(z[0].x), __float_as_uint(z[0].y), 0x0040);
   const uint32_t hi = __byte_perm(__float_as_uint(z[1].x), __float_as_uint(z[1].y), 0x0040);
   return __byte_perm(lo, hi, 0x5410);
 }
-// sqrt.approx is within 2^-23, relative; with the roundings beside it and those
-// of the exact formula that is 127 * 3.0e-7 for m and, with r's own root, 255 *
-// 4.2e-7 for r.
-constexpr float kNearM = 0.5f - 6e-5f, kNearR = 0.5f - 1.6e-4f;
+// The approximate code of m is sqrt.approx of |m| times 127^2 rcp.approx(scale):
+// relative errors of 2^-23 each, the product's halved by the root, and those
+// of the exact formula, 4.2e-7 in all or 5.3e-5 of 127. r has a root of its own
+// and the scale's: 5.4e-7, or 1.4e-4 of 255.
+constexpr float kNearM = 0.5f - 7e-5f, kNearR = 0.5f - 1.8e-4f;
+
+// Below this largest v of a block its roots are exact: the approximate root
+// takes v < 2^-126 for zero, which decides no code where v is 1e-12 of the
+// largest (a fourth root of 1.1e-3, 0.27 of a code), but would in such a block.
+constexpr float kSmallV = 1e-26f;
+
+// A warp's lane in an entry of the state: its first element there, and in the
+// state's arrays.
+template <typename P, typename G>
+struct Lane {
+  P* p;
+  const G* g;
+  __nv_bfloat16* copy;
+  int64_t at;
+  int left;  // elements of the entry from here on, at most a chunk's
+  float gs, step, rbc2, keep;
+};
+
+// A warp's 256 elements lie over its lanes as two groups of 128, four
+// neighbours per lane in each, so that a load of fp32 is one run of 512 bytes;
+// with 8-bit states, whose codes are a byte each, as eight neighbours per lane.
+template <int kBits>
+struct Layout {
+  static constexpr int kLane = kBits == 8 ? 8 : 4;   // from lane to lane
+  static constexpr int kGap = kBits == 8 ? 4 : 128;  // from a lane's first four to its others
+};
+
+// With 8-bit states there is enough to compute that a warp's next blocks are
+// copied to shared memory ahead (cp.async): each lane copies what it will read
+// itself, so nothing waits for another thread and no registers hold what is on
+// its way.
+template <typename P, typename G>
+struct Ahead {
+  struct Slot {  // one block of a warp
+    P p[32][8];
+    G g[32][8];
+    uint2 mc[32], rc[32];
+  };
+  static constexpr int kSlots = sizeof(Slot) <= 2048 ? 3 : 2;  // at most 6 KB per warp
+  Slot slot[Step<8>::kWarps][kSlots];
+};
+template <int kBytes>
+__device__ __forceinline__ void copy_ahead(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(dst))), "l"(src), "n"(kBytes)
+               : "memory");
+}
+template <typename P, typename G>
+__device__ __forceinline__ void copy_block(const AdamArgs& a, const Lane<P, G>& e, int tile, typename Ahead<P, G>::Slot& s) {
+  const int at = tile * Step<8>::kTile, lane = static_cast<int>(threadIdx.x & 31);
+  const int64_t so = e.at + at;
+#pragma unroll
+  for (int i = 0; i < 8; i += 16 / static_cast<int>(sizeof(G))) copy_ahead<16>(&s.g[lane][i], e.g + at + i);
+#pragma unroll
+  for (int i = 0; i < 8; i += 16 / static_cast<int>(sizeof(P))) copy_ahead<16>(&s.p[lane][i], e.p + at + i);
+  copy_ahead<8>(&s.mc[lane], static_cast<const int8_t*>(a.m) + so);
+  copy_ahead<8>(&s.rc[lane], static_cast<const uint8_t*>(a.v) + so);
+}
+
+// The warp's 256 elements of a tile. kVec: all there and aligned (with 8-bit
+// states, copied ahead, and their scales here). False: a moment has become
+// non-finite.
+template <typename P, typename G, int kBits, bool kVec>
+__device__ __forceinline__ bool step_block(const AdamArgs& a, const Lane<P, G>& e, int tile, const typename Ahead<P, G>::Slot* ahead,
+                                           float ms, float rs) {
+  constexpr int kGap = Layout<kBits>::kGap;
+  const int at = tile * Step<kBits>::kTile, left = e.left - at, lane = static_cast<int>(threadIdx.x & 31);
+  const int64_t so = e.at + at;
+  float pv[8], gv[8];
+  if (kBits == 8 && kVec) {
+    near8(ahead->g[lane], gv);
+    near8(ahead->p[lane], pv);
+  } else {
+    load8<kGap, kVec>(e.g + at, left, gv);
+    load8<kGap, kVec>(e.p + at, left, pv);
+  }
+  bool fine;
+  if (kBits == 32) {
+    float m[8], v[8];
+    float *ma = static_cast<float*>(a.m) + so, *va = static_cast<float*>(a.v) + so;
+    load8<kGap, true>(ma, 0, m);
+    load8<kGap, true>(va, 0, v);
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = gv[i] * e.gs;
+      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(x, a.one_minus_b1));
+      v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(x, x), a.one_minus_b2));
+      const float u = __fdiv_rn(m[i], fmaf(__fsqrt_rn(v[i]), e.rbc2, a.eps));
+      pv[i] = fmaf(pv[i], e.keep, -(u * e.step));
+      top = max_mag(top, m[i], v[i]);
+    }
+    fine = top <= FLT_MAX;
+    store8<kGap, true>(ma, 0, m);
+    store8<kGap, true>(va, 0, v);
+  } else {
+    uint2* ma = reinterpret_cast<uint2*>(static_cast<int8_t*>(a.m) + so);
+    uint2* ra = reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.v) + so);
+    if (!kVec) ms = a.m_scale[so / kBlock], rs = a.r_scale[so / kBlock];
+    const uint2 mq = kVec ? ahead->mc[lane] : __ldcs(ma), rq = kVec ? ahead->rc[lane] : __ldcs(ra);
+    uint32_t mc[2] = {mq.x, mq.y}, rc[2] = {rq.x, rq.y};
+    float2 m[4], v[4], r[4];
+    float mt = 0.f, vt = 0.f, least = FLT_MAX;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      decode_m4(mc[j], ms, m + 2 * j);
+      decode_r4(rc[j], rs, v + 2 * j);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = mul2(make_float2(gv[2 * i], gv[2 * i + 1]), splat(e.gs));
+      m[i] = sum2(mul2(m[i], splat(a.b1)), mul2(x, splat(a.one_minus_b1)), a.one);
+      v[i] = sum2(mul2(mul2(v[i], v[i]), splat(a.b2)), mul2(mul2(x, x), splat(a.one_minus_b2)), a.one);
+      mt = max_mag(mt, m[i].x, m[i].y);
+      vt = max_mag(vt, v[i].x, v[i].y);
+      least = fminf(least, fminf(v[i].x, v[i].y));
+    }
+    mt = warp_max_mag(mt), vt = warp_max_mag(vt);
+    fine = mt <= FLT_MAX && vt <= FLT_MAX;
+    const bool small = vt < kSmallV;
+    if (!small) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = make_float2(sqrt_approx(v[i].x), sqrt_approx(v[i].y));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = make_float2(__fsqrt_rn(v[i].x), __fsqrt_rn(v[i].y));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 d = fma2(r[i], splat(e.rbc2), splat(a.eps));
+      const float2 u = mul2(mul2(m[i], make_float2(rcp_approx(d.x), rcp_approx(d.y))), splat(-e.step));
+      const float2 q = fma2(make_float2(pv[2 * i], pv[2 * i + 1]), splat(e.keep), u);
+      pv[2 * i] = q.x, pv[2 * i + 1] = q.y;
+    }
+    float ms_new = block_scale(mt), rs_new = block_scale(__fsqrt_rn(vt));
+    // zero for blocks held as zero (rcp of their largest would overflow)
+    const float mi = ms_new > 0.f ? rcp_approx(mt) * (127.f * 127.f) : 0.f, ri = rs_new > 0.f ? rsqrt_approx(vt) * (255.f * 255.f) : 0.f;
+    // a root above zero: a code of at least one
+    auto floor_r = [&](float2 k, float2 w) {
+      k = make_float2(fmaxf(k.x, 1.f), fmaxf(k.y, 1.f));
+      if (least == 0.f) k = make_float2(w.x > 0.f ? k.x : 0.f, w.y > 0.f ? k.y : 0.f);
+      return k;
+    };
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float2 y[2];
+      float worst = 0.f, unused = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 s = mul2(m[2 * j + i], splat(mi));
+        y[i] = make_float2(copysignf(sqrt_approx(fabsf(s.x)), s.x), copysignf(sqrt_approx(fabsf(s.y)), s.y));
+      }
+      mc[j] = pack_codes(y, &worst);
+      if (worst > kNearM) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 s = m[2 * j + i];
+          y[i] = make_float2(copysignf(code_exact(fabsf(s.x), ms_new, 127.f), s.x), copysignf(code_exact(fabsf(s.y), ms_new, 127.f), s.y));
+        }
+        mc[j] = pack_codes(y, &unused);
+      }
+      worst = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 s = mul2(r[2 * j + i], splat(ri));
+        y[i] = floor_r(make_float2(sqrt_approx(s.x), sqrt_approx(s.y)), v[2 * j + i]);
+      }
+      rc[j] = pack_codes(y, &worst);
+      if (worst > kNearR || small) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float2 s = v[2 * j + i];
+          y[i] = floor_r(make_float2(code_exact(__fsqrt_rn(s.x), rs_new, 255.f), code_exact(__fsqrt_rn(s.y), rs_new, 255.f)), s);
+        }
+        rc[j] = pack_codes(y, &unused);
+      }
+    }
+    __stcs(ma, make_uint2(mc[0], mc[1]));
+    __stcs(ra, make_uint2(rc[0], rc[1]));
+    if (!fine) ms_new = rs_new = __int_as_float(0x7fc00000);  // no code says NaN: the block's scale does
+    if (lane == 0) a.m_scale[so / kBlock] = ms_new, a.r_scale[so / kBlock] = rs_new;
+  }
+  store8<kGap, kVec>(e.p + at, left, pv);
+  if (e.copy) store8<kGap, kVec>(e.copy + at, left, pv);
+  return fine;
+}
 
 template <typename P, typename G, int kBits>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs a) {
+__global__ void __launch_bounds__(Step<kBits>::kThreads, Step<kBits>::kPerSm) adamw_kernel(const __grid_constant__ AdamArgs a) {
   pdl_allow_dependents();
-  const int64_t chunk = a.chunk0 + blockIdx.x;
-  const int ei = a.chunk_entry[chunk];
-  const AdamEntry E = a.entries[ei];
-  const int lane = threadIdx.x & 31;
-  const int64_t base = (chunk - E.chunk0) * kAdamChunk + (threadIdx.x >> 5) * kBlock;  // the warp's block of E
-  P* p = static_cast<P*>(a.params[ei - a.entry0]);
-  const G* g = static_cast<const G*>(a.grads[ei - a.entry0]);
-  __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(a.copies[ei - a.entry0]);
+  const Chunk c = a.chunks_of[a.chunk0 + blockIdx.x];
+  P* p = static_cast<P*>(a.params[c.entry - a.entry0]) + c.first;
+  const G* g = static_cast<const G*>(a.grads[c.entry - a.entry0]) + c.first;
+  __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(a.copies[c.entry - a.entry0]);
   pdl_wait_predecessor();
-  float gs = 1.f;
+  Lane<P, G> e;
+  e.gs = 1.f;
   if (a.grad_scale) {
-    gs = *a.grad_scale;
-    if (!(fabsf(gs) <= FLT_MAX)) {  // every block sees it: nothing changes, the step does not count
+    e.gs = *a.grad_scale;
+    if (!(fabsf(e.gs) <= FLT_MAX)) {  // every block sees it: nothing changes, the step does not count
       if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(&a.clock->nonfinite, 0, kSkipped);
       return;
     }
   }
-  const float step = __fmul_rn(a.lr, a.clock->inv_bc1);
-  const float rbc2 = a.clock->inv_sqrt_bc2;
-  const float keep = 1.f - a.lr * a.wd * E.decay;
-  if (base < E.numel) {
-    const bool full = base + kBlock <= E.numel;
-    const bool pvec = full && (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(P) - 1)) == 0;
-    const bool gvec = full && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
-    const bool cvec = full && (reinterpret_cast<uintptr_t>(copy) & 7u) == 0;
-    const int64_t at = base + 4 * lane;
-    float pv[8], gv[8];  // two groups of four, 128 apart
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      load4(g + at + 128 * j, E.numel - at - 128 * j, gvec, gv + 4 * j);
-      load4(p + at + 128 * j, E.numel - at - 128 * j, pvec, pv + 4 * j);
-    }
-    const int64_t so = E.off + at;  // the state's arrays are padded to whole blocks
-    const int64_t sb = (E.off + base) / kBlock;
-    bool bad;
-    if (kBits == 32) {
-      float m[8], v[8];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        Quad<float>::load(static_cast<const float*>(a.m) + so + 128 * j, m + 4 * j);
-        Quad<float>::load(static_cast<const float*>(a.v) + so + 128 * j, v + 4 * j);
-      }
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = gv[i] * gs;
-        m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(x, a.one_minus_b1));
-        v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(x, x), a.one_minus_b2));
-        const float u = __fdiv_rn(m[i], fmaf(__fsqrt_rn(v[i]), rbc2, a.eps));
-        pv[i] = fmaf(pv[i], keep, -(u * step));
-        top = max_nan(top, max_nan(fabsf(m[i]), v[i]));
-      }
-      bad = !(top <= FLT_MAX);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        Quad<float>::store(static_cast<float*>(a.m) + so + 128 * j, m + 4 * j);
-        Quad<float>::store(static_cast<float*>(a.v) + so + 128 * j, v + 4 * j);
-      }
-    } else {
-      const float ms = a.m_scale[sb], rs = a.r_scale[sb];
-      uint32_t mc[2], rc[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        mc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(a.m) + so + 128 * j));
-        rc[j] = __ldcs(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + so + 128 * j));
-      }
-      float2 m[4], v[4], r[4];
-      float mt = 0.f, vt = 0.f;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        decode_m4(mc[j], ms, m + 2 * j);
-        decode_r4(rc[j], rs, v + 2 * j);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 x = mul2(make_float2(gv[2 * i], gv[2 * i + 1]), splat(gs));
-        m[i] = sum2(mul2(m[i], splat(a.b1)), mul2(x, splat(a.one_minus_b1)), a.one);
-        v[i] = sum2(mul2(mul2(v[i], v[i]), splat(a.b2)), mul2(mul2(x, x), splat(a.one_minus_b2)), a.one);
-        mt = max_nan(mt, max_nan(fabsf(m[i].x), fabsf(m[i].y)));
-        vt = max_nan(vt, max_nan(v[i].x, v[i].y));
-        r[i] = make_float2(sqrt_approx(v[i].x), sqrt_approx(v[i].y));
-        const float2 d = fma2(r[i], splat(rbc2), splat(a.eps));
-        const float2 u = mul2(mul2(m[i], make_float2(rcp_approx(d.x), rcp_approx(d.y))), splat(-step));
-        const float2 q = fma2(make_float2(pv[2 * i], pv[2 * i + 1]), splat(keep), u);
-        pv[2 * i] = q.x, pv[2 * i + 1] = q.y;
-      }
-      mt = warp_max(mt), vt = warp_max(vt);
-      bad = !(mt <= FLT_MAX) || !(vt <= FLT_MAX);
-      float mi, ri;
-      float ms_new = block_scale(mt, &mi), rs_new = block_scale(__fsqrt_rn(vt), &ri);
-      if (bad) ms_new = rs_new = __int_as_float(0x7fc00000);  // no code says NaN: the block's scale does
-      float worst_m = 0.f, worst_r = 0.f;
-      float2 y[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float2 s = mul2(m[2 * j + i], splat(mi));
-          const float2 k = mul2(make_float2(sqrt_approx(fabsf(s.x)), sqrt_approx(fabsf(s.y))), splat(127.f));
-          y[i] = make_float2(copysignf(k.x, s.x), copysignf(k.y, s.y));
-        }
-        mc[j] = pack_codes(y, &worst_m);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float2 s = mul2(r[2 * j + i], splat(ri));
-          const float2 k = mul2(make_float2(sqrt_approx(s.x), sqrt_approx(s.y)), splat(255.f));
-          // above zero, at least one
-          y[i] = make_float2(fmaxf(k.x, __saturatef(k.x * 1e38f)), fmaxf(k.y, __saturatef(k.y * 1e38f)));
-        }
-        rc[j] = pack_codes(y, &worst_r);
-      }
-      float unused = 0.f;
-      if (worst_m > kNearM) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float2 s = m[2 * j + i];
-            y[i] = make_float2(copysignf(code_exact(fabsf(s.x), mi, 127.f), s.x), copysignf(code_exact(fabsf(s.y), mi, 127.f), s.y));
-          }
-          mc[j] = pack_codes(y, &unused);
-        }
-      }
-      if (worst_r > kNearR) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float2 s = v[2 * j + i];
-            const float kx = code_exact(__fsqrt_rn(s.x), ri, 255.f), ky = code_exact(__fsqrt_rn(s.y), ri, 255.f);
-            y[i] = make_float2(fmaxf(kx, __saturatef(kx * 1e38f)), fmaxf(ky, __saturatef(ky * 1e38f)));
-          }
-          rc[j] = pack_codes(y, &unused);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<int8_t*>(a.m) + so + 128 * j), mc[j]);
-        __stcs(reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + so + 128 * j), rc[j]);
-      }
-      if (lane == 0) a.m_scale[sb] = ms_new, a.r_scale[sb] = rs_new;
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      store4(p + at + 128 * j, E.numel - at - 128 * j, pvec, pv + 4 * j);
-      if (copy) store4(copy + at + 128 * j, E.numel - at - 128 * j, cvec, pv + 4 * j);
-    }
-    if (bad) atomicCAS(&a.clock->nonfinite, 0, ei + 1);
-  }
+  e.step = a.lr * a.clock->inv_bc1;
+  e.rbc2 = a.clock->inv_sqrt_bc2;
+  e.keep = 1.f - a.lr * a.wd * c.decay;
   if (a.last) {
-    __syncthreads();  // every thread of this block has read the clock
+    // The last block to have read the clock moves it on. (At the end, this
+    // barrier would hold every warp until the block's slowest.)
+    __syncthreads();
     if (threadIdx.x == 0 && atomicInc(&a.clock->ticket, gridDim.x - 1) == gridDim.x - 1)
       set_clock(a.clock, a.clock->b1t * a.beta1, a.clock->b2t * a.beta2, a.clock->steps + 1);
   }
+  // the lane's first element; the state's arrays are padded to whole blocks
+  const int first = static_cast<int>(threadIdx.x >> 5) * kBlock, at = first + Layout<kBits>::kLane * static_cast<int>(threadIdx.x & 31);
+  const bool aligned = ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(copy)) & 15u) == 0;
+  e.p = p + at, e.g = g + at, e.copy = copy ? copy + c.first + at : nullptr;
+  e.at = c.off + at;
+  e.left = c.left - at;
+  // the warp's tiles that begin in the entry, and those that are whole and aligned
+  constexpr int kTile = Step<kBits>::kTile;
+  const int left = c.left - first, tiles = left <= 0 ? 0 : (left + kTile - 1) / kTile;
+  const int whole = !aligned || tiles == 0 ? 0 : left - (tiles - 1) * kTile >= kBlock ? tiles : tiles - 1;
+  bool fine = true;
+  if (kBits == 8) {
+    using A = Ahead<P, G>;
+    __shared__ __align__(16) uint8_t room[kBits == 8 ? sizeof(A) : 16];
+    auto& slots = reinterpret_cast<A*>(room)->slot[threadIdx.x >> 5];
+    auto ahead = [&](int i, int s) {
+      if (i < whole) copy_block(a, e, i, slots[s]);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int s = 0; s < A::kSlots - 1; ++s) ahead(s, s);
+    int s = 0;
+    const float* msp = a.m_scale + e.at / kBlock;
+    const float* rsp = a.r_scale + e.at / kBlock;
+    float ms = 0.f, rs = 0.f;
+    if (whole > 0) ms = *msp, rs = *rsp;
+#pragma unroll 1
+    for (int i = 0; i < whole; ++i) {
+      ahead(i + A::kSlots - 1, s == 0 ? A::kSlots - 1 : s - 1);
+      const float ms_now = ms, rs_now = rs;
+      if (i + 1 < whole) ms = msp[(i + 1) * (kTile / kBlock)], rs = rsp[(i + 1) * (kTile / kBlock)];
+      asm volatile("cp.async.wait_group %0;" ::"n"(A::kSlots - 1) : "memory");
+      fine = step_block<P, G, kBits, true>(a, e, i, &slots[s], ms_now, rs_now) && fine;
+      if (++s == A::kSlots) s = 0;
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < whole; ++i) fine = step_block<P, G, kBits, true>(a, e, i, nullptr, 0.f, 0.f) && fine;
+  }
+#pragma unroll 1
+  for (int i = whole; i < tiles; ++i) fine = step_block<P, G, kBits, false>(a, e, i, nullptr, 0.f, 0.f) && fine;
+  if (!fine) atomicCAS(&a.clock->nonfinite, 0, c.entry + 1);
 }
 
 // out[0] = sqrt(sum g^2), out[1] = the coefficient that brings it to at most
@@ -418,26 +580,43 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   pdl_wait_predecessor();
   __shared__ WideSum sh[2][kAdamThreads / 32];
   __shared__ bool final_block;
-  const int lane = threadIdx.x & 31;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int64_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-    const int64_t chunk = a.chunk0 + c;
-    const int ei = a.chunk_entry[chunk];
-    const int64_t numel = a.entries[ei].numel;
-    const int64_t base = (chunk - a.entries[ei].chunk0) * kAdamChunk + (threadIdx.x >> 5) * kBlock;
-    if (base >= numel) continue;
-    const G* g = static_cast<const G*>(a.grads[ei - a.entry0]);
-    const bool vec = base + kBlock <= numel && (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(G) - 1)) == 0;
-    const int64_t at = base + 4 * lane;
-    float x[8];
-    load4(g + at, numel - at, vec, x);
-    load4(g + at + 128, numel - at - 128, vec, x + 4);
+  constexpr int N = 16 / sizeof(G);  // elements of a 16-byte load
+  float2 acc[N / 2] = {};
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  constexpr int kWarps = kAdamThreads / 32;
+  for (int64_t u = blockIdx.x * kWarps + (threadIdx.x >> 5); u < a.chunks << a.shift; u += static_cast<int64_t>(gridDim.x) * kWarps) {
+    const Chunk ch = a.chunks_of[a.chunk0 + (u >> a.shift)];
+    const int at = static_cast<int>(u - (u >> a.shift << a.shift)) * a.unit, n = min(a.unit, ch.left - at);
+    if (n <= 0) continue;
+    const G* g = static_cast<const G*>(a.grads[ch.entry - a.entry0]) + ch.first + at;
+    // to the next 16-byte boundary one by one, as the rest that fills none at the end
+    const int lead = static_cast<int>(((16u - (reinterpret_cast<uintptr_t>(g) & 15u)) & 15u) / sizeof(G));
+    const int head = min(lead, n), quads = (n - head) / N;
+    if (lane < head) {
+      const float x = to_f(g[lane]);
+      acc[0].x = fmaf(x, x, acc[0].x);
+    }
+    const int tail = head + quads * N + lane;
+    if (tail < n) {
+      const float x = to_f(g[tail]);
+      acc[0].y = fmaf(x, x, acc[0].y);
+    }
+    const uint4* q = reinterpret_cast<const uint4*>(g + head);
+#pragma unroll 8
+    for (int i = lane; i < quads; i += 32) {
+      const uint4 w = __ldcs(q + i);
+      G h[N];
+      memcpy(h, &w, 16);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = fmaf(x[i], x[i], acc[i]);
+      for (int k = 0; k < N / 2; ++k) {
+        const float2 x = make_float2(to_f(h[2 * k]), to_f(h[2 * k + 1]));
+        acc[k] = fma2(x, x, acc[k]);
+      }
+    }
   }
   WideSum t;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) t.add(acc[i]);
+  for (int k = 0; k < N / 2; ++k) t.add(acc[k].x), t.add(acc[k].y);
   const float s = block_total(t, sh[0]);
   if (threadIdx.x == 0) {
     a.partials[a.part0 + blockIdx.x] = s;
@@ -493,16 +672,15 @@ size_t dtype_bytes(int t) { return t == MEQ_F32 ? 4 : 2; }
 
 struct meq_adamw {
   int n = 0;
-  std::vector<AdamEntry> entries;
   std::vector<Part> parts;
   meq_adamw_options opt{};
   int64_t elements = 0;  // of the padded state arrays
-  int device = 0, total_parts = 0;
+  int device = 0, total_parts = 0, norm_shift = 0;
+  int64_t chunk = 0;
   char* arena = nullptr;
   void *d_m = nullptr, *d_v = nullptr;
   float *d_ms = nullptr, *d_rs = nullptr;
-  AdamEntry* d_entries = nullptr;
-  int32_t* d_chunk_entry = nullptr;
+  Chunk* d_chunks = nullptr;
   AdamClock* d_clock = nullptr;
   float* d_partials = nullptr;
   cudaStream_t last_stream = nullptr;
@@ -548,23 +726,33 @@ int64_t pad_block(int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; }
 // Entries, launches and the arena's layout; host only.
 struct Plan {
   int64_t elements = 0, chunks = 0, persistent = 0, total = 0;
-  int64_t o_m = 0, o_v = 0, o_ms = 0, o_rs = 0, o_entries = 0, o_chunks = 0, o_clock = 0, o_partials = 0;
+  int64_t o_m = 0, o_v = 0, o_ms = 0, o_rs = 0, o_chunks = 0, o_clock = 0, o_partials = 0;
   int total_parts = 0;
+  int64_t chunk = 0;  // elements of one
+  int norm_shift = 0;
   std::vector<AdamEntry> entries;
   std::vector<Part> parts;
 };
 Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_adamw_options& o, int sms) {
   Plan P;
   P.entries.resize(n);
+  int64_t numel = 0;
+  for (int i = 0; i < n; ++i) numel += shapes[i].rows * shapes[i].cols;
+  // longer chunks as long as there are some four for every block that the SMs hold
+  const bool small = o.state_bits == 8;
+  P.chunk = small ? Step<8>::kMinChunk : Step<32>::kMinChunk;
+  const int64_t most = small ? Step<8>::kMaxChunk : Step<32>::kMaxChunk;
+  const int64_t resident = static_cast<int64_t>(sms) * (small ? Step<8>::kPerSm : Step<32>::kPerSm);
+  while (P.chunk < most && numel >= 4 * resident * 2 * P.chunk) P.chunk *= 2;
+  while (P.chunk >> P.norm_shift > kNormUnit) ++P.norm_shift;
   for (int i = 0; i < n; ++i) {
     AdamEntry& E = P.entries[i];
     E.numel = shapes[i].rows * shapes[i].cols;
     E.off = P.elements;
     E.chunk0 = P.chunks;
     E.decay = decay ? decay[i] : 1.f;
-    E.pad = 0;
     P.elements += pad_block(E.numel);
-    P.chunks += (E.numel + kAdamChunk - 1) / kAdamChunk;
+    P.chunks += (E.numel + P.chunk - 1) / P.chunk;
   }
   for (int i = 0; i < n; i += kMaxEntries) {
     Part p{};
@@ -573,7 +761,8 @@ Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_ada
     p.chunk0 = P.entries[i].chunk0;
     p.chunks = (i + p.entries < n ? P.entries[i + p.entries].chunk0 : P.chunks) - p.chunk0;
     const int64_t most = static_cast<int64_t>(sms) * kNormBlocksPerSm;
-    p.norm_blocks = static_cast<int>(p.chunks < most ? p.chunks : most);
+    const int64_t blocks = ((p.chunks << P.norm_shift) + kAdamThreads / 32 - 1) / (kAdamThreads / 32);
+    p.norm_blocks = static_cast<int>(blocks < most ? blocks : most);
     p.part0 = P.total_parts;
     P.total_parts += p.norm_blocks;
     P.parts.push_back(p);
@@ -588,8 +777,7 @@ Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_ada
   P.o_v = add(P.elements * each);
   P.o_ms = add(scales);
   P.o_rs = add(scales);
-  P.o_entries = add(static_cast<int64_t>(n) * sizeof(AdamEntry));
-  P.o_chunks = add(P.chunks * 4);
+  P.o_chunks = add(P.chunks * static_cast<int64_t>(sizeof(Chunk)));
   P.o_clock = add(sizeof(AdamClock));
   P.o_partials = add(static_cast<int64_t>(P.total_parts) * 4);
   P.persistent = 2 * (P.elements * each + scales);
@@ -624,8 +812,8 @@ meq_status check_device(meq_adamw* st) {
 
 template <typename P, typename G>
 cudaError_t launch_adamw(int bits, const AdamArgs& a, unsigned grid, cudaStream_t s) {
-  if (bits == 32) return launch_pdl(adamw_kernel<P, G, 32>, dim3(grid), dim3(kAdamThreads), 0, s, 1, a);
-  return launch_pdl(adamw_kernel<P, G, 8>, dim3(grid), dim3(kAdamThreads), 0, s, 1, a);
+  if (bits == 32) return launch_pdl(adamw_kernel<P, G, 32>, dim3(grid), dim3(Step<32>::kThreads), 0, s, 1, a);
+  return launch_pdl(adamw_kernel<P, G, 8>, dim3(grid), dim3(Step<8>::kThreads), 0, s, 1, a);
 }
 template <typename P>
 cudaError_t launch_adamw(const meq_adamw_options& o, const AdamArgs& a, unsigned grid, cudaStream_t s) {
@@ -678,10 +866,13 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
     if (ms != MEQ_OK) return ms;
     Plan P = make_plan(shapes, decay, n, o, sms);
     if (!check_plan(P, &why)) return fail(nullptr, MEQ_ERR_INVALID_ARG, why);
-    std::vector<int32_t> chunk_entry(static_cast<size_t>(P.chunks));
+    const int64_t size = P.chunk;
+    std::vector<Chunk> chunks;
+    chunks.reserve(static_cast<size_t>(P.chunks));
     for (int i = 0; i < n; ++i) {
-      const int64_t end = i + 1 < n ? P.entries[i + 1].chunk0 : P.chunks;
-      for (int64_t c = P.entries[i].chunk0; c < end; ++c) chunk_entry[static_cast<size_t>(c)] = i;
+      const AdamEntry& E = P.entries[i];
+      for (int64_t at = 0; at < E.numel; at += size)
+        chunks.push_back(Chunk{at, E.off + at, static_cast<int32_t>(E.numel - at < size ? E.numel - at : size), i, E.decay, 0});
     }
     AdamClock clock;
     std::memset(&clock, 0, sizeof(clock));
@@ -697,7 +888,7 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
     } own{new meq_adamw()};
     meq_adamw* st = own.st;
     st->n = n, st->opt = o, st->device = dev;
-    st->elements = P.elements, st->total_parts = P.total_parts;
+    st->elements = P.elements, st->total_parts = P.total_parts, st->norm_shift = P.norm_shift, st->chunk = P.chunk;
     cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&st->arena), static_cast<size_t>(P.total));
     if (e != cudaSuccess) {
       cudaGetLastError();
@@ -707,18 +898,15 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
     char* A = st->arena;
     st->d_m = A + P.o_m, st->d_v = A + P.o_v;
     st->d_ms = reinterpret_cast<float*>(A + P.o_ms), st->d_rs = reinterpret_cast<float*>(A + P.o_rs);
-    st->d_entries = reinterpret_cast<AdamEntry*>(A + P.o_entries);
-    st->d_chunk_entry = reinterpret_cast<int32_t*>(A + P.o_chunks);
+    st->d_chunks = reinterpret_cast<Chunk*>(A + P.o_chunks);
     st->d_clock = reinterpret_cast<AdamClock*>(A + P.o_clock);
     st->d_partials = reinterpret_cast<float*>(A + P.o_partials);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     e = cudaMemsetAsync(A, 0, static_cast<size_t>(P.total), s);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_entries, P.entries.data(), sizeof(AdamEntry) * n, cudaMemcpyHostToDevice, s);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_chunk_entry, chunk_entry.data(), 4 * chunk_entry.size(), cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_chunks, chunks.data(), sizeof(Chunk) * chunks.size(), cudaMemcpyHostToDevice, s);
     if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_clock, &clock, sizeof(clock), cudaMemcpyHostToDevice, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_CUDA, std::string("initialising the AdamW state failed: ") + cudaGetErrorString(e));
-    st->entries = std::move(P.entries);
     st->parts = std::move(P.parts);
     st->last_stream = s;
     own.st = nullptr;
@@ -738,8 +926,9 @@ meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float ma
     if (ms != MEQ_OK) return ms;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     NormArgs a;
-    a.entries = st->d_entries, a.chunk_entry = st->d_chunk_entry, a.clock = st->d_clock, a.partials = st->d_partials;
+    a.chunks_of = st->d_chunks, a.clock = st->d_clock, a.partials = st->d_partials;
     a.out = out, a.max_norm = max_norm, a.parts = st->total_parts;
+    a.shift = st->norm_shift, a.unit = static_cast<int32_t>(st->chunk >> st->norm_shift);
     for (size_t k = 0; k < st->parts.size(); ++k) {
       const Part& p = st->parts[k];
       a.entry0 = p.entry0, a.chunk0 = p.chunk0, a.chunks = p.chunks, a.part0 = p.part0;
@@ -770,7 +959,7 @@ meq_status meq_adamw_step(void* const* params, const void* const* grads, void* c
     if (ms != MEQ_OK) return ms;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     AdamArgs a;
-    a.entries = st->d_entries, a.chunk_entry = st->d_chunk_entry, a.clock = st->d_clock;
+    a.chunks_of = st->d_chunks, a.clock = st->d_clock;
     a.m = st->d_m, a.v = st->d_v, a.m_scale = st->d_ms, a.r_scale = st->d_rs, a.grad_scale = grad_scale;
     a.beta1 = st->opt.beta1, a.beta2 = st->opt.beta2;
     a.b1 = static_cast<float>(a.beta1), a.one_minus_b1 = static_cast<float>(1.0 - a.beta1);
