@@ -349,6 +349,32 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
   return r;
 }
 
+// z - log(sum_j exp(z_j)) from a row's maximum m and sum s, rounded about once:
+// z - m and the part of log(s) that its exponent gives, a multiple of log(2),
+// are added with their rounding errors, and log of s's significand, below
+// log(2), joins those. (The log-ratios of an answer are summed over hundreds of
+// tokens: half an ulp of lse and of log(s) each, and any common bias, show.)
+constexpr float kLn2 = 0.693147182f, kLn2Lo = -1.90465421e-9f;  // log(2) in two parts
+// ex2.approx is low by 5.0e-8 of its value on average for negative arguments (measured over [-20, 0]).
+constexpr float kExpBias = 5.0e-8f;
+__device__ __forceinline__ float two_sum(float a, float b, float* error) {
+  const float s = __fadd_rn(a, b), v = __fadd_rn(s, -a);
+  *error = __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -v)), __fadd_rn(b, -v));
+  return s;
+}
+__device__ __forceinline__ float log_prob(float z, MaxSum t) {
+  if (!(t.s >= FLT_MIN && t.s <= FLT_MAX)) return (z - t.m) - logf(t.s);
+  const uint32_t bits = __float_as_uint(t.s);
+  const float k = static_cast<float>(static_cast<int>(bits >> 23) - 127);
+  const float log_part = logf(__uint_as_float((bits & 0x007FFFFFu) | 0x3F800000u));
+  const float ln = __fmul_rn(k, kLn2), off = fmaf(k, kLn2, -ln);
+  float e0, e1;
+  const float d = two_sum(z, -t.m, &e0), r = two_sum(d, -ln, &e1);
+  const float tail = (e0 + e1) - ((off + fmaf(k, kLn2Lo, kExpBias)) + log_part);
+  // an infinite d has no error terms
+  return fabsf(d) <= FLT_MAX ? r + tail : d;
+}
+
 // The policy loss of one token: its terms, unweighted, and dL/dlogp.
 struct TokenLoss {
   float surrogate, k3, clipped, slope;

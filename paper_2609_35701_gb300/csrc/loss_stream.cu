@@ -484,12 +484,12 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
           for (uint32_t k = 1; k < ctas; ++k) t = join(t, sh.cta[group][b][k]);
         }
         if (!ok) t.m = t.s = __int_as_float(0x7fc00000);
-        const float logs = logf(t.s), logp = (e.zt - t.m) - logs;
+        const float logp = log_prob(e.zt, t);
         const bool leader = rank == 0 && lane == 0;
         if (leader) a.logp[row] = logp;
         if (!kPolicy) {
           if (leader) {
-            if (a.lse) a.lse[row] = t.m + logs;
+            if (a.lse) a.lse[row] = -log_prob(0.f, t);
             if (a.stat) a.stat[row] = make_float2(t.m, t.s);
             if (a.coef) a.coef[row] = 0.f;
           }

@@ -175,12 +175,12 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
     }
   }
   const MaxSum all = row_join(ws, sh, rank, ctas);
-  const float logs = logf(all.s);
-  const float logp = (zt - all.m) - logs;
+  if (!kPolicy && threadIdx.x >= 32) return;
+  const float logp = log_prob(zt, all);
   if (!kPolicy) {
     if (leader) {
       a.logp[row] = logp;
-      if (a.lse) a.lse[row] = all.m + logs;
+      if (a.lse) a.lse[row] = -log_prob(0.f, all);
       if (a.stat) a.stat[row] = make_float2(all.m, all.s);
       if (a.coef) a.coef[row] = 0.f;
     }
