@@ -544,10 +544,12 @@ StreamShape shape_for(int64_t cols, int elem_bytes, bool policy) {
   const int slot = policy ? Cfg<true>::kSlot : Cfg<false>::kSlot;
   s.share = static_cast<int>(share);
   s.rounds = static_cast<int>((share + slot - 1) / slot);
-  // Rows of which the ring holds three go to a group each, which costs one join
-  // per group and row (8192 x 32000 bf16: 83 us, by slots 138); longer ones
-  // would leave two groups idle (2048 x 151936: 111 us, by slots 104).
-  s.by_slots = !policy && kGroups * s.rounds > Cfg<false>::kSlots ? 1 : 0;
+  // Three groups take a row each where the ring holds one row and more to come,
+  // with one join per group and row; a longer row is shared by the groups slot
+  // by slot, since waiting for its own slots would idle two of them. Rows -> slots, us:
+  // 4096 x 32000 bf16 54 -> 107, x 65000 89 -> 110, x 100000 152 -> 150,
+  // 2048 x 151936 111 -> 104.
+  s.by_slots = !policy && s.rounds > Cfg<false>::kSlots ? 1 : 0;
   return s;
 }
 

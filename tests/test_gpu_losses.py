@@ -228,6 +228,47 @@ def test_many_long_rows(meq, dtype, rows, cols, pad, shift, scored):
     assert torch.equal(again.grad, r.grad) and torch.equal(again.sums, r.sums)
 
 
+@pytest.mark.parametrize("scored", ["none", "one", "runs"])
+@pytest.mark.parametrize("cols", [25000, 100000])
+def test_masks_that_leave_little(meq, cols, scored):
+    """No row scored, one, or long runs of each, among many long rows."""
+    rows = 1300
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    z = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
+    t = torch.full((rows,), -100, device="cuda")
+    if scored == "one":
+        t[777] = 5
+    elif scored == "runs":
+        t[:300], t[700:705], t[1299] = 3, 0, cols - 1
+    on = t >= 0
+    want = torch.where(on, torch.stack([torch.log_softmax(z[i].double(), 0)[max(int(t[i]), 0)] for i in range(rows)]), 0.0)
+    r = meq.token_logprobs(z, t)
+    assert ((r.logp.double() - want).abs() <= 2.0 ** -17).all() and not r.logp[~on].any()
+    zero = torch.zeros(rows, device="cuda")
+    r = meq.policy_loss(z, t, r.logp, zero + 1, zero + 1, grad=True)   # ratios of 1 but for rounding: the loss counts the scored rows
+    assert abs(float(r.loss) + float(on.sum())) <= 2.0 ** -16 * float(on.sum())
+    assert not r.grad[~on].any() and bool((r.grad[on] != 0).any(1).all() if on.any() else True)
+
+
+def test_offsets_past_32_bits_in_a_long_batch(meq):
+    """490000 rows of 24000 equal logits, 23.5 GB: log-probabilities of -log(24000), a gradient of 1/24000 each."""
+    rows, cols = 490000, 24000
+    z = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    t = torch.arange(rows, device="cuda") % cols
+    t[::3] = -1
+    on = t >= 0
+    r = meq.token_logprobs(z, t)
+    assert ((r.logp.double() + math.log(cols)).abs()[on] <= 2.0 ** -17).all() and not r.logp[~on].any()
+    zero = torch.zeros(rows, device="cuda")
+    r = meq.policy_loss(z, t, r.logp, zero + 1, zero + 1, grad=z)
+    assert abs(float(r.loss) + float(on.sum())) <= 2.0 ** -16 * float(on.sum())
+    # c = -1: softmax - onehot
+    assert not z[~on].any()
+    rowsum = torch.cat([x.float().sum(1) for x in z.split(20000)])
+    assert (rowsum[on].abs() < 2.0 ** -7).all()   # 23999 bf16 values of 1/24000 and one of 1/24000 - 1
+    assert (z.gather(1, t.clamp(min=0)[:, None])[:, 0][on].float() + 1 < 2.0 ** -8).all()
+
+
 @pytest.mark.parametrize("cols,pad,gpad,gshift", [(1001, 0, 0, 1), (1001, 0, 1, 0), (1000, 8, 0, 3), (4099, 1, 6, 0)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_gradient_rows_at_other_offsets_than_the_logits(meq, dtype, cols, pad, gpad, gshift):
