@@ -1,4 +1,6 @@
-// Shared-memory barriers (mbarrier) and cluster addressing.
+// Shared-memory barriers (mbarrier) and cluster addressing, for the streamed
+// rows of the losses. The Newton-Schulz GEMM keeps helpers of its own: the
+// benchmark ties its recorded DRAM traffic to the text of that file.
 #pragma once
 
 #include <stdint.h>
