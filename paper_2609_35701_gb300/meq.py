@@ -1,8 +1,9 @@
-"""Thin ctypes binding of the MeqMuon C ABI (include/meq.h).
+"""Thin ctypes binding of the C ABI (include/meq.h): MeqMuon, AdamW and the
+losses of fine-tuning.
 
-Argument marshalling only: every step of the optimizer runs in the CUDA
-library. There is no fallback: if libmeq.so is missing or fails to load,
-importing this module raises.
+Argument marshalling only: every step of the optimizers and every loss runs in
+the CUDA library. There is no fallback: if libmeq.so is missing or fails to
+load, importing this module raises.
 """
 from __future__ import annotations
 
@@ -279,26 +280,27 @@ def _require_cuda(t, dtype_name, numel, what, device=None):
         raise ValueError(f"{what} is on cuda:{t.device.index}, the state on cuda:{device}")
 
 
-def _stream_handle(stream):
+def _stream_handle(stream, device=None):
+    """The stream's handle, or that of the current stream (of `device`, if the caller knows the current one)."""
     if stream is None:
         import torch
         # the raw handle: torch.cuda.current_stream() builds a Stream object, which takes longer than a launch
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device))
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
 
 
-def _empty(size, dtype_name, device, stream):
+def _empty(size, dtype, device, stream):
     """An uninitialised CUDA tensor whose memory belongs to the stream that the call runs on."""
     import torch
 
     if stream is None:
-        return torch.empty(size, dtype=getattr(torch, dtype_name), device=f"cuda:{device}")
+        return torch.empty(size, dtype=dtype, device=device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(size, dtype=getattr(torch, dtype_name), device=f"cuda:{device}")
+        return torch.empty(size, dtype=dtype, device=device)
 
 
 class MeqMuon:
@@ -533,6 +535,15 @@ class AdamW:
         for k in self._numels:
             self.offsets.append(at)
             at += -(-k // self.BLOCK) * self.BLOCK
+        self._cuda = torch.device("cuda", self._device)
+        p, size = [ctypes.c_void_p() for _ in range(4)], ctypes.c_int64()
+        self._check(lib.meq_adamw_state_ptrs(self._st, *[ctypes.byref(x) for x in p], ctypes.byref(size)))
+        p, k = [x.value for x in p], size.value
+        if self._opts.state_bits == 32:
+            self._arrays = [("m", p[0], k, "<f4"), ("v", p[1], k, "<f4")]
+        else:
+            self._arrays = [("m_code", p[0], k, "|i1"), ("r_code", p[1], k, "|u1"), ("m_scale", p[2], k // self.BLOCK, "<f4"),
+                            ("r_scale", p[3], k // self.BLOCK, "<f4")]
 
     def _check(self, s):
         if s != MEQ_OK:
@@ -555,7 +566,9 @@ class AdamW:
     def grad_norm(self, grads, max_norm=float("inf"), out=None, stream=None):
         """(norm, clipping coefficient) of the gradients as a CUDA tensor of two floats, without a host sync."""
         if out is None:
-            out = _empty(2, "float32", self._device, stream)
+            import torch
+
+            out = _empty(2, torch.float32, self._device, stream)
         else:
             _require_cuda(out, "float32", 2, "out", self._device)
         g = self._pointers(grads, self._grad_dtype, "grads")
@@ -587,23 +600,17 @@ class AdamW:
         checkpoint and copy into them to resume."""
         import torch
 
-        p = [ctypes.c_void_p() for _ in range(4)]
-        n = ctypes.c_int64()
-        self._check(lib.meq_adamw_state_ptrs(self._st, *[ctypes.byref(x) for x in p], ctypes.byref(n)))
-        k = n.value
-        if self._opts.state_bits == 32:
-            named = [("m", p[0], k, "<f4"), ("v", p[1], k, "<f4")]
-        else:
-            named = [("m_code", p[0], k, "|i1"), ("r_code", p[1], k, "|u1"), ("m_scale", p[2], k // self.BLOCK, "<f4"),
-                     ("r_scale", p[3], k // self.BLOCK, "<f4")]
-        return {name: torch.as_tensor(_DeviceArray(self, ptr.value, (size,), ts), device=f"cuda:{self._device}")
-                for name, ptr, size, ts in named}
+        if not self._st:
+            raise MeqError(1, "the state is closed")
+        return {name: torch.as_tensor(_DeviceArray(self, ptr, (size,), ts), device=self._cuda) for name, ptr, size, ts in self._arrays}
 
     def read_values(self, m=None, v=None, stream=None):
         """(m, v) as fp32 CUDA tensors laid out as the state's arrays (entry i at offsets[i])."""
+        import torch
+
         k = self.offsets[-1] + -(-self._numels[-1] // self.BLOCK) * self.BLOCK
-        m = _empty(k, "float32", self._device, stream) if m is None else m
-        v = _empty(k, "float32", self._device, stream) if v is None else v
+        m = _empty(k, torch.float32, self._device, stream) if m is None else m
+        v = _empty(k, torch.float32, self._device, stream) if v is None else v
         _require_cuda(m, "float32", k, "m", self._device)
         _require_cuda(v, "float32", k, "v", self._device)
         self._check(lib.meq_adamw_read_values(self._st, ctypes.c_void_p(m.data_ptr()), ctypes.c_void_p(v.data_ptr()),
@@ -651,42 +658,39 @@ class PolicyLoss(collections.namedtuple("PolicyLoss", "sums logp grad")):
 
 
 def _logits_args(logits, what="logits"):
-    """(dtype name, rows, cols, row stride) of a CUDA matrix whose columns are consecutive."""
-    name = str(logits.dtype)[6:]
-    if not logits.is_cuda or name not in DTYPES or logits.dim() != 2:
+    """(meq_dtype, rows, cols, row stride) of a CUDA matrix whose columns are consecutive."""
+    kind = DTYPES.get(str(logits.dtype)[6:])
+    if kind is None or not logits.is_cuda or logits.dim() != 2:
         raise ValueError(f"{what} must be a CUDA matrix of one of {sorted(DTYPES)}")
     rows, cols = logits.shape
     ld, step = logits.stride()
     if cols < 1 or (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{what} must have consecutive columns in rows that do not overlap")
-    return name, rows, cols, max(ld, cols)
+    return kind, rows, cols, max(ld, cols)
 
 
-def _vector(t, dtype_name, n, device, what):
+def _vector(t, dtype, n, device, what):
     """The device pointer of a contiguous CUDA vector, or None."""
     if t is None:
         return None
-    import torch
-
-    if not (t.dtype is getattr(torch, dtype_name) and t.get_device() == device and t.numel() == n and t.is_contiguous()):
-        _require_cuda(t, dtype_name, n, what, device)
+    if not (t.dtype is dtype and t.get_device() == device and t.numel() == n and t.is_contiguous()):
+        _require_cuda(t, str(dtype)[6:], n, what, device)
     return t.data_ptr()
 
 
-def _grad_for(logits, grad, stream):
-    """The gradient's tensor: None, the given one, or (True) a new one whose rows
-    lie in their 16 bytes as the logits' do."""
+def _grad_for(logits, rows, cols, ld, grad, stream):
+    """The gradient's tensor, its pointer and row stride: none, the given one, or
+    (True) a new one whose rows lie in their 16 bytes as the logits' do."""
     if grad is None or grad is False:
-        return None, 0
-    name, rows, cols, ld = _logits_args(logits)
+        return None, None, 0
     if grad is True:
         n = 16 // logits.element_size()
         lead, ldg = logits.data_ptr() % 16 // logits.element_size(), cols + (ld - cols) % n
-        flat = _empty(rows * ldg + n, name, logits.device.index, stream)
-        return flat.as_strided((rows, cols), (ldg, 1), lead), ldg
+        grad = _empty(rows * ldg + n, logits.dtype, logits.device, stream).as_strided((rows, cols), (ldg, 1), lead)
+        return grad, grad.data_ptr(), ldg
     if grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.device != logits.device:
         raise ValueError("grad must have the logits' shape, type and device")
-    return grad, _logits_args(grad, "grad")[3]
+    return grad, grad.data_ptr(), _logits_args(grad, "grad")[3]
 
 
 def _current_device(t, what):
@@ -707,12 +711,14 @@ def token_logprobs(logits, targets, stream=None):
     """Log-probabilities of the target tokens and the rows' log-sum-exp
     (meq_token_logprobs). logits: CUDA matrix, fp32, bf16 or fp16, one row per
     token; targets: int64, negative where a row is not scored."""
-    name, rows, cols, ld = _logits_args(logits)
+    import torch
+
+    kind, rows, cols, ld = _logits_args(logits)
     device = _current_device(logits, "logits")
-    t = _vector(targets, "int64", rows, device, "targets")
-    logp, lse = _empty(rows, "float32", device, stream), _empty(rows, "float32", device, stream)
-    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, logp.data_ptr(), lse.data_ptr(),
-                                       _stream_handle(stream)))
+    t = _vector(targets, torch.int64, rows, device, "targets")
+    logp, lse = _empty(rows, torch.float32, logits.device, stream), _empty(rows, torch.float32, logits.device, stream)
+    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), kind, rows, cols, ld, t, logp.data_ptr(), lse.data_ptr(),
+                                       _stream_handle(stream, device)))
     return TokenLogprobs(logp, lse)
 
 
@@ -722,19 +728,21 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
     the logits (meq_policy_loss). grad: True for a new tensor, or the tensor to
     write (it may be logits). sums holds the loss, its surrogate and KL parts
     and the clipped weight; loss is the first of them."""
-    name, rows, cols, ld = _logits_args(logits)
-    device = _current_device(logits, "logits")
-    vectors = [_vector(t, "float32", rows, device, what) for t, what in
-               ((old_logp, "old_logp"), (advantages, "advantages"), (weights, "weights"), (ref_logp, "ref_logp"))]
-    t = _vector(targets, "int64", rows, device, "targets")
-    scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
-    grad, ldg = _grad_for(logits, grad, stream)
-    work = _empty(lib.meq_loss_work_floats(rows, 0), "float32", device, stream)
-    sums, logp = _empty(4, "float32", device, stream), _empty(rows, "float32", device, stream)
-    _check_loss(lib.meq_policy_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, *vectors, float(clip_low),
-                                    float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(),
-                                    None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
-                                    _stream_handle(stream)))
+    import torch
+
+    f32 = torch.float32
+    kind, rows, cols, ld = _logits_args(logits)
+    device, where = _current_device(logits, "logits"), logits.device
+    old, adv = _vector(old_logp, f32, rows, device, "old_logp"), _vector(advantages, f32, rows, device, "advantages")
+    w, ref = _vector(weights, f32, rows, device, "weights"), _vector(ref_logp, f32, rows, device, "ref_logp")
+    t = _vector(targets, torch.int64, rows, device, "targets")
+    scale = _vector(grad_scale, f32, 1, device, "grad_scale")
+    grad, g, ldg = _grad_for(logits, rows, cols, ld, grad, stream)
+    work = _empty(lib.meq_loss_work_floats(rows, 0), f32, where, stream)
+    sums, logp = _empty(4, f32, where, stream), _empty(rows, f32, where, stream)
+    _check_loss(lib.meq_policy_loss(logits.data_ptr(), kind, rows, cols, ld, t, old, adv, w, ref, float(clip_low),
+                                    float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(), g, ldg, scale,
+                                    work.data_ptr(), _stream_handle(stream, device)))
     return PolicyLoss(sums, logp, grad)
 
 
@@ -743,20 +751,22 @@ def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, l
     """The paired preference loss and, if asked for, the gradient of the logits
     (meq_preference_loss). starts: int64 CUDA vector of 2 pairs + 1 row offsets,
     preferred and other answer in turn; grad as in policy_loss."""
-    name, rows, cols, ld = _logits_args(logits)
-    device = _current_device(logits, "logits")
-    if starts.numel() < 3 or starts.numel() % 2 == 0:
-        raise ValueError("starts must hold 2 pairs + 1 offsets")
+    import torch
+
+    f32 = torch.float32
+    kind, rows, cols, ld = _logits_args(logits)
+    device, where = _current_device(logits, "logits"), logits.device
     pairs = starts.numel() // 2
-    st = _vector(starts, "int64", 2 * pairs + 1, device, "starts")
-    vectors = [_vector(t, "float32", rows, device, what) for t, what in ((ref_logp, "ref_logp"), (weights, "weights"))]
-    t = _vector(targets, "int64", rows, device, "targets")
-    scale = _vector(grad_scale, "float32", 1, device, "grad_scale")
-    grad, ldg = _grad_for(logits, grad, stream)
-    work = _empty(lib.meq_loss_work_floats(rows, pairs), "float32", device, stream)
-    logp, margins, loss = (_empty(n, "float32", device, stream) for n in (rows, pairs, ()))
-    _check_loss(lib.meq_preference_loss(logits.data_ptr(), DTYPES[name], rows, cols, ld, t, st, pairs, *vectors, float(beta),
-                                        float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(),
-                                        None if grad is None else grad.data_ptr(), ldg, scale, work.data_ptr(),
-                                        _stream_handle(stream)))
+    if pairs < 1 or starts.numel() != 2 * pairs + 1:
+        raise ValueError("starts must hold 2 pairs + 1 offsets")
+    st = _vector(starts, torch.int64, 2 * pairs + 1, device, "starts")
+    ref, w = _vector(ref_logp, f32, rows, device, "ref_logp"), _vector(weights, f32, rows, device, "weights")
+    t = _vector(targets, torch.int64, rows, device, "targets")
+    scale = _vector(grad_scale, f32, 1, device, "grad_scale")
+    grad, g, ldg = _grad_for(logits, rows, cols, ld, grad, stream)
+    work = _empty(lib.meq_loss_work_floats(rows, pairs), f32, where, stream)
+    logp, margins, loss = _empty(rows, f32, where, stream), _empty(pairs, f32, where, stream), _empty((), f32, where, stream)
+    _check_loss(lib.meq_preference_loss(logits.data_ptr(), kind, rows, cols, ld, t, st, pairs, ref, w, float(beta),
+                                        float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(), g, ldg,
+                                        scale, work.data_ptr(), _stream_handle(stream, device)))
     return PreferenceLoss(loss, margins, logp, grad)
