@@ -7,7 +7,7 @@
 //                 of slots, one mbarrier pair each
 //   warp 1      : schedule: finds the CTA's rows and passes them on, with the
 //                 row's scalars and slots, through a ring of entries
-//   the others  : three groups. With a gradient they take the rows in turn, so
+//   the others  : groups of warps. With a gradient they take the rows in turn, so
 //                 that some compute while others wait for their row's sum:
 //                 statistics slot by slot; then the group's first warp joins the
 //                 warps' sums, works out the row's coefficient and hands it to
@@ -38,26 +38,25 @@ namespace meq {
 namespace loss {
 namespace {
 
-constexpr int kGroups = 3;
-constexpr int kUnitPieces = 4;                     // per lane: a warp's unit is 128 pieces, 2 KB
-constexpr int kUnit = 32 * kUnitPieces;
 constexpr int kRingBytes = 224 * 1024;
 constexpr float kSlack = 16.f;                     // logits above a warp's reference before it moves
-// With a gradient, where rows stay in the ring until it is written, seven warps
-// of a group and 16 slots of 14 KB (8192 x 32000 bf16: 182 us, with eight 196;
-// 2048 x 151936: 204 and 200); for statistics eight, and 14 slots of 16 KB.
-template <bool kPolicy>
+// kPieces: a lane's pieces of a warp's unit. With a gradient, where rows stay in
+// the ring until it is written, four groups of five warps: while one joins its
+// sums and another writes, two take in rows. Groups x warps 4 x 5, 3 x 7, 4 x 6,
+// 5 x 4, us: 8192 x 32000 bf16 171, 185, 170, 182; 4096 x 50001 134, 149, 149, 147.
+template <bool kPolicy, int kPieces>
 struct Cfg {
-  static constexpr int kUserWarps = kPolicy ? 7 : 8;  // of a group
+  static constexpr int kGroups = kPolicy ? 4 : 3, kUserWarps = kPolicy ? 5 : 8;
+  static constexpr int kUnit = 32 * kPieces;
   static constexpr int kUsers = kGroups * kUserWarps;
   static constexpr int kThreads = kUsers * 32 + 64;
   static constexpr int kSlot = kUserWarps * kUnit;    // pieces of a slot: one unit per warp
   static constexpr int kSlots = kRingBytes / (kSlot * 16);
 };
-constexpr int kMostSlots = Cfg<true>::kSlots, kMostUsers = Cfg<false>::kUsers;
-static_assert(Cfg<false>::kSlots <= kMostSlots && Cfg<true>::kUsers <= kMostUsers && kMostUsers <= 32 && kMostSlots <= 32, "");
+constexpr int kMostSlots = Cfg<true, 4>::kSlots, kMostUsers = Cfg<false, 4>::kUsers, kMostGroups = Cfg<true, 4>::kGroups;
+static_assert(kMostUsers <= 32 && kMostSlots <= 32, "a lane, or a bit, for each");
 constexpr int kEntries = 8;
-constexpr int kMaxShare = 76 * 1024;               // of a row per CTA: the ring holds three
+constexpr int kMaxShare = 76 * 1024;               // of a row per CTA: the ring holds 2.8
 constexpr int kMaxCtas = 8;
 constexpr unsigned long long kWaitNs = 4000000000ull;
 
@@ -82,11 +81,11 @@ struct RowResult {
 struct StreamShared {
   uint64_t full[kMostSlots], empty[kMostSlots];
   uint64_t entry_full[kEntries], entry_empty[kEntries];
-  uint64_t joined[kGroups][2], exchange[kGroups][2], ready[kGroups][2];
+  uint64_t joined[kMostGroups][2], exchange[kMostGroups][2], ready[kMostGroups][2];
   Entry entry[kEntries];
   MaxSum warp[2][kMostUsers];
-  MaxSum cta[kGroups][2][kMaxCtas];
-  RowResult result[kGroups][2];
+  MaxSum cta[kMostGroups][2][kMaxCtas];
+  RowResult result[kMostGroups][2];
   uint32_t claimed;  // slot uses whose copies are under way
   int stop;
 };
@@ -98,6 +97,7 @@ struct StreamShape {
   int share;   // pieces of a row per CTA, at most
   int rounds;  // slots per share
   int by_slots;  // statistics: 1: the groups take a row's slots in turn, 0: they take the rows in turn
+  int pieces;    // of a unit, per lane
 };
 
 // All lanes of a warp; the same answer in each. False: gave up.
@@ -170,12 +170,12 @@ __device__ __forceinline__ void send(uint32_t addr_cluster, uint32_t bar_cluster
 // reference (-inf before the first finite logit).
 struct Running {
   float ref = -INFINITY, c = 0.f, fix = 1.f, s = 0.f;
-  template <typename T>
-  __device__ __forceinline__ void add(const uint4 (&q)[kUnitPieces]) {
+  template <typename T, int P>
+  __device__ __forceinline__ void add(const uint4 (&q)[P]) {
     constexpr int H = Elem<T>::N / 2;
     typename Elem<T>::Max top = Elem<T>::none();
 #pragma unroll
-    for (int j = 0; j < kUnitPieces; ++j) top = Elem<T>::max_of(top, q[j]);
+    for (int j = 0; j < P; ++j) top = Elem<T>::max_of(top, q[j]);
     float m = Elem<T>::value(top);
     if (__any_sync(0xffffffffu, m > ref + kSlack)) {
 #pragma unroll
@@ -184,10 +184,10 @@ struct Running {
       s = s * fix * exp_diff(ref, m) / b.fix;
       ref = m, c = b.c, fix = b.fix;
     }
-    float2 a[kUnitPieces] = {make_float2(s, 0.f)};  // sums side by side: one would be a chain of additions
+    float2 a[P] = {make_float2(s, 0.f)};  // sums side by side: one would be a chain of additions
     if (fabsf(ref) <= kFar || ref == -INFINITY) {
 #pragma unroll
-      for (int j = 0; j < kUnitPieces; ++j) {
+      for (int j = 0; j < P; ++j) {
         float2 x[H];
         Elem<T>::unpack(q[j], x);
 #pragma unroll
@@ -199,7 +199,7 @@ struct Running {
       }
     } else {  // +inf gives NaN
 #pragma unroll
-      for (int j = 0; j < kUnitPieces; ++j) {
+      for (int j = 0; j < P; ++j) {
         float2 x[H];
         Elem<T>::unpack(q[j], x);
 #pragma unroll
@@ -207,7 +207,7 @@ struct Running {
       }
     }
 #pragma unroll
-    for (int j = 1; j < kUnitPieces; ++j) a[0] = add2(a[0], a[j]);
+    for (int j = 1; j < P; ++j) a[0] = add2(a[0], a[j]);
     s = a[0].x + a[0].y;
   }
   __device__ __forceinline__ MaxSum total() const {  // of the warp, for every lane
@@ -229,10 +229,11 @@ __device__ __forceinline__ MaxSum lanes_join(MaxSum t) {
   return t;
 }
 
-template <typename T, bool kPolicy>
-__global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const RowArgs a, const StreamShape shape) {
-  using C = Cfg<kPolicy>;
-  constexpr int kSlots = C::kSlots, kSlot = C::kSlot, kUserWarps = C::kUserWarps;
+template <typename T, bool kPolicy, int kPieces>
+__global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_kernel(const RowArgs a, const StreamShape shape) {
+  using C = Cfg<kPolicy, kPieces>;
+  constexpr int kSlots = C::kSlots, kSlot = C::kSlot, kUnit = C::kUnit, kUserWarps = C::kUserWarps, kGroups = C::kGroups;
+  static_assert(C::kSlots <= kMostSlots && C::kUsers <= kMostUsers && C::kGroups <= kMostGroups, "");
   const bool by_slots = !kPolicy && shape.by_slots != 0;
   pdl_allow_dependents();
   extern __shared__ uint8_t smem_raw[];
@@ -403,10 +404,10 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
         uint4* d = reinterpret_cast<uint4*>(g + (k0 * Row<T>::N - r.lead));
         if (same && whole(k0)) {
 #pragma unroll
-          for (int j = 0; j < kUnitPieces; ++j) __stcs(d + 32 * j, f(j));
+          for (int j = 0; j < kPieces; ++j) __stcs(d + 32 * j, f(j));
         } else {
 #pragma unroll 1
-          for (int j = 0; j < kUnitPieces; ++j) {
+          for (int j = 0; j < kPieces; ++j) {
             const int k = k0 + 32 * j;
             if (k >= hi) break;
             if (same && k >= r.begin && k < r.end) __stcs(d + 32 * j, f(j));
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
         uint4* at = reinterpret_cast<uint4*>(ring) + slot * kSlot + uw * kUnit + lane;
         if (!whole(k0)) {
 #pragma unroll 1
-          for (int j = 0; j < kUnitPieces; ++j) {
+          for (int j = 0; j < kPieces; ++j) {
             const int k = k0 + 32 * j;
             if (k >= hi) at[32 * j] = Row<T>::none();
             else if (k < r.begin) at[32 * j] = e.head;
@@ -453,14 +454,14 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
           // before the slot's next copy, which another proxy writes
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        uint4 q[kUnitPieces];
+        uint4 q[kPieces];
 #pragma unroll
-        for (int j = 0; j < kUnitPieces; ++j) q[j] = at[32 * j];
+        for (int j = 0; j < kPieces; ++j) q[j] = at[32 * j];
         if (!kPolicy) {
           __syncwarp();
           if (lane == 0) mbar_arrive_local(smem_u32(&sh.empty[slot]));
         }
-        sum.add<T>(q);
+        sum.add<T, kPieces>(q);
         if (++slot == kSlots) slot = 0, phase ^= 1u;
       }
       MaxSum t = sum.total();
@@ -521,7 +522,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
           if (s.c == 0.f) store_unit(k0, [](int) { return make_uint4(0u, 0u, 0u, 0u); });
           else if (!s.far) store_unit(k0, [&](int j) { return s.template piece<false, T>(at[32 * j]); });
           else store_unit(k0, [&](int j) { return s.template piece<true, T>(at[32 * j]); });
-          if (s.c != 0.f && target_piece < hi && holds<T, kUnitPieces>(r, k0, e.token)) g[e.token] = Elem<T>::make(s.at_target(e.zt));
+          if (s.c != 0.f && target_piece < hi && holds<T, kPieces>(r, k0, e.token)) g[e.token] = Elem<T>::make(s.at_target(e.zt));
         }
         __syncwarp();
         if (lane == 0) mbar_arrive_local(smem_u32(&sh.empty[slot]));
@@ -534,29 +535,36 @@ __global__ void __launch_bounds__(Cfg<kPolicy>::kThreads, 1) stream_kernel(const
   if (ctas > 1) cluster_sync_all();  // no CTA leaves while another may still write to it
 }
 
-StreamShape shape_for(int64_t cols, int elem_bytes, bool policy) {
-  const int n = 16 / elem_bytes;
-  const int64_t pieces = (cols + 2 * n - 2) / n;  // of a row that starts anywhere
-  StreamShape s{1, 0, 0, 0};
-  if (policy)
-    while (s.ctas < kMaxCtas && (pieces + s.ctas - 1) / s.ctas * 16 > kMaxShare) s.ctas *= 2;
-  const int64_t share = ((pieces + s.ctas - 1) / s.ctas + kUnit - 1) / kUnit * kUnit;
-  const int slot = policy ? Cfg<true>::kSlot : Cfg<false>::kSlot;
-  s.share = static_cast<int>(share);
-  s.rounds = static_cast<int>((share + slot - 1) / slot);
+template <bool kPolicy, int kPieces>
+StreamShape shape_with(int64_t row_pieces, int ctas) {
+  using C = Cfg<kPolicy, kPieces>;
+  const int64_t share = ((row_pieces + ctas - 1) / ctas + C::kUnit - 1) / C::kUnit * C::kUnit;
+  const int rounds = static_cast<int>((share + C::kSlot - 1) / C::kSlot);
   // Three groups take a row each where the ring holds one row and more to come,
   // with one join per group and row; a longer row is shared by the groups slot
   // by slot, since waiting for its own slots would idle two of them. Rows -> slots, us:
   // 4096 x 32000 bf16 54 -> 107, x 65000 89 -> 110, x 100000 152 -> 150,
   // 2048 x 151936 111 -> 104.
-  s.by_slots = !policy && s.rounds > Cfg<false>::kSlots ? 1 : 0;
-  return s;
+  return StreamShape{ctas, static_cast<int>(share), rounds, !kPolicy && rounds > C::kSlots ? 1 : 0, kPieces};
+}
+StreamShape shape_for(int64_t cols, int elem_bytes, bool policy) {
+  const int n = 16 / elem_bytes;
+  const int64_t pieces = (cols + 2 * n - 2) / n;  // of a row that starts anywhere
+  if (!policy) return shape_with<false, 4>(pieces, 1);
+  int ctas = 1;
+  while (ctas < kMaxCtas && (pieces + ctas - 1) / ctas * 16 > kMaxShare) ctas *= 2;
+  // Slots of 10 KB, 22 of them; where they hold fewer than three rows, 17 of
+  // 12.5 KB, which a row of 70 to 76 KB fills better. 10 -> 12.5 KB, us:
+  // 2048 x 151936 bf16 206 -> 193, 1024 x 151936 fp32 200 -> 189;
+  // 4096 x 50001 bf16 134 -> 144, x 40000 108 -> 116, 8192 x 32000 171 -> 174.
+  const StreamShape s = shape_with<true, 4>(pieces, ctas);
+  return 3 * s.rounds > Cfg<true, 4>::kSlots ? shape_with<true, 5>(pieces, ctas) : s;
 }
 
 // Clusters of `ctas` CTAs of one kernel that the device holds at a time, asked once per device.
-template <typename T, bool kPolicy>
+template <typename T, bool kPolicy, int kPieces>
 cudaError_t prepared_clusters(int ctas, int* clusters) {
-  auto* kernel = stream_kernel<T, kPolicy>;
+  auto* kernel = stream_kernel<T, kPolicy, kPieces>;
   constexpr int kMaxDevices = 64;
   static std::mutex mu;
   static int known[kMaxDevices][kMaxCtas + 1] = {};
@@ -576,7 +584,7 @@ cudaError_t prepared_clusters(int ctas, int* clusters) {
     } else {
       cudaLaunchConfig_t cfg = {};
       cfg.gridDim = dim3(static_cast<unsigned>(ctas));
-      cfg.blockDim = dim3(Cfg<kPolicy>::kThreads);
+      cfg.blockDim = dim3(Cfg<kPolicy, kPieces>::kThreads);
       cfg.dynamicSmemBytes = kStreamSmem;
       cudaLaunchAttribute attr;
       attr.id = cudaLaunchAttributeClusterDimension;
@@ -594,15 +602,20 @@ cudaError_t prepared_clusters(int ctas, int* clusters) {
   return cudaSuccess;
 }
 
-template <typename T, bool kPolicy>
-cudaError_t launch(const RowArgs& a, cudaStream_t st) {
-  const StreamShape s = shape_for(a.cols, sizeof(T), kPolicy);
+template <typename T, bool kPolicy, int kPieces>
+cudaError_t launch(const RowArgs& a, const StreamShape& s, cudaStream_t st) {
   int clusters = 0;
-  const cudaError_t e = prepared_clusters<T, kPolicy>(s.ctas, &clusters);
+  const cudaError_t e = prepared_clusters<T, kPolicy, kPieces>(s.ctas, &clusters);
   if (e != cudaSuccess) return e;
   if (clusters > a.rows) clusters = static_cast<int>(a.rows);
-  return launch_pdl(stream_kernel<T, kPolicy>, dim3(static_cast<unsigned>(clusters * s.ctas)), dim3(Cfg<kPolicy>::kThreads), kStreamSmem,
-                    st, s.ctas, a, s);
+  return launch_pdl(stream_kernel<T, kPolicy, kPieces>, dim3(static_cast<unsigned>(clusters * s.ctas)),
+                    dim3(Cfg<kPolicy, kPieces>::kThreads), kStreamSmem, st, s.ctas, a, s);
+}
+template <typename T>
+cudaError_t launch(const RowArgs& a, bool policy, cudaStream_t st) {
+  const StreamShape s = shape_for(a.cols, sizeof(T), policy);
+  if (!policy) return launch<T, false, 4>(a, s, st);
+  return s.pieces == 4 ? launch<T, true, 4>(a, s, st) : launch<T, true, 5>(a, s, st);
 }
 
 }  // namespace
@@ -610,21 +623,24 @@ cudaError_t launch(const RowArgs& a, cudaStream_t st) {
 // The other form holds a row in the registers of a CTA or a cluster, one row
 // after another per CTA: less to set up for few or short rows, but nothing is
 // loaded while a row is reduced and written. Measured, that form -> this one, us:
-//   bf16 gradient   304 x 50001 17.8 -> 19.2, 608 x 50001 32.3 -> 29.6, 4096 x 50001 185 -> 147,
-//                   152 x 100000 20.5 -> 19.1, 4096 x 151936 530 -> 380; 4096 x 32000 89.5 -> 88.6,
-//                   4096 x 16000 48.4 -> 60.9
-//   bf16 statistics 608 x 32000 8.7 -> 9.9, 1216 x 32000 17.7 -> 16.0, 152 x 100000 12.0 -> 8.3,
-//                   4096 x 151936 341 -> 192; 4096 x 16000 25.1 -> 30.8
+//   bf16 gradient   4096 x 16000 48.7 -> 58.7, x 24001 87.4 -> 72.5, x 32000 89.6 -> 89.6, x 50001 188 -> 132,
+//                   608 x 32000 17.6 -> 19.5, 304 x 50001 17.3 -> 17.8, 608 x 50001 32.7 -> 28.0,
+//                   152 x 100000 20.5 -> 19.1
+//   fp32 gradient   4096 x 12000 72.8 -> 76.4, x 16000 86.6 -> 97.9, x 18000 114 -> 107, x 32000 190 -> 182
+//   bf16 statistics 4096 x 16000 26.4 -> 33.0, x 24001 49.4 -> 43.1, x 32000 53.1 -> 45.9, x 50001 119 -> 71.6,
+//                   608 x 32000 9.0 -> 10.5, 1216 x 32000 18.7 -> 16.6, 152 x 100000 12.0 -> 8.3
+//   fp32 statistics 4096 x 12000 40.2 -> 35.6, x 16000 44.3 -> 43.3
 bool stream_suits(int64_t rows, int64_t cols, int elem_bytes, bool policy) {
   const int64_t row_bytes = cols * elem_bytes;
-  if (policy && shape_for(cols, elem_bytes, policy).rounds > Cfg<true>::kSlots) return false;
-  return (row_bytes >= 48000 && rows * row_bytes >= 50000000) || (row_bytes >= 192000 && rows >= 128);
+  if (policy && shape_for(cols, elem_bytes, policy).rounds > Cfg<true, 5>::kSlots) return false;
+  const int64_t least = policy && elem_bytes == 4 ? 66000 : 48000;
+  return (row_bytes >= least && rows * row_bytes >= 50000000) || (row_bytes >= 192000 && rows >= 128);
 }
 
 cudaError_t launch_stream(const RowArgs& a, int type, bool policy, cudaStream_t st) {
-  if (type == MEQ_F32) return policy ? launch<float, true>(a, st) : launch<float, false>(a, st);
-  if (type == MEQ_BF16) return policy ? launch<__nv_bfloat16, true>(a, st) : launch<__nv_bfloat16, false>(a, st);
-  return policy ? launch<__half, true>(a, st) : launch<__half, false>(a, st);
+  if (type == MEQ_F32) return launch<float>(a, policy, st);
+  if (type == MEQ_BF16) return launch<__nv_bfloat16>(a, policy, st);
+  return launch<__half>(a, policy, st);
 }
 
 }  // namespace loss

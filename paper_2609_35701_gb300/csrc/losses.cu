@@ -37,7 +37,7 @@ constexpr int kChunkPieces = 32 * kPieces;  // of a warp
 constexpr int kMaxCluster = 8;
 constexpr int kRowThreads = 512;    // most threads of a CTA before the cluster grows
 constexpr int kRowThreadsMax = 1024;
-constexpr int kGradThreads = 256;
+constexpr int kGradThreads = 128;
 constexpr int kGradPieces = 4;
 
 __device__ __forceinline__ uint32_t cluster_size() {
