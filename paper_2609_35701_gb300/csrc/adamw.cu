@@ -9,12 +9,19 @@
 // One pass: 28 bytes per element with everything in fp32 (p, m, v read and
 // written, g read), so HBM bounds it. A launch covers up to kMaxEntries
 // entries, whose pointers travel in the kernel's arguments (no copy to the
-// device before a step), and a block 2048 consecutive elements of one entry: a
-// warp takes 256 of them as two groups of 128, so that every load and store of
-// a warp is one run of 512 bytes (fp32), and all loads are issued before the
-// first is used.
+// device before a step), and a block a chunk of one entry, longer ones in larger
+// states. A warp takes 256 elements at a time, in fp32 as two groups of 128, so
+// that every load and store of a warp is one run of 512 bytes and all loads are
+// issued before the first is used.
 //
-// 8-bit states: 256 elements, one warp's share, have an fp32 scale each for m
+// Measured on 67.1M elements, with the time of the bytes at the measured copy
+// rate (6.79 TB/s) in brackets, us: fp32 277 (277), bf16 parameters and gradients
+// with fp32 moments 222 (218), 8-bit moments 123 (99), the same with fp32 parameters
+// 162 (139); the norm of fp32 gradients 42.7 (39.6), of bf16 ones 24.3 (19.8);
+// the values of 8-bit moments 108 (99).
+//
+// 8-bit states, which instructions bound as much as HBM (some 50 per element, 74%
+// of the issue slots): 256 elements, one warp's share, have an fp32 scale each for m
 // and for r = sqrt(v), the largest |m| and r of the block, and a code per
 // element:
 //
@@ -570,7 +577,8 @@ __global__ void __launch_bounds__(Step<kBits>::kThreads, Step<kBits>::kPerSm) ad
 }
 
 // out[0] = sqrt(sum g^2), out[1] = the coefficient that brings it to at most
-// max_norm. Bound by the one read of the gradients. A thread adds the squares
+// max_norm. Bound by the one read of the gradients, of which a warp takes up to
+// 2048 elements at a time. A thread adds the squares
 // of its share in fp32 (eight sums side by side), the rest is added as
 // WideSum; the blocks' sums lie in `partials` and the last block to finish adds them up,
 // in an order that does not depend on which block that is.
@@ -636,7 +644,8 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   }
 }
 
-// The values that the 8-bit states stand for.
+// The values that the 8-bit states stand for: two bytes read and eight written
+// per element, which bound it. A thread takes four elements.
 __global__ void __launch_bounds__(kAdamThreads) adamw_values_kernel(const uint32_t* __restrict__ m_code,
                                                                     const uint32_t* __restrict__ r_code,
                                                                     const float* __restrict__ m_scale,

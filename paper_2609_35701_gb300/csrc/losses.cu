@@ -7,16 +7,22 @@
 // is a function of the rows' logp, so the gradient of a row is one coefficient
 // c = dL/dlogp times ([j = t] - softmax_j).
 //
-// Policy loss: c depends on the row alone. A row is read once, held in
+// HBM bounds all of them: two exponentials per element stand against 4 bytes
+// moved (bf16, with the gradient).
+//
+// Policy loss: c depends on the row alone, so a row is read once, kept on chip
+// and its gradient written from there: the floor. Few or short rows are held in
 // registers (8 pieces of 16 bytes per thread) by one CTA or a cluster of up to
 // 8, reduced (warp, CTA, then the cluster's CTAs through distributed shared
-// memory) and its gradient written from the registers: the traffic is one read
-// and one write of the logits, the floor. Rows that no cluster holds take
-// three launches (statistics, coefficients, gradient).
+// memory): 4096 x 16000 bf16 49 us (39 at the measured copy rate, 6.79 TB/s).
+// Many long ones are streamed through shared memory, in a file of their own.
+// Rows that neither holds take three launches (statistics, coefficients,
+// gradient).
 //
 // Preference loss: c needs the sums over the two answers of a pair, so the
 // logits are read again for the gradient, last rows first: those are the ones
-// that the statistics pass left in L2.
+// that the statistics pass left in L2. 9600 x 32000 bf16 313 us (272 for two
+// reads and a write at the copy rate).
 //
 // Rows start at any element: a row is cut at the 16-byte boundaries of its
 // address, and only its first and last piece are moved element by element.
@@ -37,6 +43,9 @@ constexpr int kChunkPieces = 32 * kPieces;  // of a warp
 constexpr int kMaxCluster = 8;
 constexpr int kRowThreads = 512;    // most threads of a CTA before the cluster grows
 constexpr int kRowThreadsMax = 1024;
+// 16-byte pieces per thread and threads of the gradient pass: 8 KB of a row per
+// block. 9600 x 32000 bf16, pieces x threads 4 x 128, 4 x 256, 8 x 256, 2 x 256,
+// 4 x 512, us: 212, 213, 215, 213, 219; 2048 x 50001 fp32 147, 148, 151, 149, 155.
 constexpr int kGradThreads = 128;
 constexpr int kGradPieces = 4;
 
@@ -125,9 +134,12 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[kPieces]) {
   return w;
 }
 
-// One CTA or cluster per row. kPolicy: the whole row is in registers, and its
-// loss and gradient follow; else the row's statistics alone, in as many rounds
-// as it takes.
+// One CTA or cluster per row, in one pass over it. kPolicy: the whole row is in
+// registers, and its loss and gradient follow; else the row's statistics alone,
+// in as many rounds as it takes. Bound by HBM where there are many rows
+// (4096 x 16000 bf16: 49 and 26 us, 39 and 19 at the copy rate), else by latency:
+// with the launch of the sums 24 x 32000 fp32 takes 7.6 us, and the statistics of
+// 16 x 151936 bf16 4.7.
 template <typename T, bool kPolicy>
 __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
   pdl_allow_dependents();
@@ -230,7 +242,8 @@ struct Total {
 };
 
 // Gradient of the logits from each row's statistics and coefficient, the last
-// rows first (x, the part of a row, runs faster than y, the row).
+// rows first (x, the part of a row, runs faster than y, the row). Bound by HBM:
+// 4096 x 50001 bf16 122 us alone, the copy rate.
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, const Total total) {
   pdl_allow_dependents();
@@ -262,7 +275,8 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, con
 }
 
 // One block per pair: the weighted sums of logp - ref over the two answers,
-// the loss, and the coefficients of their rows.
+// the loss, and the coefficients of their rows. A few bytes per row: latency
+// bounds it.
 __global__ void __launch_bounds__(kThreads) pair_kernel(const RowArgs a, const int64_t* __restrict__ starts, float beta,
                                                         float smoothing, float inv_pairs, float* __restrict__ margins,
                                                         float* __restrict__ pair_loss) {
