@@ -41,6 +41,8 @@ namespace {
 constexpr int kPieces = 8;          // 16-byte pieces per thread
 constexpr int kChunkPieces = 32 * kPieces;  // of a warp
 constexpr int kMaxCluster = 8;
+constexpr int kShortThreads = 128;
+constexpr int kShortPerSm = 64;     // blocks per SM at most (1000000 x 256 bf16: 16, 64, any number, us: 565, 550, 637)
 constexpr int kRowThreads = 512;    // most threads of a CTA before the cluster grows
 constexpr int kRowThreadsMax = 1024;
 // 16-byte pieces per thread and threads of the gradient pass: 8 KB of a row per
@@ -92,12 +94,12 @@ __device__ __forceinline__ MaxSum row_join(MaxSum w, RowShared& sh, uint32_t ran
 }
 
 // max and sum of exponentials over a warp's pieces, for all its lanes
-template <typename T>
-__device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[kPieces]) {
+template <typename T, int P>
+__device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
   MaxSum w;
   typename Elem<T>::Max top = Elem<T>::none();
 #pragma unroll
-  for (int j = 0; j < kPieces; ++j) top = Elem<T>::max_of(top, q[j]);
+  for (int j = 0; j < P; ++j) top = Elem<T>::max_of(top, q[j]);
   float m = Elem<T>::value(top);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -107,7 +109,7 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[kPieces]) {
   if (fabsf(m) <= kFar || m == -INFINITY) {
     const ExpBase b(finite_or_zero(m));
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
+    for (int j = 0; j < P; ++j) {
       float2 x[H];
       Elem<T>::unpack(q[j], x);
 #pragma unroll
@@ -121,7 +123,7 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[kPieces]) {
   } else {
     // far from zero (+inf gives NaN)
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
+    for (int j = 0; j < P; ++j) {
       float2 x[H];
       Elem<T>::unpack(q[j], x);
 #pragma unroll
@@ -212,6 +214,74 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
   store_grad(r, g, same, first, k0, q, GradScale(c, all.m, all.s), token, zt);
 }
 
+// Rows of up to 32 P pieces (4 KB with P = 8), a warp each: no joins. The
+// instructions that a row takes whatever its length (some 300) bound it below
+// 1 KB, HBM above. 1000000 x 256 bf16 with the gradient and its sums 550 us (151 at
+// the copy rate), a CTA per row 1768; 200000 x 2000 289 (236). With the logits of a
+// warp's next row loaded while it works on one a fifth slower: registers.
+template <typename T, bool kPolicy, int P>
+__global__ void __launch_bounds__(kShortThreads) short_kernel(const RowArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  struct Scalars {
+    int64_t target;
+    float w, old_logp, advantage, ref_logp;
+  };
+  auto fetch = [&](int64_t row) {
+    Scalars s{-1, 1.f, 0.f, 0.f, 0.f};
+    if (row < a.rows) {
+      s.target = a.targets[row];
+      if (a.weights) s.w = a.weights[row];
+      if (kPolicy) {
+        s.old_logp = a.old_logp[row], s.advantage = a.advantages[row];
+        if (a.kl != 0.f) s.ref_logp = a.ref_logp[row];
+      }
+    }
+    return s;
+  };
+  constexpr int kWarps = kShortThreads / 32;
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kWarps;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const float gs = kPolicy && a.grad_scale ? *a.grad_scale : 1.f;
+  for (Scalars next = fetch(row); row < a.rows; row += stride) {
+    const Scalars s = next;
+    next = fetch(row + stride);
+    const Row<T> r(a.logits, row, a.ld, a.cols);
+    T* g = kPolicy && a.grad ? static_cast<T*>(a.grad) + row * a.ld_grad : nullptr;
+    const bool same = same_offset(r.p, g);
+    float logp = 0.f, lse = 0.f, c = 0.f, zt = 0.f;
+    MaxSum all{0.f, 1.f};
+    float4 terms = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int token = s.target < a.cols ? static_cast<int>(s.target) : kNoToken;
+    uint4 q[P];
+    if (s.target >= 0 && s.w != 0.f) {  // else not scored: the logits are not read
+      zt = token != kNoToken ? Elem<T>::get(r.p + token) : __int_as_float(0x7fc00000);
+      r.load(0, lane, q);
+      all = warp_stats<T>(q);
+      zt = __shfl_sync(0xffffffffu, zt, 0);  // read by now: the gradient may lie in the logits' place
+      logp = log_prob(zt, all);
+      if (!kPolicy) lse = -log_prob(0.f, all);
+      if (kPolicy) {
+        const TokenLoss t = policy_token(logp, s.old_logp, s.advantage, &s.ref_logp, a.clip_lo, a.clip_hi, a.kl);
+        terms = make_float4(s.w * (t.surrogate + a.kl * t.k3), s.w * t.surrogate, s.w * t.k3, s.w * t.clipped);
+        c = s.w * t.slope * gs;
+      }
+    }
+    if (lane == 0) {
+      a.logp[row] = logp;
+      if (!kPolicy && a.lse) a.lse[row] = lse;
+      if (!kPolicy && a.stat) a.stat[row] = make_float2(all.m, all.s);
+      if (!kPolicy && a.coef) a.coef[row] = 0.f;
+      if (kPolicy) a.terms[row] = terms;
+    }
+    if (g) {
+      if (c == 0.f) store_zeros<T, P>(r, g, same, 0, lane);
+      else store_grad(r, g, same, 0, lane, q, GradScale(c, all.m, all.s), token, zt);
+    }
+  }
+}
+
 // The policy terms and coefficients of rows whose statistics are known.
 __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const RowArgs a) {
   pdl_allow_dependents();
@@ -242,9 +312,10 @@ struct Total {
 };
 
 // Gradient of the logits from each row's statistics and coefficient, the last
-// rows first (x, the part of a row, runs faster than y, the row). Bound by HBM:
+// rows first (x, the part of a row, runs faster than y, the row, or kRows of them,
+// each a part of the block's warps). Bound by HBM:
 // 4096 x 50001 bf16 122 us alone, the copy rate.
-template <typename T>
+template <typename T, int kRows>
 __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, const Total total) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
@@ -252,9 +323,11 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, con
     __shared__ WideSum sh[kGradThreads / 32];
     total.write(sh);
   }
-  for (int64_t row = a.rows - 1 - blockIdx.y; row >= 0; row -= gridDim.y) {
+  constexpr int kWarps = kGradThreads / 32, kOfRow = kWarps / kRows;
+  const int warp = static_cast<int>(threadIdx.x >> 5);
+  for (int64_t row = a.rows - 1 - (static_cast<int64_t>(blockIdx.y) * kRows + warp / kOfRow); row >= 0; row -= gridDim.y * kRows) {
     const Row<T> r(a.logits, row, a.ld, a.cols);
-    const int first = (static_cast<int>(blockIdx.x) * (kGradThreads / 32) + static_cast<int>(threadIdx.x >> 5)) * 32 * kGradPieces;
+    const int first = (static_cast<int>(blockIdx.x) * kWarps + warp % kOfRow) * 32 * kGradPieces;
     const int k0 = first + static_cast<int>(threadIdx.x & 31);
     T* g = static_cast<T*>(a.grad) + row * a.ld_grad;
     const bool same = same_offset(r.p, g);
@@ -317,25 +390,30 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const RowArgs a, const i
 }
 
 constexpr int kSumThreads = 512;
+constexpr int64_t kSumRows = 8192;  // of a block
 __global__ void __launch_bounds__(kSumThreads) total_kernel(const Total total) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
   __shared__ WideSum sh[kSumThreads / 32];
   total.write(sh);
 }
-// The four sums of the policy loss over the rows' terms, each in a fixed order.
-__global__ void __launch_bounds__(kSumThreads) policy_sums_kernel(const float4* __restrict__ terms, int64_t rows, float* __restrict__ sums) {
+// The four sums of the policy loss over the rows' terms, each in a fixed order:
+// a block adds up `per` of the n terms, which lie `stride` apart, into sums, or
+// (NULL) into the first of them. Latency bounds it: a block takes 5 us for 8192.
+__global__ void __launch_bounds__(kSumThreads) policy_sums_kernel(float4* terms, int64_t n, int64_t stride, int64_t per, float* sums) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
   __shared__ WideSum sh[4][kSumThreads / 32];
   WideSum s[4];
-  for (int64_t i = threadIdx.x; i < rows; i += kSumThreads) {
-    const float4 q = terms[i];
+  const int64_t first = blockIdx.x * per, end = min(first + per, n);
+  for (int64_t i = first + threadIdx.x; i < end; i += kSumThreads) {
+    const float4 q = terms[i * stride];
     s[0].add(q.x), s[1].add(q.y), s[2].add(q.z), s[3].add(q.w);
   }
+  if (!sums) sums = reinterpret_cast<float*>(terms + first * stride);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float t = block_total(s[k], sh[k]);
+    const float t = block_total(s[k], sh[k]);  // every term has been read
     if (threadIdx.x == 0) sums[k] = t;
   }
 }
@@ -366,11 +444,13 @@ int elem_bytes(int type) { return type == MEQ_F32 ? 4 : 2; }
 struct RowShape {
   int ctas, threads;
   bool held;  // the row fits into the cluster's registers
+  int lanes;  // a warp holds the row, with this many pieces per lane (0: it does not)
+  int sms;
 };
 RowShape row_shape(int64_t rows, int64_t cols, int type, int sms) {
   const int n = 16 / elem_bytes(type);
   const int64_t pieces = (cols + 2 * n - 2) / n;  // of a row that starts anywhere
-  RowShape s{1, 32, true};
+  RowShape s{1, 32, true, 0, sms};
   auto need = [&](int ctas) { return (pieces + static_cast<int64_t>(ctas) * kPieces - 1) / (static_cast<int64_t>(ctas) * kPieces); };
   while (s.ctas < kMaxCluster && need(s.ctas) > kRowThreads) s.ctas *= 2;
   // few rows: more SMs to each
@@ -378,25 +458,50 @@ RowShape row_shape(int64_t rows, int64_t cols, int type, int sms) {
   const int64_t t = (need(s.ctas) + 31) / 32 * 32;
   s.held = t <= kRowThreadsMax;
   s.threads = static_cast<int>(s.held ? t : kRowThreads);
+  if (pieces <= 32 * kPieces)
+    for (s.lanes = 1; pieces > 32 * s.lanes;) s.lanes *= 2;
   return s;
+}
+
+template <typename T, bool kPolicy>
+cudaError_t launch_short(const RowArgs& a, const RowShape& s, cudaStream_t st) {
+  constexpr int kWarps = kShortThreads / 32;
+  const int64_t blocks = (a.rows + kWarps - 1) / kWarps, most = static_cast<int64_t>(s.sms) * kShortPerSm;
+  const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most)), block(kShortThreads);
+  if (s.lanes == 1) return launch_pdl(short_kernel<T, kPolicy, 1>, grid, block, 0, st, 1, a);
+  if (s.lanes == 2) return launch_pdl(short_kernel<T, kPolicy, 2>, grid, block, 0, st, 1, a);
+  if (s.lanes == 4) return launch_pdl(short_kernel<T, kPolicy, 4>, grid, block, 0, st, 1, a);
+  return launch_pdl(short_kernel<T, kPolicy, 8>, grid, block, 0, st, 1, a);
 }
 
 template <bool kPolicy>
 cudaError_t launch_rows_of(const RowArgs& a, int type, const RowShape& s, cudaStream_t st) {
   if (stream_suits(a.rows, a.cols, elem_bytes(type), kPolicy)) return launch_stream(a, type, kPolicy, st);
+  if (s.lanes) {
+    if (type == MEQ_F32) return launch_short<float, kPolicy>(a, s, st);
+    if (type == MEQ_BF16) return launch_short<__nv_bfloat16, kPolicy>(a, s, st);
+    return launch_short<__half, kPolicy>(a, s, st);
+  }
   const dim3 grid(static_cast<unsigned>(a.rows * s.ctas)), block(s.threads);
   if (type == MEQ_F32) return launch_pdl(row_kernel<float, kPolicy>, grid, block, 0, st, s.ctas, a);
   if (type == MEQ_BF16) return launch_pdl(row_kernel<__nv_bfloat16, kPolicy>, grid, block, 0, st, s.ctas, a);
   return launch_pdl(row_kernel<__half, kPolicy>, grid, block, 0, st, s.ctas, a);
 }
 
+template <typename T>
+cudaError_t launch_grad(const RowArgs& a, const Total& total, cudaStream_t st) {
+  constexpr int kWarps = kGradThreads / 32;
+  constexpr int64_t per = kGradPieces * kGradThreads;
+  const int64_t pieces = (a.cols + 2 * Elem<T>::N - 2) / Elem<T>::N;
+  // rows that a warp covers: as many of a block as it has warps (1000000 x 256 bf16: 900 -> 380 us)
+  const int64_t rows = pieces * kWarps <= per ? kWarps : 1, blocks = (a.rows + rows - 1) / rows;
+  const dim3 grid(static_cast<unsigned>((pieces + per - 1) / per), static_cast<unsigned>(blocks < 65535 ? blocks : 65535)), block(kGradThreads);
+  return launch_pdl(rows == 1 ? grad_kernel<T, 1> : grad_kernel<T, kWarps>, grid, block, 0, st, 1, a, total);
+}
 cudaError_t launch_grad(const RowArgs& a, const Total& total, int type, cudaStream_t st) {
-  const int n = 16 / elem_bytes(type);
-  const int64_t pieces = (a.cols + 2 * n - 2) / n, per = kGradPieces * kGradThreads;
-  const dim3 grid(static_cast<unsigned>((pieces + per - 1) / per), static_cast<unsigned>(a.rows < 65535 ? a.rows : 65535)), block(kGradThreads);
-  if (type == MEQ_F32) return launch_pdl(grad_kernel<float>, grid, block, 0, st, 1, a, total);
-  if (type == MEQ_BF16) return launch_pdl(grad_kernel<__nv_bfloat16>, grid, block, 0, st, 1, a, total);
-  return launch_pdl(grad_kernel<__half>, grid, block, 0, st, 1, a, total);
+  if (type == MEQ_F32) return launch_grad<float>(a, total, st);
+  if (type == MEQ_BF16) return launch_grad<__nv_bfloat16>(a, total, st);
+  return launch_grad<__half>(a, total, st);
 }
 
 int device_sms(cudaError_t* e) {
@@ -495,7 +600,15 @@ meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t c
         }
       }
     }
-    e = launch_pdl(policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, 1, reinterpret_cast<const float4*>(work), rows, sums);
+    float4* terms = reinterpret_cast<float4*>(work);
+    const int64_t blocks = (rows + kSumRows - 1) / kSumRows;
+    if (blocks <= 1) {
+      e = launch_pdl(policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, 1, terms, rows, int64_t(1), rows, sums);
+    } else {
+      e = launch_pdl(policy_sums_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kSumThreads), 0, st, 1, terms, rows, int64_t(1), kSumRows,
+                     static_cast<float*>(nullptr));
+      if (e == cudaSuccess) e = launch_pdl(policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, 1, terms, blocks, kSumRows, blocks, sums);
+    }
     return launch_status(e, "meq_policy_loss", "sum launch");
   });
 }

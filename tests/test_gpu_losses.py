@@ -228,6 +228,36 @@ def test_many_long_rows(meq, dtype, rows, cols, pad, shift, scored):
     assert torch.equal(again.grad, r.grad) and torch.equal(again.sums, r.sums)
 
 
+# many rows that a warp holds (up to 4 KB), of one to eight 16-byte pieces per lane, and the first that it does not
+SHORT = [("bf16", 20000, 256, 0, 0), ("bf16", 9001, 250, 1, 3), ("fp32", 17000, 100, 0, 1), ("fp16", 9000, 1000, 0, 0),
+         ("fp32", 8193, 1021, 3, 0), ("bf16", 6000, 2034, 0, 0), ("bf16", 4100, 2035, 2, 0), ("fp16", 30000, 3, 0, 1)]
+
+
+@pytest.mark.parametrize("dtype,rows,cols,pad,shift", SHORT)
+def test_many_short_rows(meq, dtype, rows, cols, pad, shift):
+    z, t, g = _tokens(rows, cols, dtype, rows + cols, pad, shift)
+    t[::7] = -1
+    t[5000:5100] = -100
+    r = _check_policy(meq, z, t, g, 0.05, dtype, True)
+    logp, _, dist = _rows64(z, t)
+    on = _np(t) >= 0
+    one = meq.token_logprobs(z, t)
+    zt = _np(z)[np.arange(rows), np.maximum(_np(t).astype(int), 0)]
+    assert (np.abs(_np(one.logp) - logp) <= _tol(logp, dist))[on].all() and not _np(one.logp)[~on].any() and not _np(one.lse)[~on].any()
+    assert (np.abs(_np(one.lse) - (zt - logp)) <= _tol(logp, dist) + 2.0 ** -22 * np.abs(zt - logp))[on].all()
+    args = (t, one.logp, torch.ones(rows, device="cuda"), None, one.logp)
+    a = meq.policy_loss(z, *args, kl_coef=0.1, grad=True)
+    b = meq.policy_loss(z, *args, kl_coef=0.1, grad=z)  # in place
+    assert torch.equal(a.grad, b.grad) and torch.equal(a.sums, b.sums) and torch.equal(a.logp, b.logp)
+    assert r.grad.shape == b.grad.shape
+
+
+@pytest.mark.parametrize("dtype,cols,pad,shift", [("bf16", 256, 0, 0), ("fp32", 301, 1, 1), ("fp16", 1500, 0, 0), ("bf16", 2035, 2, 0)])
+def test_preference_of_many_short_rows(meq, dtype, cols, pad, shift):
+    lengths = [700, 1, 0, 333, 1024, 90, 5, 2001]
+    test_preference_loss(meq, dtype, lengths, cols, pad, shift, 0.1)
+
+
 @pytest.mark.parametrize("scored", ["none", "one", "runs"])
 @pytest.mark.parametrize("cols", [25000, 100000])
 def test_masks_that_leave_little(meq, cols, scored):
