@@ -451,7 +451,8 @@ meq_status meq_token_logprobs(const void* logits, int type, int64_t rows, int64_
 int64_t meq_loss_work_floats(int64_t rows, int64_t pairs);
 
 /* The clipped policy loss with a KL term. With r = exp(logp - old_logp),
- * A = advantages, d = ref_logp - logp:
+ * A = advantages, d = ref_logp - logp (logp before it is rounded to fp32, so r of
+ * one's own logp is 1 but for that rounding):
  *
  *   L = sum_i w_i (s_i + kl_coef k_i)
  *   s = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A),  k = exp(d) - d - 1

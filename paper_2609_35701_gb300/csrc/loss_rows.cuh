@@ -362,7 +362,9 @@ __device__ __forceinline__ float two_sum(float a, float b, float* error) {
   *error = __fadd_rn(__fadd_rn(a, -__fadd_rn(s, -v)), __fadd_rn(b, -v));
   return s;
 }
-__device__ __forceinline__ float log_prob(float z, MaxSum t) {
+// *rest: what the last rounding took off.
+__device__ __forceinline__ float log_prob(float z, MaxSum t, float* rest) {
+  *rest = 0.f;
   if (!(t.s >= FLT_MIN && t.s <= FLT_MAX)) return (z - t.m) - logf(t.s);
   const uint32_t bits = __float_as_uint(t.s);
   const float k = static_cast<float>(static_cast<int>(bits >> 23) - 127);
@@ -371,18 +373,24 @@ __device__ __forceinline__ float log_prob(float z, MaxSum t) {
   float e0, e1;
   const float d = two_sum(z, -t.m, &e0), r = two_sum(d, -ln, &e1);
   const float tail = (e0 + e1) - ((off + fmaf(k, kLn2Lo, kExpBias)) + log_part);
-  // an infinite d has no error terms
-  return fabsf(d) <= FLT_MAX ? r + tail : d;
+  if (!(fabsf(d) <= FLT_MAX)) return d;  // an infinite d has no error terms
+  return two_sum(r, tail, rest);
+}
+__device__ __forceinline__ float log_prob(float z, MaxSum t) {
+  float rest;
+  return log_prob(z, t, &rest);
 }
 
-// The policy loss of one token: its terms, unweighted, and dL/dlogp.
+// The policy loss of one token: its terms, unweighted, and dL/dlogp. The ratio is
+// of logp + rest: half an ulp of a log-probability, 5e-7 at -11, is most of the
+// error of a sum of advantages that cancel.
 struct TokenLoss {
   float surrogate, k3, clipped, slope;
 };
-__device__ __forceinline__ TokenLoss policy_token(float logp, float old_logp, float adv, const float* ref, float lo, float hi,
+__device__ __forceinline__ TokenLoss policy_token(float logp, float rest, float old_logp, float adv, const float* ref, float lo, float hi,
                                                   float kl) {
   TokenLoss t;
-  const float ratio = expf(logp - old_logp);
+  const float ratio = expf((logp - old_logp) + rest);
   const float plain = ratio * adv, bounded = fminf(fmaxf(ratio, lo), hi) * adv;
   const bool cut = plain > bounded;
   // a NaN ratio stays one: neither comparison holds for it
@@ -391,7 +399,7 @@ __device__ __forceinline__ TokenLoss policy_token(float logp, float old_logp, fl
   t.clipped = cut ? 1.f : 0.f;
   t.k3 = 0.f;
   if (kl != 0.f) {
-    const float d = *ref - logp;
+    const float d = (*ref - logp) - rest;
     const float em = expm1f(d);
     t.k3 = em - d;
     t.slope -= kl * em;

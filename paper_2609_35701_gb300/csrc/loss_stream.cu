@@ -492,7 +492,8 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
           for (uint32_t k = 1; k < ctas; ++k) t = join(t, sh.cta[group][b][k]);
         }
         if (!ok) t.m = t.s = __int_as_float(0x7fc00000);
-        const float logp = log_prob(e.zt, t);
+        float rest;
+        const float logp = log_prob(e.zt, t, &rest);
         const bool leader = rank == 0 && lane == 0;
         if (leader) a.logp[row] = logp;
         if (!kPolicy) {
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
             if (a.coef) a.coef[row] = 0.f;
           }
         } else {
-          const TokenLoss l = policy_token(logp, e.old_logp, e.advantage, &e.ref_logp, a.clip_lo, a.clip_hi, a.kl);
+          const TokenLoss l = policy_token(logp, rest, e.old_logp, e.advantage, &e.ref_logp, a.clip_lo, a.clip_hi, a.kl);
           if (leader)
             a.terms[row] = make_float4(e.weight * (l.surrogate + a.kl * l.k3), e.weight * l.surrogate, e.weight * l.k3, e.weight * l.clipped);
           if (lane == 0) {

@@ -190,7 +190,8 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
   }
   const MaxSum all = row_join(ws, sh, rank, ctas);
   if (!kPolicy && threadIdx.x >= 32) return;
-  const float logp = log_prob(zt, all);
+  float rest;
+  const float logp = log_prob(zt, all, &rest);
   if (!kPolicy) {
     if (leader) {
       a.logp[row] = logp;
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
     }
     return;
   }
-  const TokenLoss t = policy_token(logp, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
+  const TokenLoss t = policy_token(logp, rest, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
   if (leader) {
     a.logp[row] = logp;
     a.terms[row] = make_float4(w * (t.surrogate + a.kl * t.k3), w * t.surrogate, w * t.k3, w * t.clipped);
@@ -260,10 +261,11 @@ __global__ void __launch_bounds__(kShortThreads) short_kernel(const RowArgs a) {
       r.load(0, lane, q);
       all = warp_stats<T>(q);
       zt = __shfl_sync(0xffffffffu, zt, 0);  // read by now: the gradient may lie in the logits' place
-      logp = log_prob(zt, all);
+      float rest;
+      logp = log_prob(zt, all, &rest);
       if (!kPolicy) lse = -log_prob(0.f, all);
       if (kPolicy) {
-        const TokenLoss t = policy_token(logp, s.old_logp, s.advantage, &s.ref_logp, a.clip_lo, a.clip_hi, a.kl);
+        const TokenLoss t = policy_token(logp, rest, s.old_logp, s.advantage, &s.ref_logp, a.clip_lo, a.clip_hi, a.kl);
         terms = make_float4(s.w * (t.surrogate + a.kl * t.k3), s.w * t.surrogate, s.w * t.k3, s.w * t.clipped);
         c = s.w * t.slope * gs;
       }
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const RowArgs a)
   const float w = a.weights ? a.weights[row] : 1.f;
   float4 terms = make_float4(0.f, 0.f, 0.f, 0.f);
   if (a.targets[row] >= 0 && w != 0.f) {
-    const TokenLoss t = policy_token(a.logp[row], a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
+    const TokenLoss t = policy_token(a.logp[row], 0.f, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
     terms = make_float4(w * (t.surrogate + a.kl * t.k3), w * t.surrogate, w * t.k3, w * t.clipped);
     a.coef[row] = w * t.slope * (a.grad_scale ? *a.grad_scale : 1.f);
   }
