@@ -365,7 +365,10 @@ typedef struct {
   int grad_type;       /* a meq_dtype; default MEQ_F32 */
 } meq_adamw_options;
 
-typedef struct meq_adamw meq_adamw; /* opaque */
+/* Opaque. Like a meq_state, one host thread drives it at a time, and its calls
+ * follow one another in the order of the streams that they are given: use one,
+ * or order them with events. */
+typedef struct meq_adamw meq_adamw;
 
 void meq_adamw_default_options(meq_adamw_options* opt);
 /* Bytes of the moments (with their scales) and of everything else the state

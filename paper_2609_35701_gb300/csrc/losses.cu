@@ -316,7 +316,8 @@ struct Total {
 // Gradient of the logits from each row's statistics and coefficient, the last
 // rows first (x, the part of a row, runs faster than y, the row, or kRows of them,
 // each a part of the block's warps). Bound by HBM:
-// 4096 x 50001 bf16 122 us alone, the copy rate.
+// 4096 x 50001 bf16 122 us alone, the copy rate. After the statistics, first rows
+// first -> last rows first: 9600 x 32000 214 -> 209 us, 1600 x 32000 34 -> 31.
 template <typename T, int kRows>
 __global__ void __launch_bounds__(kGradThreads) grad_kernel(const RowArgs a, const Total total) {
   pdl_allow_dependents();
