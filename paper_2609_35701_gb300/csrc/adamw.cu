@@ -325,6 +325,12 @@ constexpr float kNearM = 0.5f - 7e-5f, kNearR = 0.5f - 1.8e-4f;
 // largest (a fourth root of 1.1e-3, 0.27 of a code), but would in such a block.
 constexpr float kSmallV = 1e-26f;
 
+// The approximate codes of m hold for blocks whose largest |m| lies between
+// these: below, 127^2 over it comes near overflow (and is infinite under 4.8e-35);
+// above, its approximate reciprocal is taken for zero (from 2^126). Codes of
+// other blocks are formed exactly.
+constexpr float kLeastM = 0x1p-112f, kMostM = 0x1p125f;
+
 // A warp's lane in an entry of the state: its first element there, and in the
 // state's arrays.
 template <typename P, typename G>
@@ -453,6 +459,7 @@ __device__ __forceinline__ bool step_block(const AdamArgs& a, const Lane<P, G>& 
       pv[2 * i] = q.x, pv[2 * i + 1] = q.y;
     }
     float ms_new = block_scale(mt), rs_new = block_scale(__fsqrt_rn(vt));
+    const bool odd_m = !(mt >= kLeastM && mt <= kMostM);
     // zero for blocks held as zero (rcp of their largest would overflow)
     const float mi = ms_new > 0.f ? rcp_approx(mt) * (127.f * 127.f) : 0.f, ri = rs_new > 0.f ? rsqrt_approx(vt) * (255.f * 255.f) : 0.f;
     // a root above zero: a code of at least one
@@ -471,7 +478,7 @@ __device__ __forceinline__ bool step_block(const AdamArgs& a, const Lane<P, G>& 
         y[i] = make_float2(copysignf(sqrt_approx(fabsf(s.x)), s.x), copysignf(sqrt_approx(fabsf(s.y)), s.y));
       }
       mc[j] = pack_codes(y, &worst);
-      if (worst > kNearM) {
+      if (worst > kNearM || odd_m) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float2 s = m[2 * j + i];

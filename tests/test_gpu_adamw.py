@@ -362,6 +362,61 @@ def test_tiny_and_huge_moments_in_8_bits(meq):
     opt.close()
 
 
+def _codes(x, most):
+    """Codes and scales of blocks of 256 in fp32, each operation rounded once (float32 arithmetic on the CPU)."""
+    b = x.view(-1, 256)
+    top = b.abs().amax(1)
+    scale = torch.where(top < 2.0 ** -126, torch.zeros_like(top), top)
+    inv = torch.where(scale > 0, 1.0 / scale, torch.zeros_like(scale))
+    q = torch.round(most * torch.sqrt(b.abs() * inv[:, None]))
+    q = q * torch.sign(b) if most == 127.0 else torch.where(b > 0, q.clamp(min=1.0), q)
+    return q.view(-1), scale
+
+
+# 300 and 257 elements end in a padded block; shift 1 takes the element-by-element path
+@pytest.mark.parametrize("n,shift", [(256, 0), (300, 0), (257, 0), (512, 1)])
+def test_8bit_codes_of_m_of_any_size(meq, n, shift):
+    """Blocks whose largest |m| lies anywhere from the least normal number up: the codes are those of the formula
+    bit for bit, zeros among the elements and in the padding keep code 0."""
+    tops = [1.2e-38, 1e-37, 1e-36, 4e-35, 4.7e-35, 4.8e-35, 6e-35, 1e-34, 3e-34, 1e-20, 1.0, 1e15]
+    g = torch.Generator().manual_seed(n)
+    for top in tops:
+        x = torch.randn(n, generator=g) * torch.exp(1.5 * torch.randn(n, generator=g))
+        x = x * (top / float(x.abs().max()))
+        x[::7] = 0.0
+        x[3], x[n - 1] = top, -top        # the largest |m| of both blocks
+        opt = meq.AdamW([(1, n)], beta1=0.0, beta2=B2, eps=EPS, state_bits=8)
+        grad = torch.zeros(n + 4, device="cuda")[shift:shift + n]
+        grad.copy_(x)
+        opt.step([torch.zeros(1, n, device="cuda")], [grad.view(1, n)], 1e-3)
+        opt.sync()
+        held = torch.zeros(-(-n // 256) * 256)
+        held[:n] = x                      # beta1 = 0: m is the gradient
+        code, scale = _codes(held, 127.0)
+        st = opt.state()
+        assert torch.equal(st["m_scale"].cpu(), scale), top
+        assert torch.equal(st["m_code"].cpu().float(), code), top
+        opt.close()
+
+
+def test_8bit_codes_of_the_largest_m(meq):
+    """Moments near the largest fp32 number, put into the state: a step with no gradient keeps their codes."""
+    opt = meq.AdamW([(2, 256)], beta1=0.9, beta2=B2, eps=EPS, state_bits=8)
+    st = opt.state()
+    code = torch.randint(-127, 128, (512,), generator=torch.Generator().manual_seed(1))
+    code[::5], code[0], code[256] = 0, 127, -127
+    st["m_code"].copy_(code)
+    st["m_scale"].copy_(torch.tensor([9.6e37, 3.4e38]))
+    top = st["m_scale"].cpu() * 0.9
+    torch.cuda.synchronize()
+    p, z = torch.zeros(2, 256, device="cuda"), torch.zeros(2, 256, device="cuda")
+    opt.step([p], [z], 1e-3)
+    opt.sync()
+    st = opt.state()
+    assert torch.equal(st["m_code"].cpu().long(), code) and (st["m_scale"].cpu() / top - 1).abs().max() < 1e-6
+    opt.close()
+
+
 def test_streams_and_graph_capture(meq):
     shapes = [(100, 100), (1, 100)]
     ps, gs = _make(shapes, "float32", "float32", 8)
