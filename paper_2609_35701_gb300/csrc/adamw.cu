@@ -324,6 +324,9 @@ constexpr float kNearM = 0.5f - 7e-5f, kNearR = 0.5f - 1.8e-4f;
 // takes v < 2^-126 for zero, which decides no code where v is 1e-12 of the
 // largest (a fourth root of 1.1e-3, 0.27 of a code), but would in such a block.
 constexpr float kSmallV = 1e-26f;
+// The largest root that is taken for zero. The update divides by it times
+// 1/sqrt(1 - b2^t), plus eps: where eps does not drown it, every root is exact.
+constexpr float kLostRoot = 0x1p-63f;
 
 // The approximate codes of m hold for blocks whose largest |m| lies between
 // these: below, 127^2 over it comes near overflow (and is infinite under 4.8e-35);
@@ -341,6 +344,7 @@ struct Lane {
   int64_t at;
   int left;  // elements of the entry from here on, at most a chunk's
   float gs, step, rbc2, keep;
+  float small_v;  // 8-bit states: blocks with a largest v below take exact roots
 };
 
 // A warp's 256 elements lie over its lanes as two groups of 128, four
@@ -443,7 +447,7 @@ __device__ __forceinline__ bool step_block(const AdamArgs& a, const Lane<P, G>& 
     }
     mt = warp_max_mag(mt), vt = warp_max_mag(vt);
     fine = mt <= FLT_MAX && vt <= FLT_MAX;
-    const bool small = vt < kSmallV;
+    const bool small = vt < e.small_v;
     if (!small) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) r[i] = make_float2(sqrt_approx(v[i].x), sqrt_approx(v[i].y));
@@ -532,6 +536,7 @@ __global__ void __launch_bounds__(Step<kBits>::kThreads, Step<kBits>::kPerSm) ad
   e.step = a.lr * a.clock->inv_bc1;
   e.rbc2 = a.clock->inv_sqrt_bc2;
   e.keep = 1.f - a.lr * a.wd * c.decay;
+  e.small_v = kLostRoot * e.rbc2 > 0x1p-25f * a.eps ? INFINITY : kSmallV;
   if (a.last) {
     // The last block to have read the clock moves it on. (At the end, this
     // barrier would hold every warp until the block's slowest.)

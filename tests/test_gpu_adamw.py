@@ -399,6 +399,27 @@ def test_8bit_codes_of_m_of_any_size(meq, n, shift):
         opt.close()
 
 
+@pytest.mark.parametrize("eps", [1e-36, 1e-30, 1e-20, 1e-14, 1e-8])
+@pytest.mark.parametrize("n,shift", [(512, 0), (300, 0), (256, 3)])
+def test_8bit_update_with_a_small_eps(meq, eps, n, shift):
+    """Gradients of 1e-19 and 3e-19 beside 1e-10 in one block: the roots of the small ones, whose squares are no
+    normal fp32 numbers, still count beside any eps. An element of v is off by at most two spacings of 2^-149 beside
+    its roundings, its root by half as much of itself."""
+    lr = 1e-3
+    opt = meq.AdamW([(1, n)], beta1=B1, beta2=B2, eps=eps, state_bits=8)
+    grad, p = torch.zeros(n + 4, device="cuda")[shift:shift + n], torch.zeros(n + 4, device="cuda")[shift:shift + n]
+    grad.copy_(torch.tensor([1e-10, 1e-19, -3e-19, 1e-12]).repeat(n // 4 + 1)[:n])
+    opt.step([p.view(1, n)], [grad.view(1, n)], lr)
+    opt.sync()
+    g = _np(grad)
+    v = (1 - B2) * g * g
+    root = np.sqrt(v) / math.sqrt(1 - B2)
+    want = -lr * g / (root + eps)
+    tol = 2.0 ** -18 + 2.0 ** -149 / v * root / (root + eps)
+    assert (np.abs(_np(p) - want) <= np.abs(want) * tol + 2.0 ** -149).all(), np.max(np.abs(_np(p) / want - 1))
+    opt.close()
+
+
 def test_8bit_codes_of_the_largest_m(meq):
     """Moments near the largest fp32 number, put into the state: a step with no gradient keeps their codes."""
     opt = meq.AdamW([(2, 256)], beta1=0.9, beta2=B2, eps=EPS, state_bits=8)
