@@ -62,7 +62,7 @@ struct Step {
 constexpr int kMaxEntries = 256;          // pointers of one launch: 6 KB of its arguments
 constexpr int kNormBlocksPerSm = 6;
 constexpr int kNormUnit = 2048;           // most elements of a warp's turn in the norm
-constexpr int kSkipped = 0x7fffffff;      // value of AdamClock::nonfinite: a step was skipped
+constexpr int kSkipped = 0x7fffffff;      // value of AdamShared::nonfinite: a step was skipped
 
 struct AdamEntry {  // host
   int64_t numel;
@@ -79,17 +79,23 @@ struct __align__(16) Chunk {
   int32_t pad;
 };
 
-// What the next step needs of the number of steps so far; the last block of a
-// step moves it on, so a step that is skipped on the device does not count.
+// What a step needs of the number of steps before it. A step reads one of two,
+// which the turn of a block's chunk names, and one of its blocks writes the
+// other for the next step; every block moves its own chunk's turn on. So nothing
+// that a step reads is written by another block of it, and no block waits for
+// others (a ticket per block with the fences that it needs took 1 us of a small
+// step and 2 to 6% of a large one in 8 bits). A step that is skipped on the device
+// writes neither and does not count.
 struct AdamClock {
-  double b1t, b2t;          // b1^t, b2^t of the next step
-  float inv_bc1;            // 1 / (1 - b1^t)
-  float inv_sqrt_bc2;       // 1 / sqrt(1 - b2^t)
-  long long steps;          // steps done
-  unsigned int ticket;      // blocks of this step that are done (0 between steps)
-  unsigned int norm_ticket; // the same for the norm
-  int nonfinite;            // 0, 1 + entry with a non-finite moment, or kSkipped
-  int pad;
+  double b1t, b2t;     // b1^t, b2^t of the step
+  float inv_bc1;       // 1 / (1 - b1^t)
+  float inv_sqrt_bc2;  // 1 / sqrt(1 - b2^t)
+  long long steps;     // steps done before it
+};
+struct AdamShared {
+  AdamClock clock[2];
+  unsigned int norm_ticket;  // blocks of the norm that are done (0 between its launches)
+  int nonfinite;             // 0, 1 + entry with a non-finite moment, or kSkipped
 };
 
 __host__ __device__ inline void set_clock(AdamClock* c, double b1t, double b2t, long long steps) {
@@ -101,7 +107,8 @@ __host__ __device__ inline void set_clock(AdamClock* c, double b1t, double b2t, 
 
 struct AdamArgs {
   const Chunk* chunks_of;  // of the state
-  AdamClock* clock;
+  uint32_t* turns;         // of the chunks: which clock is this step's
+  AdamShared* shared;
   void* m;              // fp32, or int8 codes
   void* v;              // fp32, or uint8 codes of sqrt(v)
   float* m_scale;       // 8-bit states: one per block
@@ -119,7 +126,7 @@ struct AdamArgs {
 
 struct NormArgs {
   const Chunk* chunks_of;  // of the state
-  AdamClock* clock;
+  AdamShared* shared;
   float* partials;
   float* out;
   float max_norm;
@@ -529,20 +536,22 @@ __global__ void __launch_bounds__(Step<kBits>::kThreads, Step<kBits>::kPerSm) ad
   if (a.grad_scale) {
     e.gs = *a.grad_scale;
     if (!(fabsf(e.gs) <= FLT_MAX)) {  // every block sees it: nothing changes, the step does not count
-      if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(&a.clock->nonfinite, 0, kSkipped);
+      if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(&a.shared->nonfinite, 0, kSkipped);
       return;
     }
   }
-  e.step = a.lr * a.clock->inv_bc1;
-  e.rbc2 = a.clock->inv_sqrt_bc2;
+  uint32_t* turn = a.turns + a.chunk0 + blockIdx.x;
+  const uint32_t which = *turn;
+  const AdamClock* now = a.shared->clock + which;
+  e.step = a.lr * now->inv_bc1;
+  e.rbc2 = now->inv_sqrt_bc2;
   e.keep = 1.f - a.lr * a.wd * c.decay;
   e.small_v = kLostRoot * e.rbc2 > 0x1p-25f * a.eps ? INFINITY : kSmallV;
-  if (a.last) {
-    // The last block to have read the clock moves it on. (At the end, this
-    // barrier would hold every warp until the block's slowest.)
-    __syncthreads();
-    if (threadIdx.x == 0 && atomicInc(&a.clock->ticket, gridDim.x - 1) == gridDim.x - 1)
-      set_clock(a.clock, a.clock->b1t * a.beta1, a.clock->b2t * a.beta2, a.clock->steps + 1);
+  __syncthreads();  // every thread has its turn
+  if (threadIdx.x == 0) {
+    *turn = which ^ 1u;
+    if (a.last && blockIdx.x == 0)
+      set_clock(a.shared->clock + (which ^ 1u), now->b1t * a.beta1, now->b2t * a.beta2, now->steps + 1);
   }
   // the lane's first element; the state's arrays are padded to whole blocks
   const int first = static_cast<int>(threadIdx.x >> 5) * kBlock, at = first + Layout<kBits>::kLane * static_cast<int>(threadIdx.x & 31);
@@ -585,7 +594,7 @@ __global__ void __launch_bounds__(Step<kBits>::kThreads, Step<kBits>::kPerSm) ad
   }
 #pragma unroll 1
   for (int i = whole; i < tiles; ++i) fine = step_block<P, G, kBits, false>(a, e, i, nullptr, 0.f, 0.f) && fine;
-  if (!fine) atomicCAS(&a.clock->nonfinite, 0, c.entry + 1);
+  if (!fine) atomicCAS(&a.shared->nonfinite, 0, c.entry + 1);
 }
 
 // out[0] = sqrt(sum g^2), out[1] = the coefficient that brings it to at most
@@ -641,7 +650,7 @@ __global__ void __launch_bounds__(kAdamThreads) grad_norm_kernel(const __grid_co
   if (threadIdx.x == 0) {
     a.partials[a.part0 + blockIdx.x] = s;
     __threadfence();
-    final_block = a.last && atomicInc(&a.clock->norm_ticket, gridDim.x - 1) == gridDim.x - 1;
+    final_block = a.last && atomicInc(&a.shared->norm_ticket, gridDim.x - 1) == gridDim.x - 1;
   }
   __syncthreads();
   if (!final_block) return;
@@ -702,7 +711,8 @@ struct meq_adamw {
   void *d_m = nullptr, *d_v = nullptr;
   float *d_ms = nullptr, *d_rs = nullptr;
   Chunk* d_chunks = nullptr;
-  AdamClock* d_clock = nullptr;
+  uint32_t* d_turns = nullptr;
+  AdamShared* d_shared = nullptr;
   float* d_partials = nullptr;
   cudaStream_t last_stream = nullptr;
   std::string last_error;
@@ -747,7 +757,7 @@ int64_t pad_block(int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; }
 // Entries, launches and the arena's layout; host only.
 struct Plan {
   int64_t elements = 0, chunks = 0, persistent = 0, total = 0;
-  int64_t o_m = 0, o_v = 0, o_ms = 0, o_rs = 0, o_chunks = 0, o_clock = 0, o_partials = 0;
+  int64_t o_m = 0, o_v = 0, o_ms = 0, o_rs = 0, o_chunks = 0, o_turns = 0, o_shared = 0, o_partials = 0;
   int total_parts = 0;
   int64_t chunk = 0;  // elements of one
   int norm_shift = 0;
@@ -799,7 +809,8 @@ Plan make_plan(const meq_shape* shapes, const float* decay, int n, const meq_ada
   P.o_ms = add(scales);
   P.o_rs = add(scales);
   P.o_chunks = add(P.chunks * static_cast<int64_t>(sizeof(Chunk)));
-  P.o_clock = add(sizeof(AdamClock));
+  P.o_turns = add(P.chunks * 4);
+  P.o_shared = add(sizeof(AdamShared));
   P.o_partials = add(static_cast<int64_t>(P.total_parts) * 4);
   P.persistent = 2 * (P.elements * each + scales);
   return P;
@@ -895,9 +906,9 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
       for (int64_t at = 0; at < E.numel; at += size)
         chunks.push_back(Chunk{at, E.off + at, static_cast<int32_t>(E.numel - at < size ? E.numel - at : size), i, E.decay, 0});
     }
-    AdamClock clock;
-    std::memset(&clock, 0, sizeof(clock));
-    set_clock(&clock, o.beta1, o.beta2, 0);
+    AdamClock clock[2];
+    set_clock(clock, o.beta1, o.beta2, 0);
+    clock[1] = clock[0];
 
     struct Owner {  // of the state until it is handed out
       meq_adamw* st;
@@ -920,12 +931,13 @@ meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, co
     st->d_m = A + P.o_m, st->d_v = A + P.o_v;
     st->d_ms = reinterpret_cast<float*>(A + P.o_ms), st->d_rs = reinterpret_cast<float*>(A + P.o_rs);
     st->d_chunks = reinterpret_cast<Chunk*>(A + P.o_chunks);
-    st->d_clock = reinterpret_cast<AdamClock*>(A + P.o_clock);
+    st->d_turns = reinterpret_cast<uint32_t*>(A + P.o_turns);
+    st->d_shared = reinterpret_cast<AdamShared*>(A + P.o_shared);
     st->d_partials = reinterpret_cast<float*>(A + P.o_partials);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     e = cudaMemsetAsync(A, 0, static_cast<size_t>(P.total), s);
     if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_chunks, chunks.data(), sizeof(Chunk) * chunks.size(), cudaMemcpyHostToDevice, s);
-    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_clock, &clock, sizeof(clock), cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(st->d_shared->clock, clock, sizeof(clock), cudaMemcpyHostToDevice, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return fail(nullptr, MEQ_ERR_CUDA, std::string("initialising the AdamW state failed: ") + cudaGetErrorString(e));
     st->parts = std::move(P.parts);
@@ -947,7 +959,7 @@ meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float ma
     if (ms != MEQ_OK) return ms;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     NormArgs a;
-    a.chunks_of = st->d_chunks, a.clock = st->d_clock, a.partials = st->d_partials;
+    a.chunks_of = st->d_chunks, a.shared = st->d_shared, a.partials = st->d_partials;
     a.out = out, a.max_norm = max_norm, a.parts = st->total_parts;
     a.shift = st->norm_shift, a.unit = static_cast<int32_t>(st->chunk >> st->norm_shift);
     for (size_t k = 0; k < st->parts.size(); ++k) {
@@ -980,7 +992,7 @@ meq_status meq_adamw_step(void* const* params, const void* const* grads, void* c
     if (ms != MEQ_OK) return ms;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     AdamArgs a;
-    a.chunks_of = st->d_chunks, a.clock = st->d_clock;
+    a.chunks_of = st->d_chunks, a.turns = st->d_turns, a.shared = st->d_shared;
     a.m = st->d_m, a.v = st->d_v, a.m_scale = st->d_ms, a.r_scale = st->d_rs, a.grad_scale = grad_scale;
     a.beta1 = st->opt.beta1, a.beta2 = st->opt.beta2;
     a.b1 = static_cast<float>(a.beta1), a.one_minus_b1 = static_cast<float>(1.0 - a.beta1);
@@ -1045,11 +1057,11 @@ meq_status meq_adamw_steps(meq_adamw* st, int64_t* steps) {
   if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
   return guarded(st, [&]() -> meq_status {
     if (!steps) return fail(st, MEQ_ERR_INVALID_ARG, "steps is NULL");
-    AdamClock c;
+    AdamClock c[2];
     cudaError_t e = cudaStreamSynchronize(st->last_stream);
-    if (e == cudaSuccess) e = cudaMemcpy(&c, st->d_clock, sizeof(c), cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess) e = cudaMemcpy(c, st->d_shared->clock, sizeof(c), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(st, e, "reading the step count");
-    *steps = c.steps;
+    *steps = c[0].steps > c[1].steps ? c[0].steps : c[1].steps;  // the next step's is the later one
     return MEQ_OK;
   });
 }
@@ -1058,12 +1070,12 @@ meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps) {
   if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
   return guarded(st, [&]() -> meq_status {
     if (steps < 0) return fail(st, MEQ_ERR_INVALID_ARG, "steps must be >= 0");
-    AdamClock c;
-    std::memset(&c, 0, sizeof(c));
-    set_clock(&c, std::pow(st->opt.beta1, static_cast<double>(steps) + 1.0),
+    AdamClock c[2];  // alike, whichever the next step reads
+    set_clock(c, std::pow(st->opt.beta1, static_cast<double>(steps) + 1.0),
               std::pow(st->opt.beta2, static_cast<double>(steps) + 1.0), steps);
+    c[1] = c[0];
     cudaError_t e = cudaStreamSynchronize(st->last_stream);
-    if (e == cudaSuccess) e = cudaMemcpy(st->d_clock, &c, offsetof(AdamClock, ticket), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = cudaMemcpy(st->d_shared->clock, c, sizeof(c), cudaMemcpyHostToDevice);
     if (e != cudaSuccess) return cuda_fail(st, e, "writing the step count");
     return MEQ_OK;
   });
@@ -1075,11 +1087,11 @@ meq_status meq_adamw_sync(meq_adamw* st) {
     cudaError_t e = cudaStreamSynchronize(st->last_stream);
     if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamSynchronize");
     int bad = 0;
-    e = cudaMemcpy(&bad, &st->d_clock->nonfinite, sizeof(int), cudaMemcpyDeviceToHost);
+    e = cudaMemcpy(&bad, &st->d_shared->nonfinite, sizeof(int), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(st, e, "reading the non-finite flag");
     if (bad == 0) return MEQ_OK;
     const int zero = 0;
-    e = cudaMemcpy(&st->d_clock->nonfinite, &zero, sizeof(int), cudaMemcpyHostToDevice);
+    e = cudaMemcpy(&st->d_shared->nonfinite, &zero, sizeof(int), cudaMemcpyHostToDevice);
     if (e != cudaSuccess) return cuda_fail(st, e, "clearing the non-finite flag");
     if (bad == kSkipped) return fail(st, MEQ_ERR_NONFINITE, "a step was skipped: its gradient coefficient was not finite");
     return fail(st, MEQ_ERR_NONFINITE, "non-finite moment (gradient, or a previous non-finite step) in entry " + std::to_string(bad - 1));

@@ -264,6 +264,50 @@ def test_more_entries_than_one_launch_takes(meq):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_every_block_of_a_step_reads_the_same_clock(meq, bits):
+    """200 steps, one after another, of some 18000 (8 bits) or 4500 blocks: every element has the same moments and
+    gradients, so any block that read the corrections of the next step would give other parameters."""
+    shape = (1024, 8999)
+    opt = meq.AdamW([shape], beta1=B1, beta2=B2, eps=EPS, state_bits=bits)
+    p, g = torch.zeros(shape, device="cuda"), torch.full(shape, 0.5, device="cuda")
+    for _ in range(200):
+        opt.step([p], [g], 1e-2)
+    opt.sync()
+    assert opt.steps == 200 and bool((p == p[0, 0]).all())
+    # m and v are exact multiples of the gradient but for their roundings: the corrected update is 1 to 2^-16 in each step
+    assert abs(float(p[0, 0]) + 200 * 1e-2) <= 200 * 1e-2 * 2 ** -16 + 200 * 2.0 ** -23
+    opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("before", [0, 1, 2])
+def test_the_step_count_set_after_any_number_of_steps(meq, bits, before):
+    """set_steps counts for the very next step whatever came before, skipped steps do not count, and 300 entries
+    (two launches) move it on once."""
+    shapes = [(1, 300 + i) for i in range(300)]
+    kw = dict(beta1=B1, beta2=B2, eps=EPS, state_bits=bits)
+    ps, gs = _make(shapes, "float32", "float32", 6)
+    qs, a, b = [p.clone() for p in ps], meq.AdamW(shapes, **kw), meq.AdamW(shapes, **kw)
+    scrap = [p.clone() for p in ps]
+    for _ in range(before):
+        a.step(scrap, gs, 1e-3)
+    for v in a.state().values():
+        v.zero_()
+    torch.cuda.synchronize()
+    nan = torch.tensor([float("nan")], device="cuda")
+    for opt, x in ((a, ps), (b, qs)):
+        opt.set_steps(7)
+        assert opt.steps == 7
+        for _ in range(3):
+            opt.step(x, gs, 1e-3)
+            opt.step(x, gs, 1e-3, grad_scale=nan)
+        assert opt.steps == 10
+    assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+    a.close()
+    b.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_entries_do_not_depend_on_the_list(meq, bits):
     shapes = [(33, 77), (1, 5000), (128, 128)]
     kw = dict(beta1=B1, beta2=B2, eps=EPS, state_bits=bits)
