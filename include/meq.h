@@ -367,7 +367,9 @@ typedef struct {
 
 /* Opaque. Like a meq_state, one host thread drives it at a time, and its calls
  * follow one another in the order of the streams that they are given: use one,
- * or order them with events. */
+ * or order them with events. meq_adamw_steps, _set_steps, _sync and _free wait
+ * for the stream of the last call; once a call has been captured into a graph,
+ * for the whole device, since replays may run on any stream. */
 typedef struct meq_adamw meq_adamw;
 
 void meq_adamw_default_options(meq_adamw_options* opt);
@@ -405,15 +407,15 @@ meq_status meq_adamw_state_ptrs(meq_adamw* st, void** m, void** v, float** m_sca
  * of *elements each, laid out as the state's (16-byte aligned; either may be
  * NULL). */
 meq_status meq_adamw_read_values(meq_adamw* st, float* m, float* v, void* cuda_stream);
-/* Number of steps done (synchronises the state's last stream), and its
- * overwriting, to resume. Skipped steps do not count. */
+/* Number of steps done (waits for the state's work), and its overwriting, to
+ * resume. Skipped steps do not count. */
 meq_status meq_adamw_steps(meq_adamw* st, int64_t* steps);
 meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps);
 /* Wait for the state's work; then MEQ_ERR_NONFINITE if since the last sync a
  * step was skipped or left a non-finite moment (meq_adamw_last_error names the
  * entry; such a step is not skipped). Each report clears the condition. */
 meq_status meq_adamw_sync(meq_adamw* st);
-/* Releases the state (synchronises its last stream first). NULL is a no-op. */
+/* Releases the state (waits for its work first). NULL is a no-op. */
 meq_status meq_adamw_free(meq_adamw* st);
 const char* meq_adamw_last_error(const meq_adamw* st);
 

@@ -715,6 +715,7 @@ struct meq_adamw {
   AdamShared* d_shared = nullptr;
   float* d_partials = nullptr;
   cudaStream_t last_stream = nullptr;
+  bool captured = false;  // a call was captured: replays run on any stream, unseen by the host
   std::string last_error;
 };
 
@@ -840,6 +841,24 @@ meq_status check_device(meq_adamw* st) {
   if (dev != st->device)
     return fail(st, MEQ_ERR_INVALID_ARG, "the state is on device " + std::to_string(st->device) + ", the current device is " + std::to_string(dev));
   return MEQ_OK;
+}
+
+// What the state's calls wait for: the stream of the last one, and of a state
+// whose calls were captured, whose replays do not pass here, the whole device.
+void enqueued(meq_adamw* st, cudaStream_t s) {
+  st->last_stream = s;
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(s, &status) != cudaSuccess) cudaGetLastError();
+  if (status != cudaStreamCaptureStatusNone) st->captured = true;
+}
+cudaError_t wait_for_all(meq_adamw* st) {
+  if (!st->captured) return cudaStreamSynchronize(st->last_stream);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev != st->device) e = cudaSetDevice(st->device);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (dev != st->device) cudaSetDevice(dev);
+  return e;
 }
 
 template <typename P, typename G>
@@ -973,7 +992,7 @@ meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float ma
                                                       : launch_pdl(grad_norm_kernel<__half>, grid, block, 0, s, 1, a);
       if (e != cudaSuccess) return cuda_fail(st, e, "gradient norm launch");
     }
-    st->last_stream = s;
+    enqueued(st, s);
     return MEQ_OK;
   });
 }
@@ -1012,7 +1031,7 @@ meq_status meq_adamw_step(void* const* params, const void* const* grads, void* c
                                                     : launch_adamw<__nv_bfloat16>(st->opt, a, grid, s);
       if (e != cudaSuccess) return cuda_fail(st, e, "AdamW launch");
     }
-    st->last_stream = s;
+    enqueued(st, s);
     return MEQ_OK;
   });
 }
@@ -1048,7 +1067,7 @@ meq_status meq_adamw_read_values(meq_adamw* st, float* m, float* v, void* cuda_s
                      static_cast<const float*>(st->d_ms), static_cast<const float*>(st->d_rs), quads, m, v);
     }
     if (e != cudaSuccess) return cuda_fail(st, e, "reading the AdamW state");
-    st->last_stream = s;
+    enqueued(st, s);
     return MEQ_OK;
   });
 }
@@ -1058,7 +1077,7 @@ meq_status meq_adamw_steps(meq_adamw* st, int64_t* steps) {
   return guarded(st, [&]() -> meq_status {
     if (!steps) return fail(st, MEQ_ERR_INVALID_ARG, "steps is NULL");
     AdamClock c[2];
-    cudaError_t e = cudaStreamSynchronize(st->last_stream);
+    cudaError_t e = wait_for_all(st);
     if (e == cudaSuccess) e = cudaMemcpy(c, st->d_shared->clock, sizeof(c), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(st, e, "reading the step count");
     *steps = c[0].steps > c[1].steps ? c[0].steps : c[1].steps;  // the next step's is the later one
@@ -1074,7 +1093,7 @@ meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps) {
     set_clock(c, std::pow(st->opt.beta1, static_cast<double>(steps) + 1.0),
               std::pow(st->opt.beta2, static_cast<double>(steps) + 1.0), steps);
     c[1] = c[0];
-    cudaError_t e = cudaStreamSynchronize(st->last_stream);
+    cudaError_t e = wait_for_all(st);
     if (e == cudaSuccess) e = cudaMemcpy(st->d_shared->clock, c, sizeof(c), cudaMemcpyHostToDevice);
     if (e != cudaSuccess) return cuda_fail(st, e, "writing the step count");
     return MEQ_OK;
@@ -1084,8 +1103,8 @@ meq_status meq_adamw_set_steps(meq_adamw* st, int64_t steps) {
 meq_status meq_adamw_sync(meq_adamw* st) {
   if (!st) return fail(nullptr, MEQ_ERR_INVALID_ARG, "state is NULL");
   return guarded(st, [&]() -> meq_status {
-    cudaError_t e = cudaStreamSynchronize(st->last_stream);
-    if (e != cudaSuccess) return cuda_fail(st, e, "cudaStreamSynchronize");
+    cudaError_t e = wait_for_all(st);
+    if (e != cudaSuccess) return cuda_fail(st, e, "waiting for the state's work");
     int bad = 0;
     e = cudaMemcpy(&bad, &st->d_shared->nonfinite, sizeof(int), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(st, e, "reading the non-finite flag");
@@ -1100,7 +1119,7 @@ meq_status meq_adamw_sync(meq_adamw* st) {
 
 meq_status meq_adamw_free(meq_adamw* st) {
   if (!st) return MEQ_OK;
-  cudaStreamSynchronize(st->last_stream);
+  wait_for_all(st);
   if (st->arena) cudaFree(st->arena);
   delete st;
   return MEQ_OK;

@@ -510,7 +510,9 @@ class _DeviceArray:
 class AdamW:
     """AdamW over a fixed list of parameters (rows, cols), with moments in 32
     or 8 bits (meq_adamw_init). decay: a factor of the weight decay per entry
-    (default 1); options beta1, beta2, eps, state_bits."""
+    (default 1); options beta1, beta2, eps, state_bits. steps, set_steps, sync
+    and close wait for the stream of the last call, or, once a call has been
+    captured into a graph, for the device."""
 
     BLOCK = 256  # each entry's moments start at a multiple of this many elements
 

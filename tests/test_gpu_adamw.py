@@ -508,6 +508,43 @@ def test_streams_and_graph_capture(meq):
     b.close()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_host_calls_wait_for_replays_on_any_stream(meq, bits):
+    """A captured step replayed on a stream that no call was made on, behind 50 ms of other work: steps, set_steps and
+    sync see what the replays do."""
+    shapes = [(100, 100), (1, 100)]
+    ps, gs = _make(shapes, "float32", "float32", 8)
+    scale = torch.ones(1, device="cuda")
+    opt = meq.AdamW(shapes, state_bits=bits)
+    opt.step(ps, gs, 1e-3, grad_scale=scale)
+    torch.cuda.synchronize()
+    graph, side, other = torch.cuda.CUDAGraph(), torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=other):
+        opt.step(ps, gs, 1e-3, grad_scale=scale)
+
+    def replays(n):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+            for _ in range(n):
+                graph.replay()
+
+    replays(3)
+    assert opt.steps == 4
+    replays(2)
+    opt.set_steps(10)
+    torch.cuda.synchronize()
+    assert opt.steps == 10
+    scale.fill_(float("inf"))
+    torch.cuda.synchronize()
+    replays(1)
+    with pytest.raises(meq.MeqError) as e:
+        opt.sync()
+    assert e.value.status == 4 and "skipped" in str(e.value)
+    assert opt.steps == 10
+    replays(1)
+    opt.close()
+
+
 def test_8bit_training_follows_32bit(meq):
     """A noisy least-squares problem ends where 32-bit states end. The same formulas in plain arithmetic
     end 0.04 % apart; 5 % leaves room for another order of the sums."""
