@@ -442,14 +442,22 @@ const char* meq_adamw_last_error(const meq_adamw* st);
  * work: device scratch of meq_loss_work_floats floats, 16-byte aligned, free
  *   again when the enqueued kernels have run.
  * Softmax statistics and all scalars are fp32, sums over rows compensated, all
- * in fixed orders: results repeat bit for bit. Nothing is allocated, and the
- * calls may come from several threads. rows may be 0. Limits: rows <= 2^27,
+ * in fixed orders: results repeat bit for bit. A kernel's own waits are bounded
+ * (4 s, and time that the context is switched out does not end one alone): a
+ * thread block that gives up writes NaN as every result of all its rows, so the
+ * sums become NaN too. Nothing is allocated, and the calls may come from several
+ * threads. rows may be 0. Limits: rows <= 2^27,
  * cols <= 2^28. */
 
 /* logp (rows floats) and, if lse is not NULL, log sum_j exp(z_ij) (0 for rows
  * that are not scored). */
 meq_status meq_token_logprobs(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
                               float* logp, float* lse, void* cuda_stream);
+
+/* Diagnostic, for the calling thread's next loss calls: the limit of the
+ * kernels' waits (0: the usual 4 s) and a row whose data never arrives where rows
+ * are streamed through shared memory (-1: none), so that a wait runs out. */
+meq_status meq_debug_loss_wait(float timeout_ms, int64_t withheld_row);
 
 /* Floats of `work` for a loss over rows tokens and (meq_preference_loss) pairs
  * pairs (0: meq_policy_loss). Host only. */

@@ -411,6 +411,9 @@ __device__ __forceinline__ TokenLoss policy_token(float logp, float rest, float 
 // streamed through shared memory. False: the rows do not suit it.
 bool stream_suits(int64_t rows, int64_t cols, int elem_bytes, bool policy);
 cudaError_t launch_stream(const RowArgs& a, int type, bool policy, cudaStream_t st);
+// The limit of the streamed kernel's waits (0: the usual one) and a row whose data never comes (-1: none), for the
+// calling thread's next launches.
+void stream_wait(unsigned long long ns, int64_t withheld);
 
 }  // namespace loss
 }  // namespace meq

@@ -34,8 +34,10 @@
 // 86 (77), 4096 x 151936 192 (183). Of 8192 x 32000 with 80% of the rows scored at
 // random, 172 (139) and 80 (62): some CTAs have more of them than others.
 //
-// Every wait is bounded. On expiry the CTA writes NaN as the row's result, and
-// its roles stop.
+// Every wait is bounded. On expiry the roles of the CTA (and, for want of its
+// messages, of its cluster) stop, and when all have, every row of it gets NaN for
+// all its results, the gradient too: neither what a buffer held before nor, with
+// the gradient in their place, logits are left standing as results.
 #include <mutex>
 
 #include "loss_rows.cuh"
@@ -66,6 +68,9 @@ constexpr int kEntries = 8;
 constexpr int kMaxShare = 76 * 1024;               // of a row per CTA: the ring holds 2.8
 constexpr int kMaxCtas = 8;
 constexpr unsigned long long kWaitNs = 4000000000ull;
+// A wait gives up after the limit's time and at least this many polls: time that
+// passes while the context is switched out polls nothing.
+constexpr uint32_t kLeastPolls = 1024, kMostPolls = 1u << 28;
 
 struct Entry {
   const void* logits;  // of the row
@@ -85,6 +90,11 @@ struct RowResult {
   int ok;
 };
 
+struct Limit {
+  unsigned long long ns;  // of a wait
+  int stop;               // a wait has run out
+};
+
 struct StreamShared {
   uint64_t full[kMostSlots], empty[kMostSlots];
   uint64_t entry_full[kEntries], entry_empty[kEntries];
@@ -94,7 +104,7 @@ struct StreamShared {
   MaxSum cta[kMostGroups][2][kMaxCtas];
   RowResult result[kMostGroups][2];
   uint32_t claimed;  // slot uses whose copies are under way
-  int stop;
+  Limit limit;
 };
 constexpr int kStreamSmem = kRingBytes + static_cast<int>(sizeof(StreamShared)) + 128;
 static_assert(kStreamSmem <= 232448, "shared memory budget of one sm_103a CTA");
@@ -105,35 +115,35 @@ struct StreamShape {
   int rounds;  // slots per share
   int by_slots;  // statistics: 1: the groups take a row's slots in turn, 0: they take the rows in turn
   int pieces;    // of a unit, per lane
+  unsigned long long wait_ns;
+  int64_t withheld;  // for a test: a row whose first slot is never filled (none: -1)
 };
 
+// Whether a wait that began at t0 gives up at poll `it` (looked at in every 128th).
+__device__ __forceinline__ bool gives_up(volatile Limit* limit, uint64_t t0, uint32_t it) {
+  return limit->stop != 0 || (global_ns() - t0 > limit->ns && it >= kLeastPolls) || it >= kMostPolls;
+}
 // All lanes of a warp; the same answer in each. False: gave up.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* stop) {
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile Limit* limit) {
   const unsigned FULL = 0xffffffffu;
   if (__all_sync(FULL, mbar_try_wait(bar, parity))) return true;
   const uint64_t t0 = global_ns();
   for (uint32_t it = 1;; ++it) {
     if (__all_sync(FULL, mbar_try_wait(bar, parity))) return true;
-    if ((it & 127u) == 0) {
-      if (__any_sync(FULL, *stop != 0)) return false;
-      if (__any_sync(FULL, global_ns() - t0 > kWaitNs || it >= (1u << 28))) {
-        *stop = 1;
-        return false;
-      }
+    if ((it & 127u) == 0 && __any_sync(FULL, gives_up(limit, t0, it))) {
+      limit->stop = 1;
+      return false;
     }
   }
 }
-__device__ __forceinline__ bool wait_one(uint32_t bar, uint32_t parity, volatile int* stop) {
+__device__ __forceinline__ bool wait_one(uint32_t bar, uint32_t parity, volatile Limit* limit) {
   if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = global_ns();
   for (uint32_t it = 1;; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 127u) == 0) {
-      if (*stop != 0) return false;
-      if (global_ns() - t0 > kWaitNs || it >= (1u << 28)) {
-        *stop = 1;
-        return false;
-      }
+    if ((it & 127u) == 0 && gives_up(limit, t0, it)) {
+      limit->stop = 1;
+      return false;
     }
   }
 }
@@ -141,7 +151,7 @@ __device__ __forceinline__ bool wait_one(uint32_t bar, uint32_t parity, volatile
 // use filled; its barrier is then still in the phase before, whose parity says
 // "complete". So a slot is waited for only once its use has been claimed,
 // which the other group's release of it precedes.
-__device__ __forceinline__ bool wait_claimed(const uint32_t* claimed, uint32_t use, volatile int* stop) {
+__device__ __forceinline__ bool wait_claimed(const uint32_t* claimed, uint32_t use, volatile Limit* limit) {
   const unsigned FULL = 0xffffffffu;
   const uint32_t addr = smem_u32(claimed);
   uint64_t t0 = 0;
@@ -151,9 +161,8 @@ __device__ __forceinline__ bool wait_claimed(const uint32_t* claimed, uint32_t u
     if (__all_sync(FULL, static_cast<int32_t>(n - use) > 0)) return true;
     if ((it & 127u) == 0) {
       if (it == 0) t0 = global_ns();
-      if (__any_sync(FULL, *stop != 0)) return false;
-      if (__any_sync(FULL, global_ns() - t0 > kWaitNs || it >= (1u << 28))) {
-        *stop = 1;
+      if (__any_sync(FULL, gives_up(limit, t0, it))) {
+        limit->stop = 1;
         return false;
       }
     }
@@ -236,8 +245,34 @@ __device__ __forceinline__ MaxSum lanes_join(MaxSum t) {
   return t;
 }
 
+// NaN for all results of all rows of the CTA's cluster, of whose gradient it takes its share.
+template <typename T, bool kPolicy>
+__device__ __forceinline__ void lose_rows(const RowArgs& a, uint32_t ctas) {
+  const float nan = __int_as_float(0x7fc00000);
+  const uint32_t rank = ctas == 1 ? 0u : cluster_rank();
+  for (int64_t row = blockIdx.x / ctas; row < a.rows; row += gridDim.x / ctas) {
+    if (rank == 0 && threadIdx.x == 0) {
+      a.logp[row] = nan;
+      if (a.lse) a.lse[row] = nan;
+      if (a.stat) a.stat[row] = make_float2(nan, nan);
+      if (a.coef) a.coef[row] = nan;
+      if (kPolicy) a.terms[row] = make_float4(nan, nan, nan, nan);
+    }
+    if (kPolicy && a.grad) {
+      T* g = static_cast<T*>(a.grad) + row * a.ld_grad;
+      for (int64_t i = static_cast<int64_t>(rank) * blockDim.x + threadIdx.x; i < a.cols; i += static_cast<int64_t>(ctas) * blockDim.x)
+        g[i] = Elem<T>::make(nan);
+    }
+  }
+}
+
+template <typename T, bool kPolicy>
+__device__ __noinline__ void lose_rows_called(const RowArgs& a, uint32_t ctas) {
+  lose_rows<T, kPolicy>(a, ctas);
+}
+
 template <typename T, bool kPolicy, int kPieces>
-__global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_kernel(const RowArgs a, const StreamShape shape) {
+__global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_kernel(const __grid_constant__ RowArgs a, const StreamShape shape) {
   using C = Cfg<kPolicy, kPieces>;
   constexpr int kSlots = C::kSlots, kSlot = C::kSlot, kUnit = C::kUnit, kUserWarps = C::kUserWarps, kGroups = C::kGroups;
   static_assert(C::kSlots <= kMostSlots && C::kUsers <= kMostUsers && C::kGroups <= kMostGroups, "");
@@ -248,7 +283,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
   StreamShared& sh = *reinterpret_cast<StreamShared*>(ring + kRingBytes);
   const uint32_t ctas = static_cast<uint32_t>(shape.ctas), rank = ctas == 1 ? 0u : cluster_rank();
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-  volatile int* stop = &sh.stop;
+  volatile Limit* stop = &sh.limit;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(smem_u32(&sh.full[i]), 1);
@@ -263,7 +298,8 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
       mbar_init(smem_u32(&sh.exchange[i / 2][i % 2]), ctas);
       mbar_init(smem_u32(&sh.ready[i / 2][i % 2]), 1);
     }
-    sh.stop = 0;
+    sh.limit.ns = shape.wait_ns;
+    sh.limit.stop = 0;
     sh.claimed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -293,7 +329,9 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
           }
           const int c0 = lo + c * kSlot, w0 = max(c0, r.begin), w1 = min(c0 + kSlot, hi);
           const uint32_t bar = smem_u32(&sh.full[slot]);
-          if (w1 > w0) {
+          const bool withheld = row == shape.withheld && c == 0;
+          if (withheld) {
+          } else if (w1 > w0) {
             mbar_expect_tx(bar, static_cast<uint32_t>(w1 - w0) * 16u);
             bulk_copy(smem_u32(ring) + static_cast<uint32_t>(slot * kSlot + (w0 - c0)) * 16u, r.p + (w0 * Row<T>::N - r.lead),
                       static_cast<uint32_t>(w1 - w0) * 16u, bar);
@@ -302,15 +340,15 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
           }
           ++use;
           asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(&sh.claimed)), "r"(use) : "memory");
-          filled |= 1u << slot;
+          if (!withheld) filled |= 1u << slot;
           filled_phase = (filled_phase & ~(1u << slot)) | (phase << slot);
           if (++slot == kSlots) slot = 0, phase ^= 1u;
         }
       }
       // every copy has landed before the CTA leaves
-      int none = 0;
+      Limit own{sh.limit.ns, 0};
       for (int s = 0; s < kSlots; ++s)
-        if ((filled >> s) & 1u) wait_one(smem_u32(&sh.full[s]), (filled_phase >> s) & 1u, &none);
+        if ((filled >> s) & 1u) wait_one(smem_u32(&sh.full[s]), (filled_phase >> s) & 1u, &own);
     }
     __syncwarp();
   } else if (warp == 1) {
@@ -491,7 +529,6 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
           t = sh.cta[group][b][0];
           for (uint32_t k = 1; k < ctas; ++k) t = join(t, sh.cta[group][b][k]);
         }
-        if (!ok) t.m = t.s = __int_as_float(0x7fc00000);
         float rest;
         const float logp = log_prob(e.zt, t, &rest);
         const bool leader = rank == 0 && lane == 0;
@@ -540,8 +577,24 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
     __syncwarp();
   }
   __syncthreads();
-  if (ctas > 1) cluster_sync_all();  // no CTA leaves while another may still write to it
+  if (ctas > 1) {
+    if (stop->stop != 0) __nanosleep(100000);  // messages on their way (a microsecond) have arrived
+    if (stop->stop != 0 && threadIdx.x < ctas)
+      asm volatile("st.shared::cluster.u32 [%0], 1;" ::"r"(map_to_rank(smem_u32(&sh.limit.stop), threadIdx.x)) : "memory");
+    __syncwarp();
+    cluster_sync_all();  // no CTA leaves while another may still write to it
+  }
+  if (stop->stop != 0) {
+    // With five pieces a lane has no register to spare: inlined, it spills, 195 -> 206 us for 2048 x 151936 bf16.
+    // With four, called instead of inlined, 4096 x 50001 takes 141 us for 134, statistics 74 for 72.5.
+    if (kPieces > 4) lose_rows_called<T, kPolicy>(a, ctas);
+    else lose_rows<T, kPolicy>(a, ctas);
+  }
 }
+
+// Of the calling thread's next launches (meq_debug_loss_wait).
+thread_local unsigned long long g_wait_ns = kWaitNs;
+thread_local int64_t g_withheld = -1;
 
 template <bool kPolicy, int kPieces>
 StreamShape shape_with(int64_t row_pieces, int ctas) {
@@ -553,7 +606,7 @@ StreamShape shape_with(int64_t row_pieces, int ctas) {
   // by slot, since waiting for its own slots would idle two of them. Rows -> slots, us:
   // 4096 x 32000 bf16 54 -> 107, x 65000 89 -> 110, x 100000 152 -> 150,
   // 2048 x 151936 111 -> 104.
-  return StreamShape{ctas, static_cast<int>(share), rounds, !kPolicy && rounds > C::kSlots ? 1 : 0, kPieces};
+  return StreamShape{ctas, static_cast<int>(share), rounds, !kPolicy && rounds > C::kSlots ? 1 : 0, kPieces, g_wait_ns, g_withheld};
 }
 StreamShape shape_for(int64_t cols, int elem_bytes, bool policy) {
   const int n = 16 / elem_bytes;
@@ -643,6 +696,11 @@ bool stream_suits(int64_t rows, int64_t cols, int elem_bytes, bool policy) {
   if (policy && shape_for(cols, elem_bytes, policy).rounds > Cfg<true, 5>::kSlots) return false;
   const int64_t least = policy && elem_bytes == 4 ? 66000 : 48000;
   return (row_bytes >= least && rows * row_bytes >= 50000000) || (row_bytes >= 192000 && rows >= 128);
+}
+
+void stream_wait(unsigned long long ns, int64_t withheld) {
+  g_wait_ns = ns ? ns : kWaitNs;
+  g_withheld = withheld;
 }
 
 cudaError_t launch_stream(const RowArgs& a, int type, bool policy, cudaStream_t st) {

@@ -559,6 +559,14 @@ meq_status meq_token_logprobs(const void* logits, int type, int64_t rows, int64_
   });
 }
 
+meq_status meq_debug_loss_wait(float timeout_ms, int64_t withheld_row) {
+  return guarded([&]() -> meq_status {
+    if (!(timeout_ms >= 0.f && timeout_ms <= 60000.f)) return fail(MEQ_ERR_INVALID_ARG, "meq_debug_loss_wait: timeout_ms must be in 0..60000");
+    stream_wait(static_cast<unsigned long long>(static_cast<double>(timeout_ms) * 1e6), withheld_row);
+    return MEQ_OK;
+  });
+}
+
 int64_t meq_loss_work_floats(int64_t rows, int64_t pairs) { return rows < 0 || pairs < 0 ? 0 : 7 * rows + pairs + 4; }
 
 meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,

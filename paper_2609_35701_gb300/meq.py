@@ -76,6 +76,7 @@ EXPORTED = [
     "meq_adamw_state_ptrs", "meq_adamw_read_values", "meq_adamw_steps", "meq_adamw_set_steps", "meq_adamw_sync",
     "meq_adamw_free", "meq_adamw_last_error",
     "meq_token_logprobs", "meq_loss_work_floats", "meq_policy_loss", "meq_preference_loss",
+    "meq_debug_loss_wait",
 ]
 HIDDEN, REMAINING_2D, VECTOR = 0, 1, 2  # meq_kind
 RULE_MEQMUON, RULE_MUON = 0, 1          # meq_update_rule
@@ -187,6 +188,8 @@ def _load():
     lib.meq_policy_loss.restype = I
     lib.meq_preference_loss.argtypes = [P, I, I64, I64, I64, P, P, I64, P, P, F, F, P, P, P, P, I64, P, P, P]
     lib.meq_preference_loss.restype = I
+    lib.meq_debug_loss_wait.argtypes = [F, I64]
+    lib.meq_debug_loss_wait.restype = I
     return lib
 
 
@@ -707,6 +710,11 @@ def _current_device(t, what):
 def _check_loss(s):
     if s != MEQ_OK:
         raise MeqError(s, lib.meq_last_error(None).decode())
+
+
+def debug_loss_wait(timeout_ms=0.0, withheld_row=-1):
+    """Diagnostic (meq_debug_loss_wait): the limit of the loss kernels' waits and a row whose data never comes."""
+    _check_loss(lib.meq_debug_loss_wait(float(timeout_ms), int(withheld_row)))
 
 
 def token_logprobs(logits, targets, stream=None):

@@ -280,6 +280,60 @@ def test_masks_that_leave_little(meq, cols, scored):
     assert not r.grad[~on].any() and bool((r.grad[on] != 0).any(1).all() if on.any() else True)
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 700, 40003), ("fp32", 330, 50001), ("bf16", 305, 151936)])
+@pytest.mark.parametrize("place", ["apart", "in place"])
+def test_a_wait_that_runs_out_gives_nan(meq, dtype, rows, cols, place):
+    """The data of one row never comes, the waits' limit is 20 ms: the kernel ends, every row of that block (or cluster of
+    blocks) is NaN in all its results, every other row is right, and so is the next call."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    z = _matrix(rows, cols, dtype)
+    z.copy_(torch.randn(rows, cols, generator=g, device="cuda"))
+    t = torch.randint(0, cols, (rows,), generator=g, device="cuda")
+    t[::3] = -1
+    row = 103
+    assert int(t[row]) >= 0
+    adv, w = torch.linspace(0.5, 1.5, rows, device="cuda"), torch.full((rows,), 1.0 / rows, device="cuda")
+    plain = meq.token_logprobs(z, t)
+    good = meq.policy_loss(z, t, plain.logp, adv, w, grad=True)
+    assert bool(torch.isfinite(good.loss)) and bool(torch.isfinite(good.grad).all())
+    try:
+        meq.debug_loss_wait(20.0, row)
+        stats = meq.token_logprobs(z, t)
+        bad = meq.policy_loss(z, t, plain.logp, adv, w, grad=z.clone() if place == "apart" else z)
+        torch.cuda.synchronize()
+    finally:
+        meq.debug_loss_wait()
+    for got, want in ((stats.logp, plain.logp), (stats.lse, plain.lse), (bad.logp, good.logp), (bad.grad, good.grad)):
+        lost = torch.isnan(got).view(rows, -1)
+        assert bool((lost.any(1) == lost.all(1)).all())
+        lost = lost.any(1)
+        assert bool(lost[row]) and int(lost.sum()) < rows // 4
+        at = lost.nonzero()[:, 0]
+        assert at.numel() < 2 or len(set((at[1:] - at[:-1]).tolist())) == 1   # a block's rows lie a fixed number apart
+        assert torch.equal(got[~lost], want[~lost])
+    assert bool(torch.isnan(bad.sums).all())
+    if place == "in place":
+        return
+    again = meq.policy_loss(z, t, plain.logp, adv, w, grad=True)
+    assert torch.equal(again.grad, good.grad) and torch.equal(again.sums, good.sums)
+
+
+def test_a_wait_that_runs_out_in_the_preference_loss(meq):
+    rows, cols = 700, 40003
+    z = torch.randn(rows, cols, device="cuda").bfloat16()
+    t, starts, ref = torch.full((rows,), 5, device="cuda"), torch.tensor([0, 200, 350, 500, 700], device="cuda"), torch.zeros(rows, device="cuda")
+    try:
+        meq.debug_loss_wait(20.0, 103)
+        r = meq.preference_loss(z, t, starts, ref, grad=True)
+        torch.cuda.synchronize()
+    finally:
+        meq.debug_loss_wait()
+    assert bool(torch.isnan(r.loss)) and bool(torch.isnan(r.margins[0])) and bool(torch.isnan(r.grad[103]).all())
+    assert bool(torch.isnan(r.logp[103]))
+    with pytest.raises(meq.MeqError):
+        meq.debug_loss_wait(-1.0)
+
+
 def test_offsets_past_32_bits_in_a_long_batch(meq):
     """490000 rows of 24000 equal logits, 23.5 GB: log-probabilities of -log(24000), a gradient of 1/24000 each."""
     rows, cols = 490000, 24000
