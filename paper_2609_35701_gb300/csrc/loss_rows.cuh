@@ -36,6 +36,12 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The largest of the warp's values, NaN aside.
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 // exp(a - b) for the few joins of statistics (0 for a = -inf and any finite b)
 __device__ __forceinline__ float exp_diff(float a, float b) { return exp2_approx((a - b) * kLog2e); }
 
@@ -56,6 +62,8 @@ struct ExpBase {
     fix_hi = exp2_approx(-off);
   }
 };
+// The exponential of one element relative to c, as the sums take it.
+__device__ __forceinline__ float exp_at(float x, float c) { return exp2_approx(fmaf(x, kLog2eLo, fmaf(x, kLog2e, -c))); }
 
 template <typename T>
 struct Elem;  // 16-bit and 32-bit logits
@@ -336,10 +344,15 @@ __device__ __forceinline__ void store_zeros(const Row<T>& r, T* g, bool same, in
   r.template store<P>(g, same, first, k0, q, [](uint4 piece) { return piece; });
 }
 
-// Running maximum and sum of exponentials relative to it.
+// Maximum and sum of exponentials relative to it. The maximum's own is exactly 1
+// in the sum (the approximate one is taken off again, and the rest made
+// relative to the maximum), so that a token of probability one has the
+// log-probability 0.
 struct MaxSum {
   float m, s;
 };
+// From a sum whose terms are exp(z - m) / fix, with the maximum's own as it was added.
+__device__ __forceinline__ float exact_top(float sum, float own, float fix) { return fmaf(sum - own, fix, 1.f); }
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
   MaxSum r;
@@ -355,7 +368,8 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
 // log(2), joins those. (The log-ratios of an answer are summed over hundreds of
 // tokens: half an ulp of lse and of log(s) each, and any common bias, show.)
 constexpr float kLn2 = 0.693147182f, kLn2Lo = -1.90465421e-9f;  // log(2) in two parts
-// ex2.approx is low by 5.0e-8 of its value on average for negative arguments (measured over [-20, 0]).
+// ex2.approx is low by 5.0e-8 of its value on average for negative arguments (measured over [-20, 0]): the sum is,
+// but for the maximum's own 1.
 constexpr float kExpBias = 5.0e-8f;
 __device__ __forceinline__ float two_sum(float a, float b, float* error) {
   const float s = __fadd_rn(a, b), v = __fadd_rn(s, -a);
@@ -372,7 +386,8 @@ __device__ __forceinline__ float log_prob(float z, MaxSum t, float* rest) {
   const float ln = __fmul_rn(k, kLn2), off = fmaf(k, kLn2, -ln);
   float e0, e1;
   const float d = two_sum(z, -t.m, &e0), r = two_sum(d, -ln, &e1);
-  const float tail = (e0 + e1) - ((off + fmaf(k, kLn2Lo, kExpBias)) + log_part);
+  const float bias = __fdividef(kExpBias * (t.s - 1.f), t.s);
+  const float tail = (e0 + e1) - ((off + fmaf(k, kLn2Lo, bias)) + log_part);
   if (!(fabsf(d) <= FLT_MAX)) return d;  // an infinite d has no error terms
   return two_sum(r, tail, rest);
 }

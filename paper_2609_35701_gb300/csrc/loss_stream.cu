@@ -186,16 +186,17 @@ __device__ __forceinline__ void send(uint32_t addr_cluster, uint32_t bar_cluster
 // reference (-inf before the first finite logit).
 struct Running {
   float ref = -INFINITY, c = 0.f, fix = 1.f, s = 0.f;
+  float top = -INFINITY;  // the lane's largest logit
   template <typename T, int P>
   __device__ __forceinline__ void add(const uint4 (&q)[P]) {
     constexpr int H = Elem<T>::N / 2;
-    typename Elem<T>::Max top = Elem<T>::none();
+    typename Elem<T>::Max tops = Elem<T>::none();
 #pragma unroll
-    for (int j = 0; j < P; ++j) top = Elem<T>::max_of(top, q[j]);
-    float m = Elem<T>::value(top);
+    for (int j = 0; j < P; ++j) tops = Elem<T>::max_of(tops, q[j]);
+    float m = Elem<T>::value(tops);
+    top = fmaxf(top, m);
     if (__any_sync(0xffffffffu, m > ref + kSlack)) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      m = warp_max(m);
       const ExpBase b(fabsf(m) <= kFar ? m : 0.f);
       s = s * fix * exp_diff(ref, m) / b.fix;
       ref = m, c = b.c, fix = b.fix;
@@ -227,17 +228,18 @@ struct Running {
     s = a[0].x + a[0].y;
   }
   __device__ __forceinline__ MaxSum total() const {  // of the warp, for every lane
-    MaxSum t{ref, s * fix};
+    MaxSum t{warp_max(top), s};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
+    if (t.m == -INFINITY) return t;
+    const float own = fabsf(ref) <= kFar ? exp_at(t.m, c) : exp_diff(t.m, ref);
+    t.s = exact_top(t.s, own, fix * exp_diff(ref, t.m));
     return t;
   }
 };
 // Over the warp, the same in each lane.
 __device__ __forceinline__ MaxSum lanes_join(MaxSum t) {
-  float m = t.m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float m = warp_max(t.m);
   t.s *= exp_diff(t.m, finite_or_zero(m));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);

@@ -70,9 +70,7 @@ __device__ __forceinline__ MaxSum row_join(MaxSum w, RowShared& sh, uint32_t ran
   __syncthreads();
   MaxSum t{-INFINITY, 0.f};
   if (lane < warps) t = sh.warp[lane];
-  float m = t.m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float m = warp_max(t.m);
   t.s *= exp_diff(t.m, finite_or_zero(m));
   t.m = m;
 #pragma unroll
@@ -100,14 +98,14 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
   typename Elem<T>::Max top = Elem<T>::none();
 #pragma unroll
   for (int j = 0; j < P; ++j) top = Elem<T>::max_of(top, q[j]);
-  float m = Elem<T>::value(top);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float m = warp_max(Elem<T>::value(top));
   w.m = m;
   constexpr int H = Elem<T>::N / 2;
   float2 s = make_float2(0.f, 0.f);
+  float own = 1.f, fix = 1.f;  // the maximum's own term as it is in the sum
   if (fabsf(m) <= kFar || m == -INFINITY) {
     const ExpBase b(finite_or_zero(m));
+    own = exp_at(m, b.c), fix = b.fix;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       float2 x[H];
@@ -119,7 +117,6 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
         s = add2(s, make_float2(exp2_approx(z.x), exp2_approx(z.y)));
       }
     }
-    w.s = (s.x + s.y) * b.fix;
   } else {
     // far from zero (+inf gives NaN)
 #pragma unroll
@@ -129,10 +126,11 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
 #pragma unroll
       for (int e = 0; e < H; ++e) s = add2(s, make_float2(exp_diff(x[e].x, m), exp_diff(x[e].y, m)));
     }
-    w.s = s.x + s.y;
   }
+  w.s = s.x + s.y;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) w.s += __shfl_xor_sync(0xffffffffu, w.s, o);
+  if (m != -INFINITY) w.s = exact_top(w.s, own, fix);
   return w;
 }
 
