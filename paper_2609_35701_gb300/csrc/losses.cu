@@ -282,7 +282,9 @@ __global__ void __launch_bounds__(kShortThreads) short_kernel(const RowArgs a) {
   }
 }
 
-// The policy terms and coefficients of rows whose statistics are known.
+// The policy terms and coefficients of rows whose statistics are known, from which logp is worked out once more for
+// what its rounding took off. Latency bounds it: one gathered logit per row.
+template <typename T>
 __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const RowArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
@@ -290,8 +292,13 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const RowArgs a)
   if (row >= a.rows) return;
   const float w = a.weights ? a.weights[row] : 1.f;
   float4 terms = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (a.targets[row] >= 0 && w != 0.f) {
-    const TokenLoss t = policy_token(a.logp[row], 0.f, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
+  const int64_t target = a.targets[row];
+  if (target >= 0 && w != 0.f) {
+    const float2 stat = a.stat[row];
+    const float zt = target < a.cols ? Elem<T>::get(static_cast<const T*>(a.logits) + row * a.ld + target) : __int_as_float(0x7fc00000);
+    float rest;
+    const float logp = log_prob(zt, MaxSum{stat.x, stat.y}, &rest);
+    const TokenLoss t = policy_token(logp, rest, a.old_logp[row], a.advantages[row], a.ref_logp + row, a.clip_lo, a.clip_hi, a.kl);
     terms = make_float4(w * (t.surrogate + a.kl * t.k3), w * t.surrogate, w * t.k3, w * t.clipped);
     a.coef[row] = w * t.slope * (a.grad_scale ? *a.grad_scale : 1.f);
   }
@@ -489,6 +496,13 @@ cudaError_t launch_rows_of(const RowArgs& a, int type, const RowShape& s, cudaSt
   return launch_pdl(row_kernel<__half, kPolicy>, grid, block, 0, st, s.ctas, a);
 }
 
+cudaError_t launch_terms(const RowArgs& a, int type, cudaStream_t st) {
+  const dim3 grid(static_cast<unsigned>((a.rows + kThreads - 1) / kThreads)), block(kThreads);
+  if (type == MEQ_F32) return launch_pdl(policy_terms_kernel<float>, grid, block, 0, st, 1, a);
+  if (type == MEQ_BF16) return launch_pdl(policy_terms_kernel<__nv_bfloat16>, grid, block, 0, st, 1, a);
+  return launch_pdl(policy_terms_kernel<__half>, grid, block, 0, st, 1, a);
+}
+
 template <typename T>
 cudaError_t launch_grad(const RowArgs& a, const Total& total, cudaStream_t st) {
   constexpr int kWarps = kGradThreads / 32;
@@ -601,7 +615,7 @@ meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t c
         a.stat = reinterpret_cast<float2*>(work + 4 * rows), a.coef = work + 6 * rows;
         e = launch_rows_of<false>(a, type, s, st);
         if (e != cudaSuccess) return launch_status(e, "meq_policy_loss", "statistics launch");
-        e = launch_pdl(policy_terms_kernel, dim3(static_cast<unsigned>((rows + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, 1, a);
+        e = launch_terms(a, type, st);
         if (e != cudaSuccess) return launch_status(e, "meq_policy_loss", "terms launch");
         if (grad) {
           e = launch_grad(a, Total{}, type, st);

@@ -504,6 +504,23 @@ def test_a_token_of_probability_one(meq, dtype, rows, cols, shift, mask):
     assert float(r.loss) == float(r.sums[1]) and abs(float(r.loss) + 1) <= 2.0 ** -20
 
 
+# a CTA, a cluster, streamed by one CTA and by a cluster, and rows that no cluster holds: few, and streamed
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 3, 4186), ("bf16", 4, 50011), ("bf16", 700, 40110), ("bf16", 320, 100050), ("fp32", 3, 262391),
+                                             ("bf16", 2, 530191), ("bf16", 130, 870657)])
+def test_ratios_are_of_unrounded_log_probabilities(meq, dtype, rows, cols):
+    """Rows of equal logits: logp = -log(cols), whose rounding to fp32 adds about 4.7e-7 to it. With that rounded value
+    as old_logp every ratio is below 1 by as much. Allowed: 5e-8 (the correction of approximate exponentials, which are
+    exact here), 9e-8 for log(cols) and its additions, two ulps of the ratio (1.2e-7), and 6e-8 for the rounded sum."""
+    z, t = _matrix(rows, cols, dtype), torch.arange(rows, device="cuda")
+    old = np.float32(-math.log(cols))
+    ratio = math.exp(-math.log(cols) - float(old))
+    assert ratio < 1 - 4.5e-7
+    one = torch.ones(rows, device="cuda")
+    r = meq.policy_loss(z, t, torch.full((rows,), float(old), device="cuda"), one)
+    assert abs(float(r.sums[1]) / (-rows * ratio) - 1) <= 3.2e-7
+    assert abs(float(r.loss) / (-rows * ratio) - 1) <= 3.2e-7
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_probable_tokens_have_no_common_bias(meq, dtype):
     """8192 tokens with p > 0.998. A sum next to 1 is rounded at most eleven times on its way, by 2^-24 each: the mean
