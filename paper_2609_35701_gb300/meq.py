@@ -698,6 +698,14 @@ def _grad_for(logits, rows, cols, ld, grad, stream):
     return grad, grad.data_ptr(), _logits_args(grad, "grad")[3]
 
 
+def _overwritten(tensors):
+    """Tells autograd that the caller's tensors were written (through their pointers, which it does not see): a backward
+    pass that had saved one of them raises instead of using the new values."""
+    import torch
+
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _current_device(t, what):
     import torch
 
@@ -736,7 +744,8 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
                 grad=None, grad_scale=None, stream=None):
     """The clipped policy loss with a KL term and, if asked for, the gradient of
     the logits (meq_policy_loss). grad: True for a new tensor, or the tensor to
-    write (it may be logits). sums holds the loss, its surrogate and KL parts
+    write (it may be logits, unless autograd has saved them for a backward pass
+    to come, which then raises). sums holds the loss, its surrogate and KL parts
     and the clipped weight; loss is the first of them."""
     import torch
 
@@ -747,12 +756,14 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
     w, ref = _vector(weights, f32, rows, device, "weights"), _vector(ref_logp, f32, rows, device, "ref_logp")
     t = _vector(targets, torch.int64, rows, device, "targets")
     scale = _vector(grad_scale, f32, 1, device, "grad_scale")
-    grad, g, ldg = _grad_for(logits, rows, cols, ld, grad, stream)
+    given, (grad, g, ldg) = grad, _grad_for(logits, rows, cols, ld, grad, stream)
     work = _empty(lib.meq_loss_work_floats(rows, 0), f32, where, stream)
     sums, logp = _empty(4, f32, where, stream), _empty(rows, f32, where, stream)
     _check_loss(lib.meq_policy_loss(logits.data_ptr(), kind, rows, cols, ld, t, old, adv, w, ref, float(clip_low),
                                     float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(), g, ldg, scale,
                                     work.data_ptr(), _stream_handle(stream, device)))
+    if grad is not None and grad is given:
+        _overwritten(grad)
     return PolicyLoss(sums, logp, grad)
 
 
@@ -773,10 +784,12 @@ def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, l
     ref, w = _vector(ref_logp, f32, rows, device, "ref_logp"), _vector(weights, f32, rows, device, "weights")
     t = _vector(targets, torch.int64, rows, device, "targets")
     scale = _vector(grad_scale, f32, 1, device, "grad_scale")
-    grad, g, ldg = _grad_for(logits, rows, cols, ld, grad, stream)
+    given, (grad, g, ldg) = grad, _grad_for(logits, rows, cols, ld, grad, stream)
     work = _empty(lib.meq_loss_work_floats(rows, pairs), f32, where, stream)
     logp, margins, loss = _empty(rows, f32, where, stream), _empty(pairs, f32, where, stream), _empty((), f32, where, stream)
     _check_loss(lib.meq_preference_loss(logits.data_ptr(), kind, rows, cols, ld, t, st, pairs, ref, w, float(beta),
                                         float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(), g, ldg,
                                         scale, work.data_ptr(), _stream_handle(stream, device)))
+    if grad is not None and grad is given:
+        _overwritten(grad)
     return PreferenceLoss(loss, margins, logp, grad)

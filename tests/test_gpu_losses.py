@@ -606,6 +606,38 @@ def test_determinism_streams_and_graphs(meq):
         assert all(torch.equal(x, y) for x, y in zip(a, c))
 
 
+@pytest.mark.parametrize("loss", ["policy", "preference"])
+def test_a_gradient_over_saved_logits_is_noticed(meq, loss):
+    """Logits that their own function keeps for its backward pass (a soft cap by tanh): written over by their gradient,
+    backward raises; with the gradient elsewhere, or logits that nothing keeps, it runs."""
+    n, cols = 12, 300
+    t = torch.arange(n, device="cuda")
+    zero, one = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+
+    def call(z, grad):
+        if loss == "policy":
+            return meq.policy_loss(z, t, zero - 5.0, one, one / n, grad=grad)
+        return meq.preference_loss(z, t, torch.tensor([0, 5, n], device="cuda"), zero, grad=grad)
+
+    for kept in (True, False):
+        x = torch.randn(n, cols, device="cuda", requires_grad=True)
+        y = torch.tanh(x) if kept else x * 2.0
+        call(y.detach(), True).grad      # a new tensor: nothing is written over
+        y.backward(call(y.detach(), True).grad, retain_graph=True)
+        want, x.grad = x.grad, None
+        z = y.detach()
+        r = call(z, z)
+        if kept:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.backward(r.grad)
+        else:
+            y.backward(r.grad)
+            assert torch.equal(x.grad, want)
+    with torch.inference_mode():         # tensors without a version counter
+        z = torch.randn(n, cols, device="cuda")
+        assert call(z, z).grad is z
+
+
 def test_no_rows(meq):
     z = torch.zeros(0, 100, device="cuda")
     e, t = torch.zeros(0, device="cuda"), torch.zeros(0, dtype=torch.int64, device="cuda")
