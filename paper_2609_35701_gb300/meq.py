@@ -585,7 +585,8 @@ class AdamW:
         """One step on lists of contiguous CUDA tensors (params updated in place).
         grad_scale: a CUDA float32 tensor of one element that multiplies the
         gradients (not finite: the step is skipped); copies: bf16 tensors that
-        receive the updated parameters."""
+        receive the updated parameters. A backward pass still to come that has
+        saved a parameter or copy raises."""
         if grad_scale is not None:
             _require_cuda(grad_scale, "float32", 1, "grad_scale", self._device)
         p = self._pointers(params, self._param_dtype, "params")
@@ -598,6 +599,9 @@ class AdamW:
         self._check(lib.meq_adamw_step(p.buffer_info()[0], g.buffer_info()[0], None if c is None else c.buffer_info()[0],
                                        self._st, float(lr), float(weight_decay),
                                        None if grad_scale is None else grad_scale.data_ptr(), _stream_handle(stream)))
+        _overwritten(params)
+        if copies is not None:
+            _overwritten(copies)
 
     def state(self):
         """The state's own arrays as CUDA tensors: m and v, or m_code, r_code and

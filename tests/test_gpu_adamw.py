@@ -545,6 +545,21 @@ def test_host_calls_wait_for_replays_on_any_stream(meq, bits):
     opt.close()
 
 
+def test_parameters_written_before_their_backward_pass_are_noticed(meq):
+    """A parameter that a backward pass still to come has saved: after a step (or a copy into it) backward raises."""
+    for through_copy in (False, True):
+        dt = torch.bfloat16 if through_copy else torch.float32
+        w = torch.randn(16, 16, device="cuda").to(dt)
+        x = torch.randn(4, 16, device="cuda", dtype=dt, requires_grad=True)
+        y = (x @ w).sum()
+        opt = meq.AdamW([(16, 16)])
+        p = torch.randn(16, 16, device="cuda") if through_copy else w
+        opt.step([p], [torch.ones(16, 16, device="cuda")], 1e-3, copies=[w] if through_copy else None)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+        opt.close()
+
+
 def test_8bit_training_follows_32bit(meq):
     """A noisy least-squares problem ends where 32-bit states end. The same formulas in plain arithmetic
     end 0.04 % apart; 5 % leaves room for another order of the sums."""
