@@ -318,6 +318,65 @@ def test_a_wait_that_runs_out_gives_nan(meq, dtype, rows, cols, place):
     assert torch.equal(again.grad, good.grad) and torch.equal(again.sums, good.sums)
 
 
+@pytest.mark.parametrize("dtype,rows,cols,pad,shift", [c for c in STREAMED if c[2] not in (20011, 262147)])
+def test_many_long_rows_without_a_gradient(meq, dtype, rows, cols, pad, shift):
+    """The loss alone is the same, bit for bit, as with its gradient (which the tests above compare with 64 bits)."""
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    z = _matrix(rows, cols, dtype, pad, shift)
+    z.copy_(3.0 * torch.randn(rows, cols, generator=g, device="cuda"))
+    t = torch.randint(-cols // 2, cols, (rows,), generator=g, device="cuda")
+    old, adv = torch.full((rows,), -math.log(cols) - 4.0, device="cuda"), torch.randn(rows, generator=g, device="cuda")
+    keep = z.clone()
+    with_grad = meq.policy_loss(z, t, old, adv, ref_logp=old, kl_coef=0.1, grad=True)
+    alone = [meq.policy_loss(z, t, old, adv, ref_logp=old, kl_coef=0.1) for _ in range(2)]
+    for r in alone:
+        assert r.grad is None and torch.equal(r.sums, with_grad.sums) and torch.equal(r.logp, with_grad.logp)
+    assert bool(torch.isfinite(with_grad.loss)) and torch.equal(z, keep)
+
+
+def test_calls_from_several_threads(meq):
+    """Four host threads, a stream each, calls of every form and refused calls among them: the results are those of one
+    thread, and a refusal's text is that of the thread's own call."""
+    import threading
+
+    shapes = [("bf16", 400, 40003), ("fp32", 9, 4111), ("fp16", 3000, 250), ("bf16", 310, 151936)]
+    data, want = [], []
+
+    def calls(i, stream=None):
+        z, t, v, starts = data[i]
+        out = list(meq.token_logprobs(z, t, stream=stream)) + list(meq.policy_loss(z, t, v, v + 1, grad=True, stream=stream))
+        r = meq.preference_loss(z, t, starts, v, grad=True, stream=stream)
+        return out + [r.loss, r.margins, r.logp, r.grad]
+
+    for i, (dtype, rows, cols) in enumerate(shapes):
+        z, t, _ = _tokens(rows, cols, dtype, i)
+        data.append((z, t, torch.full((rows,), -9.0, device="cuda"), torch.tensor([0, rows // 3, rows], device="cuda")))
+        want.append([x.clone() for x in calls(i)])
+    torch.cuda.synchronize()
+    failures, start = [], threading.Barrier(len(shapes))
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            start.wait()
+            for _ in range(15):
+                got = calls(i, stream)
+                name = ("clip_low", "kl_coef")[i % 2]
+                with pytest.raises(meq.MeqError, match=name):
+                    meq.policy_loss(*data[i][:2], data[i][2], data[i][2], **{name: -1.0}, stream=stream)
+                stream.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want[i]))
+        except BaseException as e:  # noqa: BLE001 - reported by the main thread
+            failures.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(shapes))]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failures, failures
+
+
 def test_a_wait_that_runs_out_in_the_preference_loss(meq):
     rows, cols = 700, 40003
     z = torch.randn(rows, cols, device="cuda").bfloat16()
