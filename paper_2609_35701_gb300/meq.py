@@ -589,19 +589,20 @@ class AdamW:
         saved a parameter or copy raises."""
         if grad_scale is not None:
             _require_cuda(grad_scale, "float32", 1, "grad_scale", self._device)
+        import torch
+
         p = self._pointers(params, self._param_dtype, "params")
         g = self._pointers(grads, self._grad_dtype, "grads")
         c = None
         if copies is not None:
-            import torch
-
             c = self._pointers(copies, torch.bfloat16, "copies")
         self._check(lib.meq_adamw_step(p.buffer_info()[0], g.buffer_info()[0], None if c is None else c.buffer_info()[0],
                                        self._st, float(lr), float(weight_decay),
                                        None if grad_scale is None else grad_scale.data_ptr(), _stream_handle(stream)))
-        _overwritten(params)
+        written = torch.autograd.graph.increment_version  # through pointers, which autograd does not see
+        written(params)
         if copies is not None:
-            _overwritten(copies)
+            written(copies)
 
     def state(self):
         """The state's own arrays as CUDA tensors: m and v, or m_code, r_code and
@@ -702,14 +703,6 @@ def _grad_for(logits, rows, cols, ld, grad, stream):
     return grad, grad.data_ptr(), _logits_args(grad, "grad")[3]
 
 
-def _overwritten(tensors):
-    """Tells autograd that the caller's tensors were written (through their pointers, which it does not see): a backward
-    pass that had saved one of them raises instead of using the new values."""
-    import torch
-
-    torch.autograd.graph.increment_version(tensors)
-
-
 def _current_device(t, what):
     import torch
 
@@ -767,7 +760,7 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
                                     float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(), g, ldg, scale,
                                     work.data_ptr(), _stream_handle(stream, device)))
     if grad is not None and grad is given:
-        _overwritten(grad)
+        torch.autograd.graph.increment_version(grad)  # written through its pointer, which autograd does not see
     return PolicyLoss(sums, logp, grad)
 
 
@@ -795,5 +788,5 @@ def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, l
                                         float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(), g, ldg,
                                         scale, work.data_ptr(), _stream_handle(stream, device)))
     if grad is not None and grad is given:
-        _overwritten(grad)
+        torch.autograd.graph.increment_version(grad)  # written through its pointer, which autograd does not see
     return PreferenceLoss(loss, margins, logp, grad)
