@@ -184,17 +184,16 @@ __device__ __forceinline__ void send(uint32_t addr_cluster, uint32_t bar_cluster
 
 // A warp's running sum of exponentials, each lane's part relative to the same
 // reference (-inf before the first finite logit).
+template <typename T>
 struct Running {
   float ref = -INFINITY, c = 0.f, fix = 1.f, s = 0.f;
-  float top = -INFINITY;  // the lane's largest logit
-  template <typename T, int P>
+  typename Elem<T>::Max top = Elem<T>::none();  // the lane's largest logit
+  template <int P>
   __device__ __forceinline__ void add(const uint4 (&q)[P]) {
     constexpr int H = Elem<T>::N / 2;
-    typename Elem<T>::Max tops = Elem<T>::none();
 #pragma unroll
-    for (int j = 0; j < P; ++j) tops = Elem<T>::max_of(tops, q[j]);
-    float m = Elem<T>::value(tops);
-    top = fmaxf(top, m);
+    for (int j = 0; j < P; ++j) top = Elem<T>::max_of(top, q[j]);
+    float m = Elem<T>::value(top);
     if (__any_sync(0xffffffffu, m > ref + kSlack)) {
       m = warp_max(m);
       const ExpBase b(fabsf(m) <= kFar ? m : 0.f);
@@ -228,7 +227,7 @@ struct Running {
     s = a[0].x + a[0].y;
   }
   __device__ __forceinline__ MaxSum total() const {  // of the warp, for every lane
-    MaxSum t{warp_max(top), s};
+    MaxSum t{warp_max(Elem<T>::value(top)), s};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
     if (t.m == -INFINITY) return t;
@@ -477,7 +476,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
       const int b = joins & 1;
       const uint32_t parity = (joins >> 1) & 1u;
       ++joins;
-      Running sum;
+      Running<T> sum;
       int slot = e.slot;
       uint32_t phase = e.phase;
       bool ok = true;
@@ -508,7 +507,7 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
           __syncwarp();
           if (lane == 0) mbar_arrive_local(smem_u32(&sh.empty[slot]));
         }
-        sum.add<T, kPieces>(q);
+        sum.template add<kPieces>(q);
         if (++slot == kSlots) slot = 0, phase ^= 1u;
       }
       MaxSum t = sum.total();
