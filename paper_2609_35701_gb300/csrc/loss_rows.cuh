@@ -351,8 +351,6 @@ __device__ __forceinline__ void store_zeros(const Row<T>& r, T* g, bool same, in
 struct MaxSum {
   float m, s;
 };
-// From a sum whose terms are exp(z - m) / fix, with the maximum's own as it was added.
-__device__ __forceinline__ float exact_top(float sum, float own, float fix) { return fmaf(sum - own, fix, 1.f); }
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
   MaxSum r;

@@ -90,6 +90,12 @@ struct RowResult {
   int ok;
 };
 
+// A warp's maximum, its own exponential left out of the sum of the others',
+// which is relative to ref.
+struct WarpSum {
+  float m, rest, ref;
+};
+
 struct Limit {
   unsigned long long ns;  // of a wait
   int stop;               // a wait has run out
@@ -100,7 +106,7 @@ struct StreamShared {
   uint64_t entry_full[kEntries], entry_empty[kEntries];
   uint64_t joined[kMostGroups][2], exchange[kMostGroups][2], ready[kMostGroups][2];
   Entry entry[kEntries];
-  MaxSum warp[2][kMostUsers];
+  WarpSum warp[2][kMostUsers];
   MaxSum cta[kMostGroups][2][kMaxCtas];
   RowResult result[kMostGroups][2];
   uint32_t claimed;  // slot uses whose copies are under way
@@ -226,24 +232,22 @@ struct Running {
     for (int j = 1; j < P; ++j) a[0] = add2(a[0], a[j]);
     s = a[0].x + a[0].y;
   }
-  __device__ __forceinline__ MaxSum total() const {  // of the warp, for every lane
-    MaxSum t{warp_max(Elem<T>::value(top)), s};
+  __device__ __forceinline__ WarpSum total() const {  // of the warp, for every lane
+    WarpSum t{warp_max(Elem<T>::value(top)), s, ref};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
-    if (t.m == -INFINITY) return t;
-    const float own = fabsf(ref) <= kFar ? exp_at(t.m, c) : exp_diff(t.m, ref);
-    t.s = exact_top(t.s, own, fix * exp_diff(ref, t.m));
+    for (int o = 16; o > 0; o >>= 1) t.rest += __shfl_xor_sync(0xffffffffu, t.rest, o);
+    if (t.m != -INFINITY) t.rest = (t.rest - (fabsf(ref) <= kFar ? exp_at(t.m, c) : exp_diff(t.m, ref))) * fix;
     return t;
   }
 };
-// Over the warp, the same in each lane.
-__device__ __forceinline__ MaxSum lanes_join(MaxSum t) {
-  const float m = warp_max(t.m);
-  t.s *= exp_diff(t.m, finite_or_zero(m));
+// Over the lanes' sums, the same in each lane.
+__device__ __forceinline__ MaxSum lanes_join(WarpSum t) {
+  MaxSum r{warp_max(t.m), 0.f};
+  const float base = finite_or_zero(r.m);
+  r.s = fmaf(t.rest, exp_diff(t.ref, base), exp_diff(t.m, base));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) t.s += __shfl_xor_sync(0xffffffffu, t.s, o);
-  t.m = m;
-  return t;
+  for (int o = 16; o > 0; o >>= 1) r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+  return r;
 }
 
 // NaN for all results of all rows of the CTA's cluster, of whose gradient it takes its share.
@@ -510,18 +514,18 @@ __global__ void __launch_bounds__(Cfg<kPolicy, kPieces>::kThreads, 1) stream_ker
         sum.template add<kPieces>(q);
         if (++slot == kSlots) slot = 0, phase ^= 1u;
       }
-      MaxSum t = sum.total();
+      const WarpSum w = sum.total();
       // statistics alone: the warps run ahead, by at most the two buffers
       if (!kPolicy && joins > 2) ok = ok && wait_warp(smem_u32(&sh.ready[group][b]), parity ^ 1u, stop);
       if (ok && lane == 0) {
-        sh.warp[b][warp - 2] = t;
+        sh.warp[b][warp - 2] = w;
         mbar_arrive_local(smem_u32(&sh.joined[group][b]));
       }
       __syncwarp();
       if (first_warp) {
         ok = ok && wait_warp(smem_u32(&sh.joined[group][b]), parity, stop);
-        t = lane < (by_slots ? C::kUsers : kUserWarps) ? sh.warp[b][group * kUserWarps + lane] : MaxSum{-INFINITY, 0.f};
-        t = lanes_join(t);
+        MaxSum t = lanes_join(lane < (by_slots ? C::kUsers : kUserWarps) ? sh.warp[b][group * kUserWarps + lane]
+                                                                        : WarpSum{-INFINITY, 0.f, -INFINITY});
         if (ok && ctas > 1) {
           if (lane < static_cast<int>(ctas))
             send(map_to_rank(smem_u32(&sh.cta[group][b][rank]), lane), map_to_rank(smem_u32(&sh.exchange[group][b]), lane), t);

@@ -130,7 +130,7 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
   w.s = s.x + s.y;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) w.s += __shfl_xor_sync(0xffffffffu, w.s, o);
-  if (m != -INFINITY) w.s = exact_top(w.s, own, fix);
+  if (m != -INFINITY) w.s = fmaf(w.s - own, fix, 1.f);
   return w;
 }
 
