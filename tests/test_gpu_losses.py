@@ -620,6 +620,30 @@ def test_rows_without_an_answer_are_nan(meq):
     assert float(r.logp[0]) == float("-inf")
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 640, 40003), ("bf16", 310, 151936), ("fp32", 310, 50001)])
+def test_long_rows_without_an_answer_are_nan(meq, dtype, rows, cols):
+    """The same among many long rows, and rows of the type's lowest value alone; all other rows stay as they are."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    z = _matrix(rows, cols, dtype, 0, 1)
+    z.copy_(torch.randn(rows, cols, generator=g, device="cuda"))
+    t = torch.randint(0, cols, (rows,), generator=g, device="cuda")
+    one = torch.ones(rows, device="cuda")
+    clean = meq.policy_loss(z, t, -10 * one, one, grad=True)
+    bad = torch.tensor([5, 70, 160, 161, 299], device="cuda")
+    z[5], z[70, cols - 1], z[160, 0], z[161, cols // 2], t[299] = float("-inf"), float("inf"), float("nan"), float("nan"), cols
+    z[33] = torch.finfo(DT[dtype]).min
+    got = meq.token_logprobs(z, t)
+    r = meq.policy_loss(z, t, -10 * one, one, grad=True)
+    assert torch.equal(torch.isnan(r.logp).nonzero()[:, 0], bad) and torch.equal(torch.isnan(got.logp).nonzero()[:, 0], bad)
+    assert float(got.lse[5]) == float("-inf") and bool(torch.isnan(got.lse[[70, 160, 161]]).all()) and bool(torch.isfinite(got.lse[299]))
+    assert bool(torch.isnan(r.grad[bad]).any(1).all()) and bool(torch.isnan(r.sums[:2]).all())   # the loss, its surrogate part
+    assert abs(float(got.logp[33]) + math.log(cols)) <= 2.0 ** -17 and abs(float(r.logp[33]) + math.log(cols)) <= 2.0 ** -17
+    other = torch.ones(rows, dtype=torch.bool, device="cuda")
+    other[bad], other[33] = False, False
+    assert torch.equal(r.logp[other], clean.logp[other]) and torch.equal(r.grad[other], clean.grad[other])
+    assert bool(torch.isfinite(r.grad[33]).all())
+
+
 @pytest.mark.parametrize("loss", ["policy", "preference"])
 def test_gradient_against_differences(meq, loss):
     """The change of the loss along the gradient. Step h = 1e-2: the third-order term of a symmetric
