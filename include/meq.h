@@ -380,13 +380,17 @@ meq_status meq_adamw_state_bytes(const meq_shape* shapes, int n, const meq_adamw
 /* State for n entries on the current device, moments and step count zero.
  * decay[i] >= 0 multiplies the weight decay of entry i (NULL: 1 for all; 0 for
  * norm weights and biases); opt may be NULL. Shapes have meq_init_state's
- * limits; only their element counts matter. */
+ * limits (2^20 rows and columns, 2^34 elements). Otherwise only their element
+ * counts matter: a longer flat buffer may be given as any rows x cols with its
+ * count, or as several entries. */
 meq_status meq_adamw_init(const meq_shape* shapes, const float* decay, int n, const meq_adamw_options* opt,
                           void* cuda_stream, meq_adamw** out);
 /* out[0] = the Euclidean norm of all gradients together, out[1] = the
  * coefficient that brings it to at most max_norm (1 if it is there; NaN if the
- * norm is not finite in fp32). out: device, two floats. max_norm > 0, may be
- * infinite. Sums of squares: fp32 per thread, then compensated, in a fixed order. */
+ * sum of squares is not finite in fp32, as with a gradient that is not or a norm
+ * from 1.8e19 on). out: device, two floats. max_norm > 0, may be infinite. Sums
+ * of squares: fp32 per thread, then compensated, in a fixed order; gradients
+ * below some 1e-22 may not count. */
 meq_status meq_adamw_grad_norm(const void* const* grads, meq_adamw* st, float max_norm, float* out, void* cuda_stream);
 /* One step. params (updated in place) and grads: device, contiguous, of the
  * state's types. copies: NULL, or per entry a device bf16 tensor of its size
@@ -428,7 +432,7 @@ const char* meq_adamw_last_error(const meq_adamw* st);
  *
  * logits: device, of meq_dtype `type`, consecutive columns, rows `ld` elements
  *   apart (ld >= cols; rows may start at any element). -inf masks a token; a
- *   row with a NaN or +inf, or with -inf alone, gives NaN.
+ *   row with a NaN or +inf, or with -inf alone (whose lse is -inf), gives NaN.
  * targets: device int64. A negative target marks a row that is not scored: its
  *   logits are not read, its logp is 0, its gradient zero. A target >= cols
  *   gives NaN. In the losses a weight of 0 leaves a row out in the same way.
@@ -465,7 +469,8 @@ int64_t meq_loss_work_floats(int64_t rows, int64_t pairs);
 
 /* The clipped policy loss with a KL term. With r = exp(logp - old_logp),
  * A = advantages, d = ref_logp - logp (logp before it is rounded to fp32, so r of
- * one's own logp is 1 but for that rounding):
+ * one's own logp is 1 but for that rounding, and a clip_low or clip_high of 0
+ * takes such a row for clipped):
  *
  *   L = sum_i w_i (s_i + kl_coef k_i)
  *   s = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A),  k = exp(d) - d - 1
@@ -487,7 +492,8 @@ meq_status meq_policy_loss(const void* logits, int type, int64_t rows, int64_t c
  *   L = mean_j (-(1 - e) log sigma(x_j) - e log sigma(-x_j)),  e = label_smoothing
  *
  * starts: device, 2 pairs + 1 int64, not decreasing, within 0..rows (an answer
- * may be empty; a pair whose starts are not so gives NaN and no gradient).
+ * may be empty; a pair whose starts are not so gives NaN, itself no gradient,
+ * and rows that pairs on both sides of it share get either's).
  * ref_logp per token, as meq_token_logprobs gives it, keeps the small
  * differences that a sum over an answer would round off. Rows in no answer get
  * a zero gradient. loss: device float; margins: device, pairs floats, the x_j.

@@ -17,8 +17,11 @@
 // Measured on 67.1M elements, with the time of the bytes at the measured copy
 // rate (6.79 TB/s) in brackets, us: fp32 277 (277), bf16 parameters and gradients
 // with fp32 moments 222 (218), 8-bit moments 123 (99), the same with fp32 parameters
-// 162 (139); the norm of fp32 gradients 42.7 (39.6), of bf16 ones 24.3 (19.8);
-// the values of 8-bit moments 108 (99).
+// 161 (139); the norm of fp32 gradients 42.0 (39.6), of bf16 ones 24.2 (19.8);
+// the values of 8-bit moments 108 (99). Tensors that do not start on 16 bytes
+// move an element at a time: 285 to 288 in fp32, 230 to 235 in bf16 with fp32
+// moments, 166 to 168 and 198 to 208 in 8 bits. A 32-bit step spills 8 bytes per
+// thread at the 64 registers that four blocks per SM leave it, at no cost that shows.
 //
 // 8-bit states, which instructions bound as much as HBM (some 50 per element, 74%
 // of the issue slots): 256 elements, one warp's share, have an fp32 scale each for m

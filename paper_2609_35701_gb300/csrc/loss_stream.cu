@@ -31,8 +31,10 @@
 // in bf16, with the time of the bytes at the measured copy rate (6.79 TB/s) in
 // brackets, us: gradient 4096 x 50001 133 (121), 8192 x 32000 171 (155), 2048 x 151936
 // 193 (183), fp32 2048 x 32000 97 (77); statistics 4096 x 50001 72 (60), 8192 x 32000
-// 86 (77), 4096 x 151936 192 (183). Of 8192 x 32000 with 80% of the rows scored at
-// random, 172 (139) and 80 (62): some CTAs have more of them than others.
+// 86 (77), 4096 x 151936 193 (183). Of 8192 x 32000 with 80% of the rows scored at
+// random, 169 (139) and 80 (62): some CTAs have more of them than others. The loss
+// without its gradient takes 129 us for 8192 x 32000 (77): the slots are given
+// back in the pass that would write it.
 //
 // Every wait is bounded. On expiry the roles of the CTA (and, for want of its
 // messages, of its cluster) stop, and when all have, every row of it gets NaN for
@@ -620,9 +622,12 @@ StreamShape shape_for(int64_t cols, int elem_bytes, bool policy) {
   int ctas = 1;
   while (ctas < kMaxCtas && (pieces + ctas - 1) / ctas * 16 > kMaxShare) ctas *= 2;
   // Slots of 10 KB, 22 of them; where they hold fewer than three rows, 17 of
-  // 12.5 KB, which a row of 70 to 76 KB fills better. 10 -> 12.5 KB, us:
-  // 2048 x 151936 bf16 206 -> 193, 1024 x 151936 fp32 200 -> 189;
-  // 4096 x 50001 bf16 134 -> 144, x 40000 108 -> 116, 8192 x 32000 171 -> 174.
+  // 12.5 KB, which shares of 70 to 76 KB fill better: at 17 widths of that band
+  // (600 MB of logits each) 14 were faster by 1 to 12%, one slower by 4%.
+  // 10 -> 12.5 KB, us: bf16 x 36500 221 -> 205, x 38800 201 -> 198, x 72000
+  // 211 -> 190, x 75000 207 -> 199, x 155000 210 -> 211, fp32 x 18000 218 -> 213,
+  // x 38500 209 -> 197, x 72001 190 -> 197. Outside it: 4096 x 50001 bf16
+  // 134 -> 144, x 40000 108 -> 116, 8192 x 32000 171 -> 174.
   const StreamShape s = shape_with<true, 4>(pieces, ctas);
   return 3 * s.rounds > Cfg<true, 4>::kSlots ? shape_with<true, 5>(pieces, ctas) : s;
 }
@@ -689,13 +694,13 @@ cudaError_t launch(const RowArgs& a, bool policy, cudaStream_t st) {
 // The other form holds a row in the registers of a CTA or a cluster, one row
 // after another per CTA: less to set up for few or short rows, but nothing is
 // loaded while a row is reduced and written. Measured, that form -> this one, us:
-//   bf16 gradient   4096 x 16000 48.7 -> 58.7, x 24001 87.4 -> 72.5, x 32000 89.6 -> 89.6, x 50001 188 -> 132,
-//                   608 x 32000 17.6 -> 19.5, 304 x 50001 17.3 -> 17.8, 608 x 50001 32.7 -> 28.0,
-//                   152 x 100000 20.5 -> 19.1
-//   fp32 gradient   4096 x 12000 72.8 -> 76.4, x 16000 86.6 -> 97.9, x 18000 114 -> 107, x 32000 190 -> 182
-//   bf16 statistics 4096 x 16000 26.4 -> 33.0, x 24001 49.4 -> 43.1, x 32000 53.1 -> 45.9, x 50001 119 -> 71.6,
-//                   608 x 32000 9.0 -> 10.5, 1216 x 32000 18.7 -> 16.6, 152 x 100000 12.0 -> 8.3
-//   fp32 statistics 4096 x 12000 40.2 -> 35.6, x 16000 44.3 -> 43.3
+//   bf16 gradient   4096 x 16000 47.9 -> 59.0, x 24001 86.0 -> 72.9, x 32000 87.7 -> 91.3, x 50001 187 -> 133,
+//                   608 x 32000 17.6 -> 20.5, 304 x 50001 17.2 -> 18.2, 608 x 50001 32.4 -> 28.8,
+//                   152 x 100000 19.5 -> 20.1
+//   fp32 gradient   4096 x 12000 72.1 -> 75.5, x 16000 87.2 -> 98.6, x 18000 112 -> 107, x 32000 187 -> 186
+//   bf16 statistics 4096 x 16000 24.9 -> 32.0, x 24001 47.1 -> 41.9, x 32000 51.0 -> 45.6, x 50001 113 -> 72.2,
+//                   608 x 32000 8.1 -> 10.4, 1216 x 32000 16.8 -> 16.6, 152 x 100000 11.0 -> 10.2
+//   fp32 statistics 4096 x 12000 37.0 -> 34.5, x 16000 42.5 -> 41.7
 bool stream_suits(int64_t rows, int64_t cols, int elem_bytes, bool policy) {
   const int64_t row_bytes = cols * elem_bytes;
   if (policy && shape_for(cols, elem_bytes, policy).rounds > Cfg<true, 5>::kSlots) return false;

@@ -14,14 +14,14 @@
 // and its gradient written from there: the floor. Few or short rows are held in
 // registers (8 pieces of 16 bytes per thread) by one CTA or a cluster of up to
 // 8, reduced (warp, CTA, then the cluster's CTAs through distributed shared
-// memory): 4096 x 16000 bf16 49 us (39 at the measured copy rate, 6.79 TB/s).
+// memory): 4096 x 16000 bf16 48 us (39 at the measured copy rate, 6.79 TB/s).
 // Many long ones are streamed through shared memory, in a file of their own.
 // Rows that neither holds take three launches (statistics, coefficients,
-// gradient).
+// gradient): 256 x 600000 bf16 151 us (136 for two reads and a write).
 //
 // Preference loss: c needs the sums over the two answers of a pair, so the
 // logits are read again for the gradient, last rows first: those are the ones
-// that the statistics pass left in L2. 9600 x 32000 bf16 313 us (272 for two
+// that the statistics pass left in L2. 9600 x 32000 bf16 309 us (272 for two
 // reads and a write at the copy rate).
 //
 // Rows start at any element: a row is cut at the 16-byte boundaries of its
@@ -137,8 +137,8 @@ __device__ __forceinline__ MaxSum warp_stats(const uint4 (&q)[P]) {
 // One CTA or cluster per row, in one pass over it. kPolicy: the whole row is in
 // registers, and its loss and gradient follow; else the row's statistics alone,
 // in as many rounds as it takes. Bound by HBM where there are many rows
-// (4096 x 16000 bf16: 49 and 26 us, 39 and 19 at the copy rate), else by latency:
-// with the launch of the sums 24 x 32000 fp32 takes 7.6 us, and the statistics of
+// (4096 x 16000 bf16: 48 and 25 us, 39 and 19 at the copy rate), else by latency:
+// with the launch of the sums 24 x 32000 fp32 takes 7.7 us, and the statistics of
 // 16 x 151936 bf16 4.7.
 template <typename T, bool kPolicy>
 __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
@@ -215,8 +215,8 @@ __global__ void __launch_bounds__(kRowThreadsMax) row_kernel(const RowArgs a) {
 
 // Rows of up to 32 P pieces (4 KB with P = 8), a warp each: no joins. The
 // instructions that a row takes whatever its length (some 300) bound it below
-// 1 KB, HBM above. 1000000 x 256 bf16 with the gradient and its sums 550 us (151 at
-// the copy rate), a CTA per row 1768; 200000 x 2000 289 (236). With the logits of a
+// 1 KB, HBM above. 1000000 x 256 bf16 with the gradient and its sums 542 us (151 at
+// the copy rate), a CTA per row 1768; 200000 x 2000 288 (236). With the logits of a
 // warp's next row loaded while it works on one a fifth slower: registers.
 template <typename T, bool kPolicy, int P>
 __global__ void __launch_bounds__(kShortThreads) short_kernel(const RowArgs a) {
