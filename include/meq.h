@@ -503,6 +503,74 @@ meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64
                                float label_smoothing, float* loss, float* margins, float* logp, void* grad, int64_t ld_grad,
                                const float* grad_scale, float* work, void* cuda_stream);
 
+/* ---- norms ------------------------------------------------------------------
+ * Layer norm and RMS norm of rows of activations (tokens), with the addition to
+ * the residual stream, and their backward pass. Forward, for every row:
+ *
+ *   h = x + residual (rounded to its type; x itself without a residual)
+ *   mu = mean_j h_j (RMS norm: 0),  rstd = 1 / sqrt(mean_j (h_j - mu)^2 + eps)
+ *   y_j = (h_j - mu) rstd w_j + b_j
+ *
+ * and backward, with xhat = (h - mu) rstd and a = dy w:
+ *
+ *   dx = rstd (a - mean(a) - xhat mean(a xhat)) + dh      (RMS norm: no mean(a))
+ *   dw = sum_rows dy xhat,  db = sum_rows dy
+ *
+ * dx is the gradient of h, which both x and the residual get; dh: what the
+ * stream's later uses add to it.
+ * x, residual, y, h, dy, dh, dx: device, rows x cols of meq_dtype `type`,
+ *   consecutive columns, rows ld_* elements apart (>= cols); rows may start at
+ *   any element. Fastest where all start at multiples of 16 bytes.
+ * weight, bias: device, cols elements of weight_type (NULL: 1 and 0).
+ * mean, rstd: device, rows floats. mean NULL selects RMS norm, in both calls.
+ * In place: y may be x or the residual, h may be x or the residual (not what y
+ *   is), dx may be dy, h or dh: the same pointer and row stride. Otherwise
+ *   outputs must not overlap inputs or one another.
+ * Sums and statistics are fp32, in fixed orders: results repeat bit for bit. A
+ * row whose sum of squares is not finite in fp32 gives NaN. rows may be 0.
+ * Nothing is allocated, and the calls may come from several threads. Limits:
+ * rows <= 2^27, cols <= 2^20, eps finite and > 0. */
+meq_status meq_layer_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int type, int64_t rows, int64_t cols,
+                          const void* weight, const void* bias, int weight_type, float eps, void* y, int64_t ld_y, void* h, int64_t ld_h,
+                          float* mean, float* rstd, void* cuda_stream);
+/* Floats of `work` for meq_layer_norm_grad. Host only. */
+int64_t meq_layer_norm_work_floats(int64_t rows, int64_t cols);
+/* dh: NULL, or added to dx. dweight, dbias: NULL, or device, cols elements of
+ * grad_type, overwritten (zeros for no rows). work: device scratch of
+ * meq_layer_norm_work_floats floats, 16-byte aligned, free again when the
+ * enqueued kernels have run. */
+meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int type,
+                               int64_t rows, int64_t cols, const void* weight, int weight_type, const float* mean, const float* rstd,
+                               void* dx, int64_t ld_dx, void* dweight, void* dbias, int grad_type, float* work, void* cuda_stream);
+
+/* ---- embedding ---------------------------------------------------------------
+ * out_i = scale E[t_i] for n tokens t and a table E of vocab rows, and the
+ * gradient of the table,
+ *
+ *   dE[v] = scale sum_{i: t_i = v} g_i,
+ *
+ * where g is the gradient of out. A negative token (padding) gives a row of
+ * zeros and no gradient; one >= vocab a row of NaN and no gradient.
+ * tokens: device, n int64. table, out, grad: device, of meq_dtype table_type,
+ *   out_type and type, consecutive columns, rows ld_* elements apart (>= cols);
+ *   rows may start at any element. Fastest where all start at multiples of 16
+ *   bytes and cols is a multiple of 8. out must not overlap an input.
+ * Sums are fp32, scaled and rounded once, in a fixed order (positions in turn,
+ * in groups that depend on n and cols alone): results repeat bit for bit.
+ * Nothing is allocated, and the calls may come from several threads. n may be 0.
+ * Limits: n <= 2^27, vocab <= 2^28, cols <= 2^20. */
+meq_status meq_embedding(const int64_t* tokens, int64_t n, const void* table, int table_type, int64_t vocab, int64_t cols, int64_t ld_table,
+                         float scale, void* out, int out_type, int64_t ld_out, void* cuda_stream);
+/* Floats of `work` for meq_embedding_grad. Host only. */
+int64_t meq_embedding_work_floats(int64_t n, int64_t cols);
+/* The gradient of the table into out (vocab rows of out_type): every row is
+ * written, or with accumulate != 0 the sums are added to what the rows hold (a
+ * table shared with the head, micro-batches) and the other rows left as they
+ * are. work: device scratch of meq_embedding_work_floats floats, 16-byte
+ * aligned, free again when the enqueued kernels have run. */
+meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t cols, int64_t ld, const int64_t* tokens, int64_t vocab,
+                              float scale, void* out, int out_type, int64_t ld_out, int accumulate, float* work, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,10 +27,10 @@
 // Rows start at any element: a row is cut at the 16-byte boundaries of its
 // address, and only its first and last piece are moved element by element.
 // Sums and statistics are fp32 or wider; exponentials are of z - max.
-#include <new>
 #include <string>
 
 #include "loss_rows.cuh"
+#include "meq_call.cuh"
 #include "meq_mbar.cuh"
 
 using namespace meq;
@@ -427,27 +427,6 @@ __global__ void __launch_bounds__(kSumThreads) policy_sums_kernel(float4* terms,
 }
 
 // ------------------------------------------------------------------- host
-meq_status fail(meq_status s, const std::string& msg) {
-  meq::set_global_error(msg);
-  return s;
-}
-meq_status launch_status(cudaError_t e, const char* fn, const char* what) {
-  if (e == cudaSuccess) return MEQ_OK;
-  return fail(MEQ_ERR_CUDA, std::string(fn) + ": " + what + ": " + cudaGetErrorString(e));
-}
-template <typename F>
-meq_status guarded(F f) {
-  try {
-    return f();
-  } catch (const std::bad_alloc&) {
-    return MEQ_ERR_OOM;
-  } catch (...) {
-    return MEQ_ERR_INVALID_ARG;
-  }
-}
-
-int elem_bytes(int type) { return type == MEQ_F32 ? 4 : 2; }
-
 // How a row of `cols` elements is spread over a cluster.
 struct RowShape {
   int ctas, threads;
@@ -518,15 +497,6 @@ cudaError_t launch_grad(const RowArgs& a, const Total& total, int type, cudaStre
   if (type == MEQ_BF16) return launch_grad<__nv_bfloat16>(a, total, st);
   return launch_grad<__half>(a, total, st);
 }
-
-int device_sms(cudaError_t* e) {
-  int dev = 0, sms = 0;
-  *e = cudaGetDevice(&dev);
-  if (*e == cudaSuccess) *e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return sms;
-}
-
-bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // The checks that the three calls share; an empty text: fine.
 std::string check_logits(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,

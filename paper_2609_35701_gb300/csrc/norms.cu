@@ -1,0 +1,276 @@
+// Layer norm and RMS norm, with the addition to the residual stream, and their
+// backward pass.
+//
+// Forward, per row:  h = x + residual (rounded to its type),
+//   mu = mean(h) (RMS: 0), rstd = 1 / sqrt(mean((h - mu)^2) + eps),
+//   y = (h - mu) rstd w + b.
+// Backward, with xhat = (h - mu) rstd and a = dy w:
+//   dx = rstd (a - mean(a) - xhat mean(a xhat)) (+ dh; RMS: no mean(a)),
+//   dw = sum over rows of dy xhat,  db = sum over rows of dy.
+//
+// The variance is that of differences from the mean, not a difference of
+// squares. Sums are fp32, in fixed orders.
+#include <string>
+
+#include "meq_call.cuh"
+#include "norms.cuh"
+
+namespace meq {
+namespace norm {
+namespace {
+
+constexpr int kWideThreads = 512;
+constexpr int kWideWarps = kWideThreads / 32;
+constexpr int kTileCols = 256;        // columns of a block of the wide rows' gradient
+constexpr int64_t kMostParts = 192;   // partial sums of a column, at most
+constexpr int64_t kPartFloats = kMostParts * 16384;
+constexpr int kFoldSlices = 8;
+
+// The sum of a block's values, for every thread; sh is free again after the next barrier.
+__device__ __forceinline__ float block_sum(float x, float* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWideWarps; ++i) s += sh[i];
+  return s;
+}
+
+// A block per row, which it reads again for each step.
+template <typename T>
+__global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const ForwardArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ float sh[3][kWideWarps];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+    T* y = static_cast<T*>(a.y) + row * a.ld_y;
+    float sum = 0.f;
+    if (a.residual) {
+      const T* r = static_cast<const T*>(a.residual) + row * a.ld_residual;
+      T* h = static_cast<T*>(a.h) + row * a.ld_h;
+      for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
+        const T s = Elem<T>::make(Elem<T>::get(x + j) + Elem<T>::get(r + j));
+        h[j] = s;
+        sum += Elem<T>::get(&s);
+      }
+      x = h;
+    } else if (a.mean) {
+      for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) sum += Elem<T>::get(x + j);
+    }
+    const float n = static_cast<float>(a.cols);
+    const float mu = a.mean ? block_sum(sum, sh[0]) / n : 0.f;
+    float sq = 0.f;
+    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
+      const float d = Elem<T>::get(x + j) - mu;
+      sq = fmaf(d, d, sq);
+    }
+    const float rstd = inverse_root(block_sum(sq, sh[1]) / n, a.eps);
+    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
+      float v = (Elem<T>::get(x + j) - mu) * rstd;
+      if (a.weight) v *= load_as(a.weight, a.weight_type, j);
+      if (a.bias) v += load_as(a.bias, a.weight_type, j);
+      y[j] = Elem<T>::make(v);
+    }
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[row] = mu;
+      a.rstd[row] = rstd;
+    }
+    __syncthreads();
+  }
+}
+
+// mean(a xhat) and mean(a) of a row per block.
+template <typename T>
+__global__ void __launch_bounds__(kWideThreads) wide_sums_kernel(const BackwardArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ float sh[2][kWideWarps];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
+    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
+    float c1 = 0.f, c2 = 0.f;
+    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
+      float d = Elem<T>::get(dy + j);
+      if (a.weight) d *= load_as(a.weight, a.weight_type, j);
+      c1 = fmaf(d, (Elem<T>::get(h + j) - mu) * rstd, c1);
+      c2 += d;
+    }
+    c1 = block_sum(c1, sh[0]);
+    c2 = block_sum(c2, sh[1]);
+    if (threadIdx.x == 0) {
+      const float n = static_cast<float>(a.cols);
+      a.row_sums[2 * row] = c1 / n;
+      a.row_sums[2 * row + 1] = a.mean ? c2 / n : 0.f;
+    }
+    __syncthreads();
+  }
+}
+
+// A thread per column, over every gridDim.y-th row: dx, and the column's partial sums.
+template <typename T>
+__global__ void __launch_bounds__(kTileCols) wide_backward_kernel(const BackwardArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kTileCols + threadIdx.x;
+  if (j >= a.cols) return;
+  const float w = a.weight ? load_as(a.weight, a.weight_type, j) : 1.f;
+  float dw = 0.f, db = 0.f;
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
+    const float d = Elem<T>::get(static_cast<const T*>(a.dy) + row * a.ld_dy + j);
+    const float xhat = (Elem<T>::get(static_cast<const T*>(a.h) + row * a.ld_h + j) - mu) * rstd;
+    dw = fmaf(d, xhat, dw);
+    db += d;
+    float dx = rstd * (fmaf(d, w, -a.row_sums[2 * row + 1]) - xhat * a.row_sums[2 * row]);
+    if (a.dh) dx += Elem<T>::get(static_cast<const T*>(a.dh) + row * a.ld_dh + j);
+    static_cast<T*>(a.dx)[row * a.ld_dx + j] = Elem<T>::make(dx);
+  }
+  a.parts[static_cast<int64_t>(blockIdx.y) * a.cols + j] = dw;
+  a.parts[(static_cast<int64_t>(gridDim.y) + blockIdx.y) * a.cols + j] = db;
+}
+
+// dw and db (blockIdx.y) from the partial sums, 32 columns per block, in slices of the parts.
+__global__ void __launch_bounds__(32 * kFoldSlices) fold_parts_kernel(const float* parts, int64_t n, int64_t cols, void* dw, void* db, int type) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ float sh[kFoldSlices][32];
+  const int lane = static_cast<int>(threadIdx.x & 31), slice = static_cast<int>(threadIdx.x >> 5);
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+  void* out = blockIdx.y == 0 ? dw : db;
+  if (!out) return;
+  const float* p = parts + static_cast<int64_t>(blockIdx.y) * n * cols + j;
+  float s = 0.f;
+  if (j < cols)
+    for (int64_t i = slice; i < n; i += kFoldSlices) s += p[i * cols];
+  sh[slice][lane] = s;
+  __syncthreads();
+  if (slice == 0 && j < cols) {
+#pragma unroll
+    for (int i = 1; i < kFoldSlices; ++i) s += sh[i][lane];
+    store_as(out, type, j, s);
+  }
+}
+
+// ------------------------------------------------------------------- host
+int64_t parts_for(int64_t rows, int64_t cols) {
+  int64_t n = kPartFloats / cols;
+  if (n > kMostParts) n = kMostParts;
+  if (n > rows) n = rows;
+  return n < 1 ? 1 : n;
+}
+
+unsigned row_grid(int64_t rows) { return static_cast<unsigned>(rows < (1 << 30) ? rows : (1 << 30)); }
+
+template <typename T>
+cudaError_t launch_forward(const ForwardArgs& a, cudaStream_t st) {
+  return launch_pdl(wide_forward_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
+}
+
+template <typename T>
+cudaError_t launch_backward(const BackwardArgs& a, int64_t* parts, cudaStream_t st) {
+  *parts = parts_for(a.rows, a.cols);
+  cudaError_t e = launch_pdl(wide_sums_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(wide_backward_kernel<T>, dim3(static_cast<unsigned>((a.cols + kTileCols - 1) / kTileCols), static_cast<unsigned>(*parts)),
+                    dim3(kTileCols), 0, st, 1, a);
+}
+
+// The checks that both calls share; an empty text: fine.
+std::string check_shape(int type, int64_t rows, int64_t cols, int weight_type) {
+  if (!valid_type(type) || !valid_type(weight_type)) return "the types must be meq_dtypes";
+  if (rows < 0 || rows > (int64_t(1) << 27)) return "rows must be in 0..2^27";
+  if (cols < 1 || cols > (int64_t(1) << 20)) return "cols must be in 1..2^20";
+  return "";
+}
+std::string check_matrix(const void* p, int64_t ld, int type, int64_t rows, int64_t cols, const char* what, bool needed) {
+  if (!p) return needed && rows > 0 ? std::string(what) + " must not be NULL" : "";
+  if (!aligned_to(p, elem_bytes(type))) return std::string(what) + " is not aligned to its type";
+  if (rows > 1 && ld < cols) return "the row stride of " + std::string(what) + " must be at least cols";
+  if (ld < 0 || ld > (int64_t(1) << 40)) return "the row stride of " + std::string(what) + " must be in 0..2^40";
+  return "";
+}
+
+}  // namespace
+}  // namespace norm
+}  // namespace meq
+
+using namespace meq;
+using namespace meq::norm;
+
+extern "C" {
+
+meq_status meq_layer_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int type, int64_t rows, int64_t cols,
+                          const void* weight, const void* bias, int weight_type, float eps, void* y, int64_t ld_y, void* h, int64_t ld_h,
+                          float* mean, float* rstd, void* cuda_stream) {
+  return guarded([&]() -> meq_status {
+    std::string why = check_shape(type, rows, cols, weight_type);
+    if (why.empty()) why = check_matrix(x, ld_x, type, rows, cols, "x", true);
+    if (why.empty()) why = check_matrix(residual, ld_residual, type, rows, cols, "residual", false);
+    if (why.empty()) why = check_matrix(y, ld_y, type, rows, cols, "y", true);
+    if (why.empty()) why = check_matrix(h, ld_h, type, rows, cols, "h", residual != nullptr);
+    if (why.empty() && h && !residual) why = "h is written with a residual only";
+    if (why.empty() && h && h == y) why = "y and h must not be the same";
+    if (why.empty() && !(eps > 0.f && eps <= FLT_MAX)) why = "eps must be finite and > 0";
+    if (why.empty() && rows > 0 && !rstd) why = "rstd must not be NULL";
+    if (why.empty() && !(aligned_to(weight, elem_bytes(weight_type)) && aligned_to(bias, elem_bytes(weight_type)) && aligned_to(mean, 4) && aligned_to(rstd, 4)))
+      why = "a pointer is not aligned to its type";
+    if (!why.empty()) return fail(MEQ_ERR_INVALID_ARG, "meq_layer_norm: " + why);
+    if (rows == 0) return MEQ_OK;
+    ForwardArgs a{};
+    a.x = x, a.residual = residual, a.weight = weight, a.bias = bias, a.y = y, a.h = h, a.mean = mean, a.rstd = rstd;
+    a.rows = rows, a.cols = cols, a.ld_x = ld_x, a.ld_residual = ld_residual, a.ld_y = ld_y, a.ld_h = ld_h;
+    a.weight_type = weight_type, a.eps = eps;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = type == MEQ_F32    ? launch_forward<float>(a, st)
+                          : type == MEQ_BF16 ? launch_forward<__nv_bfloat16>(a, st)
+                                             : launch_forward<__half>(a, st);
+    return launch_status(e, "meq_layer_norm", "launch");
+  });
+}
+
+int64_t meq_layer_norm_work_floats(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 1) return 0;
+  return 2 * parts_for(rows, cols) * cols + 2 * rows;
+}
+
+meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int type,
+                               int64_t rows, int64_t cols, const void* weight, int weight_type, const float* mean, const float* rstd,
+                               void* dx, int64_t ld_dx, void* dweight, void* dbias, int grad_type, float* work, void* cuda_stream) {
+  return guarded([&]() -> meq_status {
+    std::string why = check_shape(type, rows, cols, weight_type);
+    if (why.empty() && !valid_type(grad_type)) why = "the types must be meq_dtypes";
+    if (why.empty()) why = check_matrix(dy, ld_dy, type, rows, cols, "dy", true);
+    if (why.empty()) why = check_matrix(h, ld_h, type, rows, cols, "h", true);
+    if (why.empty()) why = check_matrix(dh, ld_dh, type, rows, cols, "dh", false);
+    if (why.empty()) why = check_matrix(dx, ld_dx, type, rows, cols, "dx", true);
+    if (why.empty() && rows > 0 && !rstd) why = "rstd must not be NULL";
+    if (why.empty() && (!work || !aligned_to(work, 16))) why = "work must not be NULL and be 16-byte aligned";
+    if (why.empty() && !(aligned_to(weight, elem_bytes(weight_type)) && aligned_to(dweight, elem_bytes(grad_type)) &&
+                         aligned_to(dbias, elem_bytes(grad_type)) && aligned_to(mean, 4) && aligned_to(rstd, 4)))
+      why = "a pointer is not aligned to its type";
+    if (!why.empty()) return fail(MEQ_ERR_INVALID_ARG, "meq_layer_norm_grad: " + why);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    BackwardArgs a{};
+    a.dy = dy, a.h = h, a.dh = dh, a.weight = weight, a.mean = mean, a.rstd = rstd, a.dx = dx;
+    a.rows = rows, a.cols = cols, a.ld_dy = ld_dy, a.ld_h = ld_h, a.ld_dh = ld_dh, a.ld_dx = ld_dx;
+    a.weight_type = weight_type, a.parts = work, a.row_sums = work + 2 * parts_for(rows, cols) * cols;
+    int64_t parts = 0;
+    if (rows > 0) {
+      const cudaError_t e = type == MEQ_F32    ? launch_backward<float>(a, &parts, st)
+                            : type == MEQ_BF16 ? launch_backward<__nv_bfloat16>(a, &parts, st)
+                                               : launch_backward<__half>(a, &parts, st);
+      if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "launch");
+    }
+    if (!dweight && !dbias) return MEQ_OK;
+    const dim3 grid(static_cast<unsigned>((cols + 31) / 32), dbias ? 2u : 1u);
+    return launch_status(launch_pdl(fold_parts_kernel, grid, dim3(32 * kFoldSlices), 0, st, 1, static_cast<const float*>(work), parts, cols,
+                                    dweight, dbias, grad_type),
+                         "meq_layer_norm_grad", "sum launch");
+  });
+}
+
+}  // extern "C"

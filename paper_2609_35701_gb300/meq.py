@@ -1,8 +1,8 @@
-"""Thin ctypes binding of the C ABI (include/meq.h): MeqMuon, AdamW and the
-losses of fine-tuning.
+"""Thin ctypes binding of the C ABI (include/meq.h): MeqMuon, AdamW, the losses
+of fine-tuning, norms and embedding.
 
-Argument marshalling only: every step of the optimizers and every loss runs in
-the CUDA library. There is no fallback: if libmeq.so is missing or fails to
+Argument marshalling only: every step of the optimizers and every operator runs
+in the CUDA library. There is no fallback: if libmeq.so is missing or fails to
 load, importing this module raises.
 """
 from __future__ import annotations
@@ -77,6 +77,8 @@ EXPORTED = [
     "meq_adamw_free", "meq_adamw_last_error",
     "meq_token_logprobs", "meq_loss_work_floats", "meq_policy_loss", "meq_preference_loss",
     "meq_debug_loss_wait",
+    "meq_layer_norm", "meq_layer_norm_work_floats", "meq_layer_norm_grad",
+    "meq_embedding", "meq_embedding_work_floats", "meq_embedding_grad",
 ]
 HIDDEN, REMAINING_2D, VECTOR = 0, 1, 2  # meq_kind
 RULE_MEQMUON, RULE_MUON = 0, 1          # meq_update_rule
@@ -190,6 +192,18 @@ def _load():
     lib.meq_preference_loss.restype = I
     lib.meq_debug_loss_wait.argtypes = [F, I64]
     lib.meq_debug_loss_wait.restype = I
+    lib.meq_layer_norm.argtypes = [P, I64, P, I64, I, I64, I64, P, P, I, F, P, I64, P, I64, P, P, P]
+    lib.meq_layer_norm.restype = I
+    lib.meq_layer_norm_work_floats.argtypes = [I64, I64]
+    lib.meq_layer_norm_work_floats.restype = I64
+    lib.meq_layer_norm_grad.argtypes = [P, I64, P, I64, P, I64, I, I64, I64, P, I, P, P, P, I64, P, P, I, P, P]
+    lib.meq_layer_norm_grad.restype = I
+    lib.meq_embedding.argtypes = [P, I64, P, I, I64, I64, I64, F, P, I, I64, P]
+    lib.meq_embedding.restype = I
+    lib.meq_embedding_work_floats.argtypes = [I64, I64]
+    lib.meq_embedding_work_floats.restype = I64
+    lib.meq_embedding_grad.argtypes = [P, I, I64, I64, I64, P, I64, F, P, I, I64, I, P, P]
+    lib.meq_embedding_grad.restype = I
     return lib
 
 
@@ -712,14 +726,14 @@ def _current_device(t, what):
     return device
 
 
-def _check_loss(s):
+def _check_call(s):
     if s != MEQ_OK:
         raise MeqError(s, lib.meq_last_error(None).decode())
 
 
 def debug_loss_wait(timeout_ms=0.0, withheld_row=-1):
     """Diagnostic (meq_debug_loss_wait): the limit of the loss kernels' waits and a row whose data never comes."""
-    _check_loss(lib.meq_debug_loss_wait(float(timeout_ms), int(withheld_row)))
+    _check_call(lib.meq_debug_loss_wait(float(timeout_ms), int(withheld_row)))
 
 
 def token_logprobs(logits, targets, stream=None):
@@ -732,7 +746,7 @@ def token_logprobs(logits, targets, stream=None):
     device = _current_device(logits, "logits")
     t = _vector(targets, torch.int64, rows, device, "targets")
     logp, lse = _empty(rows, torch.float32, logits.device, stream), _empty(rows, torch.float32, logits.device, stream)
-    _check_loss(lib.meq_token_logprobs(logits.data_ptr(), kind, rows, cols, ld, t, logp.data_ptr(), lse.data_ptr(),
+    _check_call(lib.meq_token_logprobs(logits.data_ptr(), kind, rows, cols, ld, t, logp.data_ptr(), lse.data_ptr(),
                                        _stream_handle(stream, device)))
     return TokenLogprobs(logp, lse)
 
@@ -756,7 +770,7 @@ def policy_loss(logits, targets, old_logp, advantages, weights=None, ref_logp=No
     given, (grad, g, ldg) = grad, _grad_for(logits, rows, cols, ld, grad, stream)
     work = _empty(lib.meq_loss_work_floats(rows, 0), f32, where, stream)
     sums, logp = _empty(4, f32, where, stream), _empty(rows, f32, where, stream)
-    _check_loss(lib.meq_policy_loss(logits.data_ptr(), kind, rows, cols, ld, t, old, adv, w, ref, float(clip_low),
+    _check_call(lib.meq_policy_loss(logits.data_ptr(), kind, rows, cols, ld, t, old, adv, w, ref, float(clip_low),
                                     float(clip_high), float(kl_coef), sums.data_ptr(), logp.data_ptr(), g, ldg, scale,
                                     work.data_ptr(), _stream_handle(stream, device)))
     if grad is not None and grad is given:
@@ -784,9 +798,167 @@ def preference_loss(logits, targets, starts, ref_logp, weights=None, beta=0.1, l
     given, (grad, g, ldg) = grad, _grad_for(logits, rows, cols, ld, grad, stream)
     work = _empty(lib.meq_loss_work_floats(rows, pairs), f32, where, stream)
     logp, margins, loss = _empty(rows, f32, where, stream), _empty(pairs, f32, where, stream), _empty((), f32, where, stream)
-    _check_loss(lib.meq_preference_loss(logits.data_ptr(), kind, rows, cols, ld, t, st, pairs, ref, w, float(beta),
+    _check_call(lib.meq_preference_loss(logits.data_ptr(), kind, rows, cols, ld, t, st, pairs, ref, w, float(beta),
                                         float(label_smoothing), loss.data_ptr(), margins.data_ptr(), logp.data_ptr(), g, ldg,
                                         scale, work.data_ptr(), _stream_handle(stream, device)))
     if grad is not None and grad is given:
         torch.autograd.graph.increment_version(grad)  # written through its pointer, which autograd does not see
     return PreferenceLoss(loss, margins, logp, grad)
+
+
+# ---------------------------------------------------------- norms and embedding
+LayerNorm = collections.namedtuple("LayerNorm", "y h mean rstd")
+RmsNorm = collections.namedtuple("RmsNorm", "y h rstd")
+LayerNormGrad = collections.namedtuple("LayerNormGrad", "dx dweight dbias")
+RmsNormGrad = collections.namedtuple("RmsNormGrad", "dx dweight")
+
+
+def _like(t, x, what):
+    """Pointer and row stride of a matrix of x's shape, type and device (None: no matrix)."""
+    if t is None:
+        return None, 0
+    if t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
+        raise ValueError(f"{what} must have the shape, type and device of the first argument")
+    return t.data_ptr(), _logits_args(t, what)[3]
+
+
+def _columns(t, cols, device, what, dtype=None):
+    """Pointer and meq_dtype of a contiguous CUDA vector of cols elements (None: no vector)."""
+    if t is None:
+        return None, 0
+    kind = DTYPES.get(str(t.dtype)[6:])
+    if kind is None or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{what} must be of {sorted(DTYPES) if dtype is None else dtype}")
+    return _vector(t, t.dtype, cols, device, what), kind
+
+
+def _written(*given):
+    """Tensors of the caller's that were written through their pointers, which autograd does not see."""
+    import torch
+
+    for t in given:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
+def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
+    import torch
+
+    kind, rows, cols, ld = _logits_args(x, "x")
+    device = _current_device(x, "x")
+    r, ld_r = _like(residual, x, "residual")
+    w, weight_kind = _columns(weight, cols, device, "weight")
+    b, bias_kind = _columns(bias, cols, device, "bias", None if weight is None else weight.dtype)
+    if residual is None and h is not None:
+        raise ValueError("h is written with a residual only")
+    given = y, h
+    out = _empty((rows, cols), x.dtype, x.device, stream) if y is None else y
+    if residual is None:
+        h, hp, ld_h = x, None, 0
+    else:
+        h = _empty((rows, cols), x.dtype, x.device, stream) if h is None else h
+        hp, ld_h = _like(h, x, "h")
+    yp, ld_y = _like(out, x, "y")
+    mean = _empty(rows, torch.float32, x.device, stream) if centred else None
+    rstd = _empty(rows, torch.float32, x.device, stream)
+    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, bias_kind if weight is None else weight_kind, float(eps),
+                                   yp, ld_y, hp, ld_h, mean.data_ptr() if centred else None, rstd.data_ptr(), _stream_handle(stream, device)))
+    _written(*given)
+    return out, h, mean, rstd
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5, y=None, h=None, stream=None):
+    """Layer norm of the rows of x, or of h = x + residual (meq_layer_norm). x:
+    CUDA matrix, fp32, bf16 or fp16, one row per token; weight, bias: vectors of
+    one of these types; y, h: tensors to write (y may be x or residual, h the other
+    or x: the stream's in-place update), else new ones. h of the result is what was
+    normalised; mean and rstd are for the backward pass."""
+    return LayerNorm(*_norm(x, weight, bias, residual, eps, y, h, stream, True))
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, y=None, h=None, stream=None):
+    """RMS norm of the rows of x, or of h = x + residual (meq_layer_norm); arguments as in layer_norm."""
+    y, h, _, rstd = _norm(x, weight, None, residual, eps, y, h, stream, False)
+    return RmsNorm(y, h, rstd)
+
+
+def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
+    import torch
+
+    kind, rows, cols, ld = _logits_args(dy, "dy")
+    device, f32 = _current_device(dy, "dy"), torch.float32
+    hp, ld_h = _like(h, dy, "h")
+    sp, ld_s = _like(dh, dy, "dh")
+    w, weight_kind = _columns(weight, cols, device, "weight")
+    mp, rp = _vector(mean, f32, rows, device, "mean"), _vector(rstd, f32, rows, device, "rstd")
+    given = dx, dweight, dbias
+    dx = _empty((rows, cols), dy.dtype, dy.device, stream) if dx is None else dx
+    xp, ld_x = _like(dx, dy, "dx")
+    shape, dtype = (cols, f32) if weight is None else (weight.shape, weight.dtype)
+    if dweight is not None or dbias is not None:
+        dtype = (dbias if dweight is None else dweight).dtype
+    if dweight is None and weight is not None:
+        dweight = _empty(shape, dtype, dy.device, stream)
+    if dbias is None and bias:
+        dbias = _empty(shape, dtype, dy.device, stream)
+    (wp, grad_kind), (bp, bias_kind) = _columns(dweight, cols, device, "dweight"), _columns(dbias, cols, device, "dbias", dtype)
+    work = _empty(lib.meq_layer_norm_work_floats(rows, cols), f32, dy.device, stream)
+    _check_call(lib.meq_layer_norm_grad(dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp,
+                                        bias_kind if dweight is None else grad_kind, work.data_ptr(), _stream_handle(stream, device)))
+    _written(*given)
+    return dx, dweight, dbias
+
+
+def layer_norm_grad(dy, h, weight, mean, rstd, dh=None, dx=None, dweight=None, dbias=None, bias=True, stream=None):
+    """The backward pass of layer_norm (meq_layer_norm_grad) from the gradient dy
+    of y and the h, mean and rstd of its result. dh: a gradient of h to add; dx,
+    dweight, dbias: tensors to write (dx may be dy, h or dh), else new ones, of the
+    weight's type; bias False: no bias. dx is the gradient of x and of the residual."""
+    return LayerNormGrad(*_norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream))
+
+
+def rms_norm_grad(dy, h, weight, rstd, dh=None, dx=None, dweight=None, stream=None):
+    """The backward pass of rms_norm (meq_layer_norm_grad); arguments as in layer_norm_grad."""
+    dx, dweight, _ = _norm_grad(dy, h, weight, None, rstd, dh, dx, dweight, None, False, stream)
+    return RmsNormGrad(dx, dweight)
+
+
+def embedding(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
+    """scale times the table's rows of the tokens, one row per token
+    (meq_embedding). tokens: contiguous int64 CUDA tensor, negative for rows of
+    zeros; table: CUDA matrix, fp32, bf16 or fp16; out: the matrix to write, else a
+    new one of dtype (default: the table's)."""
+    import torch
+
+    table_kind, vocab, cols, ld = _logits_args(table, "table")
+    device, n = _current_device(table, "table"), tokens.numel()
+    t = _vector(tokens, torch.int64, n, device, "tokens")
+    given = out
+    if out is None:
+        out = _empty((n, cols), table.dtype if dtype is None else dtype, table.device, stream)
+    out_kind, rows, out_cols, ld_out = _logits_args(out, "out")
+    if rows != n or out_cols != cols or out.get_device() != device or (dtype is not None and out.dtype is not dtype):
+        raise ValueError("out must have a row per token, the table's columns and its device")
+    _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, float(scale), out.data_ptr(), out_kind, ld_out,
+                                  _stream_handle(stream, device)))
+    _written(given)
+    return out
+
+
+def embedding_grad(grad, tokens, out, scale=1.0, accumulate=False, stream=None):
+    """The gradient of the table into out, a matrix of the table's shape
+    (meq_embedding_grad), from the gradient of embedding's result. accumulate:
+    added to what out holds. Returns out."""
+    import torch
+
+    kind, n, cols, ld = _logits_args(grad, "grad")
+    device = _current_device(grad, "grad")
+    t = _vector(tokens, torch.int64, n, device, "tokens")
+    out_kind, vocab, out_cols, ld_out = _logits_args(out, "out")
+    if out_cols != cols or out.get_device() != device:
+        raise ValueError("out must have the gradient's columns and device")
+    work = _empty(lib.meq_embedding_work_floats(n, cols), torch.float32, grad.device, stream)
+    _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, float(scale), out.data_ptr(), out_kind, ld_out,
+                                       int(bool(accumulate)), work.data_ptr(), _stream_handle(stream, device)))
+    _written(out)
+    return out
