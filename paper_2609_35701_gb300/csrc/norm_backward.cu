@@ -1,0 +1,185 @@
+// The backward pass of the norms: rows that the registers of a group of warps
+// hold. One persistent block per SM; dy and h are read once, dx written once, and
+// the sums over rows of dy xhat and dy stay in registers until the block's last
+// row; then the block's groups are added up and leave one partial sum per column.
+#include "norm_rows.cuh"
+
+namespace meq {
+namespace norm {
+namespace {
+
+// kBias: dy is summed over rows too.
+template <int kElements, bool kBias>
+constexpr int threads_of() {
+  return kElements > 16 ? (kBias ? 384 : 512) : kElements > 8 ? 640 : 1024;
+}
+
+template <typename T, int kStep, int kPieces, bool kBias>
+__global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
+  using P = Place<T, kStep, kPieces>;
+  constexpr int H = P::H;
+  pdl_allow_dependents();
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ Exchange ex;
+  const P p(s, a.cols);
+  const int matrices = a.dh ? 3 : 2, set = 32 / s.lanes;  // rows that the group takes at once
+  const int slots = s.depth * matrices * s.slot_bytes;
+  uint8_t* mine = ring + static_cast<int64_t>(p.group * set + p.sub) * slots;
+  const uint32_t mine32 = smem_u32(mine);
+  const int64_t sets = (a.rows + set - 1) / set, step = static_cast<int64_t>(gridDim.x) * s.groups;
+  const int64_t first = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;
+  int64_t next = first;  // set whose copies start next
+  int put = 0;
+  auto copy_next = [&]() {
+    const int64_t row = next * set + p.sub;
+    if (next < sets && row < a.rows) {
+      const uint32_t at = mine32 + static_cast<uint32_t>(put * matrices * s.slot_bytes);
+      p.copy(at, a.dy, row, a.ld_dy, a.rows);
+      p.copy(at + s.slot_bytes, a.h, row, a.ld_h, a.rows);
+      if (a.dh) p.copy(at + 2 * s.slot_bytes, a.dh, row, a.ld_dh, a.rows);
+    }
+    copies_commit();
+    next += step;
+    if (++put == s.depth) put = 0;
+  };
+  auto statistics = [&](int64_t set_at) -> float2 {  // mu and rstd
+    const int64_t row = set_at * set + p.sub;
+    return set_at < sets && row < a.rows ? make_float2(a.mean ? a.mean[row] : 0.f, a.rstd[row]) : make_float2(0.f, 0.f);
+  };
+  pdl_wait_predecessor();
+  for (int i = 0; i < s.depth - 1; ++i) copy_next();
+  float2 stat = statistics(first);
+  float2 w[H], dw[H], db[kBias ? H : 1];
+  p.vector(a.weight, a.weight_type, a.weight ? 0.f : 1.f, w);
+#pragma unroll
+  for (int k = 0; k < H; ++k) dw[k] = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < (kBias ? H : 1); ++k) db[k] = make_float2(0.f, 0.f);
+  const float per = 1.f / static_cast<float>(a.cols);
+  int take = 0, turn = 0;
+  for (int64_t i = first; i < sets; i += step) {
+    const int64_t row = i * set + p.sub;
+    const bool in = row < a.rows;
+    const float2 now = stat;
+    stat = statistics(i + step);
+    copies_wait(s.depth);
+    if (kStep == 1) group_barrier(s, p.group);  // the others' copies too, and the slot before is free
+    copy_next();
+    const uint8_t* at = mine + take * matrices * s.slot_bytes;
+    if (++take == s.depth) take = 0;
+    const float2 mu = make_float2(-now.x, -now.x), rstd = make_float2(now.y, now.y);
+    float2 c1 = make_float2(0.f, 0.f), c2 = c1;
+    const uint8_t* dy = p.row_at(at, a.dy, row, a.ld_dy);
+    const uint8_t* h = p.row_at(at + s.slot_bytes, a.h, row, a.ld_h);
+    const uint8_t* dh = p.row_at(at + 2 * s.slot_bytes, a.dh, row, a.ld_dh);
+#pragma unroll
+    for (int u = 0; u < P::U; ++u) {
+      float2 x[P::W], d[P::W];
+      p.read(h, u, in, x);
+      p.read(dy, u, in, d);
+#pragma unroll
+      for (int k = 0; k < P::W; ++k) {
+        const int i = u * P::W + k;
+        x[k] = mul2(add2(x[k], mu), rstd);
+        dw[i] = fma2(d[k], x[k], dw[i]);
+        if (kBias) db[i] = add2(db[i], d[k]);
+        d[k] = mul2(d[k], w[i]);
+        c1 = fma2(d[k], x[k], c1);
+        c2 = add2(c2, d[k]);
+      }
+    }
+    const float2 c = row_sum(make_float2(c1.x + c1.y, c2.x + c2.y), s, p.group, p.warp_in, ex, turn);
+    if (!in) continue;
+    const float2 m1 = make_float2(-c.x * per, -c.x * per), m2 = a.mean ? make_float2(-c.y * per, -c.y * per) : make_float2(0.f, 0.f);
+    // dy and h once more from shared memory: kept in registers they would leave no room for the sums.
+#pragma unroll
+    for (int u = 0; u < P::U; ++u) {
+      float2 x[P::W], d[P::W];
+      p.read(h, u, true, x);
+      p.read(dy, u, true, d);
+#pragma unroll
+      for (int k = 0; k < P::W; ++k) {
+        x[k] = mul2(add2(x[k], mu), rstd);
+        d[k] = mul2(fma2(x[k], m1, fma2(d[k], w[u * P::W + k], m2)), rstd);
+      }
+      if (a.dh) {
+        p.read(dh, u, true, x);
+#pragma unroll
+        for (int k = 0; k < P::W; ++k) d[k] = add2(d[k], x[k]);
+      }
+      p.write(static_cast<T*>(a.dx) + row * a.ld_dx, u, d);
+    }
+  }
+  if (!a.parts) return;
+  // The block's groups added up, in shared memory: the ring holds 8 bytes for each of their columns.
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  const int copies = s.groups * set;
+  float* sums = reinterpret_cast<float*>(ring);
+  const int64_t cols = a.cols;
+#pragma unroll
+  for (int k = 0; k < 2 * H; ++k) {
+    const int j = p.element_col(k);
+    if (j < cols) {
+      sums[(p.group * set + p.sub) * cols + j] = k % 2 ? dw[k / 2].y : dw[k / 2].x;
+      if (kBias) sums[(copies + p.group * set + p.sub) * cols + j] = k % 2 ? db[k / 2].y : db[k / 2].x;
+    }
+  }
+  __syncthreads();
+  for (int64_t j = threadIdx.x; j < (kBias ? 2 : 1) * cols; j += blockDim.x) {
+    const bool second = j >= cols;
+    const int64_t c = second ? j - cols : j;
+    const float* from = sums + (second ? copies * cols : 0) + c;
+    float total = from[0];
+    for (int g = 1; g < copies; ++g) total += from[g * cols];
+    a.parts[((second ? gridDim.x : 0) + blockIdx.x) * cols + c] = total;
+  }
+}
+
+template <typename T, int kStep, int kPieces, bool kBias>
+cudaError_t launch(const BackwardArgs& a, const RowShape& s, int64_t grid, cudaStream_t st) {
+  auto* kernel = row_backward_kernel<T, kStep, kPieces, kBias>;
+  const cudaError_t e = allow_ring(kernel);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.dh ? 3 : 2), st, 1, a, s);
+}
+
+template <typename T, bool kBias>
+bool launch_of(const BackwardArgs& a, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
+  constexpr int kN = Elem<T>::N;
+  const int matrices = a.dh ? 3 : 2;
+  const bool whole = a.cols % kN == 0 && starts_at_16<T>(a.dy, a.ld_dy) && starts_at_16<T>(a.h, a.ld_h) && starts_at_16<T>(a.dh, a.ld_dh) &&
+                     starts_at_16<T>(a.dx, a.ld_dx);
+  RowShape s;
+  int pieces = 0;
+  if (!row_shape(a.cols, whole ? kN : 1, sizeof(T), matrices, kBias, whole ? kWholePieces : kSingles, 4, &s, &pieces)) return false;
+  const int set = 32 / s.lanes;
+  const int64_t sets = (a.rows + set - 1) / set;
+  *parts = sets < sms ? sets : sms;
+  if (whole)
+    *e = pieces == 1   ? launch<T, kN, 1, kBias>(a, s, *parts, st)
+         : pieces == 2 ? launch<T, kN, 2, kBias>(a, s, *parts, st)
+         : pieces == 3 ? launch<T, kN, 3, kBias>(a, s, *parts, st)
+                       : launch<T, kN, 4, kBias>(a, s, *parts, st);
+  else
+    *e = pieces == 2    ? launch<T, 1, 2, kBias>(a, s, *parts, st)
+         : pieces == 8  ? launch<T, 1, 8, kBias>(a, s, *parts, st)
+         : pieces == 16 ? launch<T, 1, 16, kBias>(a, s, *parts, st)
+                        : launch<T, 1, 32, kBias>(a, s, *parts, st);
+  return true;
+}
+template <typename T>
+bool launch_of(const BackwardArgs& a, bool bias, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
+  return bias ? launch_of<T, true>(a, sms, parts, st, e) : launch_of<T, false>(a, sms, parts, st, e);
+}
+
+}  // namespace
+
+bool launch_row_backward(const BackwardArgs& a, int type, bool bias, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
+  if (type == MEQ_F32) return launch_of<float>(a, bias, sms, parts, st, e);
+  if (type == MEQ_BF16) return launch_of<__nv_bfloat16>(a, bias, sms, parts, st, e);
+  return launch_of<__half>(a, bias, sms, parts, st, e);
+}
+
+}  // namespace norm
+}  // namespace meq

@@ -13,7 +13,7 @@
 #include <string>
 
 #include "meq_call.cuh"
-#include "norms.cuh"
+#include "norm_rows.cuh"
 
 namespace meq {
 namespace norm {
@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(kTileCols) wide_backward_kernel(const Backward
     if (a.dh) dx += Elem<T>::get(static_cast<const T*>(a.dh) + row * a.ld_dh + j);
     static_cast<T*>(a.dx)[row * a.ld_dx + j] = Elem<T>::make(dx);
   }
+  if (!a.parts) return;
   a.parts[static_cast<int64_t>(blockIdx.y) * a.cols + j] = dw;
   a.parts[(static_cast<int64_t>(gridDim.y) + blockIdx.y) * a.cols + j] = db;
 }
@@ -166,12 +167,12 @@ int64_t parts_for(int64_t rows, int64_t cols) {
 unsigned row_grid(int64_t rows) { return static_cast<unsigned>(rows < (1 << 30) ? rows : (1 << 30)); }
 
 template <typename T>
-cudaError_t launch_forward(const ForwardArgs& a, cudaStream_t st) {
+cudaError_t launch_wide_forward(const ForwardArgs& a, cudaStream_t st) {
   return launch_pdl(wide_forward_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
 }
 
 template <typename T>
-cudaError_t launch_backward(const BackwardArgs& a, int64_t* parts, cudaStream_t st) {
+cudaError_t launch_wide_backward(const BackwardArgs& a, int64_t* parts, cudaStream_t st) {
   *parts = parts_for(a.rows, a.cols);
   cudaError_t e = launch_pdl(wide_sums_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
   if (e != cudaSuccess) return e;
@@ -225,9 +226,13 @@ meq_status meq_layer_norm(const void* x, int64_t ld_x, const void* residual, int
     a.rows = rows, a.cols = cols, a.ld_x = ld_x, a.ld_residual = ld_residual, a.ld_y = ld_y, a.ld_h = ld_h;
     a.weight_type = weight_type, a.eps = eps;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = type == MEQ_F32    ? launch_forward<float>(a, st)
-                          : type == MEQ_BF16 ? launch_forward<__nv_bfloat16>(a, st)
-                                             : launch_forward<__half>(a, st);
+    cudaError_t e;
+    const int sms = device_sms(&e);
+    if (e != cudaSuccess) return launch_status(e, "meq_layer_norm", "device attributes");
+    if (!launch_row_forward(a, type, sms, st, &e))
+      e = type == MEQ_F32    ? launch_wide_forward<float>(a, st)
+          : type == MEQ_BF16 ? launch_wide_forward<__nv_bfloat16>(a, st)
+                             : launch_wide_forward<__half>(a, st);
     return launch_status(e, "meq_layer_norm", "launch");
   });
 }
@@ -257,12 +262,17 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
     BackwardArgs a{};
     a.dy = dy, a.h = h, a.dh = dh, a.weight = weight, a.mean = mean, a.rstd = rstd, a.dx = dx;
     a.rows = rows, a.cols = cols, a.ld_dy = ld_dy, a.ld_h = ld_h, a.ld_dh = ld_dh, a.ld_dx = ld_dx;
-    a.weight_type = weight_type, a.parts = work, a.row_sums = work + 2 * parts_for(rows, cols) * cols;
+    a.weight_type = weight_type, a.parts = dweight || dbias ? work : nullptr, a.row_sums = work + 2 * parts_for(rows, cols) * cols;
     int64_t parts = 0;
     if (rows > 0) {
-      const cudaError_t e = type == MEQ_F32    ? launch_backward<float>(a, &parts, st)
-                            : type == MEQ_BF16 ? launch_backward<__nv_bfloat16>(a, &parts, st)
-                                               : launch_backward<__half>(a, &parts, st);
+      cudaError_t e;
+      int sms = device_sms(&e);
+      if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "device attributes");
+      if (sms > parts_for(rows, cols)) sms = static_cast<int>(parts_for(rows, cols));  // what work has room for
+      if (!launch_row_backward(a, type, dbias != nullptr, sms, &parts, st, &e))
+        e = type == MEQ_F32    ? launch_wide_backward<float>(a, &parts, st)
+            : type == MEQ_BF16 ? launch_wide_backward<__nv_bfloat16>(a, &parts, st)
+                               : launch_wide_backward<__half>(a, &parts, st);
       if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "launch");
     }
     if (!dweight && !dbias) return MEQ_OK;
