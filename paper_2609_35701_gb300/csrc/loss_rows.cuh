@@ -66,33 +66,6 @@ struct ExpBase {
 // The exponential of one element relative to c, as the sums take it.
 __device__ __forceinline__ float exp_at(float x, float c) { return exp2_approx(fmaf(x, kLog2eLo, fmaf(x, kLog2e, -c))); }
 
-// The 128 bits of a piece moved by one element towards its end or its start,
-// with the element that comes in or has gone out (edges of a row only).
-__device__ __forceinline__ void push_front(uint4& q, uint32_t bits, float) {
-  q = make_uint4(bits, q.x, q.y, q.z);
-}
-template <typename T>
-__device__ __forceinline__ void push_front(uint4& q, uint32_t bits, T) {
-  q.w = __funnelshift_l(q.z, q.w, 16);
-  q.z = __funnelshift_l(q.y, q.z, 16);
-  q.y = __funnelshift_l(q.x, q.y, 16);
-  q.x = (q.x << 16) | bits;
-}
-__device__ __forceinline__ uint32_t pop_front(uint4& q, float) {
-  const uint32_t bits = q.x;
-  q = make_uint4(q.y, q.z, q.w, 0u);
-  return bits;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t pop_front(uint4& q, T) {
-  const uint32_t bits = q.x & 0xFFFFu;
-  q.x = __funnelshift_r(q.x, q.y, 16);
-  q.y = __funnelshift_r(q.y, q.z, 16);
-  q.z = __funnelshift_r(q.z, q.w, 16);
-  q.w >>= 16;
-  return bits;
-}
-
 // A row cut at the 16-byte boundaries of its address: piece k holds elements
 // k N - lead .. k N - lead + N - 1 of the row, as far as they exist. Pieces
 // `begin` .. `end` - 1 exist whole; at most the first and the last do not. A

@@ -96,4 +96,31 @@ struct Elem<__half> {
   static __device__ __forceinline__ __half make(float x) { return __float2half_rn(x); }
 };
 
+// The 128 bits of a piece moved by one element towards its end or its start,
+// with the element that comes in or has gone out (edges of a row only).
+__device__ __forceinline__ void push_front(uint4& q, uint32_t bits, float) {
+  q = make_uint4(bits, q.x, q.y, q.z);
+}
+template <typename T>
+__device__ __forceinline__ void push_front(uint4& q, uint32_t bits, T) {
+  q.w = __funnelshift_l(q.z, q.w, 16);
+  q.z = __funnelshift_l(q.y, q.z, 16);
+  q.y = __funnelshift_l(q.x, q.y, 16);
+  q.x = (q.x << 16) | bits;
+}
+__device__ __forceinline__ uint32_t pop_front(uint4& q, float) {
+  const uint32_t bits = q.x;
+  q = make_uint4(q.y, q.z, q.w, 0u);
+  return bits;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pop_front(uint4& q, T) {
+  const uint32_t bits = q.x & 0xFFFFu;
+  q.x = __funnelshift_r(q.x, q.y, 16);
+  q.y = __funnelshift_r(q.y, q.z, 16);
+  q.z = __funnelshift_r(q.z, q.w, 16);
+  q.w >>= 16;
+  return bits;
+}
+
 }  // namespace meq

@@ -14,17 +14,16 @@ constexpr int threads_of() {
   return kElements > 16 ? (kBias ? 384 : 512) : kElements > 8 ? 640 : 1024;
 }
 
-template <typename T, int kStep, int kPieces, bool kBias>
-__global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
-  using P = Place<T, kStep, kPieces>;
-  constexpr int H = P::H;
+template <typename T, int kPieces, bool kShifted, bool kBias>
+__global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
+  using P = Place<T, kPieces, kShifted>;
+  constexpr int H = P::H, W = P::W;
   pdl_allow_dependents();
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Exchange ex;
   const P p(s, a.cols);
   const int matrices = a.dh ? 3 : 2, set = 32 / s.lanes;  // rows that the group takes at once
-  const int slots = s.depth * matrices * s.slot_bytes;
-  uint8_t* mine = ring + static_cast<int64_t>(p.group * set + p.sub) * slots;
+  uint8_t* mine = ring + (static_cast<int>(threadIdx.x >> 5) * set + p.sub) * (s.depth * matrices * s.slot_bytes);
   const uint32_t mine32 = smem_u32(mine);
   const int64_t sets = (a.rows + set - 1) / set, step = static_cast<int64_t>(gridDim.x) * s.groups;
   const int64_t first = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;
@@ -34,9 +33,9 @@ __global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_b
     const int64_t row = next * set + p.sub;
     if (next < sets && row < a.rows) {
       const uint32_t at = mine32 + static_cast<uint32_t>(put * matrices * s.slot_bytes);
-      p.copy(at, a.dy, row, a.ld_dy, a.rows);
-      p.copy(at + s.slot_bytes, a.h, row, a.ld_h, a.rows);
-      if (a.dh) p.copy(at + 2 * s.slot_bytes, a.dh, row, a.ld_dh, a.rows);
+      p.copy(at, a.dy, row, a.ld_dy, a.rows, a.cols);
+      p.copy(at + s.slot_bytes, a.h, row, a.ld_h, a.rows, a.cols);
+      if (a.dh) p.copy(at + 2 * s.slot_bytes, a.dh, row, a.ld_dh, a.rows, a.cols);
     }
     copies_commit();
     next += step;
@@ -50,7 +49,7 @@ __global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_b
   for (int i = 0; i < s.depth - 1; ++i) copy_next();
   float2 stat = statistics(first);
   float2 w[H], dw[H], db[kBias ? H : 1];
-  p.vector(a.weight, a.weight_type, a.weight ? 0.f : 1.f, w);
+  p.vector(a.weight, a.weight_type, 1.f, w);
 #pragma unroll
   for (int k = 0; k < H; ++k) dw[k] = make_float2(0.f, 0.f);
 #pragma unroll
@@ -63,51 +62,50 @@ __global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_b
     const float2 now = stat;
     stat = statistics(i + step);
     copies_wait(s.depth);
-    if (kStep == 1) group_barrier(s, p.group);  // the others' copies too, and the slot before is free
+    if (kShifted) __syncwarp();  // the other lanes' copies too, and the slot before is free
     copy_next();
     const uint8_t* at = mine + take * matrices * s.slot_bytes;
     if (++take == s.depth) take = 0;
     const float2 mu = make_float2(-now.x, -now.x), rstd = make_float2(now.y, now.y);
     float2 c1 = make_float2(0.f, 0.f), c2 = c1;
-    const uint8_t* dy = p.row_at(at, a.dy, row, a.ld_dy);
-    const uint8_t* h = p.row_at(at + s.slot_bytes, a.h, row, a.ld_h);
-    const uint8_t* dh = p.row_at(at + 2 * s.slot_bytes, a.dh, row, a.ld_dh);
+    const uint8_t *dy = at, *h = at + s.slot_bytes, *dh = at + 2 * s.slot_bytes;
+    const int lead_dy = p.lead(a.dy, row, a.ld_dy), lead_h = p.lead(a.h, row, a.ld_h), lead_dh = p.lead(a.dh, row, a.ld_dh);
 #pragma unroll
-    for (int u = 0; u < P::U; ++u) {
-      float2 x[P::W], d[P::W];
-      p.read(h, u, in, x);
-      p.read(dy, u, in, d);
+    for (int k = 0; k < kPieces; ++k) {
+      float2 x[W], d[W];
+      p.read(h, lead_h, k, in, x);
+      p.read(dy, lead_dy, k, in, d);
 #pragma unroll
-      for (int k = 0; k < P::W; ++k) {
-        const int i = u * P::W + k;
-        x[k] = mul2(add2(x[k], mu), rstd);
-        dw[i] = fma2(d[k], x[k], dw[i]);
-        if (kBias) db[i] = add2(db[i], d[k]);
-        d[k] = mul2(d[k], w[i]);
-        c1 = fma2(d[k], x[k], c1);
-        c2 = add2(c2, d[k]);
+      for (int e = 0; e < W; ++e) {
+        const int j = k * W + e;
+        x[e] = mul2(add2(x[e], mu), rstd);
+        dw[j] = fma2(d[e], x[e], dw[j]);
+        if (kBias) db[j] = add2(db[j], d[e]);
+        d[e] = mul2(d[e], w[j]);
+        c1 = fma2(d[e], x[e], c1);
+        c2 = add2(c2, d[e]);
       }
     }
     const float2 c = row_sum(make_float2(c1.x + c1.y, c2.x + c2.y), s, p.group, p.warp_in, ex, turn);
-    if (!in) continue;
     const float2 m1 = make_float2(-c.x * per, -c.x * per), m2 = a.mean ? make_float2(-c.y * per, -c.y * per) : make_float2(0.f, 0.f);
     // dy and h once more from shared memory: kept in registers they would leave no room for the sums.
+    uint4 before = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int u = 0; u < P::U; ++u) {
-      float2 x[P::W], d[P::W];
-      p.read(h, u, true, x);
-      p.read(dy, u, true, d);
+    for (int k = 0; k < kPieces; ++k) {
+      float2 x[W], d[W];
+      p.read(h, lead_h, k, in, x);
+      p.read(dy, lead_dy, k, in, d);
 #pragma unroll
-      for (int k = 0; k < P::W; ++k) {
-        x[k] = mul2(add2(x[k], mu), rstd);
-        d[k] = mul2(fma2(x[k], m1, fma2(d[k], w[u * P::W + k], m2)), rstd);
+      for (int e = 0; e < W; ++e) {
+        x[e] = mul2(add2(x[e], mu), rstd);
+        d[e] = mul2(fma2(x[e], m1, fma2(d[e], w[k * W + e], m2)), rstd);
       }
       if (a.dh) {
-        p.read(dh, u, true, x);
+        p.read(dh, lead_dh, k, in, x);
 #pragma unroll
-        for (int k = 0; k < P::W; ++k) d[k] = add2(d[k], x[k]);
+        for (int e = 0; e < W; ++e) d[e] = add2(d[e], x[e]);
       }
-      p.write(static_cast<T*>(a.dx) + row * a.ld_dx, u, d);
+      p.write(static_cast<T*>(a.dx) + row * a.ld_dx, k, d, in, before);
     }
   }
   if (!a.parts) return;
@@ -120,7 +118,7 @@ __global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_b
 #pragma unroll
   for (int k = 0; k < 2 * H; ++k) {
     const int j = p.element_col(k);
-    if (j < cols) {
+    if (p.has_element(k)) {
       sums[(p.group * set + p.sub) * cols + j] = k % 2 ? dw[k / 2].y : dw[k / 2].x;
       if (kBias) sums[(copies + p.group * set + p.sub) * cols + j] = k % 2 ? db[k / 2].y : db[k / 2].x;
     }
@@ -136,41 +134,34 @@ __global__ void __launch_bounds__(threads_of<kStep * kPieces, kBias>(), 1) row_b
   }
 }
 
-template <typename T, int kStep, int kPieces, bool kBias>
+template <typename T, int kPieces, bool kShifted, bool kBias>
 cudaError_t launch(const BackwardArgs& a, const RowShape& s, int64_t grid, cudaStream_t st) {
-  auto* kernel = row_backward_kernel<T, kStep, kPieces, kBias>;
+  auto* kernel = row_backward_kernel<T, kPieces, kShifted, kBias>;
   const cudaError_t e = allow_ring(kernel);
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.dh ? 3 : 2), st, 1, a, s);
 }
 
-template <typename T, bool kBias>
+template <typename T, bool kShifted, bool kBias>
 bool launch_of(const BackwardArgs& a, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
-  constexpr int kN = Elem<T>::N;
-  const int matrices = a.dh ? 3 : 2;
-  const bool whole = a.cols % kN == 0 && starts_at_16<T>(a.dy, a.ld_dy) && starts_at_16<T>(a.h, a.ld_h) && starts_at_16<T>(a.dh, a.ld_dh) &&
-                     starts_at_16<T>(a.dx, a.ld_dx);
   RowShape s;
   int pieces = 0;
-  if (!row_shape(a.cols, whole ? kN : 1, sizeof(T), matrices, kBias, whole ? kWholePieces : kSingles, 4, &s, &pieces)) return false;
+  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.dh ? 3 : 2, kBias, &s, &pieces)) return false;
   const int set = 32 / s.lanes;
   const int64_t sets = (a.rows + set - 1) / set;
   *parts = sets < sms ? sets : sms;
-  if (whole)
-    *e = pieces == 1   ? launch<T, kN, 1, kBias>(a, s, *parts, st)
-         : pieces == 2 ? launch<T, kN, 2, kBias>(a, s, *parts, st)
-         : pieces == 3 ? launch<T, kN, 3, kBias>(a, s, *parts, st)
-                       : launch<T, kN, 4, kBias>(a, s, *parts, st);
-  else
-    *e = pieces == 2    ? launch<T, 1, 2, kBias>(a, s, *parts, st)
-         : pieces == 8  ? launch<T, 1, 8, kBias>(a, s, *parts, st)
-         : pieces == 16 ? launch<T, 1, 16, kBias>(a, s, *parts, st)
-                        : launch<T, 1, 32, kBias>(a, s, *parts, st);
+  *e = pieces == 1   ? launch<T, 1, kShifted, kBias>(a, s, *parts, st)
+       : pieces == 2 ? launch<T, 2, kShifted, kBias>(a, s, *parts, st)
+       : pieces == 3 ? launch<T, 3, kShifted, kBias>(a, s, *parts, st)
+                     : launch<T, 4, kShifted, kBias>(a, s, *parts, st);
   return true;
 }
 template <typename T>
 bool launch_of(const BackwardArgs& a, bool bias, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
-  return bias ? launch_of<T, true>(a, sms, parts, st, e) : launch_of<T, false>(a, sms, parts, st, e);
+  const bool aligned = a.cols % Elem<T>::N == 0 && starts_at_16<T>(a.dy, a.ld_dy) && starts_at_16<T>(a.h, a.ld_h) && starts_at_16<T>(a.dh, a.ld_dh) &&
+                       starts_at_16<T>(a.dx, a.ld_dx);
+  if (aligned) return bias ? launch_of<T, false, true>(a, sms, parts, st, e) : launch_of<T, false, false>(a, sms, parts, st, e);
+  return bias ? launch_of<T, true, true>(a, sms, parts, st, e) : launch_of<T, true, false>(a, sms, parts, st, e);
 }
 
 }  // namespace

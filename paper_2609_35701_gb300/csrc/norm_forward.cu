@@ -6,32 +6,32 @@ namespace meq {
 namespace norm {
 namespace {
 
-template <typename T, int kStep, int kPieces>
+template <typename T, int kPieces>
 constexpr int threads_of() {
-  return kStep * kPieces > 16 ? 512 : kStep * kPieces > 8 ? 640 : 1024;
+  return Elem<T>::N * kPieces > 16 ? 512 : Elem<T>::N * kPieces > 8 ? 640 : 1024;
 }
 
-template <typename T, int kStep, int kPieces>
-__global__ void __launch_bounds__(threads_of<T, kStep, kPieces>(), 1) row_forward_kernel(const __grid_constant__ ForwardArgs a, const RowShape s) {
-  using P = Place<T, kStep, kPieces>;
-  constexpr int H = P::H;
+template <typename T, int kPieces, bool kShifted>
+__global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kernel(const __grid_constant__ ForwardArgs a, const RowShape s) {
+  using P = Place<T, kPieces, kShifted>;
+  constexpr int H = P::H, W = P::W;
   pdl_allow_dependents();
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Exchange ex;
   const P p(s, a.cols);
   const int matrices = a.residual ? 2 : 1, set = 32 / s.lanes;  // rows that the group takes at once
-  const int slots = s.depth * matrices * s.slot_bytes;
-  uint8_t* mine = ring + static_cast<int64_t>(p.group * set + p.sub) * slots;
+  uint8_t* mine = ring + (static_cast<int>(threadIdx.x >> 5) * set + p.sub) * (s.depth * matrices * s.slot_bytes);
   const uint32_t mine32 = smem_u32(mine);
   const int64_t sets = (a.rows + set - 1) / set, step = static_cast<int64_t>(gridDim.x) * s.groups;
-  int64_t next = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;  // set whose copies start next
+  const int64_t first = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;
+  int64_t next = first;  // set whose copies start next
   int put = 0;
   auto copy_next = [&]() {
     const int64_t row = next * set + p.sub;
     if (next < sets && row < a.rows) {
       const uint32_t at = mine32 + static_cast<uint32_t>(put * matrices * s.slot_bytes);
-      p.copy(at, a.x, row, a.ld_x, a.rows);
-      if (a.residual) p.copy(at + s.slot_bytes, a.residual, row, a.ld_residual, a.rows);
+      p.copy(at, a.x, row, a.ld_x, a.rows, a.cols);
+      if (a.residual) p.copy(at + s.slot_bytes, a.residual, row, a.ld_residual, a.rows, a.cols);
     }
     copies_commit();
     next += step;
@@ -40,34 +40,34 @@ __global__ void __launch_bounds__(threads_of<T, kStep, kPieces>(), 1) row_forwar
   pdl_wait_predecessor();
   for (int i = 0; i < s.depth - 1; ++i) copy_next();
   float2 w[H], b[H];
-  p.vector(a.weight, a.weight_type, a.weight ? 0.f : 1.f, w);
+  p.vector(a.weight, a.weight_type, 1.f, w);
   p.vector(a.bias, a.weight_type, 0.f, b);
   const float per = 1.f / static_cast<float>(a.cols);
   int take = 0, turn = 0;
-  for (int64_t i = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x; i < sets; i += step) {
+  for (int64_t i = first; i < sets; i += step) {
     const int64_t row = i * set + p.sub;
     const bool in = row < a.rows;
     copies_wait(s.depth);
-    if (kStep == 1) group_barrier(s, p.group);  // the others' copies too, and the slot before is free
+    if (kShifted) __syncwarp();  // the other lanes' copies too, and the slot before is free
     copy_next();
     const uint8_t* at = mine + take * matrices * s.slot_bytes;
     if (++take == s.depth) take = 0;
     float2 v[H];
-    const uint8_t* x = p.row_at(at, a.x, row, a.ld_x);
-    const uint8_t* r = p.row_at(at + s.slot_bytes, a.residual, row, a.ld_residual);
+    const int lead = p.lead(a.x, row, a.ld_x), lead_r = p.lead(a.residual, row, a.ld_residual);
+    uint4 before = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int u = 0; u < P::U; ++u) {
-      float2 y[P::W];
-      p.read(x, u, in, y);
+    for (int k = 0; k < kPieces; ++k) {
+      float2 x[W];
+      p.read(at, lead, k, in, x);
       if (a.residual) {
-        float2 z[P::W];
-        p.read(r, u, in, z);
+        float2 r[W];
+        p.read(at + s.slot_bytes, lead_r, k, in, r);
 #pragma unroll
-        for (int k = 0; k < P::W; ++k) y[k] = round_pair<T>(add2(y[k], z[k]));
-        if (in) p.write(static_cast<T*>(a.h) + row * a.ld_h, u, y);
+        for (int e = 0; e < W; ++e) x[e] = round_pair<T>(add2(x[e], r[e]));
+        p.write(static_cast<T*>(a.h) + row * a.ld_h, k, x, in, before);
       }
 #pragma unroll
-      for (int k = 0; k < P::W; ++k) v[u * P::W + k] = y[k];
+      for (int e = 0; e < W; ++e) v[k * W + e] = x[e];
     }
     float mu = 0.f;
     if (a.mean) {
@@ -77,57 +77,57 @@ __global__ void __launch_bounds__(threads_of<T, kStep, kPieces>(), 1) row_forwar
       mu = row_sum(make_float2(sum.x + sum.y, 0.f), s, p.group, p.warp_in, ex, turn).x * per;
 #pragma unroll
       for (int k = 0; k < H; ++k) v[k] = add2(v[k], make_float2(-mu, -mu));
-      p.clip(v);
+      if (!p.whole()) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) p.clip(k, v + k * W);
+      }
     }
     float2 sq = mul2(v[0], v[0]);
 #pragma unroll
     for (int k = 1; k < H; ++k) sq = fma2(v[k], v[k], sq);
     const float var = row_sum(make_float2(sq.x + sq.y, 0.f), s, p.group, p.warp_in, ex, turn).x * per;
     const float rstd = inverse_root(var, a.eps);
-    if (!in) continue;
 #pragma unroll
-    for (int k = 0; k < H; ++k) v[k] = fma2(mul2(v[k], make_float2(rstd, rstd)), w[k], b[k]);
+    for (int k = 0; k < kPieces; ++k) {
+      float2 y[W];
 #pragma unroll
-    for (int u = 0; u < P::U; ++u) p.write(static_cast<T*>(a.y) + row * a.ld_y, u, v + u * P::W);
-    if (p.t == 0) {
+      for (int e = 0; e < W; ++e) y[e] = fma2(mul2(v[k * W + e], make_float2(rstd, rstd)), w[k * W + e], b[k * W + e]);
+      p.write(static_cast<T*>(a.y) + row * a.ld_y, k, y, in, before);
+    }
+    if (in && p.warp_in == 0 && p.lane == 0) {
       if (a.mean) a.mean[row] = mu;
       a.rstd[row] = rstd;
     }
   }
 }
 
-template <typename T, int kStep, int kPieces>
+template <typename T, int kPieces, bool kShifted>
 cudaError_t launch(const ForwardArgs& a, const RowShape& s, int sms, cudaStream_t st) {
-  const int set = 32 / s.lanes, bytes = ring_bytes(s, a.residual ? 2 : 1);
+  const int set = 32 / s.lanes;
   const int64_t sets = (a.rows + set - 1) / set;
-  auto* kernel = row_forward_kernel<T, kStep, kPieces>;
+  auto* kernel = row_forward_kernel<T, kPieces, kShifted>;
   const cudaError_t e = allow_ring(kernel);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(sets < sms ? sets : sms)), dim3(32 * s.warps * s.groups), bytes, st, 1, a, s);
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(sets < sms ? sets : sms)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.residual ? 2 : 1),
+                    st, 1, a, s);
 }
 
-template <typename T>
+template <typename T, bool kShifted>
 bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
-  constexpr int kN = Elem<T>::N;
-  const int matrices = a.residual ? 2 : 1;
-  const bool whole = a.cols % kN == 0 && starts_at_16<T>(a.x, a.ld_x) && starts_at_16<T>(a.y, a.ld_y) && starts_at_16<T>(a.residual, a.ld_residual) &&
-                     starts_at_16<T>(a.h, a.ld_h);
   RowShape s;
   int pieces = 0;
-  if (whole) {
-    if (!row_shape(a.cols, kN, sizeof(T), matrices, false, kWholePieces, 4, &s, &pieces)) return false;
-    *e = pieces == 1   ? launch<T, kN, 1>(a, s, sms, st)
-         : pieces == 2 ? launch<T, kN, 2>(a, s, sms, st)
-         : pieces == 3 ? launch<T, kN, 3>(a, s, sms, st)
-                       : launch<T, kN, 4>(a, s, sms, st);
-  } else {
-    if (!row_shape(a.cols, 1, sizeof(T), matrices, false, kSingles, 4, &s, &pieces)) return false;
-    *e = pieces == 2    ? launch<T, 1, 2>(a, s, sms, st)
-         : pieces == 8  ? launch<T, 1, 8>(a, s, sms, st)
-         : pieces == 16 ? launch<T, 1, 16>(a, s, sms, st)
-                        : launch<T, 1, 32>(a, s, sms, st);
-  }
+  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.residual ? 2 : 1, false, &s, &pieces)) return false;
+  *e = pieces == 1   ? launch<T, 1, kShifted>(a, s, sms, st)
+       : pieces == 2 ? launch<T, 2, kShifted>(a, s, sms, st)
+       : pieces == 3 ? launch<T, 3, kShifted>(a, s, sms, st)
+                     : launch<T, 4, kShifted>(a, s, sms, st);
   return true;
+}
+template <typename T>
+bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
+  const bool aligned = a.cols % Elem<T>::N == 0 && starts_at_16<T>(a.x, a.ld_x) && starts_at_16<T>(a.y, a.ld_y) &&
+                       starts_at_16<T>(a.residual, a.ld_residual) && starts_at_16<T>(a.h, a.ld_h);
+  return aligned ? launch_of<T, false>(a, sms, st, e) : launch_of<T, true>(a, sms, st, e);
 }
 
 }  // namespace

@@ -1,17 +1,18 @@
 // Rows of activations on their way through the norms' persistent kernels: how a
 // row is shared out to threads, copied ahead into shared memory, and reduced.
 //
-// A group of `warps` warps takes a row at a time; of short rows a warp takes
-// several at once, `lanes` lanes each. Column j of a row belongs to the same
-// thread in every row, so weights stay in registers, and so do the sums over
-// rows of the weight's gradient.
+// A group of `warps` warps takes a row at a time, each warp consecutive columns
+// of it; of short rows a warp takes several at once, `lanes` lanes each. Piece k
+// of a lane is 16 bytes' worth of columns, the same ones in every row, so weights
+// stay in registers, and so do the sums over rows of the weight's gradient.
 //
 // Rows are copied into a ring of slots (cp.async) `depth` - 1 rows ahead, which
 // keeps enough bytes on their way whatever the registers leave of the
-// occupancy. Where every row starts at 16 bytes a thread copies the 16-byte
-// pieces that it reads itself, and no thread waits for another. Else (kStep 1)
-// the group copies the 16-byte words that hold the row, and each thread picks
-// its elements out of them, wherever the row starts.
+// occupancy. Where every row starts at 16 bytes a thread copies the pieces that
+// it reads itself, and no thread waits for another. Else (kShifted) a warp copies
+// the 16-byte words that hold its columns, a lane's piece is shifted out of two
+// of them, and pieces are shifted back into words, with the neighbour lane's, to
+// be stored: nothing but the ends of a warp's columns goes element by element.
 #pragma once
 
 #include <map>
@@ -33,7 +34,7 @@ struct RowShape {
   int warps;       // of a row's group (1 when lanes < 32)
   int groups;      // of a block
   int depth;       // slots of a row's ring
-  int slot_bytes;  // of one matrix's row
+  int slot_bytes;  // of one matrix's row, or a warp's part of it
 };
 
 // The partial sums of a block's warps.
@@ -52,93 +53,153 @@ __device__ __forceinline__ void copies_wait(int depth) {
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+// Bytes `from` .. `from` + 15 of the 32 bytes of a and b (from: a multiple of the element's size, at most 16).
+template <typename T>
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int from) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (from & 16) {
+    return b;
+  }
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = from & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = from & 4 ? w[i + 1] : w[i];
+  if (sizeof(T) == 2) {
+    const int bits = (from & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A thread's place in its row.
-template <typename T, int kStep, int kPieces>
+template <typename T, int kPieces, bool kShifted>
 struct Place {
-  static constexpr int E = kStep * kPieces, H = E / 2;  // elements of a thread, and pairs of them
-  int cols, threads, t;  // threads of a row, and which of them this is
-  int group, sub, warp_in;
-  __device__ __forceinline__ Place(const RowShape& s, int64_t cols_) {
-    const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-    cols = static_cast<int>(cols_);
+  static constexpr int N = Elem<T>::N, H = kPieces * N / 2, W = N / 2;  // pairs of elements: of a thread, of a piece
+  int lanes, lane, group, sub, warp_in;
+  int left;  // columns from the thread's first one to the row's end (negative: it has none)
+  int segment, segment_bytes;  // the warp's first column, and the bytes of its columns
+  __device__ __forceinline__ Place(const RowShape& s, int64_t cols) {
+    const int warp = static_cast<int>(threadIdx.x >> 5);
+    lanes = kPieces > 1 ? 32 : s.lanes;
+    lane = static_cast<int>(threadIdx.x & 31) & (lanes - 1);
+    sub = static_cast<int>(threadIdx.x & 31) / lanes;
     group = warp / s.warps;
     warp_in = warp - group * s.warps;
-    sub = lane / s.lanes;
-    threads = s.warps * s.lanes;
-    t = warp_in * s.lanes + (lane - sub * s.lanes);
+    segment = warp_in * 32 * kPieces * N;
+    const int rest = static_cast<int>(cols) - segment;
+    left = rest - lane * N;
+    segment_bytes = max(0, min(rest, lanes * kPieces * N)) * static_cast<int>(sizeof(T));
   }
-  // Column of the thread's piece k.
-  __device__ __forceinline__ int col(int k) const { return (t + k * threads) * kStep; }
+  // Column of piece k's first element, relative to the segment.
+  __device__ __forceinline__ int col(int k) const { return (lane + k * lanes) * N; }
+  __device__ __forceinline__ bool has(int k) const { return k * lanes * N < left; }
+  // Whether all elements of all pieces exist.
+  __device__ __forceinline__ bool whole() const { return (kPieces - 1) * lanes * N + N <= left; }
+  __device__ __forceinline__ int lead(const void* base, int64_t row, int64_t ld) const {
+    return kShifted ? static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const T*>(base) + row * ld) & 15) : 0;
+  }
 
-  // Starts the copies of row `row` of a matrix into a slot. [lo, hi): the matrix's bytes.
-  __device__ __forceinline__ void copy(uint32_t slot, const void* base, int64_t row, int64_t ld, int64_t rows) const {
-    const T* p = static_cast<const T*>(base) + row * ld;
-    if (kStep > 1) {
+  // Starts the copies of the warp's columns of a matrix's row into a slot.
+  __device__ __forceinline__ void copy(uint32_t slot, const void* base, int64_t row, int64_t ld, int64_t rows, int64_t cols) const {
+    const T* p = static_cast<const T*>(base) + row * ld + segment;
+    if (!kShifted) {
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
-        if (col(k) < cols) copy_async16(slot + static_cast<uint32_t>(t + k * threads) * 16u, p + col(k));
+        if (has(k)) copy_async16(slot + static_cast<uint32_t>(lane + k * lanes) * 16u, p + col(k));
     } else {
-      // Words that reach beyond the matrix's first or last element go element by element.
       const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~static_cast<uintptr_t>(15);
       const uintptr_t lo = reinterpret_cast<uintptr_t>(base), hi = lo + ((rows - 1) * ld + cols) * sizeof(T);
-      const int words = static_cast<int>((at - first + cols * sizeof(T) + 15) / 16);
-      for (int i = t; i < words; i += threads) {
+      const int bytes = static_cast<int>(at - first) + segment_bytes;
+#pragma unroll
+      for (int k = 0; k <= kPieces; ++k) {
+        const int i = lane + k * lanes;
+        if ((k == kPieces && lane > 0) || i * 16 >= bytes || segment_bytes == 0) continue;
         const uintptr_t w = first + static_cast<uintptr_t>(i) * 16;
-        if (w >= lo && w + 16 <= hi) {
-          copy_async16(slot + static_cast<uint32_t>(i) * 16u, reinterpret_cast<const void*>(w));
-        } else {
-#pragma unroll 1
-          for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
-            if (w + b < at || w + b >= at + cols * sizeof(T)) continue;
-            const uint32_t d = slot + static_cast<uint32_t>(i) * 16u + b;
-            if (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(d), "r"(*reinterpret_cast<const uint32_t*>(w + b)) : "memory");
-            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(d), "h"(*reinterpret_cast<const uint16_t*>(w + b)) : "memory");
-          }
-        }
+        if (w >= lo && w + 16 <= hi) copy_async16(slot + static_cast<uint32_t>(i) * 16u, reinterpret_cast<const void*>(w));
+        else copy_end(slot + static_cast<uint32_t>(i) * 16u, w, lo, hi);
       }
     }
   }
-  // The thread's elements in units that lie together: pieces, or pairs of single elements.
-  static constexpr int U = kStep > 1 ? kPieces : H, W = H / U;  // units, pairs of each
-  // Where a row's elements start in its slot.
-  __device__ __forceinline__ const uint8_t* row_at(const uint8_t* slot, const void* base, int64_t row, int64_t ld) const {
-    return kStep > 1 ? slot : slot + (reinterpret_cast<uintptr_t>(static_cast<const T*>(base) + row * ld) & 15);
-  }
-  // Unit u of a row that lies in a slot; 0 beyond the row.
-  __device__ __forceinline__ void read(const uint8_t* at, int u, bool in, float2 (&x)[W]) const {
-    if (kStep > 1) {
-      uint4 q = make_uint4(0, 0, 0, 0);
-      if (in && col(u) < cols) q = reinterpret_cast<const uint4*>(at)[t + u * threads];
-      Elem<T>::unpack(q, x);
-    } else {
-      const T* p = reinterpret_cast<const T*>(at);
-      x[0].x = in && col(2 * u) < cols ? Elem<T>::get(p + col(2 * u)) : 0.f;
-      x[0].y = in && col(2 * u + 1) < cols ? Elem<T>::get(p + col(2 * u + 1)) : 0.f;
+  // A word that reaches beyond the matrix's first or last element: the elements in it.
+  static __device__ __noinline__ void copy_end(uint32_t slot, uintptr_t w, uintptr_t lo, uintptr_t hi) {
+#pragma unroll 1
+    for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
+      if (w + b < lo || w + b >= hi) continue;
+      if (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(slot + b), "r"(*reinterpret_cast<const uint32_t*>(w + b)) : "memory");
+      else asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot + b), "h"(*reinterpret_cast<const uint16_t*>(w + b)) : "memory");
     }
   }
-  __device__ __forceinline__ void write(T* row, int u, const float2* x) const {
-    if (kStep > 1) {
-      if (col(u) < cols) *reinterpret_cast<uint4*>(row + col(u)) = Elem<T>::pack(x);
-    } else {
-      if (col(2 * u) < cols) row[col(2 * u)] = Elem<T>::make(x[0].x);
-      if (col(2 * u + 1) < cols) row[col(2 * u + 1)] = Elem<T>::make(x[0].y);
-    }
-  }
-  // Column of element i (of E), and a vector's elements there (`none` beyond the row).
-  __device__ __forceinline__ int element_col(int i) const { return col(i / kStep) + i % kStep; }
-  __device__ __forceinline__ void vector(const void* v, int type, float none, float2 (&x)[H]) const {
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      x[i].x = v && element_col(2 * i) < cols ? load_as(v, type, element_col(2 * i)) : none;
-      x[i].y = v && element_col(2 * i + 1) < cols ? load_as(v, type, element_col(2 * i + 1)) : none;
-    }
+  // Piece k of a row in a slot; 0 beyond the row.
+  __device__ __forceinline__ void read(const uint8_t* slot, int lead, int k, bool in, float2 (&x)[W]) const {
+    uint4 q = make_uint4(0, 0, 0, 0);
+    const uint4* at = reinterpret_cast<const uint4*>(slot) + lane + k * lanes;
+    if (in && has(k)) q = kShifted ? shifted<T>(at[0], at[1], lead) : at[0];
+    Elem<T>::unpack(q, x);
+    if (kShifted && !whole()) clip(k, x);
   }
   // Sets the elements beyond the row to zero.
-  __device__ __forceinline__ void clip(float2 (&x)[H]) const {
+  __device__ __forceinline__ void clip(int k, float2* x) const {
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      if (k * lanes * N + 2 * e >= left) x[e].x = 0.f;
+      if (k * lanes * N + 2 * e + 1 >= left) x[e].y = 0.f;
+    }
+  }
+  // Writes piece k of a row that starts at `row`, in order of k; `before` carries the piece before. All lanes of the warp call it.
+  __device__ __forceinline__ void write(T* row, int k, const float2* x, bool in, uint4& before) const {
+    const uint4 q = Elem<T>::pack(x);
+    if (!kShifted) {
+      if (in && has(k)) *reinterpret_cast<uint4*>(row + segment + col(k)) = q;
+      return;
+    }
+    uint8_t* p = reinterpret_cast<uint8_t*>(row + segment);
+    const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
+    const bool last = lane == lanes - 1;
+    const int from = static_cast<int>(threadIdx.x & 31) + (lane == 0 ? lanes - 1 : -1);
+    uint4 prev;
+    prev.x = __shfl_sync(kFull, last ? before.x : q.x, from);
+    prev.y = __shfl_sync(kFull, last ? before.y : q.y, from);
+    prev.z = __shfl_sync(kFull, last ? before.z : q.z, from);
+    prev.w = __shfl_sync(kFull, last ? before.w : q.w, from);
+    before = q;
+    const int o = 16 * (lane + k * lanes) - lead;  // of the word, relative to the segment
+    if (!in) return;
+    const uint4 w = shifted<T>(prev, q, 16 - lead);
+    if (o >= 0 && o + 16 <= segment_bytes) *reinterpret_cast<uint4*>(p + o) = w;
+    else write_end(p, o, w);
+    if (k == kPieces - 1 && last && lead > 0) write_end(p, o + 16, shifted<T>(q, make_uint4(0, 0, 0, 0), 16 - lead));
+  }
+  // The elements of a word that belong to the segment.
+  __device__ __forceinline__ void write_end(uint8_t* p, int o, uint4 w) const {
+    if (o + 16 <= 0 || o >= segment_bytes) return;
+#pragma unroll 1
+    for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
+      const uint32_t bits = pop_front(w, T());
+      if (o + b >= 0 && o + b < segment_bytes) *reinterpret_cast<typename Elem<T>::Bits*>(p + o + b) = static_cast<typename Elem<T>::Bits>(bits);
+    }
+  }
+  // Column of element i (of 2 H), whether it exists, and a vector's elements there (`none` without a vector).
+  __device__ __forceinline__ int element_col(int i) const { return segment + col(i / N) + i % N; }
+  __device__ __forceinline__ bool has_element(int i) const { return i / N * lanes * N + i % N < left; }
+  __device__ __forceinline__ void vector(const void* v, int type, float none, float2 (&x)[H]) const {
+    if (!v) {
+#pragma unroll
+      for (int i = 0; i < H; ++i) x[i] = make_float2(none, none);
+    } else if (type == MEQ_F32) {  // outside the loops: the loads of all elements are on their way together
+      vector_of(static_cast<const float*>(v), x);
+    } else if (type == MEQ_BF16) {
+      vector_of(static_cast<const __nv_bfloat16*>(v), x);
+    } else {
+      vector_of(static_cast<const __half*>(v), x);
+    }
+  }
+  template <typename V>
+  __device__ __forceinline__ void vector_of(const V* v, float2 (&x)[H]) const {
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-      if (element_col(2 * i) >= cols) x[i].x = 0.f;
-      if (element_col(2 * i + 1) >= cols) x[i].y = 0.f;
+      x[i].x = has_element(2 * i) ? Elem<V>::get(v + element_col(2 * i)) : 0.f;
+      x[i].y = has_element(2 * i + 1) ? Elem<V>::get(v + element_col(2 * i + 1)) : 0.f;
     }
   }
 };
@@ -173,8 +234,7 @@ __device__ __forceinline__ float2 round_pair(float2 x) {
 }
 
 // ------------------------------------------------------------------- host
-// Pieces (and single elements) per thread that the kernels are compiled for.
-constexpr int kWholePieces[] = {1, 2, 3, 4}, kSingles[] = {2, 8, 16, 32};
+constexpr int kMostPieces = 4;  // per thread
 
 template <typename T>
 bool starts_at_16(const void* p, int64_t ld) {
@@ -207,34 +267,36 @@ inline int most_warps(int elements, bool heavy) {
   return elements > 8 ? 20 : 32;
 }
 
-// How rows of `cols` elements are shared out, `step` of them together, with `matrices` copied per row and
-// at most `most` pieces per thread. pieces: per thread, as the kernels are compiled for. False: they are too long.
-inline bool row_shape(int64_t cols, int step, int elem_size, int matrices, bool heavy, const int* compiled, int n_compiled, RowShape* s, int* pieces) {
-  const int64_t units = (cols + step - 1) / step;
-  s->lanes = 32, s->warps = 1;
-  if (units <= 16 * compiled[0]) {
-    *pieces = compiled[0];
+// How rows of `cols` elements, n of them to a piece, are shared out, with `matrices` copied per row. False: they
+// are too long.
+inline bool row_shape(int64_t cols, int n, bool shift, int matrices, bool heavy, RowShape* s, int* pieces) {
+  const int64_t units = (cols + n - 1) / n;
+  s->lanes = 32, s->warps = 1, *pieces = 1;
+  if (units <= 16) {
     s->lanes = 1;
-    while (static_cast<int64_t>(s->lanes) * compiled[0] < units) s->lanes *= 2;
+    while (s->lanes < units) s->lanes *= 2;
   } else {
-    const int most = compiled[n_compiled - 1];
-    const int64_t warps = (units + 32 * most - 1) / (32 * most);
-    if (warps > most_warps(step * most, heavy)) return false;
-    s->warps = static_cast<int>(warps);
-    const int64_t each = (units + 32 * warps - 1) / (32 * warps);
-    for (int i = n_compiled - 1; i >= 0 && compiled[i] >= each; --i) *pieces = compiled[i];
+    // Instructions per row: a warp's pieces, whether they exist or not, and about as many as one piece takes beside them.
+    int64_t least = INT64_MAX;
+    for (int k = kMostPieces; k >= 1; --k) {
+      const int64_t warps = (units + 32 * k - 1) / (32 * k);
+      if (warps > most_warps(n * k, heavy) || warps * (k + 1) >= least) continue;
+      least = warps * (k + 1);
+      s->warps = static_cast<int>(warps), *pieces = k;
+    }
+    if (least == INT64_MAX) return false;
   }
-  s->groups = most_warps(step * *pieces, heavy) / s->warps;
+  s->groups = most_warps(n * *pieces, heavy) / s->warps;
   if (s->warps > 1 && s->groups > 15) s->groups = 15;  // named barriers
-  s->slot_bytes = step > 1 ? s->warps * s->lanes * *pieces * 16 : static_cast<int>((cols * elem_size + 30) / 16 * 16);
-  auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * (32 / s->lanes) * depth * matrices * s->slot_bytes <= kRingBudget; };
+  s->slot_bytes = (s->lanes * *pieces + (shift ? 1 : 0)) * 16;
+  auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes <= kRingBudget; };
   while (s->groups > 1 && !fits(2)) --s->groups;
   if (!fits(2)) return false;
   s->depth = kMostDepth;
   while (!fits(s->depth)) --s->depth;
   return true;
 }
-inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
+inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
 
 // Shapes and launches, in files of their own. False: the rows are too long, nothing was launched.
 bool launch_row_forward(const ForwardArgs& a, int type, int sms, cudaStream_t st, cudaError_t* e);
