@@ -9,29 +9,29 @@ namespace norm {
 namespace {
 
 // kBias: dy is summed over rows too.
-template <int kElements, bool kBias>
+template <int kElements>
 constexpr int threads_of() {
-  return kElements > 16 ? (kBias ? 384 : 512) : kElements > 8 ? 640 : 1024;
+  return kElements > 16 ? 512 : kElements > 8 ? 640 : 1024;
 }
 
 template <typename T, int kPieces, bool kShifted, bool kBias>
-__global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
+__global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
   using P = Place<T, kPieces, kShifted>;
   constexpr int H = P::H, W = P::W;
   pdl_allow_dependents();
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Exchange ex;
   const P p(s, a.cols);
-  const int matrices = a.dh ? 3 : 2, set = 32 / s.lanes;  // rows that the group takes at once
+  const int matrices = a.dh ? 3 : 2, set = kPieces > 1 ? 1 : 32 / s.lanes;  // rows that the group takes at once
   uint8_t* mine = ring + (static_cast<int>(threadIdx.x >> 5) * set + p.sub) * (s.depth * matrices * s.slot_bytes);
   const uint32_t mine32 = smem_u32(mine);
-  const int64_t sets = (a.rows + set - 1) / set, step = static_cast<int64_t>(gridDim.x) * s.groups;
-  const int64_t first = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;
-  int64_t next = first;  // set whose copies start next
+  const uint32_t rows = static_cast<uint32_t>(a.rows), sets = (rows + set - 1) / set, step = gridDim.x * s.groups;
+  const uint32_t first = p.group * gridDim.x + blockIdx.x;
+  uint32_t next = first;  // set whose copies start next
   int put = 0;
   auto copy_next = [&]() {
-    const int64_t row = next * set + p.sub;
-    if (next < sets && row < a.rows) {
+    const uint32_t row = next * set + p.sub;
+    if (next < sets && row < rows) {
       const uint32_t at = mine32 + static_cast<uint32_t>(put * matrices * s.slot_bytes);
       p.copy(at, a.dy, row, a.ld_dy, a.rows, a.cols);
       p.copy(at + s.slot_bytes, a.h, row, a.ld_h, a.rows, a.cols);
@@ -41,10 +41,11 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) 
     next += step;
     if (++put == s.depth) put = 0;
   };
-  auto statistics = [&](int64_t set_at) -> float2 {  // mu and rstd
-    const int64_t row = set_at * set + p.sub;
-    return set_at < sets && row < a.rows ? make_float2(a.mean ? a.mean[row] : 0.f, a.rstd[row]) : make_float2(0.f, 0.f);
+  auto statistics = [&](uint32_t set_at) -> float2 {  // mu and rstd
+    const uint32_t row = set_at * set + p.sub;
+    return set_at < sets && row < rows ? make_float2(a.mean ? a.mean[row] : 0.f, a.rstd[row]) : make_float2(0.f, 0.f);
   };
+  if (s.warps > 1) clear(ex);
   pdl_wait_predecessor();
   for (int i = 0; i < s.depth - 1; ++i) copy_next();
   float2 stat = statistics(first);
@@ -56,9 +57,9 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) 
   for (int k = 0; k < (kBias ? H : 1); ++k) db[k] = make_float2(0.f, 0.f);
   const float per = 1.f / static_cast<float>(a.cols);
   int take = 0, turn = 0;
-  for (int64_t i = first; i < sets; i += step) {
-    const int64_t row = i * set + p.sub;
-    const bool in = row < a.rows;
+  for (uint32_t i = first; i < sets; i += step) {
+    const uint32_t row = i * set + p.sub;
+    const bool in = row < rows;
     const float2 now = stat;
     stat = statistics(i + step);
     copies_wait(s.depth);
@@ -86,10 +87,11 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) 
         c2 = add2(c2, d[e]);
       }
     }
-    const float2 c = row_sum(make_float2(c1.x + c1.y, c2.x + c2.y), s, p.group, p.warp_in, ex, turn);
-    const float2 m1 = make_float2(-c.x * per, -c.x * per), m2 = a.mean ? make_float2(-c.y * per, -c.y * per) : make_float2(0.f, 0.f);
+    float c[2] = {c1.x + c1.y, c2.x + c2.y};
+    row_sum<2, (kPieces > 1)>(c, s, p, ex, turn);
+    const float2 m1 = make_float2(-c[0] * per, -c[0] * per), m2 = a.mean ? make_float2(-c[1] * per, -c[1] * per) : make_float2(0.f, 0.f);
     // dy and h once more from shared memory: kept in registers they would leave no room for the sums.
-    uint4 before = make_uint4(0, 0, 0, 0);
+    typename P::Writer out(static_cast<T*>(a.dx) + P::row_offset(row, a.ld_dx), p, in);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       float2 x[W], d[W];
@@ -105,32 +107,35 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces, kBias>(), 1) 
 #pragma unroll
         for (int e = 0; e < W; ++e) d[e] = add2(d[e], x[e]);
       }
-      p.write(static_cast<T*>(a.dx) + row * a.ld_dx, k, d, in, before);
+      p.write(out, k, d);
     }
+    p.finish(out);
   }
   if (!a.parts) return;
   // The block's groups added up, in shared memory: the ring holds 8 bytes for each of their columns.
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  const int copies = s.groups * set;
+  const int copies = s.groups * set, mine_at = p.group * set + p.sub;
+  const int wide = s.warps * s.lanes * kPieces * P::N;  // columns with those that do not exist
   float* sums = reinterpret_cast<float*>(ring);
-  const int64_t cols = a.cols;
 #pragma unroll
-  for (int k = 0; k < 2 * H; ++k) {
-    const int j = p.element_col(k);
-    if (p.has_element(k)) {
-      sums[(p.group * set + p.sub) * cols + j] = k % 2 ? dw[k / 2].y : dw[k / 2].x;
-      if (kBias) sums[(copies + p.group * set + p.sub) * cols + j] = k % 2 ? db[k / 2].y : db[k / 2].x;
-    }
+  for (int k = 0; k < H; k += 2) {
+    const int j = p.element_col(2 * k);
+    *reinterpret_cast<float4*>(sums + mine_at * wide + j) = make_float4(dw[k].x, dw[k].y, dw[k + 1].x, dw[k + 1].y);
+    if (kBias) *reinterpret_cast<float4*>(sums + (copies + mine_at) * wide + j) = make_float4(db[k].x, db[k].y, db[k + 1].x, db[k + 1].y);
   }
   __syncthreads();
-  for (int64_t j = threadIdx.x; j < (kBias ? 2 : 1) * cols; j += blockDim.x) {
-    const bool second = j >= cols;
-    const int64_t c = second ? j - cols : j;
-    const float* from = sums + (second ? copies * cols : 0) + c;
-    float total = from[0];
-    for (int g = 1; g < copies; ++g) total += from[g * cols];
-    a.parts[((second ? gridDim.x : 0) + blockIdx.x) * cols + c] = total;
+  const int cols = static_cast<int>(a.cols);
+#pragma unroll
+  for (int v = 0; v < (kBias ? 2 : 1); ++v) {
+    float* to = a.parts + (static_cast<int64_t>(v) * gridDim.x + blockIdx.x) * cols;
+    for (int j = static_cast<int>(threadIdx.x); j < cols; j += static_cast<int>(blockDim.x)) {
+      const float* from = sums + v * copies * wide + j;
+      float total = from[0];
+#pragma unroll 4
+      for (int g = 1; g < copies; ++g) total += from[g * wide];
+      to[j] = total;
+    }
   }
 }
 
@@ -146,7 +151,7 @@ template <typename T, bool kShifted, bool kBias>
 bool launch_of(const BackwardArgs& a, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e) {
   RowShape s;
   int pieces = 0;
-  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.dh ? 3 : 2, kBias, &s, &pieces)) return false;
+  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.dh ? 3 : 2, &s, &pieces)) return false;
   const int set = 32 / s.lanes;
   const int64_t sets = (a.rows + set - 1) / set;
   *parts = sets < sms ? sets : sms;

@@ -19,16 +19,16 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Exchange ex;
   const P p(s, a.cols);
-  const int matrices = a.residual ? 2 : 1, set = 32 / s.lanes;  // rows that the group takes at once
+  const int matrices = a.residual ? 2 : 1, set = kPieces > 1 ? 1 : 32 / s.lanes;  // rows that the group takes at once
   uint8_t* mine = ring + (static_cast<int>(threadIdx.x >> 5) * set + p.sub) * (s.depth * matrices * s.slot_bytes);
   const uint32_t mine32 = smem_u32(mine);
-  const int64_t sets = (a.rows + set - 1) / set, step = static_cast<int64_t>(gridDim.x) * s.groups;
-  const int64_t first = static_cast<int64_t>(p.group) * gridDim.x + blockIdx.x;
-  int64_t next = first;  // set whose copies start next
+  const uint32_t rows = static_cast<uint32_t>(a.rows), sets = (rows + set - 1) / set, step = gridDim.x * s.groups;
+  const uint32_t first = p.group * gridDim.x + blockIdx.x;
+  uint32_t next = first;  // set whose copies start next
   int put = 0;
   auto copy_next = [&]() {
-    const int64_t row = next * set + p.sub;
-    if (next < sets && row < a.rows) {
+    const uint32_t row = next * set + p.sub;
+    if (next < sets && row < rows) {
       const uint32_t at = mine32 + static_cast<uint32_t>(put * matrices * s.slot_bytes);
       p.copy(at, a.x, row, a.ld_x, a.rows, a.cols);
       if (a.residual) p.copy(at + s.slot_bytes, a.residual, row, a.ld_residual, a.rows, a.cols);
@@ -37,6 +37,7 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
     next += step;
     if (++put == s.depth) put = 0;
   };
+  if (s.warps > 1) clear(ex);
   pdl_wait_predecessor();
   for (int i = 0; i < s.depth - 1; ++i) copy_next();
   float2 w[H], b[H];
@@ -44,9 +45,9 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
   p.vector(a.bias, a.weight_type, 0.f, b);
   const float per = 1.f / static_cast<float>(a.cols);
   int take = 0, turn = 0;
-  for (int64_t i = first; i < sets; i += step) {
-    const int64_t row = i * set + p.sub;
-    const bool in = row < a.rows;
+  for (uint32_t i = first; i < sets; i += step) {
+    const uint32_t row = i * set + p.sub;
+    const bool in = row < rows;
     copies_wait(s.depth);
     if (kShifted) __syncwarp();  // the other lanes' copies too, and the slot before is free
     copy_next();
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
     if (++take == s.depth) take = 0;
     float2 v[H];
     const int lead = p.lead(a.x, row, a.ld_x), lead_r = p.lead(a.residual, row, a.ld_residual);
-    uint4 before = make_uint4(0, 0, 0, 0);
+    typename P::Writer stream(static_cast<T*>(a.h) + P::row_offset(row, a.ld_h), p, in);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       float2 x[W];
@@ -64,36 +65,41 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
         p.read(at + s.slot_bytes, lead_r, k, in, r);
 #pragma unroll
         for (int e = 0; e < W; ++e) x[e] = round_pair<T>(add2(x[e], r[e]));
-        p.write(static_cast<T*>(a.h) + row * a.ld_h, k, x, in, before);
+        p.write(stream, k, x);
       }
 #pragma unroll
       for (int e = 0; e < W; ++e) v[k * W + e] = x[e];
     }
+    if (a.residual) p.finish(stream);
     float mu = 0.f;
     if (a.mean) {
       float2 sum = v[0];
 #pragma unroll
       for (int k = 1; k < H; ++k) sum = add2(sum, v[k]);
-      mu = row_sum(make_float2(sum.x + sum.y, 0.f), s, p.group, p.warp_in, ex, turn).x * per;
+      float total[1] = {sum.x + sum.y};
+      row_sum<1, (kPieces > 1)>(total, s, p, ex, turn);
+      mu = total[0] * per;
 #pragma unroll
       for (int k = 0; k < H; ++k) v[k] = add2(v[k], make_float2(-mu, -mu));
-      if (!p.whole()) {
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) p.clip(k, v + k * W);
-      }
+      for (int k = 0; k < kPieces; ++k)
+        if (!p.has(k) || (kShifted && p.ends_in(k))) p.clip(k, v + k * W);
     }
     float2 sq = mul2(v[0], v[0]);
 #pragma unroll
     for (int k = 1; k < H; ++k) sq = fma2(v[k], v[k], sq);
-    const float var = row_sum(make_float2(sq.x + sq.y, 0.f), s, p.group, p.warp_in, ex, turn).x * per;
-    const float rstd = inverse_root(var, a.eps);
+    float total[1] = {sq.x + sq.y};
+    row_sum<1, (kPieces > 1)>(total, s, p, ex, turn);
+    const float rstd = inverse_root(total[0] * per, a.eps);
+    typename P::Writer out(static_cast<T*>(a.y) + P::row_offset(row, a.ld_y), p, in);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       float2 y[W];
 #pragma unroll
       for (int e = 0; e < W; ++e) y[e] = fma2(mul2(v[k * W + e], make_float2(rstd, rstd)), w[k * W + e], b[k * W + e]);
-      p.write(static_cast<T*>(a.y) + row * a.ld_y, k, y, in, before);
+      p.write(out, k, y);
     }
+    p.finish(out);
     if (in && p.warp_in == 0 && p.lane == 0) {
       if (a.mean) a.mean[row] = mu;
       a.rstd[row] = rstd;
@@ -116,7 +122,7 @@ template <typename T, bool kShifted>
 bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
   RowShape s;
   int pieces = 0;
-  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.residual ? 2 : 1, false, &s, &pieces)) return false;
+  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.residual ? 2 : 1, &s, &pieces)) return false;
   *e = pieces == 1   ? launch<T, 1, kShifted>(a, s, sms, st)
        : pieces == 2 ? launch<T, 2, kShifted>(a, s, sms, st)
        : pieces == 3 ? launch<T, 3, kShifted>(a, s, sms, st)

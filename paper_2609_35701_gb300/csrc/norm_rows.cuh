@@ -37,9 +37,10 @@ struct RowShape {
   int slot_bytes;  // of one matrix's row, or a warp's part of it
 };
 
-// The partial sums of a block's warps.
+// The partial sums of a block's warps, those of a group in 16-byte words (zeros where it has fewer).
+constexpr int kMostSums = 64;
 struct Exchange {
-  float2 sum[2][kMostWarps];
+  float4 sum[2][2][kMostSums / 4];  // two in turn, of two values
 };
 
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
@@ -53,13 +54,10 @@ __device__ __forceinline__ void copies_wait(int depth) {
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-// Bytes `from` .. `from` + 15 of the 32 bytes of a and b (from: a multiple of the element's size, at most 16).
+// Bytes `from` .. `from` + 15 of the 32 bytes of a and b (from: a multiple of the element's size, below 16).
 template <typename T>
 __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int from) {
   uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  if (from & 16) {
-    return b;
-  }
 #pragma unroll
   for (int i = 0; i < 6; ++i) w[i] = from & 8 ? w[i + 2] : w[i];
 #pragma unroll
@@ -94,15 +92,16 @@ struct Place {
   // Column of piece k's first element, relative to the segment.
   __device__ __forceinline__ int col(int k) const { return (lane + k * lanes) * N; }
   __device__ __forceinline__ bool has(int k) const { return k * lanes * N < left; }
-  // Whether all elements of all pieces exist.
-  __device__ __forceinline__ bool whole() const { return (kPieces - 1) * lanes * N + N <= left; }
-  __device__ __forceinline__ int lead(const void* base, int64_t row, int64_t ld) const {
-    return kShifted ? static_cast<int>(reinterpret_cast<uintptr_t>(static_cast<const T*>(base) + row * ld) & 15) : 0;
+  __device__ __forceinline__ int lead(const void* base, uint32_t row, int64_t ld) const {
+    return kShifted ? static_cast<int>((static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) + row * static_cast<uint32_t>(ld) * sizeof(T)) & 15) : 0;
   }
 
+  // First element of a row, in a 32 x 64 bit product.
+  static __device__ __forceinline__ uint64_t row_offset(uint32_t row, int64_t ld) { return static_cast<uint64_t>(row) * static_cast<uint64_t>(ld); }
+
   // Starts the copies of the warp's columns of a matrix's row into a slot.
-  __device__ __forceinline__ void copy(uint32_t slot, const void* base, int64_t row, int64_t ld, int64_t rows, int64_t cols) const {
-    const T* p = static_cast<const T*>(base) + row * ld + segment;
+  __device__ __forceinline__ void copy(uint32_t slot, const void* base, uint32_t row, int64_t ld, int64_t rows, int64_t cols) const {
+    const T* p = static_cast<const T*>(base) + row_offset(row, ld) + segment;
     if (!kShifted) {
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
@@ -110,18 +109,19 @@ struct Place {
     } else {
       const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~static_cast<uintptr_t>(15);
       const uintptr_t lo = reinterpret_cast<uintptr_t>(base), hi = lo + ((rows - 1) * ld + cols) * sizeof(T);
-      const int bytes = static_cast<int>(at - first) + segment_bytes;
+      const int words = segment_bytes > 0 ? (static_cast<int>(at - first) + segment_bytes + 15) / 16 : 0;
+      const bool inside = first >= lo && first + static_cast<uintptr_t>(words) * 16 <= hi;
+      const uint32_t to = slot + static_cast<uint32_t>(lane) * 16u;
+      const uintptr_t from = first + static_cast<uintptr_t>(lane) * 16;
 #pragma unroll
       for (int k = 0; k <= kPieces; ++k) {
-        const int i = lane + k * lanes;
-        if ((k == kPieces && lane > 0) || i * 16 >= bytes || segment_bytes == 0) continue;
-        const uintptr_t w = first + static_cast<uintptr_t>(i) * 16;
-        if (w >= lo && w + 16 <= hi) copy_async16(slot + static_cast<uint32_t>(i) * 16u, reinterpret_cast<const void*>(w));
-        else copy_end(slot + static_cast<uint32_t>(i) * 16u, w, lo, hi);
+        if ((k == kPieces && lane > 0) || lane + k * lanes >= words) continue;
+        if (inside) copy_async16(to + static_cast<uint32_t>(k * lanes) * 16u, reinterpret_cast<const void*>(from + k * lanes * 16));
+        else copy_end(to + static_cast<uint32_t>(k * lanes) * 16u, from + k * lanes * 16, lo, hi);
       }
     }
   }
-  // A word that reaches beyond the matrix's first or last element: the elements in it.
+  // A word of a row whose words reach beyond the matrix's first or last element: the elements in it.
   static __device__ __noinline__ void copy_end(uint32_t slot, uintptr_t w, uintptr_t lo, uintptr_t hi) {
 #pragma unroll 1
     for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
@@ -136,8 +136,10 @@ struct Place {
     const uint4* at = reinterpret_cast<const uint4*>(slot) + lane + k * lanes;
     if (in && has(k)) q = kShifted ? shifted<T>(at[0], at[1], lead) : at[0];
     Elem<T>::unpack(q, x);
-    if (kShifted && !whole()) clip(k, x);
+    if (kShifted && ends_in(k)) clip(k, x);
   }
+  // Whether the row ends inside piece k.
+  __device__ __forceinline__ bool ends_in(int k) const { return static_cast<unsigned>(left - k * lanes * N - 1) < static_cast<unsigned>(N - 1); }
   // Sets the elements beyond the row to zero.
   __device__ __forceinline__ void clip(int k, float2* x) const {
 #pragma unroll
@@ -146,37 +148,62 @@ struct Place {
       if (k * lanes * N + 2 * e + 1 >= left) x[e].y = 0.f;
     }
   }
-  // Writes piece k of a row that starts at `row`, in order of k; `before` carries the piece before. All lanes of the warp call it.
-  __device__ __forceinline__ void write(T* row, int k, const float2* x, bool in, uint4& before) const {
+  // The pieces of a row on their way to `row`, one after another: all lanes of the warp call write for each k in turn, then finish.
+  struct Writer {
+    uint8_t* p;    // the segment
+    bool in;       // the row exists
+    int lead;
+    uint4 before;  // the piece before
+    uint4 start, end;  // the words in which the segment starts and ends, where this lane holds them
+    __device__ __forceinline__ Writer(T* row, const Place& place, bool in_) : p(reinterpret_cast<uint8_t*>(row + place.segment)), in(in_) {
+      lead = kShifted ? static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15) : 0;
+      before = start = end = make_uint4(0, 0, 0, 0);
+    }
+  };
+  // The word in which the segment ends.
+  __device__ __forceinline__ int end_word(int lead) const { return (segment_bytes + lead) / 16; }
+  __device__ __forceinline__ void write(Writer& w, int k, const float2* x) const {
     const uint4 q = Elem<T>::pack(x);
     if (!kShifted) {
-      if (in && has(k)) *reinterpret_cast<uint4*>(row + segment + col(k)) = q;
+      if (w.in && has(k)) reinterpret_cast<uint4*>(w.p)[lane + k * lanes] = q;
       return;
     }
-    uint8_t* p = reinterpret_cast<uint8_t*>(row + segment);
-    const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
     const bool last = lane == lanes - 1;
-    const int from = static_cast<int>(threadIdx.x & 31) + (lane == 0 ? lanes - 1 : -1);
+    const int from = static_cast<int>(threadIdx.x & 31) + (lane == 0 ? lanes - 1 : -1), i = lane + k * lanes;
     uint4 prev;
-    prev.x = __shfl_sync(kFull, last ? before.x : q.x, from);
-    prev.y = __shfl_sync(kFull, last ? before.y : q.y, from);
-    prev.z = __shfl_sync(kFull, last ? before.z : q.z, from);
-    prev.w = __shfl_sync(kFull, last ? before.w : q.w, from);
-    before = q;
-    const int o = 16 * (lane + k * lanes) - lead;  // of the word, relative to the segment
-    if (!in) return;
-    const uint4 w = shifted<T>(prev, q, 16 - lead);
-    if (o >= 0 && o + 16 <= segment_bytes) *reinterpret_cast<uint4*>(p + o) = w;
-    else write_end(p, o, w);
-    if (k == kPieces - 1 && last && lead > 0) write_end(p, o + 16, shifted<T>(q, make_uint4(0, 0, 0, 0), 16 - lead));
+    prev.x = __shfl_sync(kFull, last ? w.before.x : q.x, from);
+    prev.y = __shfl_sync(kFull, last ? w.before.y : q.y, from);
+    prev.z = __shfl_sync(kFull, last ? w.before.z : q.z, from);
+    prev.w = __shfl_sync(kFull, last ? w.before.w : q.w, from);
+    const uint4 word = w.lead ? shifted<T>(prev, q, 16 - w.lead) : q;
+    w.before = q;
+    if (i == end_word(w.lead)) w.end = word;
+    if (i == 0) w.start = word;
+    const int o = 16 * i - w.lead;  // of the word, relative to the segment
+    if (w.in && o >= 0 && o + 16 <= segment_bytes) *reinterpret_cast<uint4*>(w.p + o) = word;
   }
-  // The elements of a word that belong to the segment.
-  __device__ __forceinline__ void write_end(uint8_t* p, int o, uint4 w) const {
-    if (o + 16 <= 0 || o >= segment_bytes) return;
+  // The elements of the words in which the segment starts and ends, a lane each.
+  __device__ __forceinline__ void finish(Writer& w) const {
+    if (!kShifted) return;
+    const int base = static_cast<int>(threadIdx.x & 31) & ~(lanes - 1), i = end_word(w.lead);
+    // rows of one warp may start at different places: all lanes make both calls
+    write_word(w, w.start, base, -w.lead, w.lead > 0);
+    if (i == kPieces * lanes && lane == lanes - 1) w.end = shifted<T>(w.before, make_uint4(0, 0, 0, 0), (16 - w.lead) & 15);
+    write_word(w, w.end, base + (i < kPieces * lanes ? i & (lanes - 1) : lanes - 1), 16 * i - w.lead, i > 0 || w.lead == 0);
+  }
+  // Those elements of lane `from`'s word, o bytes into the segment, that belong to the segment.
+  __device__ __forceinline__ void write_word(const Writer& w, uint4 word, int from, int o, bool on) const {
+    word.x = __shfl_sync(kFull, word.x, from);
+    word.y = __shfl_sync(kFull, word.y, from);
+    word.z = __shfl_sync(kFull, word.z, from);
+    word.w = __shfl_sync(kFull, word.w, from);
 #pragma unroll 1
-    for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
-      const uint32_t bits = pop_front(w, T());
-      if (o + b >= 0 && o + b < segment_bytes) *reinterpret_cast<typename Elem<T>::Bits*>(p + o + b) = static_cast<typename Elem<T>::Bits>(bits);
+    for (int e = lane; e < N; e += lanes) {
+      const int b = o + e * static_cast<int>(sizeof(T));
+      if (!w.in || !on || b < 0 || b >= segment_bytes) continue;
+      const int at = e * static_cast<int>(sizeof(T)) / 4;
+      const uint32_t pair = at & 2 ? (at & 1 ? word.w : word.z) : (at & 1 ? word.y : word.x);
+      *reinterpret_cast<typename Elem<T>::Bits*>(w.p + b) = static_cast<typename Elem<T>::Bits>(sizeof(T) == 2 && (e & 1) ? pair >> 16 : pair);
     }
   }
   // Column of element i (of 2 H), whether it exists, and a vector's elements there (`none` without a vector).
@@ -196,6 +223,26 @@ struct Place {
   }
   template <typename V>
   __device__ __forceinline__ void vector_of(const V* v, float2 (&x)[H]) const {
+    constexpr int kLoads = N / Elem<V>::N > 0 ? N / Elem<V>::N : 1;  // 16-byte loads per piece
+    if (N >= Elem<V>::N && (reinterpret_cast<uintptr_t>(v) & 15) == 0) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+          uint4 q = make_uint4(0, 0, 0, 0);
+          const int j = k * lanes * N + l * Elem<V>::N;
+          float2* y = x + k * W + l * Elem<V>::N / 2;
+          if (j + Elem<V>::N <= left) q = *reinterpret_cast<const uint4*>(v + segment + col(k) + l * Elem<V>::N);
+          Elem<V>::unpack(q, y);
+          if (j < left && j + Elem<V>::N > left) {
+#pragma unroll
+            for (int e = 0; e < Elem<V>::N; ++e)
+              if (j + e < left) (e % 2 ? y[e / 2].y : y[e / 2].x) = Elem<V>::get(v + segment + col(k) + l * Elem<V>::N + e);
+          }
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < H; ++i) {
       x[i].x = has_element(2 * i) ? Elem<V>::get(v + element_col(2 * i)) : 0.f;
@@ -209,21 +256,44 @@ __device__ __forceinline__ void group_barrier(const RowShape& s, int group) {
   else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * s.warps) : "memory");
 }
 
-// Two sums over a row's threads, for each of them, in a fixed order. `turn`
+__device__ __forceinline__ void clear(Exchange& ex) {
+  float* p = reinterpret_cast<float*>(&ex);
+  for (int i = static_cast<int>(threadIdx.x); i < 4 * kMostSums; i += static_cast<int>(blockDim.x)) p[i] = 0.f;
+  __syncthreads();
+}
+// kValues sums over a row's threads, for each of them, in a fixed order. `turn`
 // alternates between calls: a warp may be one call ahead of its group.
-__device__ __forceinline__ float2 row_sum(float2 v, const RowShape& s, int group, int warp_in, Exchange& ex, int& turn) {
-  for (int o = s.lanes >> 1; o > 0; o >>= 1) {
-    v.x += __shfl_xor_sync(kFull, v.x, o);
-    v.y += __shfl_xor_sync(kFull, v.y, o);
+template <int kValues, bool kWarp, typename P>
+__device__ __forceinline__ void row_sum(float (&v)[kValues], const RowShape& s, const P& p, Exchange& ex, int& turn) {
+  if (kWarp) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) v[i] += __shfl_xor_sync(kFull, v[i], o);
+    }
+  } else {
+    for (int o = s.lanes >> 1; o > 0; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) v[i] += __shfl_xor_sync(kFull, v[i], o);
+    }
   }
-  if (s.warps == 1) return v;
-  float2* sum = ex.sum[turn] + group * s.warps;
-  if ((threadIdx.x & 31) == 0) sum[warp_in] = v;
-  group_barrier(s, group);
-  v = sum[0];
-  for (int w = 1; w < s.warps; ++w) v = add2(v, sum[w]);
+  if (s.warps == 1) return;
+  const int words = (s.warps + 3) / 4;
+#pragma unroll
+  for (int i = 0; i < kValues; ++i)
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<float*>(ex.sum[turn][i] + p.group * words)[p.warp_in] = v[i];
+  group_barrier(s, p.group);
+#pragma unroll
+  for (int i = 0; i < kValues; ++i) {
+    const float4* q = ex.sum[turn][i] + p.group * words;
+    float4 t = q[0];
+    for (int w = 1; w < words; ++w) {
+      const float4 u = q[w];
+      t.x += u.x, t.y += u.y, t.z += u.z, t.w += u.w;
+    }
+    v[i] = (t.x + t.y) + (t.z + t.w);
+  }
   turn ^= 1;
-  return v;
 }
 
 // Both rounded to T and widened again.
@@ -262,14 +332,11 @@ cudaError_t allow_ring(F* kernel) {
 }
 
 // Warps of a block, by the registers that a thread's elements leave.
-inline int most_warps(int elements, bool heavy) {
-  if (elements > 16) return heavy ? 12 : 16;
-  return elements > 8 ? 20 : 32;
-}
+inline int most_warps(int elements) { return elements > 16 ? 16 : elements > 8 ? 20 : 32; }
 
 // How rows of `cols` elements, n of them to a piece, are shared out, with `matrices` copied per row. False: they
 // are too long.
-inline bool row_shape(int64_t cols, int n, bool shift, int matrices, bool heavy, RowShape* s, int* pieces) {
+inline bool row_shape(int64_t cols, int n, bool shift, int matrices, RowShape* s, int* pieces) {
   const int64_t units = (cols + n - 1) / n;
   s->lanes = 32, s->warps = 1, *pieces = 1;
   if (units <= 16) {
@@ -280,13 +347,15 @@ inline bool row_shape(int64_t cols, int n, bool shift, int matrices, bool heavy,
     int64_t least = INT64_MAX;
     for (int k = kMostPieces; k >= 1; --k) {
       const int64_t warps = (units + 32 * k - 1) / (32 * k);
-      if (warps > most_warps(n * k, heavy) || warps * (k + 1) >= least) continue;
+      // shifting takes registers: four pieces of 16-bit elements spill 100 of them
+      if (shift && n * k > 24 && units <= 32 * 3 * most_warps(n * 3)) continue;
+      if (warps > most_warps(n * k) || warps * (k + 1) >= least) continue;
       least = warps * (k + 1);
       s->warps = static_cast<int>(warps), *pieces = k;
     }
     if (least == INT64_MAX) return false;
   }
-  s->groups = most_warps(n * *pieces, heavy) / s->warps;
+  s->groups = most_warps(n * *pieces) / s->warps;
   if (s->warps > 1 && s->groups > 15) s->groups = 15;  // named barriers
   s->slot_bytes = (s->lanes * *pieces + (shift ? 1 : 0)) * 16;
   auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes <= kRingBudget; };

@@ -24,7 +24,7 @@ constexpr int kWideWarps = kWideThreads / 32;
 constexpr int kTileCols = 256;        // columns of a block of the wide rows' gradient
 constexpr int64_t kMostParts = 192;   // partial sums of a column, at most
 constexpr int64_t kPartFloats = kMostParts * 16384;
-constexpr int kFoldSlices = 8;
+constexpr int kFoldSlices = 32;
 
 // The sum of a block's values, for every thread; sh is free again after the next barrier.
 __device__ __forceinline__ float block_sum(float x, float* sh) {
@@ -134,26 +134,36 @@ __global__ void __launch_bounds__(kTileCols) wide_backward_kernel(const Backward
   a.parts[(static_cast<int64_t>(gridDim.y) + blockIdx.y) * a.cols + j] = db;
 }
 
-// dw and db (blockIdx.y) from the partial sums, 32 columns per block, in slices of the parts.
+// dw and db (blockIdx.y) from the partial sums, 32 columns per block. A warp takes
+// every 32nd part, at most 6 of them, all on their way at once: 4096 columns of
+// 152 parts take @ us, most of it a launch and two trips to L2.
 __global__ void __launch_bounds__(32 * kFoldSlices) fold_parts_kernel(const float* parts, int64_t n, int64_t cols, void* dw, void* db, int type) {
   pdl_allow_dependents();
-  pdl_wait_predecessor();
-  __shared__ float sh[kFoldSlices][32];
+  __shared__ float sh[kFoldSlices][33];
   const int lane = static_cast<int>(threadIdx.x & 31), slice = static_cast<int>(threadIdx.x >> 5);
   const int64_t j = static_cast<int64_t>(blockIdx.x) * 32 + lane;
   void* out = blockIdx.y == 0 ? dw : db;
-  if (!out) return;
   const float* p = parts + static_cast<int64_t>(blockIdx.y) * n * cols + j;
-  float s = 0.f;
-  if (j < cols)
-    for (int64_t i = slice; i < n; i += kFoldSlices) s += p[i * cols];
+  pdl_wait_predecessor();
+  if (!out) return;
+  constexpr int kEach = static_cast<int>((kMostParts + kFoldSlices - 1) / kFoldSlices);
+  float x[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int64_t i = slice + k * kFoldSlices;
+    x[k] = i < n && j < cols ? p[i * cols] : 0.f;
+  }
+  float s = x[0];
+#pragma unroll
+  for (int k = 1; k < kEach; ++k) s += x[k];
   sh[slice][lane] = s;
   __syncthreads();
-  if (slice == 0 && j < cols) {
+  // warp w adds up column w: lane l's slice is l
+  s = sh[lane][slice];
 #pragma unroll
-    for (int i = 1; i < kFoldSlices; ++i) s += sh[i][lane];
-    store_as(out, type, j, s);
-  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + slice;
+  if (lane == 0 && c < cols) store_as(out, type, c, s);
 }
 
 // ------------------------------------------------------------------- host

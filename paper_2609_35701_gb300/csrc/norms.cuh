@@ -49,10 +49,13 @@ __device__ __forceinline__ void store_as(void* p, int type, int64_t i, float x) 
   else static_cast<__half*>(p)[i] = __float2half_rn(x);
 }
 
-// 1 / sqrt(var + eps), NaN where the sum of squares was not finite: a root of an
-// infinity would make the row 0.
+// 1 / sqrt(var + eps) (an approximation and a Newton step: within 2^-24 or so),
+// NaN where the sum of squares was not finite: a root of an infinity would make
+// the row 0.
 __device__ __forceinline__ float inverse_root(float var, float eps) {
-  return var <= FLT_MAX ? 1.f / sqrtf(var + eps) : __int_as_float(0x7fc00000);
+  const float x = var + eps, r = rsqrtf(x);
+  const float e = fmaf(-x * r, r, 1.f);
+  return var <= FLT_MAX && x <= FLT_MAX ? fmaf(0.5f * r, e, r) : __int_as_float(0x7fc00000);
 }
 
 }  // namespace norm
