@@ -11,19 +11,20 @@ constexpr int threads_of() {
   return Elem<T>::N * kPieces > 16 ? 512 : Elem<T>::N * kPieces > 8 ? 640 : 1024;
 }
 
-template <typename T, int kPieces, bool kShifted>
+template <typename T, int kPieces, bool kOffset>
 __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kernel(const __grid_constant__ ForwardArgs a, const RowShape s) {
-  using P = Place<T, kPieces, kShifted>;
+  using P = Place<T, kPieces, kOffset>;
   constexpr int H = P::H, W = P::W;
   pdl_allow_dependents();
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ Exchange ex;
-  const P p(s, a.cols);
+  P p(s);
   const int matrices = a.residual ? 2 : 1, set = kPieces > 1 ? 1 : 32 / s.lanes;  // rows that the group takes at once
   uint8_t* mine = ring + (static_cast<int>(threadIdx.x >> 5) * set + p.sub) * (s.depth * matrices * s.slot_bytes);
   const uint32_t mine32 = smem_u32(mine);
   const uint32_t rows = static_cast<uint32_t>(a.rows), sets = (rows + set - 1) / set, step = gridDim.x * s.groups;
   const uint32_t first = p.group * gridDim.x + blockIdx.x;
+  p.set(a.x, first * set + p.sub, a.ld_x, a.cols);
   uint32_t next = first;  // set whose copies start next
   int put = 0;
   auto copy_next = [&]() {
@@ -49,28 +50,25 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
     const uint32_t row = i * set + p.sub;
     const bool in = row < rows;
     copies_wait(s.depth);
-    if (kShifted) __syncwarp();  // the other lanes' copies too, and the slot before is free
     copy_next();
     const uint8_t* at = mine + take * matrices * s.slot_bytes;
     if (++take == s.depth) take = 0;
     float2 v[H];
-    const int lead = p.lead(a.x, row, a.ld_x), lead_r = p.lead(a.residual, row, a.ld_residual);
-    typename P::Writer stream(static_cast<T*>(a.h) + P::row_offset(row, a.ld_h), p, in);
+    T* h = p.at(a.h, row, a.ld_h);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       float2 x[W];
-      p.read(at, lead, k, in, x);
+      p.read(at, k, in, x);
       if (a.residual) {
         float2 r[W];
-        p.read(at + s.slot_bytes, lead_r, k, in, r);
+        p.read(at + s.slot_bytes, k, in, r);
 #pragma unroll
         for (int e = 0; e < W; ++e) x[e] = round_pair<T>(add2(x[e], r[e]));
-        p.write(stream, k, x);
+        if (in) p.write(h, k, x);
       }
 #pragma unroll
       for (int e = 0; e < W; ++e) v[k * W + e] = x[e];
     }
-    if (a.residual) p.finish(stream);
     float mu = 0.f;
     if (a.mean) {
       float2 sum = v[0];
@@ -83,7 +81,7 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
       for (int k = 0; k < H; ++k) v[k] = add2(v[k], make_float2(-mu, -mu));
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
-        if (!p.has(k) || (kShifted && p.ends_in(k))) p.clip(k, v + k * W);
+        if (!p.has(k) || p.part(k)) p.clip(k, v + k * W);
     }
     float2 sq = mul2(v[0], v[0]);
 #pragma unroll
@@ -91,49 +89,50 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
     float total[1] = {sq.x + sq.y};
     row_sum<1, (kPieces > 1)>(total, s, p, ex, turn);
     const float rstd = inverse_root(total[0] * per, a.eps);
-    typename P::Writer out(static_cast<T*>(a.y) + P::row_offset(row, a.ld_y), p, in);
+    if (!in) continue;
+    T* y_row = p.at(a.y, row, a.ld_y);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       float2 y[W];
 #pragma unroll
       for (int e = 0; e < W; ++e) y[e] = fma2(mul2(v[k * W + e], make_float2(rstd, rstd)), w[k * W + e], b[k * W + e]);
-      p.write(out, k, y);
+      p.write(y_row, k, y);
     }
-    p.finish(out);
-    if (in && p.warp_in == 0 && p.lane == 0) {
+    if (p.warp_in == 0 && p.lane == 0) {
       if (a.mean) a.mean[row] = mu;
       a.rstd[row] = rstd;
     }
   }
 }
 
-template <typename T, int kPieces, bool kShifted>
+template <typename T, int kPieces, bool kOffset>
 cudaError_t launch(const ForwardArgs& a, const RowShape& s, int sms, cudaStream_t st) {
   const int set = 32 / s.lanes;
   const int64_t sets = (a.rows + set - 1) / set;
-  auto* kernel = row_forward_kernel<T, kPieces, kShifted>;
+  auto* kernel = row_forward_kernel<T, kPieces, kOffset>;
   const cudaError_t e = allow_ring(kernel);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(sets < sms ? sets : sms)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.residual ? 2 : 1),
+  return launch_pdl(kernel, dim3(blocks_for(sets, sms, kOffset)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.residual ? 2 : 1),
                     st, 1, a, s);
 }
 
-template <typename T, bool kShifted>
+template <typename T, bool kOffset>
 bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
   RowShape s;
   int pieces = 0;
-  if (!row_shape(a.cols, Elem<T>::N, kShifted, a.residual ? 2 : 1, &s, &pieces)) return false;
-  *e = pieces == 1   ? launch<T, 1, kShifted>(a, s, sms, st)
-       : pieces == 2 ? launch<T, 2, kShifted>(a, s, sms, st)
-       : pieces == 3 ? launch<T, 3, kShifted>(a, s, sms, st)
-                     : launch<T, 4, kShifted>(a, s, sms, st);
+  if (!row_shape(a.cols, Elem<T>::N, kOffset, a.residual ? 2 : 1, &s, &pieces)) return false;
+  *e = pieces == 1   ? launch<T, 1, kOffset>(a, s, sms, st)
+       : pieces == 2 ? launch<T, 2, kOffset>(a, s, sms, st)
+       : pieces == 3 ? launch<T, 3, kOffset>(a, s, sms, st)
+                     : launch<T, 4, kOffset>(a, s, sms, st);
   return true;
 }
 template <typename T>
 bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
-  const bool aligned = a.cols % Elem<T>::N == 0 && starts_at_16<T>(a.x, a.ld_x) && starts_at_16<T>(a.y, a.ld_y) &&
-                       starts_at_16<T>(a.residual, a.ld_residual) && starts_at_16<T>(a.h, a.ld_h);
-  return aligned ? launch_of<T, false>(a, sms, st, e) : launch_of<T, true>(a, sms, st, e);
+  Starts<T> starts;
+  starts.add(a.x, a.ld_x, a.rows), starts.add(a.y, a.ld_y, a.rows), starts.add(a.residual, a.ld_residual, a.rows), starts.add(a.h, a.ld_h, a.rows);
+  if (!starts.alike) return false;
+  return starts.offset || a.cols % Elem<T>::N ? launch_of<T, true>(a, sms, st, e) : launch_of<T, false>(a, sms, st, e);
 }
 
 }  // namespace

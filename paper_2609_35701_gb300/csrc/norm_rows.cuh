@@ -8,11 +8,15 @@
 //
 // Rows are copied into a ring of slots (cp.async) `depth` - 1 rows ahead, which
 // keeps enough bytes on their way whatever the registers leave of the
-// occupancy. Where every row starts at 16 bytes a thread copies the pieces that
-// it reads itself, and no thread waits for another. Else (kShifted) a warp copies
-// the 16-byte words that hold its columns, a lane's piece is shifted out of two
-// of them, and pieces are shifted back into words, with the neighbour lane's, to
-// be stored: nothing but the ends of a warp's columns goes element by element.
+// occupancy; a thread copies the pieces that it reads itself, and no thread waits
+// for another.
+//
+// Rows that start elsewhere in their 16 bytes (kOffset): the grid is a multiple of
+// 8 blocks, so the rows of one thread all start at the same place in them, and its
+// pieces are cut at 16-byte boundaries once for all rows. Only a row's first and
+// last piece may be a part, which is stored element by element. (Pieces cut from
+// the row's start, shifted into place on the way in and out, took 2 to 3 times the
+// time: 16384 x 2047 bf16 @ -> @ us.)
 #pragma once
 
 #include <map>
@@ -54,161 +58,98 @@ __device__ __forceinline__ void copies_wait(int depth) {
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-// Bytes `from` .. `from` + 15 of the 32 bytes of a and b (from: a multiple of the element's size, below 16).
-template <typename T>
-__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int from) {
-  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int i = 0; i < 6; ++i) w[i] = from & 8 ? w[i + 2] : w[i];
-#pragma unroll
-  for (int i = 0; i < 5; ++i) w[i] = from & 4 ? w[i + 1] : w[i];
-  if (sizeof(T) == 2) {
-    const int bits = (from & 3) * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// A thread's place in its row.
-template <typename T, int kPieces, bool kShifted>
+// A thread's place in its rows.
+template <typename T, int kPieces, bool kOffset>
 struct Place {
   static constexpr int N = Elem<T>::N, H = kPieces * N / 2, W = N / 2;  // pairs of elements: of a thread, of a piece
   int lanes, lane, group, sub, warp_in;
-  int left;  // columns from the thread's first one to the row's end (negative: it has none)
-  int segment, segment_bytes;  // the warp's first column, and the bytes of its columns
-  __device__ __forceinline__ Place(const RowShape& s, int64_t cols) {
+  int lead;   // elements of the rows' first 16 bytes that precede them
+  int begin;  // column of the thread's first element (-lead for the first thread's)
+  int left;   // columns from there to the row's end (negative: it has none)
+  __device__ __forceinline__ explicit Place(const RowShape& s) {
     const int warp = static_cast<int>(threadIdx.x >> 5);
     lanes = kPieces > 1 ? 32 : s.lanes;
     lane = static_cast<int>(threadIdx.x & 31) & (lanes - 1);
     sub = static_cast<int>(threadIdx.x & 31) / lanes;
     group = warp / s.warps;
     warp_in = warp - group * s.warps;
-    segment = warp_in * 32 * kPieces * N;
-    const int rest = static_cast<int>(cols) - segment;
-    left = rest - lane * N;
-    segment_bytes = max(0, min(rest, lanes * kPieces * N)) * static_cast<int>(sizeof(T));
   }
-  // Column of piece k's first element, relative to the segment.
-  __device__ __forceinline__ int col(int k) const { return (lane + k * lanes) * N; }
-  __device__ __forceinline__ bool has(int k) const { return k * lanes * N < left; }
-  __device__ __forceinline__ int lead(const void* base, uint32_t row, int64_t ld) const {
-    return kShifted ? static_cast<int>((static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) + row * static_cast<uint32_t>(ld) * sizeof(T)) & 15) : 0;
+  // `row`: any of the thread's rows.
+  __device__ __forceinline__ void set(const void* base, uint32_t row, int64_t ld, int64_t cols) {
+    const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) + row * static_cast<uint32_t>(ld) * static_cast<uint32_t>(sizeof(T));
+    lead = kOffset ? static_cast<int>((at & 15) / sizeof(T)) : 0;
+    begin = (warp_in * 32 * kPieces + lane) * N - lead;
+    left = static_cast<int>(cols) - begin;
+  }
+  // Column of piece k's first element, from `begin`.
+  __device__ __forceinline__ int col(int k) const { return k * lanes * N; }
+  __device__ __forceinline__ bool has(int k) const { return col(k) < left; }
+  // Whether the row starts or ends inside piece k.
+  __device__ __forceinline__ bool part(int k) const {
+    return kOffset && ((k == 0 && begin < 0) || static_cast<unsigned>(left - col(k) - 1) < static_cast<unsigned>(N - 1));
+  }
+  __device__ __forceinline__ bool exists(int k, int e) const { return (!kOffset || k > 0 || begin + e >= 0) && col(k) + e < left; }
+  // The thread's first element of a row.
+  __device__ __forceinline__ T* at(const void* base, uint32_t row, int64_t ld) const {
+    return const_cast<T*>(static_cast<const T*>(base)) + (static_cast<int64_t>(static_cast<uint64_t>(row) * static_cast<uint64_t>(ld)) + begin);
   }
 
-  // First element of a row, in a 32 x 64 bit product.
-  static __device__ __forceinline__ uint64_t row_offset(uint32_t row, int64_t ld) { return static_cast<uint64_t>(row) * static_cast<uint64_t>(ld); }
-
-  // Starts the copies of the warp's columns of a matrix's row into a slot.
+  // Starts the copies of the thread's pieces of a matrix's row into a slot.
   __device__ __forceinline__ void copy(uint32_t slot, const void* base, uint32_t row, int64_t ld, int64_t rows, int64_t cols) const {
-    const T* p = static_cast<const T*>(base) + row_offset(row, ld) + segment;
-    if (!kShifted) {
+    const T* p = at(base, row, ld);
+    slot += static_cast<uint32_t>(lane) * 16u;
 #pragma unroll
-      for (int k = 0; k < kPieces; ++k)
-        if (has(k)) copy_async16(slot + static_cast<uint32_t>(lane + k * lanes) * 16u, p + col(k));
-    } else {
-      const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~static_cast<uintptr_t>(15);
-      const uintptr_t lo = reinterpret_cast<uintptr_t>(base), hi = lo + ((rows - 1) * ld + cols) * sizeof(T);
-      const int words = segment_bytes > 0 ? (static_cast<int>(at - first) + segment_bytes + 15) / 16 : 0;
-      const bool inside = first >= lo && first + static_cast<uintptr_t>(words) * 16 <= hi;
-      const uint32_t to = slot + static_cast<uint32_t>(lane) * 16u;
-      const uintptr_t from = first + static_cast<uintptr_t>(lane) * 16;
-#pragma unroll
-      for (int k = 0; k <= kPieces; ++k) {
-        if ((k == kPieces && lane > 0) || lane + k * lanes >= words) continue;
-        if (inside) copy_async16(to + static_cast<uint32_t>(k * lanes) * 16u, reinterpret_cast<const void*>(from + k * lanes * 16));
-        else copy_end(to + static_cast<uint32_t>(k * lanes) * 16u, from + k * lanes * 16, lo, hi);
-      }
+    for (int k = 0; k < kPieces; ++k) {
+      if (!has(k)) continue;
+      if (part(k)) copy_part(slot + static_cast<uint32_t>(k * lanes) * 16u, p + col(k), base, ld, rows, cols);
+      else copy_async16(slot + static_cast<uint32_t>(k * lanes) * 16u, p + col(k));
     }
   }
-  // A word of a row whose words reach beyond the matrix's first or last element: the elements in it.
-  static __device__ __noinline__ void copy_end(uint32_t slot, uintptr_t w, uintptr_t lo, uintptr_t hi) {
+  // 16 bytes that belong to the row in part: element by element where they reach beyond the matrix.
+  static __device__ __noinline__ void copy_part(uint32_t slot, const T* p, const void* base, int64_t ld, int64_t rows, int64_t cols) {
+    const T *lo = static_cast<const T*>(base), *hi = lo + ((rows - 1) * ld + cols);
+    if (p >= lo && p + N <= hi) {
+      copy_async16(slot, p);
+      return;
+    }
 #pragma unroll 1
-    for (int b = 0; b < 16; b += static_cast<int>(sizeof(T))) {
-      if (w + b < lo || w + b >= hi) continue;
-      if (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(slot + b), "r"(*reinterpret_cast<const uint32_t*>(w + b)) : "memory");
-      else asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot + b), "h"(*reinterpret_cast<const uint16_t*>(w + b)) : "memory");
+    for (int e = 0; e < N; ++e) {
+      if (p + e < lo || p + e >= hi) continue;
+      const uint32_t bits = *reinterpret_cast<const typename Elem<T>::Bits*>(p + e);
+      if (sizeof(T) == 4) asm volatile("st.shared.u32 [%0], %1;" ::"r"(slot + 4 * e), "r"(bits) : "memory");
+      else asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot + 2 * e), "h"(static_cast<uint16_t>(bits)) : "memory");
     }
   }
   // Piece k of a row in a slot; 0 beyond the row.
-  __device__ __forceinline__ void read(const uint8_t* slot, int lead, int k, bool in, float2 (&x)[W]) const {
+  __device__ __forceinline__ void read(const uint8_t* slot, int k, bool in, float2 (&x)[W]) const {
     uint4 q = make_uint4(0, 0, 0, 0);
-    const uint4* at = reinterpret_cast<const uint4*>(slot) + lane + k * lanes;
-    if (in && has(k)) q = kShifted ? shifted<T>(at[0], at[1], lead) : at[0];
+    if (in && has(k)) q = reinterpret_cast<const uint4*>(slot)[lane + k * lanes];
     Elem<T>::unpack(q, x);
-    if (kShifted && ends_in(k)) clip(k, x);
+    if (part(k)) clip(k, x);
   }
-  // Whether the row ends inside piece k.
-  __device__ __forceinline__ bool ends_in(int k) const { return static_cast<unsigned>(left - k * lanes * N - 1) < static_cast<unsigned>(N - 1); }
   // Sets the elements beyond the row to zero.
   __device__ __forceinline__ void clip(int k, float2* x) const {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
-      if (k * lanes * N + 2 * e >= left) x[e].x = 0.f;
-      if (k * lanes * N + 2 * e + 1 >= left) x[e].y = 0.f;
+      if (!exists(k, 2 * e)) x[e].x = 0.f;
+      if (!exists(k, 2 * e + 1)) x[e].y = 0.f;
     }
   }
-  // The pieces of a row on their way to `row`, one after another: all lanes of the warp call write for each k in turn, then finish.
-  struct Writer {
-    uint8_t* p;    // the segment
-    bool in;       // the row exists
-    int lead;
-    uint4 before;  // the piece before
-    uint4 start, end;  // the words in which the segment starts and ends, where this lane holds them
-    __device__ __forceinline__ Writer(T* row, const Place& place, bool in_) : p(reinterpret_cast<uint8_t*>(row + place.segment)), in(in_) {
-      lead = kShifted ? static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15) : 0;
-      before = start = end = make_uint4(0, 0, 0, 0);
-    }
-  };
-  // The word in which the segment ends.
-  __device__ __forceinline__ int end_word(int lead) const { return (segment_bytes + lead) / 16; }
-  __device__ __forceinline__ void write(Writer& w, int k, const float2* x) const {
+  // Writes piece k; row: the thread's first element.
+  __device__ __forceinline__ void write(T* row, int k, const float2* x) const {
+    if (!has(k)) return;
     const uint4 q = Elem<T>::pack(x);
-    if (!kShifted) {
-      if (w.in && has(k)) reinterpret_cast<uint4*>(w.p)[lane + k * lanes] = q;
+    if (!part(k)) {
+      *reinterpret_cast<uint4*>(row + col(k)) = q;
       return;
     }
-    const bool last = lane == lanes - 1;
-    const int from = static_cast<int>(threadIdx.x & 31) + (lane == 0 ? lanes - 1 : -1), i = lane + k * lanes;
-    uint4 prev;
-    prev.x = __shfl_sync(kFull, last ? w.before.x : q.x, from);
-    prev.y = __shfl_sync(kFull, last ? w.before.y : q.y, from);
-    prev.z = __shfl_sync(kFull, last ? w.before.z : q.z, from);
-    prev.w = __shfl_sync(kFull, last ? w.before.w : q.w, from);
-    const uint4 word = w.lead ? shifted<T>(prev, q, 16 - w.lead) : q;
-    w.before = q;
-    if (i == end_word(w.lead)) w.end = word;
-    if (i == 0) w.start = word;
-    const int o = 16 * i - w.lead;  // of the word, relative to the segment
-    if (w.in && o >= 0 && o + 16 <= segment_bytes) *reinterpret_cast<uint4*>(w.p + o) = word;
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    using Bits = typename Elem<T>::Bits;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (exists(k, e)) reinterpret_cast<Bits*>(row)[col(k) + e] = static_cast<Bits>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (e % 2 * 16));
   }
-  // The elements of the words in which the segment starts and ends, a lane each.
-  __device__ __forceinline__ void finish(Writer& w) const {
-    if (!kShifted) return;
-    const int base = static_cast<int>(threadIdx.x & 31) & ~(lanes - 1), i = end_word(w.lead);
-    // rows of one warp may start at different places: all lanes make both calls
-    write_word(w, w.start, base, -w.lead, w.lead > 0);
-    if (i == kPieces * lanes && lane == lanes - 1) w.end = shifted<T>(w.before, make_uint4(0, 0, 0, 0), (16 - w.lead) & 15);
-    write_word(w, w.end, base + (i < kPieces * lanes ? i & (lanes - 1) : lanes - 1), 16 * i - w.lead, i > 0 || w.lead == 0);
-  }
-  // Those elements of lane `from`'s word, o bytes into the segment, that belong to the segment.
-  __device__ __forceinline__ void write_word(const Writer& w, uint4 word, int from, int o, bool on) const {
-    word.x = __shfl_sync(kFull, word.x, from);
-    word.y = __shfl_sync(kFull, word.y, from);
-    word.z = __shfl_sync(kFull, word.z, from);
-    word.w = __shfl_sync(kFull, word.w, from);
-#pragma unroll 1
-    for (int e = lane; e < N; e += lanes) {
-      const int b = o + e * static_cast<int>(sizeof(T));
-      if (!w.in || !on || b < 0 || b >= segment_bytes) continue;
-      const int at = e * static_cast<int>(sizeof(T)) / 4;
-      const uint32_t pair = at & 2 ? (at & 1 ? word.w : word.z) : (at & 1 ? word.y : word.x);
-      *reinterpret_cast<typename Elem<T>::Bits*>(w.p + b) = static_cast<typename Elem<T>::Bits>(sizeof(T) == 2 && (e & 1) ? pair >> 16 : pair);
-    }
-  }
-  // Column of element i (of 2 H), whether it exists, and a vector's elements there (`none` without a vector).
-  __device__ __forceinline__ int element_col(int i) const { return segment + col(i / N) + i % N; }
-  __device__ __forceinline__ bool has_element(int i) const { return i / N * lanes * N + i % N < left; }
+  // A vector's elements at the thread's columns (0 beyond the row, `none` without a vector).
   __device__ __forceinline__ void vector(const void* v, int type, float none, float2 (&x)[H]) const {
     if (!v) {
 #pragma unroll
@@ -224,29 +165,23 @@ struct Place {
   template <typename V>
   __device__ __forceinline__ void vector_of(const V* v, float2 (&x)[H]) const {
     constexpr int kLoads = N / Elem<V>::N > 0 ? N / Elem<V>::N : 1;  // 16-byte loads per piece
-    if (N >= Elem<V>::N && (reinterpret_cast<uintptr_t>(v) & 15) == 0) {
+    if (!kOffset && N >= Elem<V>::N && (reinterpret_cast<uintptr_t>(v) & 15) == 0) {
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
           uint4 q = make_uint4(0, 0, 0, 0);
-          const int j = k * lanes * N + l * Elem<V>::N;
-          float2* y = x + k * W + l * Elem<V>::N / 2;
-          if (j + Elem<V>::N <= left) q = *reinterpret_cast<const uint4*>(v + segment + col(k) + l * Elem<V>::N);
-          Elem<V>::unpack(q, y);
-          if (j < left && j + Elem<V>::N > left) {
-#pragma unroll
-            for (int e = 0; e < Elem<V>::N; ++e)
-              if (j + e < left) (e % 2 ? y[e / 2].y : y[e / 2].x) = Elem<V>::get(v + segment + col(k) + l * Elem<V>::N + e);
-          }
+          if (has(k)) q = *reinterpret_cast<const uint4*>(v + begin + col(k) + l * Elem<V>::N);
+          Elem<V>::unpack(q, x + k * W + l * Elem<V>::N / 2);
         }
       }
       return;
     }
 #pragma unroll
     for (int i = 0; i < H; ++i) {
-      x[i].x = has_element(2 * i) ? Elem<V>::get(v + element_col(2 * i)) : 0.f;
-      x[i].y = has_element(2 * i + 1) ? Elem<V>::get(v + element_col(2 * i + 1)) : 0.f;
+      const int k = i / W, e = 2 * (i % W);
+      x[i].x = exists(k, e) ? Elem<V>::get(v + begin + col(k) + e) : 0.f;
+      x[i].y = exists(k, e + 1) ? Elem<V>::get(v + begin + col(k) + e + 1) : 0.f;
     }
   }
 };
@@ -306,10 +241,20 @@ __device__ __forceinline__ float2 round_pair(float2 x) {
 // ------------------------------------------------------------------- host
 constexpr int kMostPieces = 4;  // per thread
 
+// Whether the rows of the matrices (NULL: none) lie in their 16 bytes alike; *offset: they do not all start there.
 template <typename T>
-bool starts_at_16(const void* p, int64_t ld) {
-  return (reinterpret_cast<uintptr_t>(p) | (p ? ld * sizeof(T) : 0)) % 16 == 0;
-}
+struct Starts {
+  bool alike = true, offset = false;
+  uintptr_t base = 0, step = 0;
+  bool any = false;
+  void add(const void* p, int64_t ld, int64_t rows) {
+    if (!p) return;
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p) % 16, s = rows > 1 ? static_cast<uintptr_t>(ld) * sizeof(T) % 16 : 0;
+    alike = alike && (!any || (b == base && s == step));
+    base = b, step = s, any = true;
+    offset = offset || b != 0 || s != 0;
+  }
+};
 
 // Lets a kernel have the ring's shared memory, once per device.
 template <typename F>
@@ -336,8 +281,8 @@ inline int most_warps(int elements) { return elements > 16 ? 16 : elements > 8 ?
 
 // How rows of `cols` elements, n of them to a piece, are shared out, with `matrices` copied per row. False: they
 // are too long.
-inline bool row_shape(int64_t cols, int n, bool shift, int matrices, RowShape* s, int* pieces) {
-  const int64_t units = (cols + n - 1) / n;
+inline bool row_shape(int64_t cols, int n, bool offset, int matrices, RowShape* s, int* pieces) {
+  const int64_t units = (cols + (offset ? n - 1 : 0) + n - 1) / n;  // at most, wherever a row starts
   s->lanes = 32, s->warps = 1, *pieces = 1;
   if (units <= 16) {
     s->lanes = 1;
@@ -347,8 +292,6 @@ inline bool row_shape(int64_t cols, int n, bool shift, int matrices, RowShape* s
     int64_t least = INT64_MAX;
     for (int k = kMostPieces; k >= 1; --k) {
       const int64_t warps = (units + 32 * k - 1) / (32 * k);
-      // shifting takes registers: four pieces of 16-bit elements spill 100 of them
-      if (shift && n * k > 24 && units <= 32 * 3 * most_warps(n * 3)) continue;
       if (warps > most_warps(n * k) || warps * (k + 1) >= least) continue;
       least = warps * (k + 1);
       s->warps = static_cast<int>(warps), *pieces = k;
@@ -357,13 +300,18 @@ inline bool row_shape(int64_t cols, int n, bool shift, int matrices, RowShape* s
   }
   s->groups = most_warps(n * *pieces) / s->warps;
   if (s->warps > 1 && s->groups > 15) s->groups = 15;  // named barriers
-  s->slot_bytes = (s->lanes * *pieces + (shift ? 1 : 0)) * 16;
+  s->slot_bytes = s->lanes * *pieces * 16;
   auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes <= kRingBudget; };
   while (s->groups > 1 && !fits(2)) --s->groups;
   if (!fits(2)) return false;
   s->depth = kMostDepth;
   while (!fits(s->depth)) --s->depth;
   return true;
+}
+// Blocks for `sets` of rows: with an offset a multiple of 8, so that a thread's rows lie in their 16 bytes alike.
+inline unsigned blocks_for(int64_t sets, int sms, bool offset) {
+  const int64_t n = sets < sms ? sets : sms;
+  return static_cast<unsigned>(!offset ? n : n < sms || sms < 8 ? (n + 7) / 8 * 8 : n / 8 * 8);
 }
 inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
 

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(32 * kFoldSlices) fold_parts_kernel(const floa
 int64_t parts_for(int64_t rows, int64_t cols) {
   int64_t n = kPartFloats / cols;
   if (n > kMostParts) n = kMostParts;
-  if (n > rows) n = rows;
+  if (n > (rows + 7) / 8 * 8) n = (rows + 7) / 8 * 8;
   return n < 1 ? 1 : n;
 }
 
@@ -278,7 +278,7 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
       cudaError_t e;
       int sms = device_sms(&e);
       if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "device attributes");
-      if (sms > parts_for(rows, cols)) sms = static_cast<int>(parts_for(rows, cols));  // what work has room for
+      if (sms > kMostParts) sms = kMostParts;  // what work has room for
       if (!launch_row_backward(a, type, dbias != nullptr, sms, &parts, st, &e))
         e = type == MEQ_F32    ? launch_wide_backward<float>(a, &parts, st)
             : type == MEQ_BF16 ? launch_wide_backward<__nv_bfloat16>(a, &parts, st)
