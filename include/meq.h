@@ -562,7 +562,7 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
 meq_status meq_embedding(const int64_t* tokens, int64_t n, const void* table, int table_type, int64_t vocab, int64_t cols, int64_t ld_table,
                          float scale, void* out, int out_type, int64_t ld_out, void* cuda_stream);
 /* Floats of `work` for meq_embedding_grad. Host only. */
-int64_t meq_embedding_work_floats(int64_t n, int64_t cols);
+int64_t meq_embedding_work_floats(int64_t n, int64_t vocab, int64_t cols);
 /* The gradient of the table into out (vocab rows of out_type): every row is
  * written, or with accumulate != 0 the sums are added to what the rows hold (a
  * table shared with the head, micro-batches) and the other rows left as they

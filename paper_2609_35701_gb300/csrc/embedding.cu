@@ -10,11 +10,15 @@
 //   sort_kernel    one cluster sorts the pairs (token, position) by token, stably,
 //                  digit by digit, its counts exchanged through distributed shared
 //                  memory; the other blocks meanwhile mark the tokens that occur
-//                  in their share of the vocabulary, and zero the other rows
+//                  and zero rows that do not, as many as the sort leaves time for
 //   runs_kernel    a warp per chunk of 4 to 32 sorted pairs and slice of columns:
-//                  runs of one token inside the chunk are summed and written, runs
-//                  that cross its ends leave a partial sum
-//   joins_kernel   the partial sums of each crossing run, added in order
+//                  runs of one token are summed and written; one that crosses the
+//                  chunk's end is taken to its end if it is no longer than a chunk,
+//                  else it leaves partial sums. Blocks between them zero the other
+//                  rows, so that reads and writes share the memory's time.
+//   joins_kernel   the partial sums of each long run, added in order
+// Up to 128 tokens take one launch instead: a warp looks for its token's other
+// occurrences among them itself.
 #include <mutex>
 #include <string>
 
@@ -65,24 +69,34 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
     const uint32_t per_row = static_cast<uint32_t>(a.cols / 8);
     const int64_t total = a.n * per_row;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * (kLookupThreads * kLookupPieces) + threadIdx.x;
+    int64_t i[kLookupPieces], t[kLookupPieces];
+    int j[kLookupPieces];
 #pragma unroll
     for (int k = 0; k < kLookupPieces; ++k) {
       const int64_t at = first + k * kLookupThreads;
-      if (at >= total) break;
-      const int64_t i = at / per_row;
-      const int64_t j = (at - i * per_row) * 8;
-      const int64_t t = a.tokens[i];
-      float2 x[4];
-      if (t >= 0 && t < a.vocab) {
-        load8(static_cast<const Tin*>(a.table) + t * a.ld_table + j, x);
+      i[k] = at >= total ? -1 : total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(at) / per_row) : at / per_row;
+      j[k] = static_cast<int>(at - i[k] * per_row) * 8;
+      t[k] = i[k] >= 0 ? a.tokens[i[k]] : -1;
+    }
+    float2 x[kLookupPieces][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], make_float2(a.scale, a.scale));
+    for (int k = 0; k < kLookupPieces; ++k) {
+      if (t[k] >= 0 && t[k] < a.vocab) {
+        load8(static_cast<const Tin*>(a.table) + t[k] * a.ld_table + j[k], x[k]);
       } else {
-        const float v = t < 0 ? 0.f : nan;
+        const float v = t[k] < 0 ? 0.f : nan;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = make_float2(v, v);
+        for (int e = 0; e < 4; ++e) x[k][e] = make_float2(v, v);
       }
-      store8(static_cast<Tout*>(a.out) + i * a.ld_out + j, x);
+    }
+#pragma unroll
+    for (int k = 0; k < kLookupPieces; ++k) {
+      if (i[k] < 0) continue;
+      if (t[k] >= 0) {  // zeros stay zeros, whatever the scale
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] = mul2(x[k][e], make_float2(a.scale, a.scale));
+      }
+      store8(static_cast<Tout*>(a.out) + i[k] * a.ld_out + j[k], x[k]);
     }
   } else {
     const int64_t segments = (a.cols + kLookupCols - 1) / kLookupCols;
@@ -105,8 +119,8 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
 // --------------------------------------------------------------------- sort
 constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kRadixBits = 9, kRadix = 1 << kRadixBits;
-constexpr int kSortKeys = 8;      // groups of 32 keys that a warp loads ahead
-constexpr int kMarkBits = kSortWarps * kRadix * 32;  // rows that a block's marks cover at a time
+constexpr int kSortKeys = 8;                    // groups of 32 keys that a warp has in registers
+constexpr int kMarkWords = kSortWarps * kRadix; // of 32 rows each, that a block marks at a time
 
 struct SortShared {
   uint32_t hist[kSortWarps][kRadix];  // counts, then next places, of each warp's keys; the other blocks: marks
@@ -119,9 +133,12 @@ struct SortArgs {
   uint32_t n, vocab;
   int passes, bits;     // digits, and the bits of each
   uint2* pairs[2];      // the last pass writes pairs[0]
-  uint32_t* crossing;   // the number of crossing runs: zeroed
-  void* out;            // rows of tokens that do not occur are zeroed; NULL: left
+  uint32_t* crossing;   // the numbers of crossing runs: zeroed
+  void* out;            // rows of tokens that do not occur are zeroed,
   int64_t row_bytes, ld_bytes;
+  uint32_t words;       // 32 rows to a word of marks,
+  uint32_t first_words; // those of the first words here,
+  uint32_t* marks;      // the others by their marks, which are written here
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t t, uint32_t vocab) {
@@ -130,7 +147,8 @@ __device__ __forceinline__ uint32_t key_of(int64_t t, uint32_t vocab) {
 
 // Digit by digit from the lowest: a warp counts its consecutive keys' digits, the
 // counts are summed over the warps of the block and the blocks of the cluster,
-// and every key goes to its digit's next place, in the order of the keys.
+// and every key goes to its digit's next place, in the order of the keys. Lanes
+// with the same digit find one another by a ballot per bit.
 __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
   const uint32_t rank = blockIdx.x;
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
@@ -140,53 +158,65 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
   const uint32_t last = a.n - first < per ? a.n : first + per;
   const uint32_t radix = 1u << a.bits, below = (1u << lane) - 1u;
   uint32_t* hist = sh.hist[warp];
-  if (rank == 0 && threadIdx.x == 0) *a.crossing = 0;
+  if (rank == 0 && threadIdx.x < 2) a.crossing[threadIdx.x] = 0;
   for (int p = 0; p < a.passes; ++p) {
     const uint2* src = a.pairs[(a.passes - p) & 1];
     uint2* dst = a.pairs[(a.passes - p - 1) & 1];
     const int shift = p * a.bits;
-    auto load = [&](uint32_t i) -> uint2 {
-      if (p == 0) return make_uint2(key_of(a.tokens[i], a.vocab), i);
-      return __ldcg(src + i);
-    };
-    for (uint32_t d = lane; d < radix; d += 32) hist[d] = 0;
-    __syncwarp();
-    for (uint32_t base = first; base < last; base += 32 * kSortKeys) {
-      uint32_t key[kSortKeys];
+    uint2 pair[kSortKeys];
+    uint32_t same[kSortKeys];  // lanes with the same digit (0: no key)
+    auto load = [&](uint32_t base) {
 #pragma unroll
       for (int k = 0; k < kSortKeys; ++k) {
         const uint32_t i = base + 32 * k + lane;
-        key[k] = i < last ? load(i).x : 0;
+        pair[k] = make_uint2(0, 0);
+        if (i < last) pair[k] = p == 0 ? make_uint2(key_of(a.tokens[i], a.vocab), i) : __ldcg(src + i);
       }
 #pragma unroll
-      for (int k = 0; k < kSortKeys; ++k) {
-        const bool in = base + 32 * k + lane < last;
-        const uint32_t d = in ? (key[k] >> shift) & (radix - 1) : radix;
-        const uint32_t same = __match_any_sync(kFull, d);
-        if (in && (same & below) == 0) hist[d] += __popc(same);
-        __syncwarp();
+      for (int k = 0; k < kSortKeys; ++k) same[k] = __ballot_sync(kFull, base + 32 * k + lane < last);
+#pragma unroll 1
+      for (int b = 0; b < a.bits; ++b) {
+#pragma unroll
+        for (int k = 0; k < kSortKeys; ++k) {
+          const bool on = (pair[k].x >> (shift + b)) & 1;
+          const uint32_t v = __ballot_sync(kFull, on);
+          same[k] &= on ? v : ~v;
+        }
       }
+#pragma unroll
+      for (int k = 0; k < kSortKeys; ++k)
+        if (base + 32 * k + lane >= last) same[k] = 0;
+    };
+    auto digit = [&](int k) { return (pair[k].x >> shift) & (radix - 1); };
+    for (uint32_t d = lane; d < radix; d += 32) hist[d] = 0;
+    __syncwarp();
+    for (uint32_t base = first; base < last; base += 32 * kSortKeys) {
+      load(base);
+#pragma unroll
+      for (int k = 0; k < kSortKeys; ++k)
+        if (same[k] != 0 && (same[k] & below) == 0) atomicAdd(&hist[digit(k)], __popc(same[k]));
     }
     __syncthreads();
     const uint32_t d = threadIdx.x;
     if (d < radix) {
       uint32_t sum = 0;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = sh.hist[w][d];
-        sh.hist[w][d] = sum;
-        sum += c;
-      }
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) sum += sh.hist[w][d];
       sh.total[d] = sum;
     }
     cluster_sync_all();
     uint32_t all = 0, before = 0;
-    if (d < radix)
+    if (d < radix) {
+      uint32_t c[kSortCtas];
+#pragma unroll
+      for (uint32_t r = 0; r < kSortCtas; ++r)
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[r]) : "r"(map_to_rank(smem_u32(&sh.total[d]), r)) : "memory");
+#pragma unroll
       for (uint32_t r = 0; r < kSortCtas; ++r) {
-        uint32_t c;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(map_to_rank(smem_u32(&sh.total[d]), r)) : "memory");
-        before += r < rank ? c : 0;
-        all += c;
+        before += r < rank ? c[r] : 0;
+        all += c[r];
       }
+    }
     uint32_t scan = all;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -198,26 +228,28 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
     if (d < radix) {
       uint32_t at = scan - all + before;
       for (int w = 0; w < warp; ++w) at += sh.warp_sum[w];
-      for (int w = 0; w < kSortWarps; ++w) sh.hist[w][d] += at;
+#pragma unroll
+      for (int w0 = 0; w0 < kSortWarps; w0 += 8) {
+        uint32_t c[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) c[w] = sh.hist[w0 + w][d];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          sh.hist[w0 + w][d] = at;
+          at += c[w];
+        }
+      }
     }
     __syncthreads();
     for (uint32_t base = first; base < last; base += 32 * kSortKeys) {
-      uint2 pair[kSortKeys];
+      if (per > 32 * kSortKeys) load(base);  // else they are still there
 #pragma unroll
       for (int k = 0; k < kSortKeys; ++k) {
-        const uint32_t i = base + 32 * k + lane;
-        pair[k] = i < last ? load(i) : make_uint2(0, 0);
-      }
-#pragma unroll
-      for (int k = 0; k < kSortKeys; ++k) {
-        const bool in = base + 32 * k + lane < last;
-        const uint32_t digit = in ? (pair[k].x >> shift) & (radix - 1) : radix;
-        const uint32_t same = __match_any_sync(kFull, digit);
-        const uint32_t at = in ? hist[digit] : 0;
+        const uint32_t at = same[k] ? hist[digit(k)] : 0;
         __syncwarp();
-        if (in) {
-          if ((same & below) == 0) hist[digit] = at + __popc(same);
-          dst[at + __popc(same & below)] = pair[k];
+        if (same[k]) {
+          if ((same[k] & below) == 0) hist[digit(k)] = at + __popc(same[k]);
+          dst[at + __popc(same[k] & below)] = pair[k];
         }
         __syncwarp();
       }
@@ -226,24 +258,27 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
   }
 }
 
-__device__ __forceinline__ void zero_row(uint8_t* p, int64_t bytes, int lane) {
+// `threads` threads, of which this is the t-th, zero a row.
+__device__ __forceinline__ void zero_row(uint8_t* p, int64_t bytes, int t, int threads) {
   const int64_t head = min(static_cast<int64_t>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15), bytes);
   const int64_t pieces = (bytes - head) / 16, tail = head + 16 * pieces;
-  for (int64_t i = lane; i < pieces; i += 32) __stcs(reinterpret_cast<uint4*>(p + head) + i, make_uint4(0, 0, 0, 0));
-  // the ends: elements of 2 or 4 bytes
-  const int64_t e = 2 * lane;
-  if (e < head) *reinterpret_cast<uint16_t*>(p + e) = 0;
-  if (tail + e < bytes) *reinterpret_cast<uint16_t*>(p + tail + e) = 0;
+  for (int64_t i = t; i < pieces; i += threads) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0, 0, 0, 0);
+  if (t < 8) {  // the ends: elements of 2 or 4 bytes
+    const int64_t e = 2 * t;
+    if (e < head) *reinterpret_cast<uint16_t*>(p + e) = 0;
+    if (tail + e < bytes) *reinterpret_cast<uint16_t*>(p + tail + e) = 0;
+  }
 }
 
-__device__ void zero_other_rows(const SortArgs& a, SortShared& sh) {
+// Words of marks are dealt out to the blocks in turn: writes that advance through
+// memory together run at 7 TB/s, those of a far-off share per SM at 5.
+__device__ void zero_first_rows(const SortArgs& a, SortShared& sh) {
   uint32_t* marks = sh.hist[0];
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-  const int64_t blocks = gridDim.x - kSortCtas, block = blockIdx.x - kSortCtas;
-  const int64_t share = (a.vocab + blocks - 1) / blocks, end = min((block + 1) * share, static_cast<int64_t>(a.vocab));
-  for (int64_t v0 = block * share; v0 < end; v0 += kMarkBits) {
-    const int64_t rows = min(end - v0, static_cast<int64_t>(kMarkBits));
-    for (int64_t i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) marks[i] = 0;
+  const uint32_t blocks = gridDim.x - kSortCtas, block = blockIdx.x - kSortCtas;
+  for (uint32_t k0 = 0; block + blocks * static_cast<uint64_t>(k0) < a.words; k0 += kMarkWords) {
+    const uint32_t here = min((a.words - block - blocks * k0 + blocks - 1) / blocks, static_cast<uint32_t>(kMarkWords));
+    for (uint32_t i = threadIdx.x; i < here; i += kSortThreads) marks[i] = 0;
     __syncthreads();
     for (uint32_t base = 0; base < a.n; base += kSortThreads * kSortKeys) {
       int64_t t[kSortKeys];
@@ -253,12 +288,18 @@ __device__ void zero_other_rows(const SortArgs& a, SortShared& sh) {
         t[k] = i < a.n ? a.tokens[i] : -1;
       }
 #pragma unroll
-      for (int k = 0; k < kSortKeys; ++k)
-        if (t[k] >= v0 && t[k] < v0 + rows) atomicOr(&marks[(t[k] - v0) >> 5], 1u << ((t[k] - v0) & 31));
+      for (int k = 0; k < kSortKeys; ++k) {
+        const uint32_t w = key_of(t[k], kNoToken >> 1) >> 5, at = w / blocks;
+        if (t[k] >= 0 && t[k] < a.vocab && w - at * blocks == block && at - k0 < here) atomicOr(&marks[at - k0], 1u << (t[k] & 31));
+      }
     }
     __syncthreads();
-    for (int64_t i = warp; i < rows; i += kSortWarps)
-      if (((marks[i >> 5] >> (i & 31)) & 1u) == 0) zero_row(static_cast<uint8_t*>(a.out) + (v0 + i) * a.ld_bytes, a.row_bytes, lane);
+    for (uint32_t i = threadIdx.x; i < here; i += kSortThreads)
+      if (block + blocks * (k0 + i) >= a.first_words) a.marks[block + blocks * (k0 + i)] = marks[i];
+    for (uint32_t i = 0; i < here && block + blocks * (k0 + i) < a.first_words; ++i) {
+      const int64_t row = static_cast<int64_t>(block + blocks * (k0 + i)) * 32 + warp;
+      if (row < a.vocab && !((marks[i] >> warp) & 1)) zero_row(static_cast<uint8_t*>(a.out) + row * a.ld_bytes, a.row_bytes, lane, 32);
+    }
     __syncthreads();
   }
 }
@@ -269,7 +310,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const __grid_cons
   pdl_allow_dependents();
   pdl_wait_predecessor();
   if (blockIdx.x < kSortCtas) sort_pairs(a, sh);
-  else zero_other_rows(a, sh);
+  else zero_first_rows(a, sh);
 }
 
 // --------------------------------------------------------------------- runs
@@ -277,131 +318,317 @@ struct RunArgs {
   const void* grad;
   int64_t ld;
   uint32_t n, vocab;
-  int cols, chunk;       // chunk: pairs of a chunk, 4 to 32
-  const uint2* pairs;
-  uint32_t* crossing;    // [0]: number of crossing runs, then the chunks in which they start
-  float* parts;          // [chunks][2][ld_parts]: sums of a run from the chunk before, of one into the next
+  int cols, chunk;        // chunk: pairs of a chunk, 4 to 32
+  const int64_t* tokens;  // few tokens
+  const uint2* pairs;     // sorted ones
+  uint32_t* crossing;     // [0], [1]: runs with partial sums in up to, and more than, kShortParts chunks; then the chunks
+  uint32_t chunks;        // in which they start, `chunks` places for each
+  float* parts;           // [chunks][2][ld_parts]: sums of a run from the chunk before, of one into the next
   int64_t ld_parts;
   void* out;
   int64_t ld_out;
   int out_type, accumulate;
   float scale;
+  // rows to zero: those of the words from first_word on, `fill_rows` per block, of `fills` blocks among the others
+  int64_t row_bytes, ld_bytes;
+  uint32_t first_word, fill_rows, fills;
+  const uint32_t* marks;
 };
-constexpr int kRunThreads = 256;
+constexpr int kRunThreads = 256, kRunWarps = kRunThreads / 32;
+constexpr int kShortParts = 32;
+constexpr int kFewTokens = 128;
+constexpr uint32_t kFillBytes = 32768, kMostFillRows = 2048;  // of a block
 
-__device__ __forceinline__ void put(void* out, int type, int64_t i, float sum, float scale, int accumulate) {
-  if (type == MEQ_F32) {
-    float* p = static_cast<float*>(out) + i;
-    *p = accumulate ? fmaf(sum, scale, *p) : sum * scale;
-  } else if (type == MEQ_BF16) {
-    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(out) + i;
-    *p = __float2bfloat16_rn(accumulate ? fmaf(sum, scale, __bfloat162float(*p)) : sum * scale);
+// kN sums to consecutive elements of a row of the gradient; kN > 1: 16 bytes of floats, or as many elements of 16 bits, at a time.
+template <int kN>
+__device__ __forceinline__ void put(const RunArgs& a, int64_t i, const float (&sum)[kN]) {
+  float old[kN] = {};
+  if (a.out_type == MEQ_F32) {
+    float* p = static_cast<float*>(a.out) + i;
+    if constexpr (kN == 1) {
+      if (a.accumulate) old[0] = *p;
+      *p = fmaf(sum[0], a.scale, old[0]);
+    } else {
+      if (a.accumulate) {
+#pragma unroll
+        for (int e = 0; e < kN; e += 4) {
+          const float4 q = *reinterpret_cast<const float4*>(p + e);
+          old[e] = q.x, old[e + 1] = q.y, old[e + 2] = q.z, old[e + 3] = q.w;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kN; e += 4)
+        *reinterpret_cast<float4*>(p + e) = make_float4(fmaf(sum[e], a.scale, old[e]), fmaf(sum[e + 1], a.scale, old[e + 1]),
+                                                        fmaf(sum[e + 2], a.scale, old[e + 2]), fmaf(sum[e + 3], a.scale, old[e + 3]));
+    }
+    return;
+  }
+  const bool bf = a.out_type == MEQ_BF16;
+  uint16_t* p = static_cast<uint16_t*>(a.out) + i;
+  auto widen = [&](uint32_t b) {
+    return bf ? __uint_as_float(b << 16) : __half2float(__ushort_as_half(static_cast<uint16_t>(b)));
+  };
+  auto narrow = [&](float x) -> uint32_t {
+    return bf ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+  };
+  if constexpr (kN == 1) {
+    if (a.accumulate) old[0] = widen(*p);
+    *p = static_cast<uint16_t>(narrow(fmaf(sum[0], a.scale, old[0])));
   } else {
-    __half* p = static_cast<__half*>(out) + i;
-    *p = __float2half_rn(accumulate ? fmaf(sum, scale, __half2float(*p)) : sum * scale);
+    uint32_t w[kN / 2];
+    if (a.accumulate) {
+#pragma unroll
+      for (int e = 0; e < kN; e += 4) {
+        const uint2 q = *reinterpret_cast<const uint2*>(p + e);
+        old[e] = widen(q.x & 0xFFFFu), old[e + 1] = widen(q.x >> 16), old[e + 2] = widen(q.y & 0xFFFFu), old[e + 3] = widen(q.y >> 16);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kN; e += 2)
+      w[e / 2] = narrow(fmaf(sum[e], a.scale, old[e])) | narrow(fmaf(sum[e + 1], a.scale, old[e + 1])) << 16;
+    if constexpr (kN == 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   }
 }
 
-// kStep: columns that lie together in a lane (a 16-byte piece, or one element); kPieces: of those per lane.
+// A lane's columns of a slice, and their sums. kStep: columns that lie together (a 16-byte piece, or one element).
 template <typename T, int kStep, int kPieces>
-__global__ void __launch_bounds__(kRunThreads) runs_kernel(const RunArgs a) {
-  constexpr int kAhead = kStep == 1 ? 2 : (8 / kPieces > 4 ? 4 : 8 / kPieces);  // rows loaded ahead
+struct Slice {
+  static constexpr int kCols = 32 * kStep * kPieces;
+  static constexpr int kAhead = kStep == 1 ? 4 : 8 / kPieces;  // rows loaded ahead
+  int j0, cols;
+  float acc[kPieces][kStep];
+  __device__ __forceinline__ Slice(int slice, int lane, int cols_) : j0(slice * kCols + lane * kStep), cols(cols_) { clear(); }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+      for (int i = 0; i < kStep; ++i) acc[k][i] = 0.f;
+  }
+  __device__ __forceinline__ int col(int k) const { return j0 + 32 * kStep * k; }
+  struct Row {
+    uint4 q[kStep > 1 ? kPieces : 1];
+    float s[kStep > 1 ? 1 : kPieces];
+  };
+  __device__ __forceinline__ void load(Row& r, const T* row, bool in) const {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const bool on = in && col(k) < cols;
+      if constexpr (kStep == 1) r.s[k] = on ? Elem<T>::get(row + col(k)) : 0.f;
+      else r.q[k] = on ? __ldcs(reinterpret_cast<const uint4*>(row + col(k))) : make_uint4(0, 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void add(const Row& r) {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      if constexpr (kStep == 1) {
+        acc[k][0] += r.s[k];
+      } else {
+        float2 x[kStep / 2];
+        Elem<T>::unpack(r.q[k], x);
+#pragma unroll
+        for (int i = 0; i < kStep / 2; ++i) acc[k][2 * i] += x[i].x, acc[k][2 * i + 1] += x[i].y;
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const RunArgs& a, uint32_t token) const {
+    const int64_t row = static_cast<int64_t>(token) * a.ld_out;
+    if constexpr (kStep == 1) {  // what the row holds is on its way for all columns before the first is written
+      float old[kPieces] = {};
+      if (a.accumulate) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+          if (col(k) < cols) old[k] = held(a, row + col(k));
+      }
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        if (col(k) < cols) set(a, row + col(k), fmaf(acc[k][0], a.scale, old[k]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        if (col(k) < cols) put(a, row + col(k), acc[k]);
+    }
+  }
+  static __device__ __forceinline__ float held(const RunArgs& a, int64_t i) {
+    if (a.out_type == MEQ_F32) return static_cast<const float*>(a.out)[i];
+    if (a.out_type == MEQ_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.out)[i]);
+    return __half2float(static_cast<const __half*>(a.out)[i]);
+  }
+  static __device__ __forceinline__ void set(const RunArgs& a, int64_t i, float x) {
+    if (a.out_type == MEQ_F32) static_cast<float*>(a.out)[i] = x;
+    else if (a.out_type == MEQ_BF16) static_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(x);
+    else static_cast<__half*>(a.out)[i] = __float2half_rn(x);
+  }
+  __device__ __forceinline__ void leave(float* part) const {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      if (col(k) >= cols) continue;
+      if constexpr (kStep == 1) {
+        part[col(k)] = acc[k][0];
+      } else {
+#pragma unroll
+        for (int i = 0; i < kStep; i += 4)
+          *reinterpret_cast<float4*>(part + col(k) + i) = make_float4(acc[k][i], acc[k][i + 1], acc[k][i + 2], acc[k][i + 3]);
+      }
+    }
+  }
+};
+
+// Whether this block zeroes rows, and its number among those that do, or among the others.
+__device__ __forceinline__ bool fill_block(const RunArgs& a, int64_t* index) {
+  const uint64_t before = static_cast<uint64_t>(blockIdx.x) * a.fills / gridDim.x, after = (static_cast<uint64_t>(blockIdx.x) + 1) * a.fills / gridDim.x;
+  *index = static_cast<int64_t>(after != before ? before : blockIdx.x - before);
+  return after != before;
+}
+// Zeroes this block's rows but those marked(row, number in the block).
+template <typename F>
+__device__ __forceinline__ void fill_rows(const RunArgs& a, int64_t block, F marked) {
+  const int64_t row0 = static_cast<int64_t>(a.first_word) * 32 + block * a.fill_rows;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(a.fill_rows), static_cast<int64_t>(a.vocab) - row0));
+  const int threads = a.fill_rows >= kRunWarps ? 32 : kRunThreads;  // of a row
+  for (int r = static_cast<int>(threadIdx.x) / threads; r < rows; r += kRunThreads / threads)
+    if (!marked(row0 + r, r)) zero_row(static_cast<uint8_t*>(a.out) + (row0 + r) * a.ld_bytes, a.row_bytes, static_cast<int>(threadIdx.x) % threads, threads);
+}
+
+template <typename T, int kStep, int kPieces>
+__global__ void __launch_bounds__(kRunThreads) runs_kernel(const __grid_constant__ RunArgs a) {
+  using S = Slice<T, kStep, kPieces>;
+  constexpr int kAhead = S::kAhead;
   pdl_allow_dependents();
-  const int lane = static_cast<int>(threadIdx.x & 31);
-  const int slices = (a.cols + 32 * kStep * kPieces - 1) / (32 * kStep * kPieces);
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kRunThreads / 32) + (threadIdx.x >> 5);
-  const int64_t c = unit / slices;
-  const int j0 = static_cast<int>(unit - c * slices) * (32 * kStep * kPieces) + lane * kStep;  // + 32 kStep k
   pdl_wait_predecessor();
-  const int64_t first = c * a.chunk;
+  int64_t block;
+  if (fill_block(a, &block)) {
+    fill_rows(a, block, [&](int64_t row, int) { return (a.marks[row >> 5] >> (row & 31)) & 1; });
+    return;
+  }
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  const int slices = (a.cols + S::kCols - 1) / S::kCols;
+  const int64_t unit = block * kRunWarps + (threadIdx.x >> 5), c = unit / slices, first = c * a.chunk;
   if (first >= a.n) return;
-  auto key_at = [&](int64_t i) { return i >= 0 && i < a.n ? a.pairs[i].x : kNoToken; };
-  uint2 pair = make_uint2(kNoToken, 0);
-  if (lane < a.chunk && first + lane < a.n) pair = a.pairs[first + lane];
+  auto pair_at = [&](int64_t i) { return i >= 0 && i < a.n ? a.pairs[i] : make_uint2(kNoToken, 0); };
+  const uint2 pair = lane < a.chunk ? pair_at(first + lane) : make_uint2(kNoToken, 0);
+  const uint2 next = pair_at(first + a.chunk + lane), prev = pair_at(first - 1 - lane);
+  auto ones = [](uint32_t m) { return m == kFull ? 32 : __ffs(~m) - 1; };  // from the lowest bit on
   const int count = __popc(__ballot_sync(kFull, pair.x < a.vocab));  // the others come last
   if (count == 0) return;
-  const uint32_t before = key_at(first - 1), after = key_at(first + a.chunk);
+  // The runs at the chunk's ends: how far they reach beyond it (32 or more: 32), and whether one is taken whole by the chunk
+  // in which it starts.
+  const uint32_t key0 = __shfl_sync(kFull, pair.x, 0), key1 = __shfl_sync(kFull, pair.x, count - 1);
+  const int back = ones(__ballot_sync(kFull, prev.x == key0)), lead = __popc(__ballot_sync(kFull, pair.x == key0));
+  const int ahead = count == a.chunk ? ones(__ballot_sync(kFull, next.x == key1)) : 0, tail = __popc(__ballot_sync(kFull, pair.x == key1));
+  const bool through = lead == a.chunk;  // one run from end to end
+  const bool skip = back > 0 && back + lead + (through ? ahead : 0) <= a.chunk;
+  const bool take = ahead > 0 && !(through && back > 0) && tail + ahead <= a.chunk;
+  const int begin = skip ? lead : 0, end = count + (take ? ahead : 0);
+  const int part_end = back > 0 && !skip ? lead - 1 : -1;  // last pair of a run from before
+  const bool into_next = ahead > 0 && !take && !(through && back > 0);
+  S s(static_cast<int>(unit - c * slices), lane, a.cols);
   const T* grad = static_cast<const T*>(a.grad);
-  float acc[kPieces * kStep];
-#pragma unroll
-  for (int k = 0; k < kPieces * kStep; ++k) acc[k] = 0.f;
-  bool from_before = __shfl_sync(kFull, pair.x, 0) == before;
-  for (int e0 = 0; e0 < count; e0 += kAhead) {
-    uint4 q[kAhead][kPieces];
-    float s[kAhead][kPieces];
+  auto key = [&](int e) { return e < a.chunk ? __shfl_sync(kFull, pair.x, e) : __shfl_sync(kFull, next.x, e - a.chunk); };
+  for (int e0 = begin; e0 < end; e0 += kAhead) {
+    typename S::Row r[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const uint32_t pos = __shfl_sync(kFull, pair.y, (e0 + u) & 31);
-      const T* row = grad + static_cast<int64_t>(pos) * a.ld;
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k) {
-        const int j = j0 + 32 * kStep * k;
-        const bool in = e0 + u < count && j < a.cols;
-        if (kStep == 1) s[u][k] = in ? Elem<T>::get(row + j) : 0.f;
-        else q[u][k] = in ? __ldcs(reinterpret_cast<const uint4*>(row + j)) : make_uint4(0, 0, 0, 0);
-      }
+      const int e = e0 + u;
+      const uint32_t pos = e < a.chunk ? __shfl_sync(kFull, pair.y, e & 31) : __shfl_sync(kFull, next.y, (e - a.chunk) & 31);
+      s.load(r[u], grad + static_cast<int64_t>(pos) * a.ld, e < end);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int e = e0 + u;
-      if (e >= count) break;
-#pragma unroll
-      for (int k = 0; k < kPieces; ++k) {
-        if (kStep == 1) {
-          acc[k] += s[u][k];
-        } else {
-          float2 x[kStep / 2 + 1];
-          Elem<T>::unpack(q[u][k], x);
-#pragma unroll
-          for (int i = 0; i < kStep / 2; ++i) acc[k * kStep + 2 * i] += x[i].x, acc[k * kStep + 2 * i + 1] += x[i].y;
-        }
-      }
-      const uint32_t key = __shfl_sync(kFull, pair.x, e);
-      const uint32_t next = e + 1 < a.chunk ? __shfl_sync(kFull, pair.x, (e + 1) & 31) : after;
-      if (next == key && e + 1 < a.chunk) continue;
-      // the run's end in this chunk
-      const bool into_next = next == key;
-      if (!from_before && !into_next) {
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-          const int j = j0 + 32 * kStep * k;
-          if (j < a.cols) {
-#pragma unroll
-            for (int i = 0; i < kStep; ++i)
-              put(a.out, a.out_type, static_cast<int64_t>(key) * a.ld_out + j + i, acc[k * kStep + i], a.scale, a.accumulate);
-          }
+      if (e >= end) break;
+      s.add(r[u]);
+      const uint32_t k = key(e);
+      if (e + 1 < end && key(e + 1) == k) continue;
+      if (e == part_end) {
+        s.leave(a.parts + 2 * c * a.ld_parts);
+      } else if (e == end - 1 && into_next) {
+        s.leave(a.parts + (2 * c + 1) * a.ld_parts);
+        if (s.j0 == 0) {
+          const int64_t far = first + (kShortParts + 1) * static_cast<int64_t>(a.chunk);
+          const int longer = far < a.n && a.pairs[far].x == k;
+          a.crossing[2 + longer * a.chunks + atomicAdd(&a.crossing[longer], 1u)] = static_cast<uint32_t>(c);
         }
       } else {
-        float* part = a.parts + (2 * c + (from_before ? 0 : 1)) * a.ld_parts;
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-          const int j = j0 + 32 * kStep * k;
-          if (j < a.cols) {
-#pragma unroll
-            for (int i = 0; i < kStep; ++i) part[j + i] = acc[k * kStep + i];
-          }
-        }
-        if (!from_before && j0 == 0) a.crossing[1 + atomicAdd(a.crossing, 1u)] = static_cast<uint32_t>(c);
+        s.finish(a, k);
       }
-      from_before = false;
-#pragma unroll
-      for (int k = 0; k < kPieces * kStep; ++k) acc[k] = 0.f;
+      s.clear();
     }
   }
 }
 
-// The crossing runs: a block per run and 128 columns, the run's partial sums dealt out to its warps.
-constexpr int kJoinCols = 128;
-__global__ void __launch_bounds__(kRunThreads) joins_kernel(const RunArgs a) {
-  constexpr int kWarps = kRunThreads / 32;
+// Few tokens, unsorted: a warp per token and slice of columns takes its token's rows if none precedes it, in order.
+template <typename T, int kStep, int kPieces>
+__global__ void __launch_bounds__(kRunThreads) few_kernel(const __grid_constant__ RunArgs a) {
+  using S = Slice<T, kStep, kPieces>;
+  constexpr int kAhead = S::kAhead, kEach = kFewTokens / 32;
+  __shared__ uint32_t marks[kMostFillRows / 32];
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ float4 sh[kWarps][32];
+  int64_t block;
+  if (fill_block(a, &block)) {
+    for (int i = static_cast<int>(threadIdx.x); i < static_cast<int>(kMostFillRows / 32); i += kRunThreads) marks[i] = 0;
+    __syncthreads();
+    if (threadIdx.x < a.n) {
+      const int64_t at = a.tokens[threadIdx.x] - block * a.fill_rows;
+      if (at >= 0 && at < a.fill_rows) atomicOr(&marks[at >> 5], 1u << (at & 31));
+    }
+    __syncthreads();
+    fill_rows(a, block, [&](int64_t, int r) { return (marks[r >> 5] >> (r & 31)) & 1; });
+    return;
+  }
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  const int slices = (a.cols + S::kCols - 1) / S::kCols;
+  const int64_t unit = block * kRunWarps + (threadIdx.x >> 5);
+  const int i = static_cast<int>(unit / slices);
+  if (i >= static_cast<int>(a.n)) return;
+  int64_t t[kEach];
+#pragma unroll
+  for (int q = 0; q < kEach; ++q) t[q] = 32 * q + lane < static_cast<int>(a.n) ? a.tokens[32 * q + lane] : -1;
+  const int64_t token = a.tokens[i];
+  if (token < 0 || token >= a.vocab) return;
+  uint32_t hits[kEach];
+  bool precedes = false;
+#pragma unroll
+  for (int q = 0; q < kEach; ++q) {
+    hits[q] = __ballot_sync(kFull, t[q] == token);
+    precedes = precedes || (q < i / 32 && hits[q] != 0) || (q == i / 32 && (hits[q] & ((1u << (i % 32)) - 1u)) != 0);
+  }
+  if (precedes) return;
+  S s(static_cast<int>(unit - static_cast<int64_t>(i) * slices), lane, a.cols);
+#pragma unroll 1
+  for (int q = 0; q < kEach; ++q) {
+    uint32_t m = q == 0 ? hits[0] : q == 1 ? hits[1] : q == 2 ? hits[2] : hits[3];
+    while (m) {
+      typename S::Row r[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int at = 32 * q + (m ? __ffs(m) - 1 : 0);
+        s.load(r[u], static_cast<const T*>(a.grad) + static_cast<int64_t>(at) * a.ld, m != 0);
+        m &= m - 1;
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s.add(r[u]);
+    }
+  }
+  s.finish(a, static_cast<uint32_t>(token));
+}
+
+// The runs with partial sums. Of up to kShortParts chunks, a block takes 1024 columns, 128 of them a warp; of more, a block
+// takes 128 columns and deals the partial sums out to its warps.
+constexpr int kJoinCols = 128;
+__global__ void __launch_bounds__(kRunThreads) joins_kernel(const __grid_constant__ RunArgs a) {
+  pdl_allow_dependents();
+  pdl_wait_predecessor();
+  __shared__ float4 sh[kRunWarps][32];
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-  const int64_t slices = (a.cols + kJoinCols - 1) / kJoinCols, units = slices * *a.crossing;
+  const int64_t narrow = (a.cols + kJoinCols - 1) / kJoinCols, wide = (narrow + kRunWarps - 1) / kRunWarps;
+  const int64_t longs = narrow * a.crossing[1], units = longs + wide * a.crossing[0];
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int64_t c = a.crossing[1 + u / slices];
-    const int j = static_cast<int>(u % slices) * kJoinCols + 4 * lane;
+    const bool is_long = u < longs;
+    const int64_t v = is_long ? u : u - longs, per = is_long ? narrow : wide;
+    const int64_t c = a.crossing[2 + (is_long ? a.chunks : 0) + v / per];
+    const int j = static_cast<int>(is_long ? v % per : (v % per) * kRunWarps + warp) * kJoinCols + 4 * lane;
     const uint32_t token = a.pairs[c * a.chunk + a.chunk - 1].x;
     int64_t more = 0;  // chunks after c that begin with the token
     for (;;) {
@@ -414,27 +641,33 @@ __global__ void __launch_bounds__(kRunThreads) joins_kernel(const RunArgs a) {
       more += 32;
     }
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* part = a.parts + j;
     if (j < a.cols) {
-#pragma unroll 4
-      for (int64_t k = warp; k <= more; k += kWarps) {
-        const float4 x = *reinterpret_cast<const float4*>(a.parts + (2 * (c + k) + (k == 0 ? 1 : 0)) * a.ld_parts + j);
+      if (!is_long || warp == 0) s = *reinterpret_cast<const float4*>(part + (2 * c + 1) * a.ld_parts);
+#pragma unroll 8
+      for (int64_t k = is_long ? 1 + warp : 1; k <= more; k += is_long ? kRunWarps : 1) {
+        const float4 x = *reinterpret_cast<const float4*>(part + 2 * (c + k) * a.ld_parts);
         s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
       }
     }
-    sh[warp][lane] = s;
-    __syncthreads();
-    if (warp == 0) {
+    if (is_long) {
+      __syncthreads();  // sh is free
+      sh[warp][lane] = s;
+      __syncthreads();
+      if (warp != 0) continue;
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) {
+      for (int w = 1; w < kRunWarps; ++w) {
         const float4 x = sh[w][lane];
         s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
       }
-      const float v[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j + i < a.cols) put(a.out, a.out_type, static_cast<int64_t>(token) * a.ld_out + j + i, v[i], a.scale, a.accumulate);
     }
-    __syncthreads();
+    const float sum[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < a.cols) {
+        const float one[1] = {sum[e]};
+        put(a, static_cast<int64_t>(token) * a.ld_out + j + e, one);
+      }
   }
 }
 
@@ -464,6 +697,9 @@ cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
   return launch_lookup<Tin, __half>(a, st);
 }
 
+// Rows of zeros are written beside the sort at some 6 TB/s for as long as it takes.
+constexpr double kSortUs = 6.0, kSortUsPerToken = 0.00025, kFillBytesPerUs = 6.0e6;
+
 // Pairs of a chunk: fewer where few tokens would leave warps without work.
 int chunk_for(int64_t n, int64_t cols) {
   int chunk = 32;
@@ -471,17 +707,18 @@ int chunk_for(int64_t n, int64_t cols) {
   return chunk;
 }
 struct Work {
-  int64_t pairs0, pairs1, crossing, parts, floats;  // offsets in floats
+  int64_t pairs0, pairs1, crossing, marks, parts, floats;  // offsets in floats
   int64_t chunks, ld_parts;
 };
-Work work_for(int64_t n, int64_t cols) {
-  Work w;
+Work work_for(int64_t n, int64_t vocab, int64_t cols) {
+  Work w{};
+  if (n <= kFewTokens) return w;
   w.chunks = (n + chunk_for(n, cols) - 1) / chunk_for(n, cols);
   w.ld_parts = (cols + 3) / 4 * 4;
-  w.pairs0 = 0;
   w.pairs1 = 2 * n;
   w.crossing = 4 * n;
-  w.parts = (w.crossing + 1 + w.chunks + 3) / 4 * 4;
+  w.marks = w.crossing + 2 + 2 * w.chunks;
+  w.parts = (w.marks + (vocab + 31) / 32 + 3) / 4 * 4;
   w.floats = w.parts + 2 * w.chunks * w.ld_parts;
   return w;
 }
@@ -504,20 +741,22 @@ cudaError_t prepared_sort() {
 }
 
 template <typename T, int kStep, int kPieces>
-cudaError_t launch_runs(const RunArgs& a, int64_t chunks, cudaStream_t st) {
+cudaError_t launch_runs(const RunArgs& a, cudaStream_t st) {
+  constexpr int kCols = Slice<T, kStep, kPieces>::kCols;
+  const bool few = a.n <= kFewTokens;
   dim3 grid;
-  const cudaError_t e = grid_of(chunks * ((a.cols + 32 * kStep * kPieces - 1) / (32 * kStep * kPieces)), kRunThreads / 32, &grid);
+  const cudaError_t e = grid_of((few ? a.n : a.chunks) * static_cast<int64_t>((a.cols + kCols - 1) / kCols) + static_cast<int64_t>(a.fills) * kRunWarps,
+                                kRunWarps, &grid);
   if (e != cudaSuccess) return e;
-  return launch_pdl(runs_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), 0, st, 1, a);
+  return launch_pdl(few ? few_kernel<T, kStep, kPieces> : runs_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), 0, st, 1, a);
 }
 template <typename T>
-cudaError_t launch_runs_of(const RunArgs& a, int64_t chunks, cudaStream_t st) {
+cudaError_t launch_runs_of(const RunArgs& a, cudaStream_t st) {
   constexpr int kN = Elem<T>::N;
-  if (a.cols % kN != 0 || a.ld % kN != 0 || !aligned_to(a.grad, 16)) return launch_runs<T, 1, 16>(a, chunks, st);
-  const int pieces = a.cols / kN;
-  if (pieces > 64) return launch_runs<T, kN, 4>(a, chunks, st);
-  if (pieces > 32) return launch_runs<T, kN, 2>(a, chunks, st);
-  return launch_runs<T, kN, 1>(a, chunks, st);
+  const size_t out = static_cast<size_t>(kN) * elem_bytes(a.out_type) < 16 ? 8 : 16;
+  const bool whole = a.cols % kN == 0 && a.ld % kN == 0 && aligned_to(a.grad, 16) && aligned_to(a.out, out) && a.ld_out * elem_bytes(a.out_type) % out == 0;
+  if (!whole) return launch_runs<T, 1, 8>(a, st);
+  return a.cols / kN > 32 ? launch_runs<T, kN, 2>(a, st) : launch_runs<T, kN, 1>(a, st);
 }
 
 }  // namespace
@@ -551,7 +790,9 @@ meq_status meq_embedding(const int64_t* tokens, int64_t n, const void* table, in
   });
 }
 
-int64_t meq_embedding_work_floats(int64_t n, int64_t cols) { return n < 0 || cols < 1 ? 0 : work_for(n, cols).floats; }
+int64_t meq_embedding_work_floats(int64_t n, int64_t vocab, int64_t cols) {
+  return n < 0 || vocab < 1 || cols < 1 ? 0 : work_for(n, vocab, cols).floats + 4;
+}
 
 meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t cols, int64_t ld, const int64_t* tokens, int64_t vocab,
                               float scale, void* out, int out_type, int64_t ld_out, int accumulate, float* work, void* cuda_stream) {
@@ -574,27 +815,50 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
     if (e == cudaSuccess) e = prepared_sort();
     if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "device attributes");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const Work w = work_for(n, cols);
-    SortArgs s{};
-    s.tokens = tokens, s.n = static_cast<uint32_t>(n), s.vocab = static_cast<uint32_t>(vocab);
-    int bits = 1;  // of the largest key, vocab
-    while (bits < 32 && (vocab >> bits) != 0) ++bits;
-    s.passes = (bits + kRadixBits - 1) / kRadixBits;
-    s.bits = (bits + s.passes - 1) / s.passes;
-    s.pairs[0] = reinterpret_cast<uint2*>(work + w.pairs0), s.pairs[1] = reinterpret_cast<uint2*>(work + w.pairs1);
-    s.crossing = reinterpret_cast<uint32_t*>(work + w.crossing);
-    s.out = out, s.row_bytes = cols * elem_bytes(out_type), s.ld_bytes = ld_out * elem_bytes(out_type);
-    const int fill = accumulate ? 0 : (sms + kSortCtas - 1) / kSortCtas * kSortCtas - kSortCtas;
-    e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(kSortCtas + fill)), dim3(kSortThreads), sizeof(SortShared), st, kSortCtas, s);
-    if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
-    if (n == 0) return MEQ_OK;
+    const Work w = work_for(n, vocab, cols);
     RunArgs a{};
-    a.grad = grad, a.ld = ld, a.n = s.n, a.vocab = s.vocab, a.cols = static_cast<int>(cols), a.chunk = chunk_for(n, cols);
-    a.pairs = s.pairs[0], a.crossing = s.crossing, a.parts = work + w.parts, a.ld_parts = w.ld_parts;
+    a.grad = grad, a.ld = ld, a.n = static_cast<uint32_t>(n), a.vocab = static_cast<uint32_t>(vocab), a.cols = static_cast<int>(cols);
     a.out = out, a.ld_out = ld_out, a.out_type = out_type, a.accumulate = accumulate != 0, a.scale = scale;
-    e = type == MEQ_F32 ? launch_runs_of<float>(a, w.chunks, st) : type == MEQ_BF16 ? launch_runs_of<__nv_bfloat16>(a, w.chunks, st) : launch_runs_of<__half>(a, w.chunks, st);
-    if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sum launch");
-    e = launch_pdl(joins_kernel, dim3(static_cast<unsigned>(2 * sms)), dim3(kRunThreads), 0, st, 1, a);
+    a.row_bytes = cols * elem_bytes(out_type), a.ld_bytes = ld_out * elem_bytes(out_type);
+    if (!accumulate) {
+      a.fill_rows = static_cast<uint32_t>(a.row_bytes >= kFillBytes ? 1 : kFillBytes / a.row_bytes);
+      if (a.fill_rows > kMostFillRows) a.fill_rows = kMostFillRows;
+    }
+    if (n > kFewTokens) {
+      SortArgs s{};
+      s.tokens = tokens, s.n = a.n, s.vocab = a.vocab;
+      int bits = 1;  // of the largest key, vocab
+      while (bits < 32 && (vocab >> bits) != 0) ++bits;
+      s.passes = (bits + kRadixBits - 1) / kRadixBits;
+      s.bits = (bits + s.passes - 1) / s.passes;
+      s.pairs[0] = reinterpret_cast<uint2*>(work + w.pairs0), s.pairs[1] = reinterpret_cast<uint2*>(work + w.pairs1);
+      s.crossing = reinterpret_cast<uint32_t*>(work + w.crossing);
+      int fill = 0;
+      if (!accumulate) {
+        fill = (sms + kSortCtas - 1) / kSortCtas * kSortCtas - kSortCtas;
+        if (fill < kSortCtas) fill = kSortCtas;
+        s.out = out, s.row_bytes = a.row_bytes, s.ld_bytes = a.ld_bytes;
+        s.words = static_cast<uint32_t>((vocab + 31) / 32);
+        // what can be written while the tokens are sorted
+        const double bytes = (kSortUs + kSortUsPerToken * static_cast<double>(n)) * kFillBytesPerUs;
+        const double words = bytes / (32.0 * static_cast<double>(a.row_bytes));
+        s.first_words = words < s.words ? static_cast<uint32_t>(words) : s.words;
+        s.marks = reinterpret_cast<uint32_t*>(work + w.marks);
+        a.first_word = s.first_words, a.marks = s.marks;
+      }
+      e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(kSortCtas + fill)), dim3(kSortThreads), sizeof(SortShared), st, kSortCtas, s);
+      if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
+      a.pairs = s.pairs[0], a.crossing = s.crossing, a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
+      a.parts = work + w.parts, a.ld_parts = w.ld_parts;
+    } else {
+      a.tokens = tokens;
+    }
+    const int64_t rest = vocab - static_cast<int64_t>(a.first_word) * 32;
+    if (!accumulate && rest > 0) a.fills = static_cast<uint32_t>((rest + a.fill_rows - 1) / a.fill_rows);
+    e = type == MEQ_F32 ? launch_runs_of<float>(a, st) : type == MEQ_BF16 ? launch_runs_of<__nv_bfloat16>(a, st) : launch_runs_of<__half>(a, st);
+    if (e != cudaSuccess || n <= kFewTokens) return launch_status(e, "meq_embedding_grad", "sum launch");
+    const int64_t most = w.chunks * ((cols + 8 * kJoinCols - 1) / (8 * kJoinCols)), blocks = 8 * static_cast<int64_t>(sms);
+    e = launch_pdl(joins_kernel, dim3(static_cast<unsigned>(most < blocks ? most : blocks)), dim3(kRunThreads), 0, st, 1, a);
     return launch_status(e, "meq_embedding_grad", "join launch");
   });
 }

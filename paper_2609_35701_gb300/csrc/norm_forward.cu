@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(threads_of<T, kPieces>(), 1) row_forward_kerne
     if (++put == s.depth) put = 0;
   };
   if (s.warps > 1) clear(ex);
+  for (int i = 0; i < s.depth * matrices; ++i) p.clear_slot(mine + i * s.slot_bytes);
   pdl_wait_predecessor();
   for (int i = 0; i < s.depth - 1; ++i) copy_next();
   float2 w[H], b[H];
@@ -120,7 +121,7 @@ template <typename T, bool kOffset>
 bool launch_of(const ForwardArgs& a, int sms, cudaStream_t st, cudaError_t* e) {
   RowShape s;
   int pieces = 0;
-  if (!row_shape(a.cols, Elem<T>::N, kOffset, a.residual ? 2 : 1, &s, &pieces)) return false;
+  if (!row_shape(a.cols, Elem<T>::N, kOffset, a.residual ? 2 : 1, false, &s, &pieces)) return false;
   *e = pieces == 1   ? launch<T, 1, kOffset>(a, s, sms, st)
        : pieces == 2 ? launch<T, 2, kOffset>(a, s, sms, st)
        : pieces == 3 ? launch<T, 3, kOffset>(a, s, sms, st)

@@ -120,10 +120,16 @@ struct Place {
       else asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot + 2 * e), "h"(static_cast<uint16_t>(bits)) : "memory");
     }
   }
-  // Piece k of a row in a slot; 0 beyond the row.
+  // Zeroes a slot's pieces that no copy ever fills.
+  __device__ __forceinline__ void clear_slot(uint8_t* slot) const {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (!has(k)) reinterpret_cast<uint4*>(slot)[lane + k * lanes] = make_uint4(0, 0, 0, 0);
+  }
+  // Piece k of a row in a slot; 0 beyond the row. Rows that a warp takes alone all exist (`in`).
   __device__ __forceinline__ void read(const uint8_t* slot, int k, bool in, float2 (&x)[W]) const {
-    uint4 q = make_uint4(0, 0, 0, 0);
-    if (in && has(k)) q = reinterpret_cast<const uint4*>(slot)[lane + k * lanes];
+    uint4 q = reinterpret_cast<const uint4*>(slot)[lane + k * lanes];
+    if (kPieces == 1 && !in) q = make_uint4(0, 0, 0, 0);
     Elem<T>::unpack(q, x);
     if (part(k)) clip(k, x);
   }
@@ -240,6 +246,7 @@ __device__ __forceinline__ float2 round_pair(float2 x) {
 
 // ------------------------------------------------------------------- host
 constexpr int kMostPieces = 4;  // per thread
+constexpr int kMostHeld = 16;   // elements of a thread that keeps two sums of each and the weights in registers
 
 // Whether the rows of the matrices (NULL: none) lie in their 16 bytes alike; *offset: they do not all start there.
 template <typename T>
@@ -280,8 +287,8 @@ cudaError_t allow_ring(F* kernel) {
 inline int most_warps(int elements) { return elements > 16 ? 16 : elements > 8 ? 20 : 32; }
 
 // How rows of `cols` elements, n of them to a piece, are shared out, with `matrices` copied per row. False: they
-// are too long.
-inline bool row_shape(int64_t cols, int n, bool offset, int matrices, RowShape* s, int* pieces) {
+// are too long. two_sums: a thread keeps two sums per element.
+inline bool row_shape(int64_t cols, int n, bool offset, int matrices, bool two_sums, RowShape* s, int* pieces) {
   const int64_t units = (cols + (offset ? n - 1 : 0) + n - 1) / n;  // at most, wherever a row starts
   s->lanes = 32, s->warps = 1, *pieces = 1;
   if (units <= 16) {
@@ -292,6 +299,8 @@ inline bool row_shape(int64_t cols, int n, bool offset, int matrices, RowShape* 
     int64_t least = INT64_MAX;
     for (int k = kMostPieces; k >= 1; --k) {
       const int64_t warps = (units + 32 * k - 1) / (32 * k);
+      // 32 elements with their weights and two sums spill (8192 x 5461 bf16, backward: 143 us; 24 of them: @)
+      if (offset && two_sums && n * k > 24 && units <= 32 * 3 * most_warps(n * 3)) continue;
       if (warps > most_warps(n * k) || warps * (k + 1) >= least) continue;
       least = warps * (k + 1);
       s->warps = static_cast<int>(warps), *pieces = k;
@@ -301,7 +310,9 @@ inline bool row_shape(int64_t cols, int n, bool offset, int matrices, RowShape* 
   s->groups = most_warps(n * *pieces) / s->warps;
   if (s->warps > 1 && s->groups > 15) s->groups = 15;  // named barriers
   s->slot_bytes = s->lanes * *pieces * 16;
-  auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes <= kRingBudget; };
+  // the weights, where they lie beside the ring
+  const int weight_bytes = two_sums && !offset && n * *pieces > kMostHeld ? s->warps * s->lanes * *pieces * n * 4 : 0;
+  auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes + weight_bytes <= kRingBudget; };
   while (s->groups > 1 && !fits(2)) --s->groups;
   if (!fits(2)) return false;
   s->depth = kMostDepth;
@@ -313,11 +324,11 @@ inline unsigned blocks_for(int64_t sets, int sms, bool offset) {
   const int64_t n = sets < sms ? sets : sms;
   return static_cast<unsigned>(!offset ? n : n < sms || sms < 8 ? (n + 7) / 8 * 8 : n / 8 * 8);
 }
-inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
+__host__ __device__ inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
 
 // Shapes and launches, in files of their own. False: the rows are too long, nothing was launched.
 bool launch_row_forward(const ForwardArgs& a, int type, int sms, cudaStream_t st, cudaError_t* e);
-bool launch_row_backward(const BackwardArgs& a, int type, bool bias, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e);
+bool launch_row_backward(const BackwardArgs& a, int type, bool layer, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e);
 
 }  // namespace norm
 }  // namespace meq

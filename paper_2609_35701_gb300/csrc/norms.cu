@@ -279,7 +279,7 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
       int sms = device_sms(&e);
       if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "device attributes");
       if (sms > kMostParts) sms = kMostParts;  // what work has room for
-      if (!launch_row_backward(a, type, dbias != nullptr, sms, &parts, st, &e))
+      if (!launch_row_backward(a, type, mean || dbias, sms, &parts, st, &e))
         e = type == MEQ_F32    ? launch_wide_backward<float>(a, &parts, st)
             : type == MEQ_BF16 ? launch_wide_backward<__nv_bfloat16>(a, &parts, st)
                                : launch_wide_backward<__half>(a, &parts, st);

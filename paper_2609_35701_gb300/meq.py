@@ -200,7 +200,7 @@ def _load():
     lib.meq_layer_norm_grad.restype = I
     lib.meq_embedding.argtypes = [P, I64, P, I, I64, I64, I64, F, P, I, I64, P]
     lib.meq_embedding.restype = I
-    lib.meq_embedding_work_floats.argtypes = [I64, I64]
+    lib.meq_embedding_work_floats.argtypes = [I64, I64, I64]
     lib.meq_embedding_work_floats.restype = I64
     lib.meq_embedding_grad.argtypes = [P, I, I64, I64, I64, P, I64, F, P, I, I64, I, P, P]
     lib.meq_embedding_grad.restype = I
@@ -957,7 +957,7 @@ def embedding_grad(grad, tokens, out, scale=1.0, accumulate=False, stream=None):
     out_kind, vocab, out_cols, ld_out = _logits_args(out, "out")
     if out_cols != cols or out.get_device() != device:
         raise ValueError("out must have the gradient's columns and device")
-    work = _empty(lib.meq_embedding_work_floats(n, cols), torch.float32, grad.device, stream)
+    work = _empty(lib.meq_embedding_work_floats(n, vocab, cols), torch.float32, grad.device, stream)
     _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, float(scale), out.data_ptr(), out_kind, ld_out,
                                        int(bool(accumulate)), work.data_ptr(), _stream_handle(stream, device)))
     _written(out)

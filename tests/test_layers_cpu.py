@@ -62,7 +62,7 @@ def test_embedding_refusals(meq):
         (dict(ld=7), b"strides"), (dict(ld_out=7), b"strides"), (dict(grad=None), b"NULL"), (dict(tokens=None), b"NULL"), (dict(out=None), b"NULL"),
         (dict(work=None), b"work"), (dict(work=FAKE + 8), b"work"), (dict(grad=FAKE + 2), b"aligned"), (dict(out=FAKE + 2), b"aligned")])
     assert meq.lib.meq_embedding_grad(None, F32, 0, 8, 8, None, 10, 1.0, FAKE, F32, 8, 1, FAKE, None) == 0   # nothing to add
-    assert meq.lib.meq_embedding_work_floats(-1, 8) == 0 and meq.lib.meq_embedding_work_floats(100, 8) >= 4 * 100
+    assert meq.lib.meq_embedding_work_floats(-1, 9, 8) == 0 and meq.lib.meq_embedding_work_floats(1000, 9, 8) >= 4 * 1000
 
 
 def test_binding_refuses_host_tensors(meq):
