@@ -44,74 +44,61 @@ struct LookupArgs {
 
 // Eight consecutive elements, 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float2 (&x)[4]) {
-  const uint4* q = reinterpret_cast<const uint4*>(p);
-  Elem<T>::unpack(__ldg(q), x);
-  if (Elem<T>::N == 4) Elem<T>::unpack(__ldg(q + 1), x + 2);
-}
-template <typename T>
 __device__ __forceinline__ void store8(T* p, const float2 (&x)[4]) {
   uint4* q = reinterpret_cast<uint4*>(p);
   __stcs(q, Elem<T>::pack(x));
   if (Elem<T>::N == 4) __stcs(q + 1, Elem<T>::pack(x + 2));
 }
 
-constexpr int kLookupThreads = 256;
-constexpr int kLookupPieces = 4;   // of eight elements, per thread
+constexpr int kLookupThreads = 256, kLookupWarps = kLookupThreads / 32;
 constexpr int kLookupCols = 512;   // of a warp, element by element
 
-template <typename Tin, typename Tout, bool kPieces>
-__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a) {
+// A warp takes a segment of 32 kPieces pieces of eight elements of a token's row, or of shorter rows several, `lanes` lanes each.
+template <typename Tin, typename Tout, int kPieces>
+__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a, const int lanes, const int segments) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
   const float nan = __int_as_float(0x7fc00000);
-  if (kPieces) {
-    const uint32_t per_row = static_cast<uint32_t>(a.cols / 8);
-    const int64_t total = a.n * per_row;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * (kLookupThreads * kLookupPieces) + threadIdx.x;
-    int64_t i[kLookupPieces], t[kLookupPieces];
-    int j[kLookupPieces];
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kLookupWarps + (threadIdx.x >> 5);
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  const int64_t first = unit / segments * (32 / lanes);
+  const int64_t i = first + lane / lanes;
+  if (i >= a.n) return;
+  const int segment = static_cast<int>(unit % segments), cols = static_cast<int>(a.cols);
+  const int64_t t = a.tokens[i];
+  const bool known = t >= 0 && t < a.vocab;
+  const Tin* row = static_cast<const Tin*>(a.table) + (known ? t : 0) * a.ld_table;
+  Tout* out = static_cast<Tout*>(a.out) + i * a.ld_out;
+  const float none = t < 0 ? 0.f : nan;
+  if constexpr (kPieces > 0) {
+    constexpr int kLoads = 8 / Elem<Tin>::N;
+    const int j0 = (segment * kPieces * 32 + (lane & (lanes - 1))) * 8;
+    uint4 q[kPieces][kLoads];
 #pragma unroll
-    for (int k = 0; k < kLookupPieces; ++k) {
-      const int64_t at = first + k * kLookupThreads;
-      i[k] = at >= total ? -1 : total <= 0xffffffffll ? static_cast<int64_t>(static_cast<uint32_t>(at) / per_row) : at / per_row;
-      j[k] = static_cast<int>(at - i[k] * per_row) * 8;
-      t[k] = i[k] >= 0 ? a.tokens[i[k]] : -1;
-    }
-    float2 x[kLookupPieces][4];
+    for (int k = 0; k < kPieces; ++k) {  // every load, before the first store; those beyond the row read its start
+      const int j = j0 + 8 * lanes * k;
 #pragma unroll
-    for (int k = 0; k < kLookupPieces; ++k) {
-      if (t[k] >= 0 && t[k] < a.vocab) {
-        load8(static_cast<const Tin*>(a.table) + t[k] * a.ld_table + j[k], x[k]);
-      } else {
-        const float v = t[k] < 0 ? 0.f : nan;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[k][e] = make_float2(v, v);
-      }
+      for (int l = 0; l < kLoads; ++l) q[k][l] = __ldg(reinterpret_cast<const uint4*>(row + (j < cols ? j : 0)) + l);
     }
 #pragma unroll
-    for (int k = 0; k < kLookupPieces; ++k) {
-      if (i[k] < 0) continue;
-      if (t[k] >= 0) {  // zeros stay zeros, whatever the scale
+    for (int k = 0; k < kPieces; ++k) {
+      const int j = j0 + 8 * lanes * k;
+      float2 x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[k][e] = mul2(x[k][e], make_float2(a.scale, a.scale));
-      }
-      store8(static_cast<Tout*>(a.out) + i[k] * a.ld_out + j[k], x[k]);
+      for (int l = 0; l < kLoads; ++l) Elem<Tin>::unpack(q[k][l], x + 4 / kLoads * l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = known ? mul2(x[e], make_float2(a.scale, a.scale)) : make_float2(none, none);
+      if (j < cols) store8(out + j, x);
     }
   } else {
-    const int64_t segments = (a.cols + kLookupCols - 1) / kLookupCols;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kLookupThreads / 32) + (threadIdx.x >> 5);
-    const int64_t i = unit / segments;
-    if (i >= a.n) return;
-    const int64_t j0 = (unit - i * segments) * kLookupCols + (threadIdx.x & 31);
-    const int64_t t = a.tokens[i];
-    const bool known = t >= 0 && t < a.vocab;
-    const Tin* row = static_cast<const Tin*>(a.table) + (known ? t : 0) * a.ld_table;
-    Tout* out = static_cast<Tout*>(a.out) + i * a.ld_out;
+    const int j0 = segment * kLookupCols + lane;
+    typename Elem<Tin>::Bits q[kLookupCols / 32];
+#pragma unroll
+    for (int k = 0; k < kLookupCols / 32; ++k) q[k] = reinterpret_cast<const typename Elem<Tin>::Bits*>(row)[min(j0 + 32 * k, cols - 1)];
 #pragma unroll
     for (int k = 0; k < kLookupCols / 32; ++k) {
-      const int64_t j = j0 + 32 * k;
-      if (j < a.cols) out[j] = Elem<Tout>::make(known ? Elem<Tin>::get(row + j) * a.scale : t < 0 ? 0.f : nan);
+      const float x = Elem<Tin>::get(reinterpret_cast<const Tin*>(&q[k])) * a.scale;
+      if (j0 + 32 * k < cols) out[j0 + 32 * k] = Elem<Tout>::make(known ? x : none);
     }
   }
 }
@@ -173,19 +160,21 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
         if (i < last) pair[k] = p == 0 ? make_uint2(key_of(a.tokens[i], a.vocab), i) : __ldcg(src + i);
       }
 #pragma unroll
-      for (int k = 0; k < kSortKeys; ++k) same[k] = __ballot_sync(kFull, base + 32 * k + lane < last);
-#pragma unroll 1
-      for (int b = 0; b < a.bits; ++b) {
+      for (int k = 0; k < kSortKeys; ++k) {
+        same[k] = 0;
+        if (base + 32 * k >= last) continue;
+        const bool in = base + 32 * k + lane < last;
+        const uint32_t key = pair[k].x >> shift;
+        uint32_t m = __ballot_sync(kFull, in);
 #pragma unroll
-        for (int k = 0; k < kSortKeys; ++k) {
-          const bool on = (pair[k].x >> (shift + b)) & 1;
+        for (int b = 0; b < kRadixBits; ++b) {
+          if (b >= a.bits) break;
+          const bool on = key & (1u << b);
           const uint32_t v = __ballot_sync(kFull, on);
-          same[k] &= on ? v : ~v;
+          m &= v ^ (on ? 0u : kFull);
         }
+        if (in) same[k] = m;
       }
-#pragma unroll
-      for (int k = 0; k < kSortKeys; ++k)
-        if (base + 32 * k + lane >= last) same[k] = 0;
     };
     auto digit = [&](int k) { return (pair[k].x >> shift) & (radix - 1); };
     for (uint32_t d = lane; d < radix; d += 32) hist[d] = 0;
@@ -245,6 +234,7 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
       if (per > 32 * kSortKeys) load(base);  // else they are still there
 #pragma unroll
       for (int k = 0; k < kSortKeys; ++k) {
+        if (base + 32 * k >= last) break;
         const uint32_t at = same[k] ? hist[digit(k)] : 0;
         __syncwarp();
         if (same[k]) {
@@ -321,8 +311,9 @@ struct RunArgs {
   int cols, chunk;        // chunk: pairs of a chunk, 4 to 32
   const int64_t* tokens;  // few tokens
   const uint2* pairs;     // sorted ones
-  uint32_t* crossing;     // [0], [1]: runs with partial sums in up to, and more than, kShortParts chunks; then the chunks
-  uint32_t chunks;        // in which they start, `chunks` places for each
+  uint32_t* crossing;     // [0], [1]: runs with partial sums in up to, and more than, kShortParts chunks more
+  uint2* starts;          // the chunks in which they start, and their tokens: `chunks` places for each of the two kinds
+  uint32_t chunks;
   float* parts;           // [chunks][2][ld_parts]: sums of a run from the chunk before, of one into the next
   int64_t ld_parts;
   void* out;
@@ -408,21 +399,22 @@ struct Slice {
   __device__ __forceinline__ int col(int k) const { return j0 + 32 * kStep * k; }
   struct Row {
     uint4 q[kStep > 1 ? kPieces : 1];
-    float s[kStep > 1 ? 1 : kPieces];
+    typename Elem<T>::Bits s[kStep > 1 ? 1 : kPieces];
   };
-  __device__ __forceinline__ void load(Row& r, const T* row, bool in) const {
+  // Unconditional, so that the loads of several rows are on their way together: columns beyond the row read its start.
+  __device__ __forceinline__ void load(Row& r, const T* row) const {
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
-      const bool on = in && col(k) < cols;
-      if constexpr (kStep == 1) r.s[k] = on ? Elem<T>::get(row + col(k)) : 0.f;
-      else r.q[k] = on ? __ldcs(reinterpret_cast<const uint4*>(row + col(k))) : make_uint4(0, 0, 0, 0);
+      const int j = col(k) < cols ? col(k) : 0;
+      if constexpr (kStep == 1) r.s[k] = reinterpret_cast<const typename Elem<T>::Bits*>(row)[j];
+      else r.q[k] = __ldcs(reinterpret_cast<const uint4*>(row + j));
     }
   }
   __device__ __forceinline__ void add(const Row& r) {
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       if constexpr (kStep == 1) {
-        acc[k][0] += r.s[k];
+        acc[k][0] += Elem<T>::get(reinterpret_cast<const T*>(&r.s[k]));
       } else {
         float2 x[kStep / 2];
         Elem<T>::unpack(r.q[k], x);
@@ -531,7 +523,7 @@ __global__ void __launch_bounds__(kRunThreads) runs_kernel(const __grid_constant
     for (int u = 0; u < kAhead; ++u) {
       const int e = e0 + u;
       const uint32_t pos = e < a.chunk ? __shfl_sync(kFull, pair.y, e & 31) : __shfl_sync(kFull, next.y, (e - a.chunk) & 31);
-      s.load(r[u], grad + static_cast<int64_t>(pos) * a.ld, e < end);
+      s.load(r[u], grad + static_cast<int64_t>(pos) * a.ld);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -547,7 +539,7 @@ __global__ void __launch_bounds__(kRunThreads) runs_kernel(const __grid_constant
         if (s.j0 == 0) {
           const int64_t far = first + (kShortParts + 1) * static_cast<int64_t>(a.chunk);
           const int longer = far < a.n && a.pairs[far].x == k;
-          a.crossing[2 + longer * a.chunks + atomicAdd(&a.crossing[longer], 1u)] = static_cast<uint32_t>(c);
+          a.starts[longer * a.chunks + atomicAdd(&a.crossing[longer], 1u)] = make_uint2(static_cast<uint32_t>(c), k);
         }
       } else {
         s.finish(a, k);
@@ -601,14 +593,16 @@ __global__ void __launch_bounds__(kRunThreads) few_kernel(const __grid_constant_
     uint32_t m = q == 0 ? hits[0] : q == 1 ? hits[1] : q == 2 ? hits[2] : hits[3];
     while (m) {
       typename S::Row r[kAhead];
+      int rows = 0;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int at = 32 * q + (m ? __ffs(m) - 1 : 0);
-        s.load(r[u], static_cast<const T*>(a.grad) + static_cast<int64_t>(at) * a.ld, m != 0);
+        s.load(r[u], static_cast<const T*>(a.grad) + static_cast<int64_t>(m ? 32 * q + __ffs(m) - 1 : i) * a.ld);
+        if (m) ++rows;
         m &= m - 1;
       }
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) s.add(r[u]);
+      for (int u = 0; u < kAhead; ++u)
+        if (u < rows) s.add(r[u]);
     }
   }
   s.finish(a, static_cast<uint32_t>(token));
@@ -627,9 +621,10 @@ __global__ void __launch_bounds__(kRunThreads) joins_kernel(const __grid_constan
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const bool is_long = u < longs;
     const int64_t v = is_long ? u : u - longs, per = is_long ? narrow : wide;
-    const int64_t c = a.crossing[2 + (is_long ? a.chunks : 0) + v / per];
+    const uint2 start = a.starts[(is_long ? a.chunks : 0) + v / per];
+    const int64_t c = start.x;
+    const uint32_t token = start.y;
     const int j = static_cast<int>(is_long ? v % per : (v % per) * kRunWarps + warp) * kJoinCols + 4 * lane;
-    const uint32_t token = a.pairs[c * a.chunk + a.chunk - 1].x;
     int64_t more = 0;  // chunks after c that begin with the token
     for (;;) {
       const int64_t i = (c + 1 + more + lane) * a.chunk;
@@ -683,12 +678,16 @@ cudaError_t grid_of(int64_t units, int64_t per, dim3* grid) {
 template <typename Tin, typename Tout>
 cudaError_t launch_lookup(const LookupArgs& a, cudaStream_t st) {
   constexpr size_t kIn = 16 / sizeof(Tin), kOut = 16 / sizeof(Tout);
+  constexpr int kPieces = sizeof(Tin) == 4 ? 2 : 4;
   const bool pieces = a.cols % 8 == 0 && a.ld_table % kIn == 0 && a.ld_out % kOut == 0 && aligned_to(a.table, 16) && aligned_to(a.out, 16);
+  int lanes = 32;
+  if (pieces)
+    while (lanes > 1 && a.cols / 8 <= lanes / 2) lanes /= 2;
+  const int each = pieces ? 32 * kPieces * 8 : kLookupCols, segments = static_cast<int>((a.cols + each - 1) / each);
   dim3 grid;
-  const cudaError_t e = pieces ? grid_of(a.n * (a.cols / 8), kLookupThreads * kLookupPieces, &grid)
-                               : grid_of(a.n * ((a.cols + kLookupCols - 1) / kLookupCols), kLookupThreads / 32, &grid);
+  const cudaError_t e = grid_of((a.n + 32 / lanes - 1) / (32 / lanes) * segments, kLookupWarps, &grid);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pieces ? lookup_kernel<Tin, Tout, true> : lookup_kernel<Tin, Tout, false>, grid, dim3(kLookupThreads), 0, st, 1, a);
+  return launch_pdl(pieces ? lookup_kernel<Tin, Tout, kPieces> : lookup_kernel<Tin, Tout, 0>, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
 }
 template <typename Tin>
 cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
@@ -707,7 +706,7 @@ int chunk_for(int64_t n, int64_t cols) {
   return chunk;
 }
 struct Work {
-  int64_t pairs0, pairs1, crossing, marks, parts, floats;  // offsets in floats
+  int64_t pairs0, pairs1, starts, crossing, marks, parts, floats;  // offsets in floats
   int64_t chunks, ld_parts;
 };
 Work work_for(int64_t n, int64_t vocab, int64_t cols) {
@@ -716,8 +715,9 @@ Work work_for(int64_t n, int64_t vocab, int64_t cols) {
   w.chunks = (n + chunk_for(n, cols) - 1) / chunk_for(n, cols);
   w.ld_parts = (cols + 3) / 4 * 4;
   w.pairs1 = 2 * n;
-  w.crossing = 4 * n;
-  w.marks = w.crossing + 2 + 2 * w.chunks;
+  w.starts = 4 * n;
+  w.crossing = w.starts + 4 * w.chunks;
+  w.marks = w.crossing + 2;
   w.parts = (w.marks + (vocab + 31) / 32 + 3) / 4 * 4;
   w.floats = w.parts + 2 * w.chunks * w.ld_parts;
   return w;
@@ -848,7 +848,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       }
       e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(kSortCtas + fill)), dim3(kSortThreads), sizeof(SortShared), st, kSortCtas, s);
       if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
-      a.pairs = s.pairs[0], a.crossing = s.crossing, a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
+      a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint2*>(work + w.starts), a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
       a.parts = work + w.parts, a.ld_parts = w.ld_parts;
     } else {
       a.tokens = tokens;
