@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
 }
 
 // --------------------------------------------------------------------- sort
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kMostSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kRadixBits = 9, kRadix = 1 << kRadixBits;
 constexpr int kSortKeys = 8;                    // groups of 32 keys that a warp has in registers
 constexpr int kMarkWords = kSortWarps * kRadix; // of 32 rows each, that a block marks at a time
@@ -118,6 +118,7 @@ struct SortShared {
 struct SortArgs {
   const int64_t* tokens;
   uint32_t n, vocab;
+  uint32_t ctas;        // of the cluster that sorts
   int passes, bits;     // digits, and the bits of each
   uint2* pairs[2];      // the last pass writes pairs[0]
   uint32_t* crossing;   // the numbers of crossing runs: zeroed
@@ -139,7 +140,7 @@ __device__ __forceinline__ uint32_t key_of(int64_t t, uint32_t vocab) {
 __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
   const uint32_t rank = blockIdx.x;
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-  const uint32_t per = (a.n + kSortCtas * kSortWarps * 32 - 1) / (kSortCtas * kSortWarps * 32) * 32;
+  const uint32_t per = (a.n + a.ctas * kSortWarps * 32 - 1) / (a.ctas * kSortWarps * 32) * 32;
   const uint64_t first64 = static_cast<uint64_t>(rank * kSortWarps + warp) * per;
   const uint32_t first = first64 < a.n ? static_cast<uint32_t>(first64) : a.n;
   const uint32_t last = a.n - first < per ? a.n : first + per;
@@ -196,12 +197,15 @@ __device__ void sort_pairs(const SortArgs& a, SortShared& sh) {
     cluster_sync_all();
     uint32_t all = 0, before = 0;
     if (d < radix) {
-      uint32_t c[kSortCtas];
+      uint32_t c[kMostSortCtas];
 #pragma unroll
-      for (uint32_t r = 0; r < kSortCtas; ++r)
+      for (uint32_t r = 0; r < kMostSortCtas; ++r) {
+        c[r] = 0;
+        if (r < a.ctas)
         asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[r]) : "r"(map_to_rank(smem_u32(&sh.total[d]), r)) : "memory");
+      }
 #pragma unroll
-      for (uint32_t r = 0; r < kSortCtas; ++r) {
+      for (uint32_t r = 0; r < kMostSortCtas; ++r) {
         before += r < rank ? c[r] : 0;
         all += c[r];
       }
@@ -265,7 +269,7 @@ __device__ __forceinline__ void zero_row(uint8_t* p, int64_t bytes, int t, int t
 __device__ void zero_first_rows(const SortArgs& a, SortShared& sh) {
   uint32_t* marks = sh.hist[0];
   const int warp = static_cast<int>(threadIdx.x >> 5), lane = static_cast<int>(threadIdx.x & 31);
-  const uint32_t blocks = gridDim.x - kSortCtas, block = blockIdx.x - kSortCtas;
+  const uint32_t blocks = gridDim.x - a.ctas, block = blockIdx.x - a.ctas;
   for (uint32_t k0 = 0; block + blocks * static_cast<uint64_t>(k0) < a.words; k0 += kMarkWords) {
     const uint32_t here = min((a.words - block - blocks * k0 + blocks - 1) / blocks, static_cast<uint32_t>(kMarkWords));
     for (uint32_t i = threadIdx.x; i < here; i += kSortThreads) marks[i] = 0;
@@ -299,7 +303,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(const __grid_cons
   SortShared& sh = *reinterpret_cast<SortShared*>(smem_raw);
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  if (blockIdx.x < kSortCtas) sort_pairs(a, sh);
+  if (blockIdx.x < a.ctas) sort_pairs(a, sh);
   else zero_first_rows(a, sh);
 }
 
@@ -483,7 +487,7 @@ __device__ __forceinline__ void fill_rows(const RunArgs& a, int64_t block, F mar
 }
 
 template <typename T, int kStep, int kPieces>
-__global__ void __launch_bounds__(kRunThreads) runs_kernel(const __grid_constant__ RunArgs a) {
+__global__ void __launch_bounds__(kRunThreads, 4) runs_kernel(const __grid_constant__ RunArgs a) {
   using S = Slice<T, kStep, kPieces>;
   constexpr int kAhead = S::kAhead;
   pdl_allow_dependents();
@@ -697,12 +701,13 @@ cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
 }
 
 // Rows of zeros are written beside the sort at some 6 TB/s for as long as it takes.
-constexpr double kSortUs = 6.0, kSortUsPerToken = 0.00025, kFillBytesPerUs = 6.0e6;
+constexpr int64_t kWideSort = 16384;  // tokens above which 16 blocks sort, not 8
+constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 6.0e6;
 
 // Pairs of a chunk: fewer where few tokens would leave warps without work.
 int chunk_for(int64_t n, int64_t cols) {
   int chunk = 32;
-  while (chunk > 4 && (n + chunk - 1) / chunk * ((cols + 255) / 256) < 2432) chunk /= 2;
+  while (chunk > 4 && (n + chunk - 1) / chunk * ((cols + 255) / 256) < 9728) chunk /= 2;
   return chunk;
 }
 struct Work {
@@ -723,20 +728,38 @@ Work work_for(int64_t n, int64_t vocab, int64_t cols) {
   return w;
 }
 
-cudaError_t prepared_sort() {
+// Clusters of 8 or 16 blocks of the sort that the device holds at a time, asked once per device.
+cudaError_t prepared_sort(int ctas, int* clusters) {
   constexpr int kMaxDevices = 64;
   static std::mutex mu;
-  static bool known[kMaxDevices] = {};
+  static int known[kMaxDevices][2] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
-  if (!known[dev]) {
+  int& most = known[dev][ctas == 16];
+  if (most == 0) {
     e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SortShared)));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
-    known[dev] = true;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = sizeof(SortShared);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = static_cast<unsigned>(ctas);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, sort_kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorInvalidConfiguration;
+    most = n;
   }
+  *clusters = most;
   return cudaSuccess;
 }
 
@@ -812,7 +835,9 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
     if (n == 0 && accumulate) return MEQ_OK;
     cudaError_t e;
     const int sms = device_sms(&e);
-    if (e == cudaSuccess) e = prepared_sort();
+    const int ctas = n > kWideSort ? 16 : 8;
+    int clusters = 0;
+    if (e == cudaSuccess) e = prepared_sort(ctas, &clusters);
     if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "device attributes");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Work w = work_for(n, vocab, cols);
@@ -833,10 +858,10 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       s.bits = (bits + s.passes - 1) / s.passes;
       s.pairs[0] = reinterpret_cast<uint2*>(work + w.pairs0), s.pairs[1] = reinterpret_cast<uint2*>(work + w.pairs1);
       s.crossing = reinterpret_cast<uint32_t*>(work + w.crossing);
-      int fill = 0;
+      s.ctas = static_cast<uint32_t>(ctas);
+      if (accumulate) clusters = 1;
+      else if (clusters < 2) clusters = 2;
       if (!accumulate) {
-        fill = (sms + kSortCtas - 1) / kSortCtas * kSortCtas - kSortCtas;
-        if (fill < kSortCtas) fill = kSortCtas;
         s.out = out, s.row_bytes = a.row_bytes, s.ld_bytes = a.ld_bytes;
         s.words = static_cast<uint32_t>((vocab + 31) / 32);
         // what can be written while the tokens are sorted
@@ -846,7 +871,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
         s.marks = reinterpret_cast<uint32_t*>(work + w.marks);
         a.first_word = s.first_words, a.marks = s.marks;
       }
-      e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(kSortCtas + fill)), dim3(kSortThreads), sizeof(SortShared), st, kSortCtas, s);
+      e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(clusters * ctas)), dim3(kSortThreads), sizeof(SortShared), st, ctas, s);
       if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
       a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint2*>(work + w.starts), a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
       a.parts = work + w.parts, a.ld_parts = w.ld_parts;
