@@ -125,6 +125,7 @@ struct SortArgs {
   void* out;            // rows of tokens that do not occur are zeroed,
   int64_t row_bytes, ld_bytes;
   uint32_t words;       // 32 rows to a word of marks,
+  uint32_t per_block;   // 2^32 / blocks that zero rows, rounded up: w blocks < 2^32 for every word w, so that __umulhi(w, it) = w / blocks
   uint32_t first_words; // those of the first words here,
   uint32_t* marks;      // the others by their marks, which are written here
 };
@@ -283,8 +284,8 @@ __device__ void zero_first_rows(const SortArgs& a, SortShared& sh) {
       }
 #pragma unroll
       for (int k = 0; k < kSortKeys; ++k) {
-        const uint32_t w = key_of(t[k], kNoToken >> 1) >> 5, at = w / blocks;
-        if (t[k] >= 0 && t[k] < a.vocab && w - at * blocks == block && at - k0 < here) atomicOr(&marks[at - k0], 1u << (t[k] & 31));
+        const uint32_t w = static_cast<uint32_t>(t[k]) >> 5, at = __umulhi(w, a.per_block);
+        if (static_cast<uint64_t>(t[k]) < a.vocab && w - at * blocks == block && at - k0 < here) atomicOr(&marks[at - k0], 1u << (t[k] & 31));
       }
     }
     __syncthreads();
@@ -316,7 +317,7 @@ struct RunArgs {
   const int64_t* tokens;  // few tokens
   const uint2* pairs;     // sorted ones
   uint32_t* crossing;     // [0], [1]: runs with partial sums in up to, and more than, kShortParts chunks more
-  uint2* starts;          // the chunks in which they start, and their tokens: `chunks` places for each of the two kinds
+  uint4* starts;          // the chunks in which they start, their tokens and the chunks more: `chunks` places for each of the two kinds
   uint32_t chunks;
   float* parts;           // [chunks][2][ld_parts]: sums of a run from the chunk before, of one into the next
   int64_t ld_parts;
@@ -423,9 +424,25 @@ struct Slice {
         float2 x[kStep / 2];
         Elem<T>::unpack(r.q[k], x);
 #pragma unroll
-        for (int i = 0; i < kStep / 2; ++i) acc[k][2 * i] += x[i].x, acc[k][2 * i + 1] += x[i].y;
+        for (int i = 0; i < kStep / 2; ++i) {
+          const float2 sum = add2(make_float2(acc[k][2 * i], acc[k][2 * i + 1]), x[i]);
+          acc[k][2 * i] = sum.x, acc[k][2 * i + 1] = sum.y;
+        }
       }
     }
+  }
+  // Rows in a ring of a warp's shared memory, each lane its own pieces (kStep > 1).
+  static constexpr int kSlots = kStep > 1 ? 16 / kPieces : 1, kRingBytes = kStep > 1 ? kSlots * kPieces * 512 : 0;
+  __device__ __forceinline__ void copy(uint32_t ring, int slot, const T* row) const {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + static_cast<uint32_t>((slot * kPieces + k) * 512)),
+                   "l"(row + (col(k) < cols ? col(k) : 0))
+                   : "memory");
+  }
+  __device__ __forceinline__ void take(Row& r, const uint4* ring, int slot) const {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) r.q[k] = ring[(slot * kPieces + k) * 32];
   }
   __device__ __forceinline__ void finish(const RunArgs& a, uint32_t token) const {
     const int64_t row = static_cast<int64_t>(token) * a.ld_out;
@@ -487,7 +504,7 @@ __device__ __forceinline__ void fill_rows(const RunArgs& a, int64_t block, F mar
 }
 
 template <typename T, int kStep, int kPieces>
-__global__ void __launch_bounds__(kRunThreads, 4) runs_kernel(const __grid_constant__ RunArgs a) {
+__global__ void __launch_bounds__(kRunThreads, kStep > 1 ? 4 : 3) runs_kernel(const __grid_constant__ RunArgs a) {
   using S = Slice<T, kStep, kPieces>;
   constexpr int kAhead = S::kAhead;
   pdl_allow_dependents();
@@ -521,34 +538,73 @@ __global__ void __launch_bounds__(kRunThreads, 4) runs_kernel(const __grid_const
   S s(static_cast<int>(unit - c * slices), lane, a.cols);
   const T* grad = static_cast<const T*>(a.grad);
   auto key = [&](int e) { return e < a.chunk ? __shfl_sync(kFull, pair.x, e) : __shfl_sync(kFull, next.x, e - a.chunk); };
-  for (int e0 = begin; e0 < end; e0 += kAhead) {
-    typename S::Row r[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int e = e0 + u;
-      const uint32_t pos = e < a.chunk ? __shfl_sync(kFull, pair.y, e & 31) : __shfl_sync(kFull, next.y, (e - a.chunk) & 31);
-      s.load(r[u], grad + static_cast<int64_t>(pos) * a.ld);
+  auto row_of = [&](int e) {
+    const uint32_t pos = e < a.chunk ? __shfl_sync(kFull, pair.y, e & 31) : __shfl_sync(kFull, next.y, (e - a.chunk) & 31);
+    return grad + static_cast<int64_t>(pos) * a.ld;
+  };
+  uint32_t now = key(begin);
+  // After pair e: its run's sum, if it ends here.
+  auto end_run = [&](int e) {
+    const uint32_t k = now;
+    if (e + 1 < end) {
+      now = key(e + 1);
+      if (now == k) return;
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int e = e0 + u;
-      if (e >= end) break;
-      s.add(r[u]);
-      const uint32_t k = key(e);
-      if (e + 1 < end && key(e + 1) == k) continue;
-      if (e == part_end) {
-        s.leave(a.parts + 2 * c * a.ld_parts);
-      } else if (e == end - 1 && into_next) {
-        s.leave(a.parts + (2 * c + 1) * a.ld_parts);
-        if (s.j0 == 0) {
-          const int64_t far = first + (kShortParts + 1) * static_cast<int64_t>(a.chunk);
-          const int longer = far < a.n && a.pairs[far].x == k;
-          a.starts[longer * a.chunks + atomicAdd(&a.crossing[longer], 1u)] = make_uint2(static_cast<uint32_t>(c), k);
+    if (e == part_end) {
+      s.leave(a.parts + 2 * c * a.ld_parts);
+    } else if (e == end - 1 && into_next) {
+      s.leave(a.parts + (2 * c + 1) * a.ld_parts);
+      if (s.j0 < 32 * kStep) {  // the first slice's warp
+        // the chunks after this one that begin with the token: their partial sums belong to it
+        uint32_t more = 0;
+        for (int n = 32; n == 32; more += n) {
+          const int64_t i = first + (more + 1 + lane) * static_cast<int64_t>(a.chunk);
+          n = ones(__ballot_sync(kFull, i < a.n && a.pairs[i].x == k));
         }
-      } else {
-        s.finish(a, k);
+        if (lane == 0) {
+          const int longer = more > kShortParts;
+          a.starts[longer * a.chunks + atomicAdd(&a.crossing[longer], 1u)] = make_uint4(static_cast<uint32_t>(c), k, more, 0);
+        }
       }
-      s.clear();
+    } else {
+      s.finish(a, k);
+    }
+    s.clear();
+  };
+  if constexpr (kStep > 1) {
+    extern __shared__ __align__(16) uint8_t ring_raw[];
+    uint4* ring = reinterpret_cast<uint4*>(ring_raw + (threadIdx.x >> 5) * S::kRingBytes) + lane;
+    const uint32_t ring32 = smem_u32(ring);
+#pragma unroll 1
+    for (int u = 0; u < S::kSlots - 1; ++u) {
+      if (begin + u < end) s.copy(ring32, u, row_of(begin + u));
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    int slot = 0;
+#pragma unroll 1
+    for (int e = begin; e < end; ++e) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::kSlots - 2) : "memory");
+      typename S::Row r;
+      s.take(r, ring, slot);
+      s.add(r);
+      const int put = slot == 0 ? S::kSlots - 1 : slot - 1;  // the slot of the row before
+      if (e + S::kSlots - 1 < end) s.copy(ring32, put, row_of(e + S::kSlots - 1));
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++slot == S::kSlots) slot = 0;
+      end_run(e);
+    }
+  } else {
+#pragma unroll 1
+    for (int e0 = begin; e0 < end; e0 += kAhead) {
+      typename S::Row r[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s.load(r[u], row_of(min(e0 + u, end - 1)));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (e0 + u >= end) break;
+        s.add(r[u]);
+        end_run(e0 + u);
+      }
     }
   }
 }
@@ -625,20 +681,10 @@ __global__ void __launch_bounds__(kRunThreads) joins_kernel(const __grid_constan
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const bool is_long = u < longs;
     const int64_t v = is_long ? u : u - longs, per = is_long ? narrow : wide;
-    const uint2 start = a.starts[(is_long ? a.chunks : 0) + v / per];
-    const int64_t c = start.x;
+    const uint4 start = a.starts[(is_long ? a.chunks : 0) + v / per];
+    const int64_t c = start.x, more = start.z;
     const uint32_t token = start.y;
     const int j = static_cast<int>(is_long ? v % per : (v % per) * kRunWarps + warp) * kJoinCols + 4 * lane;
-    int64_t more = 0;  // chunks after c that begin with the token
-    for (;;) {
-      const int64_t i = (c + 1 + more + lane) * a.chunk;
-      const uint32_t others = __ballot_sync(kFull, i >= a.n || a.pairs[i].x != token);
-      if (others) {
-        more += __ffs(others) - 1;
-        break;
-      }
-      more += 32;
-    }
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* part = a.parts + j;
     if (j < a.cols) {
@@ -720,8 +766,8 @@ Work work_for(int64_t n, int64_t vocab, int64_t cols) {
   w.chunks = (n + chunk_for(n, cols) - 1) / chunk_for(n, cols);
   w.ld_parts = (cols + 3) / 4 * 4;
   w.pairs1 = 2 * n;
-  w.starts = 4 * n;
-  w.crossing = w.starts + 4 * w.chunks;
+  w.starts = (4 * n + 3) / 4 * 4;
+  w.crossing = w.starts + 8 * w.chunks;
   w.marks = w.crossing + 2;
   w.parts = (w.marks + (vocab + 31) / 32 + 3) / 4 * 4;
   w.floats = w.parts + 2 * w.chunks * w.ld_parts;
@@ -771,7 +817,11 @@ cudaError_t launch_runs(const RunArgs& a, cudaStream_t st) {
   const cudaError_t e = grid_of((few ? a.n : a.chunks) * static_cast<int64_t>((a.cols + kCols - 1) / kCols) + static_cast<int64_t>(a.fills) * kRunWarps,
                                 kRunWarps, &grid);
   if (e != cudaSuccess) return e;
-  return launch_pdl(few ? few_kernel<T, kStep, kPieces> : runs_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), 0, st, 1, a);
+  if (few) return launch_pdl(few_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), 0, st, 1, a);
+  constexpr int kRing = kRunWarps * Slice<T, kStep, kPieces>::kRingBytes;
+  const cudaError_t ready = allow_shared(runs_kernel<T, kStep, kPieces>, kRing);
+  if (ready != cudaSuccess) return ready;
+  return launch_pdl(runs_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), kRing, st, 1, a);
 }
 template <typename T>
 cudaError_t launch_runs_of(const RunArgs& a, cudaStream_t st) {
@@ -864,6 +914,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       if (!accumulate) {
         s.out = out, s.row_bytes = a.row_bytes, s.ld_bytes = a.ld_bytes;
         s.words = static_cast<uint32_t>((vocab + 31) / 32);
+        s.per_block = static_cast<uint32_t>(((uint64_t(1) << 32) + static_cast<unsigned>((clusters - 1) * ctas) - 1) / static_cast<unsigned>((clusters - 1) * ctas));
         // what can be written while the tokens are sorted
         const double bytes = (kSortUs + kSortUsPerToken * static_cast<double>(n)) * kFillBytesPerUs;
         const double words = bytes / (32.0 * static_cast<double>(a.row_bytes));
@@ -873,7 +924,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       }
       e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(clusters * ctas)), dim3(kSortThreads), sizeof(SortShared), st, ctas, s);
       if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
-      a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint2*>(work + w.starts), a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
+      a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint4*>(work + w.starts), a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
       a.parts = work + w.parts, a.ld_parts = w.ld_parts;
     } else {
       a.tokens = tokens;

@@ -2,6 +2,8 @@
 // of pointers.
 #pragma once
 
+#include <map>
+#include <mutex>
 #include <new>
 #include <string>
 
@@ -36,6 +38,26 @@ inline int device_sms(cudaError_t* e) {
   *e = cudaGetDevice(&dev);
   if (*e == cudaSuccess) *e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   return sms;
+}
+
+// Lets a kernel have more dynamic shared memory than 48 KB, once per device.
+template <typename F>
+cudaError_t allow_shared(F* kernel, int bytes) {
+  constexpr int kMaxDevices = 64;
+  static std::mutex mu;
+  static std::map<const void*, uint64_t> known;  // a bit per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  uint64_t& bits = known[reinterpret_cast<const void*>(kernel)];
+  if (!((bits >> dev) & 1)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    bits |= uint64_t(1) << dev;
+  }
+  return cudaSuccess;
 }
 
 inline bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }

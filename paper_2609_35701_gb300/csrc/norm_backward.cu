@@ -192,7 +192,7 @@ cudaError_t launch(const BackwardArgs& a, const RowShape& s, int64_t grid, cudaS
   constexpr int kElements = Elem<T>::N * kPieces;
   const int weights = kWeightsShared<kElements, kOffset, kLayer> ? s.warps * s.lanes * kElements * 4 : 0;
   auto* kernel = row_backward_kernel<T, kPieces, kOffset, kLayer>;
-  const cudaError_t e = allow_ring(kernel);
+  const cudaError_t e = allow_shared(kernel, kRingBudget);
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.dh ? 3 : 2) + weights, st,
                     1, a, s);

@@ -111,7 +111,7 @@ cudaError_t launch(const ForwardArgs& a, const RowShape& s, int sms, cudaStream_
   const int set = 32 / s.lanes;
   const int64_t sets = (a.rows + set - 1) / set;
   auto* kernel = row_forward_kernel<T, kPieces, kOffset>;
-  const cudaError_t e = allow_ring(kernel);
+  const cudaError_t e = allow_shared(kernel, kRingBudget);
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(blocks_for(sets, sms, kOffset)), dim3(32 * s.warps * s.groups), ring_bytes(s, a.residual ? 2 : 1),
                     st, 1, a, s);

@@ -19,9 +19,7 @@
 // time: 16384 x 2047 bf16 @ -> @ us.)
 #pragma once
 
-#include <map>
-#include <mutex>
-
+#include "meq_call.cuh"
 #include "meq_mbar.cuh"
 #include "norms.cuh"
 
@@ -262,26 +260,6 @@ struct Starts {
     offset = offset || b != 0 || s != 0;
   }
 };
-
-// Lets a kernel have the ring's shared memory, once per device.
-template <typename F>
-cudaError_t allow_ring(F* kernel) {
-  constexpr int kMaxDevices = 64;
-  static std::mutex mu;
-  static std::map<const void*, uint64_t> known;  // a bit per device
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-  std::lock_guard<std::mutex> lock(mu);
-  uint64_t& bits = known[reinterpret_cast<const void*>(kernel)];
-  if (!((bits >> dev) & 1)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBudget);
-    if (e != cudaSuccess) return e;
-    bits |= uint64_t(1) << dev;
-  }
-  return cudaSuccess;
-}
 
 // Warps of a block, by the registers that a thread's elements leave.
 inline int most_warps(int elements) { return elements > 16 ? 16 : elements > 8 ? 20 : 32; }

@@ -813,58 +813,97 @@ LayerNormGrad = collections.namedtuple("LayerNormGrad", "dx dweight dbias")
 RmsNormGrad = collections.namedtuple("RmsNormGrad", "dx dweight")
 
 
-def _like(t, x, what):
-    """Pointer and row stride of a matrix of x's shape, type and device (None: no matrix)."""
+def _matrix(t, dtype, shape, device, what):
+    """Pointer and row stride of a CUDA matrix of the given dtype, shape and device (None: no matrix)."""
     if t is None:
         return None, 0
-    if t.shape != x.shape or t.dtype is not x.dtype or t.device != x.device:
-        raise ValueError(f"{what} must have the shape, type and device of the first argument")
-    return t.data_ptr(), _logits_args(t, what)[3]
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        ld, step = t.stride()
+        if step == 1 and ld >= shape[1]:  # the usual case: six properties, each 0.1 us and more to ask
+            return t.data_ptr(), ld
+        return t.data_ptr(), _logits_args(t, what)[3]
+    raise ValueError(f"{what} must be a {tuple(shape)} CUDA matrix of {dtype} on cuda:{device}")
+
+
+_KINDS = {}  # meq_dtype by torch dtype, filled as they come: torch is not imported before it is used
+
+
+def _kind(t, what):
+    kind = _KINDS.get(t.dtype)
+    if kind is None:
+        kind = DTYPES.get(str(t.dtype)[6:])
+        if kind is None:
+            raise ValueError(f"{what} must be of one of {sorted(DTYPES)}")
+        _KINDS[t.dtype] = kind
+    return kind
 
 
 def _columns(t, cols, device, what, dtype=None):
     """Pointer and meq_dtype of a contiguous CUDA vector of cols elements (None: no vector)."""
     if t is None:
         return None, 0
-    kind = DTYPES.get(str(t.dtype)[6:])
-    if kind is None or (dtype is not None and t.dtype is not dtype):
-        raise ValueError(f"{what} must be of {sorted(DTYPES) if dtype is None else dtype}")
-    return _vector(t, t.dtype, cols, device, what), kind
+    kind = _kind(t, what)
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{what} must be of {dtype}")
+    if not (t.numel() == cols and t.get_device() == device and t.is_contiguous()):
+        _require_cuda(t, str(t.dtype)[6:], cols, what, device)
+    return t.data_ptr(), kind
+
+
+def _first(t, what):
+    """(meq_dtype, shape, row stride, device) of a call's first matrix, which has to be on the current device."""
+    import torch
+
+    kind, shape, device = _kind(t, what), t.shape, t.get_device()
+    if device < 0 or len(shape) != 2:
+        _logits_args(t, what)
+    if device != torch._C._cuda_getDevice():
+        _current_device(t, what)
+    ld, step = t.stride()
+    if step != 1 or ld < shape[1]:
+        ld = _logits_args(t, what)[3]
+    return kind, shape, ld, device
 
 
 def _written(*given):
     """Tensors of the caller's that were written through their pointers, which autograd does not see."""
     import torch
 
-    for t in given:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+    given = [t for t in given if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
 
 
 def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
     import torch
 
-    kind, rows, cols, ld = _logits_args(x, "x")
-    device = _current_device(x, "x")
-    r, ld_r = _like(residual, x, "residual")
+    kind, shape, ld, device = _first(x, "x")
+    rows, cols = shape
+    dtype, where, f32 = x.dtype, x.device, torch.float32
+    r, ld_r = _matrix(residual, dtype, shape, device, "residual")
     w, weight_kind = _columns(weight, cols, device, "weight")
-    b, bias_kind = _columns(bias, cols, device, "bias", None if weight is None else weight.dtype)
-    if residual is None and h is not None:
-        raise ValueError("h is written with a residual only")
+    if bias is None:
+        b = None
+    else:
+        b, weight_kind = _columns(bias, cols, device, "bias", None if weight is None else weight.dtype)
     given = y, h
-    out = _empty((rows, cols), x.dtype, x.device, stream) if y is None else y
+    if y is None:
+        y = _empty(shape, dtype, where, stream)
+    yp, ld_y = _matrix(y, dtype, shape, device, "y")
     if residual is None:
+        if h is not None:
+            raise ValueError("h is written with a residual only")
         h, hp, ld_h = x, None, 0
     else:
-        h = _empty((rows, cols), x.dtype, x.device, stream) if h is None else h
-        hp, ld_h = _like(h, x, "h")
-    yp, ld_y = _like(out, x, "y")
-    mean = _empty(rows, torch.float32, x.device, stream) if centred else None
-    rstd = _empty(rows, torch.float32, x.device, stream)
-    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, bias_kind if weight is None else weight_kind, float(eps),
-                                   yp, ld_y, hp, ld_h, mean.data_ptr() if centred else None, rstd.data_ptr(), _stream_handle(stream, device)))
+        if h is None:
+            h = _empty(shape, dtype, where, stream)
+        hp, ld_h = _matrix(h, dtype, shape, device, "h")
+    mean = _empty(rows, f32, where, stream) if centred else None
+    rstd = _empty(rows, f32, where, stream)
+    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, eps, yp, ld_y, hp, ld_h,
+                                   mean.data_ptr() if centred else None, rstd.data_ptr(), _stream_handle(stream, device)))
     _written(*given)
-    return out, h, mean, rstd
+    return y, h, mean, rstd
 
 
 def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5, y=None, h=None, stream=None):
@@ -885,26 +924,31 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, y=None, h=None, stream=Non
 def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
     import torch
 
-    kind, rows, cols, ld = _logits_args(dy, "dy")
-    device, f32 = _current_device(dy, "dy"), torch.float32
-    hp, ld_h = _like(h, dy, "h")
-    sp, ld_s = _like(dh, dy, "dh")
+    kind, shape, ld, device = _first(dy, "dy")
+    rows, cols = shape
+    dtype, where, f32 = dy.dtype, dy.device, torch.float32
+    hp, ld_h = _matrix(h, dtype, shape, device, "h")
+    sp, ld_s = _matrix(dh, dtype, shape, device, "dh")
     w, weight_kind = _columns(weight, cols, device, "weight")
     mp, rp = _vector(mean, f32, rows, device, "mean"), _vector(rstd, f32, rows, device, "rstd")
     given = dx, dweight, dbias
-    dx = _empty((rows, cols), dy.dtype, dy.device, stream) if dx is None else dx
-    xp, ld_x = _like(dx, dy, "dx")
-    shape, dtype = (cols, f32) if weight is None else (weight.shape, weight.dtype)
-    if dweight is not None or dbias is not None:
-        dtype = (dbias if dweight is None else dweight).dtype
+    if dx is None:
+        dx = _empty(shape, dtype, where, stream)
+    xp, ld_x = _matrix(dx, dtype, shape, device, "dx")
+    like = dweight if dweight is not None else dbias if dbias is not None else weight  # of whose type both are
+    grad_dtype, size = (f32, cols) if like is None else (like.dtype, like.shape)
     if dweight is None and weight is not None:
-        dweight = _empty(shape, dtype, dy.device, stream)
+        dweight = _empty(size, grad_dtype, where, stream)
     if dbias is None and bias:
-        dbias = _empty(shape, dtype, dy.device, stream)
-    (wp, grad_kind), (bp, bias_kind) = _columns(dweight, cols, device, "dweight"), _columns(dbias, cols, device, "dbias", dtype)
-    work = _empty(lib.meq_layer_norm_work_floats(rows, cols), f32, dy.device, stream)
+        dbias = _empty(size, grad_dtype, where, stream)
+    wp, grad_kind = _columns(dweight, cols, device, "dweight")
+    if dbias is None:
+        bp = None
+    else:
+        bp, grad_kind = _columns(dbias, cols, device, "dbias", grad_dtype)
+    work = _empty(lib.meq_layer_norm_work_floats(rows, cols), f32, where, stream)
     _check_call(lib.meq_layer_norm_grad(dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp,
-                                        bias_kind if dweight is None else grad_kind, work.data_ptr(), _stream_handle(stream, device)))
+                                        grad_kind, work.data_ptr(), _stream_handle(stream, device)))
     _written(*given)
     return dx, dweight, dbias
 
@@ -930,16 +974,17 @@ def embedding(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
     new one of dtype (default: the table's)."""
     import torch
 
-    table_kind, vocab, cols, ld = _logits_args(table, "table")
-    device, n = _current_device(table, "table"), tokens.numel()
+    table_kind, (vocab, cols), ld, device = _first(table, "table")
+    n = tokens.numel()
     t = _vector(tokens, torch.int64, n, device, "tokens")
     given = out
     if out is None:
         out = _empty((n, cols), table.dtype if dtype is None else dtype, table.device, stream)
-    out_kind, rows, out_cols, ld_out = _logits_args(out, "out")
-    if rows != n or out_cols != cols or out.get_device() != device or (dtype is not None and out.dtype is not dtype):
-        raise ValueError("out must have a row per token, the table's columns and its device")
-    _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, float(scale), out.data_ptr(), out_kind, ld_out,
+    elif dtype is not None and out.dtype is not dtype:
+        raise ValueError(f"out must be of {dtype}")
+    out_kind = _kind(out, "out")
+    op, ld_out = _matrix(out, out.dtype, (n, cols), device, "out")
+    _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, scale, op, out_kind, ld_out,
                                   _stream_handle(stream, device)))
     _written(given)
     return out
@@ -951,14 +996,13 @@ def embedding_grad(grad, tokens, out, scale=1.0, accumulate=False, stream=None):
     added to what out holds. Returns out."""
     import torch
 
-    kind, n, cols, ld = _logits_args(grad, "grad")
-    device = _current_device(grad, "grad")
+    kind, (n, cols), ld, device = _first(grad, "grad")
     t = _vector(tokens, torch.int64, n, device, "tokens")
-    out_kind, vocab, out_cols, ld_out = _logits_args(out, "out")
-    if out_cols != cols or out.get_device() != device:
-        raise ValueError("out must have the gradient's columns and device")
+    out_kind = _kind(out, "out")
+    vocab = out.shape[0]
+    op, ld_out = _matrix(out, out.dtype, (vocab, cols), device, "out")
     work = _empty(lib.meq_embedding_work_floats(n, vocab, cols), torch.float32, grad.device, stream)
-    _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, float(scale), out.data_ptr(), out_kind, ld_out,
-                                       int(bool(accumulate)), work.data_ptr(), _stream_handle(stream, device)))
+    _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, scale, op, out_kind, ld_out, bool(accumulate),
+                                       work.data_ptr(), _stream_handle(stream, device)))
     _written(out)
     return out
