@@ -933,7 +933,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
     if (!accumulate && rest > 0) a.fills = static_cast<uint32_t>((rest + a.fill_rows - 1) / a.fill_rows);
     e = type == MEQ_F32 ? launch_runs_of<float>(a, st) : type == MEQ_BF16 ? launch_runs_of<__nv_bfloat16>(a, st) : launch_runs_of<__half>(a, st);
     if (e != cudaSuccess || n <= kFewTokens) return launch_status(e, "meq_embedding_grad", "sum launch");
-    const int64_t most = w.chunks * ((cols + 8 * kJoinCols - 1) / (8 * kJoinCols)), blocks = 8 * static_cast<int64_t>(sms);
+    const int64_t most = w.chunks * ((cols + 8 * kJoinCols - 1) / (8 * kJoinCols)), blocks = 2 * static_cast<int64_t>(sms);
     e = launch_pdl(joins_kernel, dim3(static_cast<unsigned>(most < blocks ? most : blocks)), dim3(kRunThreads), 0, st, 1, a);
     return launch_status(e, "meq_embedding_grad", "join launch");
   });

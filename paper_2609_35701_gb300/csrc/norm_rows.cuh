@@ -147,11 +147,33 @@ struct Place {
       *reinterpret_cast<uint4*>(row + col(k)) = q;
       return;
     }
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    using Bits = typename Elem<T>::Bits;
+    // Part of 16 bytes: two, four and eight of them at a time, each at its own alignment.
+    uint8_t* p = reinterpret_cast<uint8_t*>(row + col(k));
+    const int from = k == 0 && begin < 0 ? -begin * static_cast<int>(sizeof(T)) : 0;
+    const int to = min((left - col(k)) * static_cast<int>(sizeof(T)), 16);
+    if (from > 0 && to < 16) {  // a row within 16 bytes
+      using Bits = typename Elem<T>::Bits;
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (exists(k, e)) reinterpret_cast<Bits*>(row)[col(k) + e] = static_cast<Bits>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (e % 2 * 16));
+      for (int e = 0; e < N; ++e)
+        if (exists(k, e)) reinterpret_cast<Bits*>(p)[e] = static_cast<Bits>(sizeof(T) == 4 ? w[e % 4] : w[e / 2] >> (e % 2 * 16));
+    } else if (from > 0) {
+      int at = from;
+      if (sizeof(T) == 2 && (at & 2)) {
+        *reinterpret_cast<uint16_t*>(p + at) = static_cast<uint16_t>((at & 8 ? (at & 4 ? q.w : q.z) : at & 4 ? q.y : q.x) >> 16);
+        at += 2;
+      }
+      if (at & 4) {
+        *reinterpret_cast<uint32_t*>(p + at) = at & 8 ? q.w : q.y;
+        at += 4;
+      }
+      if (at & 8) *reinterpret_cast<uint2*>(p + 8) = make_uint2(q.z, q.w);
+    } else {
+      if (to & 8) *reinterpret_cast<uint2*>(p) = make_uint2(q.x, q.y);
+      if (to & 4) *reinterpret_cast<uint32_t*>(p + (to & 8)) = to & 8 ? q.z : q.x;
+      if (sizeof(T) == 2 && (to & 2))
+        *reinterpret_cast<uint16_t*>(p + (to & 12)) = static_cast<uint16_t>(to & 8 ? (to & 4 ? q.w : q.z) : to & 4 ? q.y : q.x);
+    }
   }
   // A vector's elements at the thread's columns (0 beyond the row, `none` without a vector).
   __device__ __forceinline__ void vector(const void* v, int type, float none, float2 (&x)[H]) const {

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kWideThreads = 512;
 constexpr int kWideWarps = kWideThreads / 32;
-constexpr int kTileCols = 256;        // columns of a block of the wide rows' gradient
+constexpr int kTileThreads = 128;     // of a block of the wide rows' gradient
 constexpr int64_t kMostParts = 192;   // partial sums of a column, at most
 constexpr int64_t kPartFloats = kMostParts * 16384;
 constexpr int kFoldSlices = 32;
@@ -38,41 +38,85 @@ __device__ __forceinline__ float block_sum(float x, float* sh) {
   return s;
 }
 
-// A block per row, which it reads again for each step.
-template <typename T>
+// kStep elements from column j on: a 16-byte piece, or one.
+template <typename T, int kStep>
+__device__ __forceinline__ void load(const T* p, int64_t j, float (&x)[kStep]) {
+  if constexpr (kStep == 1) {
+    x[0] = Elem<T>::get(p + j);
+  } else {
+    float2 y[kStep / 2];
+    Elem<T>::unpack(*reinterpret_cast<const uint4*>(p + j), y);
+#pragma unroll
+    for (int e = 0; e < kStep / 2; ++e) x[2 * e] = y[e].x, x[2 * e + 1] = y[e].y;
+  }
+}
+template <typename T, int kStep>
+__device__ __forceinline__ void store(T* p, int64_t j, const float (&x)[kStep]) {
+  if constexpr (kStep == 1) {
+    p[j] = Elem<T>::make(x[0]);
+  } else {
+    float2 y[kStep / 2];
+#pragma unroll
+    for (int e = 0; e < kStep / 2; ++e) y[e] = make_float2(x[2 * e], x[2 * e + 1]);
+    *reinterpret_cast<uint4*>(p + j) = Elem<T>::pack(y);
+  }
+}
+
+// A block per row, which it reads again for each step (from L2, but for very long ones).
+template <typename T, int kStep>
 __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const ForwardArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
   __shared__ float sh[3][kWideWarps];
+  const int64_t first = threadIdx.x * kStep, step = kWideThreads * kStep;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
     T* y = static_cast<T*>(a.y) + row * a.ld_y;
-    float sum = 0.f;
+    float sum = 0.f, v[kStep];
     if (a.residual) {
       const T* r = static_cast<const T*>(a.residual) + row * a.ld_residual;
       T* h = static_cast<T*>(a.h) + row * a.ld_h;
-      for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
-        const T s = Elem<T>::make(Elem<T>::get(x + j) + Elem<T>::get(r + j));
-        h[j] = s;
-        sum += Elem<T>::get(&s);
+      for (int64_t j = first; j < a.cols; j += step) {
+        float z[kStep];
+        load(x, j, v);
+        load(r, j, z);
+#pragma unroll
+        for (int e = 0; e < kStep; ++e) {
+          const T held = Elem<T>::make(v[e] + z[e]);
+          v[e] = Elem<T>::get(&held);
+          sum += v[e];
+        }
+        store(h, j, v);
       }
       x = h;
     } else if (a.mean) {
-      for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) sum += Elem<T>::get(x + j);
+#pragma unroll 4
+      for (int64_t j = first; j < a.cols; j += step) {
+        load(x, j, v);
+#pragma unroll
+        for (int e = 0; e < kStep; ++e) sum += v[e];
+      }
     }
     const float n = static_cast<float>(a.cols);
     const float mu = a.mean ? block_sum(sum, sh[0]) / n : 0.f;
     float sq = 0.f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
-      const float d = Elem<T>::get(x + j) - mu;
-      sq = fmaf(d, d, sq);
+#pragma unroll 4
+    for (int64_t j = first; j < a.cols; j += step) {
+      load(x, j, v);
+#pragma unroll
+      for (int e = 0; e < kStep; ++e) sq = fmaf(v[e] - mu, v[e] - mu, sq);
     }
     const float rstd = inverse_root(block_sum(sq, sh[1]) / n, a.eps);
-    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
-      float v = (Elem<T>::get(x + j) - mu) * rstd;
-      if (a.weight) v *= load_as(a.weight, a.weight_type, j);
-      if (a.bias) v += load_as(a.bias, a.weight_type, j);
-      y[j] = Elem<T>::make(v);
+#pragma unroll 2
+    for (int64_t j = first; j < a.cols; j += step) {
+      load(x, j, v);
+#pragma unroll
+      for (int e = 0; e < kStep; ++e) {
+        v[e] = (v[e] - mu) * rstd;
+        if (a.weight) v[e] *= load_as(a.weight, a.weight_type, j + e);
+        if (a.bias) v[e] += load_as(a.bias, a.weight_type, j + e);
+      }
+      store(y, j, v);
     }
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mu;
@@ -83,7 +127,7 @@ __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const Forwar
 }
 
 // mean(a xhat) and mean(a) of a row per block.
-template <typename T>
+template <typename T, int kStep>
 __global__ void __launch_bounds__(kWideThreads) wide_sums_kernel(const BackwardArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
@@ -93,11 +137,17 @@ __global__ void __launch_bounds__(kWideThreads) wide_sums_kernel(const BackwardA
     const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
     const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
     float c1 = 0.f, c2 = 0.f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kWideThreads) {
-      float d = Elem<T>::get(dy + j);
-      if (a.weight) d *= load_as(a.weight, a.weight_type, j);
-      c1 = fmaf(d, (Elem<T>::get(h + j) - mu) * rstd, c1);
-      c2 += d;
+#pragma unroll 2
+    for (int64_t j = threadIdx.x * kStep; j < a.cols; j += kWideThreads * kStep) {
+      float d[kStep], x[kStep];
+      load(dy, j, d);
+      load(h, j, x);
+#pragma unroll
+      for (int e = 0; e < kStep; ++e) {
+        if (a.weight) d[e] *= load_as(a.weight, a.weight_type, j + e);
+        c1 = fmaf(d[e], (x[e] - mu) * rstd, c1);
+        c2 += d[e];
+      }
     }
     c1 = block_sum(c1, sh[0]);
     c2 = block_sum(c2, sh[1]);
@@ -110,28 +160,38 @@ __global__ void __launch_bounds__(kWideThreads) wide_sums_kernel(const BackwardA
   }
 }
 
-// A thread per column, over every gridDim.y-th row: dx, and the column's partial sums.
-template <typename T>
-__global__ void __launch_bounds__(kTileCols) wide_backward_kernel(const BackwardArgs a) {
+// A thread per kStep columns, over every gridDim.y-th row: dx, and the columns' partial sums.
+template <typename T, int kStep>
+__global__ void __launch_bounds__(kTileThreads) wide_backward_kernel(const BackwardArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * kTileCols + threadIdx.x;
+  const int64_t j = (static_cast<int64_t>(blockIdx.x) * kTileThreads + threadIdx.x) * kStep;
   if (j >= a.cols) return;
-  const float w = a.weight ? load_as(a.weight, a.weight_type, j) : 1.f;
-  float dw = 0.f, db = 0.f;
+  float w[kStep], dw[kStep], db[kStep];
+#pragma unroll
+  for (int e = 0; e < kStep; ++e) w[e] = a.weight ? load_as(a.weight, a.weight_type, j + e) : 1.f, dw[e] = db[e] = 0.f;
+#pragma unroll 2
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
-    const float d = Elem<T>::get(static_cast<const T*>(a.dy) + row * a.ld_dy + j);
-    const float xhat = (Elem<T>::get(static_cast<const T*>(a.h) + row * a.ld_h + j) - mu) * rstd;
-    dw = fmaf(d, xhat, dw);
-    db += d;
-    float dx = rstd * (fmaf(d, w, -a.row_sums[2 * row + 1]) - xhat * a.row_sums[2 * row]);
-    if (a.dh) dx += Elem<T>::get(static_cast<const T*>(a.dh) + row * a.ld_dh + j);
-    static_cast<T*>(a.dx)[row * a.ld_dx + j] = Elem<T>::make(dx);
+    const float mu = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], c1 = a.row_sums[2 * row], c2 = a.row_sums[2 * row + 1];
+    float d[kStep], x[kStep], r[kStep] = {};
+    load(static_cast<const T*>(a.dy) + row * a.ld_dy, j, d);
+    load(static_cast<const T*>(a.h) + row * a.ld_h, j, x);
+    if (a.dh) load(static_cast<const T*>(a.dh) + row * a.ld_dh, j, r);
+#pragma unroll
+    for (int e = 0; e < kStep; ++e) {
+      const float xhat = (x[e] - mu) * rstd;
+      dw[e] = fmaf(d[e], xhat, dw[e]);
+      db[e] += d[e];
+      r[e] += rstd * (fmaf(d[e], w[e], -c2) - xhat * c1);
+    }
+    store(static_cast<T*>(a.dx) + row * a.ld_dx, j, r);
   }
   if (!a.parts) return;
-  a.parts[static_cast<int64_t>(blockIdx.y) * a.cols + j] = dw;
-  a.parts[(static_cast<int64_t>(gridDim.y) + blockIdx.y) * a.cols + j] = db;
+#pragma unroll
+  for (int e = 0; e < kStep; ++e) {
+    a.parts[static_cast<int64_t>(blockIdx.y) * a.cols + j + e] = dw[e];
+    a.parts[(static_cast<int64_t>(gridDim.y) + blockIdx.y) * a.cols + j + e] = db[e];
+  }
 }
 
 // dw and db (blockIdx.y) from the partial sums, 32 columns per block. A warp takes
@@ -178,16 +238,27 @@ unsigned row_grid(int64_t rows) { return static_cast<unsigned>(rows < (1 << 30) 
 
 template <typename T>
 cudaError_t launch_wide_forward(const ForwardArgs& a, cudaStream_t st) {
-  return launch_pdl(wide_forward_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
+  Starts<T> starts;
+  starts.add(a.x, a.ld_x, a.rows), starts.add(a.y, a.ld_y, a.rows), starts.add(a.residual, a.ld_residual, a.rows), starts.add(a.h, a.ld_h, a.rows);
+  const bool whole = !starts.offset && a.cols % Elem<T>::N == 0;
+  return launch_pdl(whole ? wide_forward_kernel<T, Elem<T>::N> : wide_forward_kernel<T, 1>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
 }
 
+template <typename T, int kStep>
+cudaError_t launch_wide_backward(const BackwardArgs& a, int64_t parts, cudaStream_t st) {
+  const cudaError_t e = launch_pdl(wide_sums_kernel<T, kStep>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
+  if (e != cudaSuccess) return e;
+  constexpr int64_t cols = kTileThreads * kStep;
+  return launch_pdl(wide_backward_kernel<T, kStep>, dim3(static_cast<unsigned>((a.cols + cols - 1) / cols), static_cast<unsigned>(parts)),
+                    dim3(kTileThreads), 0, st, 1, a);
+}
 template <typename T>
 cudaError_t launch_wide_backward(const BackwardArgs& a, int64_t* parts, cudaStream_t st) {
+  Starts<T> starts;
+  starts.add(a.dy, a.ld_dy, a.rows), starts.add(a.h, a.ld_h, a.rows), starts.add(a.dh, a.ld_dh, a.rows), starts.add(a.dx, a.ld_dx, a.rows);
   *parts = parts_for(a.rows, a.cols);
-  cudaError_t e = launch_pdl(wide_sums_kernel<T>, dim3(row_grid(a.rows)), dim3(kWideThreads), 0, st, 1, a);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(wide_backward_kernel<T>, dim3(static_cast<unsigned>((a.cols + kTileCols - 1) / kTileCols), static_cast<unsigned>(*parts)),
-                    dim3(kTileCols), 0, st, 1, a);
+  if (!starts.offset && a.cols % Elem<T>::N == 0) return launch_wide_backward<T, Elem<T>::N>(a, *parts, st);
+  return launch_wide_backward<T, 1>(a, *parts, st);
 }
 
 // The checks that both calls share; an empty text: fine.
