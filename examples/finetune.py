@@ -9,9 +9,10 @@ Both objectives of a usual fine-tuning run, each a whole training step:
   2. policy: answers sampled from the model, rewarded where they follow the rule, several updates per
      batch with meq.policy_loss (clipped ratios, a KL term against the frozen copy).
 
-A step: the loss and the gradient of the logits in their place (bf16), torch's backward pass from
-there, then MeqMuon for the hidden matrices and AdamW with 8-bit moments, its gradients clipped to a
-norm, for the embedding, the head and the norm weight.
+A step: the model, its embedding (meq.embedding) and norm (meq.rms_norm) with their backward passes
+as autograd functions, the loss and the gradient of the logits in their place (bf16), torch's backward
+pass from there, then MeqMuon for the hidden matrices and AdamW with 8-bit moments, its gradients
+clipped to a norm, for the embedding, the head and the norm weight.
 """
 import argparse
 import os
@@ -22,6 +23,36 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2609_35701_gb300 import meq  # noqa: E402
+
+
+class Embedding(torch.autograd.Function):
+    """Rows of the table for the tokens; its gradient by sorted tokens, the same bits every time."""
+
+    @staticmethod
+    def forward(ctx, table, tokens):
+        ctx.save_for_backward(tokens)
+        ctx.table = table.shape, table.dtype
+        return meq.embedding(tokens, table.detach())
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        shape, dtype = ctx.table
+        return meq.embedding_grad(grad.contiguous(), *ctx.saved_tensors, torch.empty(shape, dtype=dtype, device=grad.device)), None
+
+
+class RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        r = meq.rms_norm(x.detach(), weight.detach())
+        ctx.save_for_backward(x, weight, r.rstd)
+        return r.y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, weight, rstd = ctx.saved_tensors
+        return tuple(meq.rms_norm_grad(grad.contiguous(), x, weight, rstd))
 
 
 class Model:
@@ -38,8 +69,8 @@ class Model:
 
     def logits(self, tokens):
         (gate, up, down), (embed, head, norm) = self.hidden, self.rest
-        x = embed[tokens]
-        h = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6) * norm
+        x = Embedding.apply(embed, tokens)
+        h = RmsNorm.apply(x, norm)
         x = x + (torch.nn.functional.silu(h @ gate.T) * (h @ up.T)) @ down.T
         return (x @ head.T).bfloat16()
 
