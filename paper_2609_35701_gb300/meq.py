@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import collections
 import ctypes
+import functools
 import operator
 import os
 
@@ -869,9 +870,12 @@ def _written(*given):
     """Tensors of the caller's that were written through their pointers, which autograd does not see."""
     import torch
 
-    given = [t for t in given if t is not None]
-    if given:
-        torch.autograd.graph.increment_version(given)
+    torch.autograd.graph.increment_version([t for t in given if t is not None])
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_work(rows, cols):
+    return lib.meq_layer_norm_work_floats(rows, cols)
 
 
 def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
@@ -888,21 +892,28 @@ def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
         b, weight_kind = _columns(bias, cols, device, "bias", None if weight is None else weight.dtype)
     given = y, h
     if y is None:
-        y = _empty(shape, dtype, where, stream)
-    yp, ld_y = _matrix(y, dtype, shape, device, "y")
+        y, ld_y = _empty(shape, dtype, where, stream), cols
+        yp = y.data_ptr()
+    else:
+        yp, ld_y = _matrix(y, dtype, shape, device, "y")
     if residual is None:
         if h is not None:
             raise ValueError("h is written with a residual only")
         h, hp, ld_h = x, None, 0
+    elif h is None:
+        h, ld_h = _empty(shape, dtype, where, stream), cols
+        hp = h.data_ptr()
     else:
-        if h is None:
-            h = _empty(shape, dtype, where, stream)
         hp, ld_h = _matrix(h, dtype, shape, device, "h")
-    mean = _empty(rows, f32, where, stream) if centred else None
+    mean = mp = None
+    if centred:
+        mean = _empty(rows, f32, where, stream)
+        mp = mean.data_ptr()
     rstd = _empty(rows, f32, where, stream)
-    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, eps, yp, ld_y, hp, ld_h,
-                                   mean.data_ptr() if centred else None, rstd.data_ptr(), _stream_handle(stream, device)))
-    _written(*given)
+    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, eps, yp, ld_y, hp, ld_h, mp, rstd.data_ptr(),
+                                   _stream_handle(stream, device)))
+    if given[0] is not None or given[1] is not None:
+        _written(*given)
     return y, h, mean, rstd
 
 
@@ -931,25 +942,30 @@ def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
     sp, ld_s = _matrix(dh, dtype, shape, device, "dh")
     w, weight_kind = _columns(weight, cols, device, "weight")
     mp, rp = _vector(mean, f32, rows, device, "mean"), _vector(rstd, f32, rows, device, "rstd")
-    given = dx, dweight, dbias
+    given = [t for t in (dx, dweight, dbias) if t is not None]
     if dx is None:
-        dx = _empty(shape, dtype, where, stream)
-    xp, ld_x = _matrix(dx, dtype, shape, device, "dx")
+        dx, ld_x = _empty(shape, dtype, where, stream), cols
+        xp = dx.data_ptr()
+    else:
+        xp, ld_x = _matrix(dx, dtype, shape, device, "dx")
     like = dweight if dweight is not None else dbias if dbias is not None else weight  # of whose type both are
     grad_dtype, size = (f32, cols) if like is None else (like.dtype, like.shape)
-    if dweight is None and weight is not None:
+    grad_kind, wp, bp = weight_kind if like is weight else _kind(like, "dweight"), None, None
+    if dweight is not None:
+        wp, _ = _columns(dweight, cols, device, "dweight")
+    elif weight is not None:
         dweight = _empty(size, grad_dtype, where, stream)
-    if dbias is None and bias:
+        wp = dweight.data_ptr()
+    if dbias is not None:
+        bp, _ = _columns(dbias, cols, device, "dbias", grad_dtype)
+    elif bias:
         dbias = _empty(size, grad_dtype, where, stream)
-    wp, grad_kind = _columns(dweight, cols, device, "dweight")
-    if dbias is None:
-        bp = None
-    else:
-        bp, grad_kind = _columns(dbias, cols, device, "dbias", grad_dtype)
-    work = _empty(lib.meq_layer_norm_work_floats(rows, cols), f32, where, stream)
+        bp = dbias.data_ptr()
+    work = _empty(_norm_work(rows, cols), f32, where, stream)
     _check_call(lib.meq_layer_norm_grad(dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp,
                                         grad_kind, work.data_ptr(), _stream_handle(stream, device)))
-    _written(*given)
+    if given:
+        _written(*given)
     return dx, dweight, dbias
 
 
@@ -986,7 +1002,8 @@ def embedding(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
     op, ld_out = _matrix(out, out.dtype, (n, cols), device, "out")
     _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, scale, op, out_kind, ld_out,
                                   _stream_handle(stream, device)))
-    _written(given)
+    if given is not None:
+        _written(given)
     return out
 
 
