@@ -42,18 +42,55 @@ struct LookupArgs {
   float scale;
 };
 
-// Eight consecutive elements, 16-byte aligned.
+// A lane's elements that lie together: 16 bytes of the result, since smaller stores cost more than what wider loads
+// win (fp32 into bf16, 65536 x 2048: 71 us, with 8-byte stores and 16-byte loads instead of two 83).
+template <typename Tout>
+constexpr int kTogether = 16 / static_cast<int>(sizeof(Tout));
+template <int kBytes>
+struct Words;
+struct Two {
+  uint4 a, b;
+};
+template <>
+struct Words<32> {
+  using type = Two;
+};
+template <>
+struct Words<16> {
+  using type = uint4;
+};
+template <>
+struct Words<8> {
+  using type = uint2;
+};
+template <typename T, int kN>
+using Piece = typename Words<kN * static_cast<int>(sizeof(T))>::type;
+
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const float2 (&x)[4]) {
-  uint4* q = reinterpret_cast<uint4*>(p);
-  __stcs(q, Elem<T>::pack(x));
-  if (Elem<T>::N == 4) __stcs(q + 1, Elem<T>::pack(x + 2));
+__device__ __forceinline__ void widen(uint4 q, float2* x) {
+  Elem<T>::unpack(q, x);
+}
+template <typename T>
+__device__ __forceinline__ void widen(uint2 q, float2* x) {
+  float2 y[4];
+  Elem<T>::unpack(make_uint4(q.x, q.y, 0, 0), y);
+  x[0] = y[0], x[1] = y[1];
+}
+template <typename T>
+__device__ __forceinline__ void widen(Two q, float2* x) {
+  Elem<T>::unpack(q.a, x);
+  Elem<T>::unpack(q.b, x + 2);
+}
+template <typename W>
+__device__ __forceinline__ W load_words(const W* p) {
+  if constexpr (sizeof(W) == 32) return Two{__ldg(&p->a), __ldg(&p->b)};
+  else return __ldg(p);
 }
 
 constexpr int kLookupThreads = 256, kLookupWarps = kLookupThreads / 32;
-constexpr int kLookupCols = 512;   // of a warp, element by element
+constexpr int kLookupCols = 512, kLookupFewCols = 128;  // of a warp, element by element: kPieces 0 and -1
 
-// A warp takes a segment of 32 kPieces pieces of eight elements of a token's row, or of shorter rows several, `lanes` lanes each.
+// A warp takes a segment of 32 kPieces pieces of a token's row, or of shorter rows several, `lanes` lanes each.
 template <typename Tin, typename Tout, int kPieces>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a, const int lanes, const int segments) {
   pdl_allow_dependents();
@@ -71,32 +108,31 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
   Tout* out = static_cast<Tout*>(a.out) + i * a.ld_out;
   const float none = t < 0 ? 0.f : nan;
   if constexpr (kPieces > 0) {
-    constexpr int kLoads = 8 / Elem<Tin>::N;
-    const int j0 = (segment * kPieces * 32 + (lane & (lanes - 1))) * 8;
-    uint4 q[kPieces][kLoads];
+    constexpr int kN = kTogether<Tout>;
+    const int j0 = (segment * kPieces * 32 + (lane & (lanes - 1))) * kN;
+    Piece<Tin, kN> q[kPieces];
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {  // every load, before the first store; those beyond the row read its start
-      const int j = j0 + 8 * lanes * k;
-#pragma unroll
-      for (int l = 0; l < kLoads; ++l) q[k][l] = __ldg(reinterpret_cast<const uint4*>(row + (j < cols ? j : 0)) + l);
+      const int j = j0 + kN * lanes * k;
+      q[k] = load_words(reinterpret_cast<const Piece<Tin, kN>*>(row + (j < cols ? j : 0)));
     }
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
-      const int j = j0 + 8 * lanes * k;
-      float2 x[4];
+      const int j = j0 + kN * lanes * k;
+      float2 x[kN / 2];
+      widen<Tin>(q[k], x);
 #pragma unroll
-      for (int l = 0; l < kLoads; ++l) Elem<Tin>::unpack(q[k][l], x + 4 / kLoads * l);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = known ? mul2(x[e], make_float2(a.scale, a.scale)) : make_float2(none, none);
-      if (j < cols) store8(out + j, x);
+      for (int e = 0; e < kN / 2; ++e) x[e] = known ? mul2(x[e], make_float2(a.scale, a.scale)) : make_float2(none, none);
+      if (j < cols) __stcs(reinterpret_cast<uint4*>(out + j), Elem<Tout>::pack(x));
     }
   } else {
-    const int j0 = segment * kLookupCols + lane;
-    typename Elem<Tin>::Bits q[kLookupCols / 32];
+    constexpr int kCols = kPieces == 0 ? kLookupCols : kLookupFewCols;
+    const int j0 = segment * kCols + lane;
+    typename Elem<Tin>::Bits q[kCols / 32];
 #pragma unroll
-    for (int k = 0; k < kLookupCols / 32; ++k) q[k] = reinterpret_cast<const typename Elem<Tin>::Bits*>(row)[min(j0 + 32 * k, cols - 1)];
+    for (int k = 0; k < kCols / 32; ++k) q[k] = reinterpret_cast<const typename Elem<Tin>::Bits*>(row)[min(j0 + 32 * k, cols - 1)];
 #pragma unroll
-    for (int k = 0; k < kLookupCols / 32; ++k) {
+    for (int k = 0; k < kCols / 32; ++k) {
       const float x = Elem<Tin>::get(reinterpret_cast<const Tin*>(&q[k])) * a.scale;
       if (j0 + 32 * k < cols) out[j0 + 32 * k] = Elem<Tout>::make(known ? x : none);
     }
@@ -727,17 +763,18 @@ cudaError_t grid_of(int64_t units, int64_t per, dim3* grid) {
 
 template <typename Tin, typename Tout>
 cudaError_t launch_lookup(const LookupArgs& a, cudaStream_t st) {
-  constexpr size_t kIn = 16 / sizeof(Tin), kOut = 16 / sizeof(Tout);
-  constexpr int kPieces = sizeof(Tin) == 4 ? 2 : 4;
-  const bool pieces = a.cols % 8 == 0 && a.ld_table % kIn == 0 && a.ld_out % kOut == 0 && aligned_to(a.table, 16) && aligned_to(a.out, 16);
+  constexpr int kN = kTogether<Tout>, kPieces = kN * sizeof(Tin) == 32 ? 2 : 4;
+  const bool pieces = a.cols % kN == 0 && a.ld_table % kN == 0 && a.ld_out % kN == 0 && aligned_to(a.table, kN * sizeof(Tin) > 16 ? 16 : kN * sizeof(Tin)) &&
+                      aligned_to(a.out, 16);
   int lanes = 32;
   if (pieces)
-    while (lanes > 1 && a.cols / 8 <= lanes / 2) lanes /= 2;
-  const int each = pieces ? 32 * kPieces * 8 : kLookupCols, segments = static_cast<int>((a.cols + each - 1) / each);
+    while (lanes > 1 && a.cols / kN <= lanes / 2) lanes /= 2;
+  const bool narrow = a.cols <= kLookupFewCols;
+  const int each = pieces ? 32 * kPieces * kN : narrow ? kLookupFewCols : kLookupCols, segments = static_cast<int>((a.cols + each - 1) / each);
   dim3 grid;
   const cudaError_t e = grid_of((a.n + 32 / lanes - 1) / (32 / lanes) * segments, kLookupWarps, &grid);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pieces ? lookup_kernel<Tin, Tout, kPieces> : lookup_kernel<Tin, Tout, 0>, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
+  return launch_pdl(pieces ? lookup_kernel<Tin, Tout, kPieces> : narrow ? lookup_kernel<Tin, Tout, -1> : lookup_kernel<Tin, Tout, 0>, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
 }
 template <typename Tin>
 cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
