@@ -790,7 +790,7 @@ constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 6.0e
 // Pairs of a chunk: fewer where few tokens would leave warps without work.
 int chunk_for(int64_t n, int64_t cols) {
   int chunk = 32;
-  while (chunk > 4 && (n + chunk - 1) / chunk * ((cols + 255) / 256) < 9728) chunk /= 2;
+  while (chunk > 4 && (n + chunk - 1) / chunk * ((cols + 255) / 256) < 4864) chunk /= 2;
   return chunk;
 }
 struct Work {
