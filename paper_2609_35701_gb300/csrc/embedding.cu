@@ -33,6 +33,12 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 constexpr uint32_t kNoToken = 0xffffffffu;
 
+// a / b in 32 bits where a fits: a division in 64 takes some 70 instructions, which were most of the lookup's.
+__device__ __forceinline__ int64_t divide(int64_t a, int b) {
+  if ((a >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
+
 // ------------------------------------------------------------------- lookup
 struct LookupArgs {
   const int64_t* tokens;
@@ -98,10 +104,10 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
   const float nan = __int_as_float(0x7fc00000);
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kLookupWarps + (threadIdx.x >> 5);
   const int lane = static_cast<int>(threadIdx.x & 31);
-  const int64_t first = unit / segments * (32 / lanes);
+  const int64_t group = divide(unit, segments), first = group * (32 / lanes);
   const int64_t i = first + lane / lanes;
   if (i >= a.n) return;
-  const int segment = static_cast<int>(unit % segments), cols = static_cast<int>(a.cols);
+  const int segment = static_cast<int>(unit - group * segments), cols = static_cast<int>(a.cols);
   const int64_t t = a.tokens[i];
   const bool known = t >= 0 && t < a.vocab;
   const Tin* row = static_cast<const Tin*>(a.table) + (known ? t : 0) * a.ld_table;
@@ -363,7 +369,7 @@ struct RunArgs {
   float scale;
   // rows to zero: those of the words from first_word on, `fill_rows` per block, of `fills` blocks among the others
   int64_t row_bytes, ld_bytes;
-  uint32_t first_word, fill_rows, fills;
+  uint32_t first_word, fill_rows, fills, every;
   const uint32_t* marks;
 };
 constexpr int kRunThreads = 256, kRunWarps = kRunThreads / 32;
@@ -523,11 +529,13 @@ struct Slice {
   }
 };
 
-// Whether this block zeroes rows, and its number among those that do, or among the others.
+// Whether this block zeroes rows, and its number among those that do, or among the others. Of the two kinds the one with
+// fewer blocks has every a.every-th block of the grid, as long as they last.
 __device__ __forceinline__ bool fill_block(const RunArgs& a, int64_t* index) {
-  const uint64_t before = static_cast<uint64_t>(blockIdx.x) * a.fills / gridDim.x, after = (static_cast<uint64_t>(blockIdx.x) + 1) * a.fills / gridDim.x;
-  *index = static_cast<int64_t>(after != before ? before : blockIdx.x - before);
-  return after != before;
+  const uint32_t fewer = min(a.fills, gridDim.x - a.fills), at = blockIdx.x / a.every;
+  const bool few = at < fewer && at * a.every == blockIdx.x;
+  *index = few ? at : blockIdx.x - min(fewer, at + 1);
+  return few == (a.fills <= gridDim.x - a.fills);
 }
 // Zeroes this block's rows but those marked(row, number in the block).
 template <typename F>
@@ -552,7 +560,7 @@ __global__ void __launch_bounds__(kRunThreads, kStep > 1 ? 4 : 3) runs_kernel(co
   }
   const int lane = static_cast<int>(threadIdx.x & 31);
   const int slices = (a.cols + S::kCols - 1) / S::kCols;
-  const int64_t unit = block * kRunWarps + (threadIdx.x >> 5), c = unit / slices, first = c * a.chunk;
+  const int64_t unit = block * kRunWarps + (threadIdx.x >> 5), c = divide(unit, slices), first = c * a.chunk;
   if (first >= a.n) return;
   auto pair_at = [&](int64_t i) { return i >= 0 && i < a.n ? a.pairs[i] : make_uint2(kNoToken, 0); };
   const uint2 pair = lane < a.chunk ? pair_at(first + lane) : make_uint2(kNoToken, 0);
@@ -668,7 +676,7 @@ __global__ void __launch_bounds__(kRunThreads) few_kernel(const __grid_constant_
   const int lane = static_cast<int>(threadIdx.x & 31);
   const int slices = (a.cols + S::kCols - 1) / S::kCols;
   const int64_t unit = block * kRunWarps + (threadIdx.x >> 5);
-  const int i = static_cast<int>(unit / slices);
+  const int i = static_cast<int>(divide(unit, slices));
   if (i >= static_cast<int>(a.n)) return;
   int64_t t[kEach];
 #pragma unroll
@@ -716,11 +724,11 @@ __global__ void __launch_bounds__(kRunThreads) joins_kernel(const __grid_constan
   const int64_t longs = narrow * a.crossing[1], units = longs + wide * a.crossing[0];
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const bool is_long = u < longs;
-    const int64_t v = is_long ? u : u - longs, per = is_long ? narrow : wide;
-    const uint4 start = a.starts[(is_long ? a.chunks : 0) + v / per];
+    const int64_t v = is_long ? u : u - longs, per = is_long ? narrow : wide, run = divide(v, static_cast<int>(per));
+    const uint4 start = a.starts[(is_long ? a.chunks : 0) + run];
     const int64_t c = start.x, more = start.z;
     const uint32_t token = start.y;
-    const int j = static_cast<int>(is_long ? v % per : (v % per) * kRunWarps + warp) * kJoinCols + 4 * lane;
+    const int j = static_cast<int>(is_long ? v - run * per : (v - run * per) * kRunWarps + warp) * kJoinCols + 4 * lane;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* part = a.parts + j;
     if (j < a.cols) {
@@ -847,13 +855,15 @@ cudaError_t prepared_sort(int ctas, int* clusters) {
 }
 
 template <typename T, int kStep, int kPieces>
-cudaError_t launch_runs(const RunArgs& a, cudaStream_t st) {
+cudaError_t launch_runs(RunArgs a, cudaStream_t st) {
   constexpr int kCols = Slice<T, kStep, kPieces>::kCols;
   const bool few = a.n <= kFewTokens;
   dim3 grid;
   const cudaError_t e = grid_of((few ? a.n : a.chunks) * static_cast<int64_t>((a.cols + kCols - 1) / kCols) + static_cast<int64_t>(a.fills) * kRunWarps,
                                 kRunWarps, &grid);
   if (e != cudaSuccess) return e;
+  const uint32_t others = grid.x - a.fills, fewer = others < a.fills ? others : a.fills;
+  a.every = fewer > 0 ? grid.x / fewer : grid.x;
   if (few) return launch_pdl(few_kernel<T, kStep, kPieces>, grid, dim3(kRunThreads), 0, st, 1, a);
   constexpr int kRing = kRunWarps * Slice<T, kStep, kPieces>::kRingBytes;
   const cudaError_t ready = allow_shared(runs_kernel<T, kStep, kPieces>, kRing);
