@@ -2,6 +2,14 @@
 // hold. One persistent block per SM; dy and h are read once, dx written once, and
 // the sums over rows of dy xhat and dy stay in registers until the block's last
 // row; then the block's groups are added up and leave one partial sum per column.
+//
+// Bound by HBM where rows are long and many, us (at the copy rate): RMS norm
+// 32768 x 4096 bf16 with dh 157 (161). The mean and the bias cost a quarter more
+// instructions (about 40 and 32 per element and thread of 8): layer norm 16384 x
+// 4096 76 (60), 16384 x 8192 169 (121), where only two groups share an SM and wait
+// for each other's barriers less than for their own. Small ones by the launch, the
+// first load, the groups' sums and the second launch: 8192 x 1024 17 (7.5), of
+// which 5 come after the last row.
 #include "norm_rows.cuh"
 
 namespace meq {
@@ -9,8 +17,8 @@ namespace norm {
 namespace {
 
 // The weights' place: with two sums over rows per element, 32 elements of a thread leave no registers for them (as
-// compiled with them, 91 bytes per thread were spilled and 16384 x 8192 took 226 us, @ with them in shared memory). Rows
-// that start at different places would need copies at each offset: theirs stay in registers.
+// compiled with them, 92 bytes per thread were spilled and 16384 x 8192 bf16 took 226 us; 169 with them in shared
+// memory). Rows that start at different places would need copies at each offset: theirs stay in registers.
 template <int kElements, bool kOffset, bool kLayer>
 constexpr bool kWeightsShared = kElements > kMostHeld && kLayer && !kOffset;
 

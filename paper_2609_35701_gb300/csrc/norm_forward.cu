@@ -1,5 +1,11 @@
 // Layer norm and RMS norm, forward: rows that the registers of a group of warps
 // hold. One persistent block per SM; each row is read once, written once.
+//
+// Bound by HBM where rows are long and many, us (at the copy rate): RMS norm
+// 32768 x 4096 bf16 with a residual 172 (161), layer norm 8192 x 2048 fp32 22.7
+// (20.1), 16384 x 2048 bf16 24 (20). Else by instructions, some 300 per warp and
+// row beside 45 per piece: 16384 x 2047, whose rows take three warps instead of
+// two, 39 (20); 6001 x 1025 with a residual 17 (7.4).
 #include "norm_rows.cuh"
 
 namespace meq {

@@ -16,7 +16,7 @@
 // pieces are cut at 16-byte boundaries once for all rows. Only a row's first and
 // last piece may be a part, which is stored element by element. (Pieces cut from
 // the row's start, shifted into place on the way in and out, took 2 to 3 times the
-// time: 16384 x 2047 bf16 @ -> @ us.)
+// time: 16384 x 2047 bf16 forward 52 us, 39 so; backward 151 and 73.)
 #pragma once
 
 #include "meq_call.cuh"
@@ -299,7 +299,7 @@ inline bool row_shape(int64_t cols, int n, bool offset, int matrices, bool two_s
     int64_t least = INT64_MAX;
     for (int k = kMostPieces; k >= 1; --k) {
       const int64_t warps = (units + 32 * k - 1) / (32 * k);
-      // 32 elements with their weights and two sums spill (8192 x 5461 bf16, backward: 143 us; 24 of them: @)
+      // 32 elements with their weights and two sums spill (8192 x 5461 bf16, backward: 143 us; 24 of them: 87)
       if (offset && two_sums && n * k > 24 && units <= 32 * 3 * most_warps(n * 3)) continue;
       if (warps > most_warps(n * k) || warps * (k + 1) >= least) continue;
       least = warps * (k + 1);

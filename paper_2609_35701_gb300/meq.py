@@ -910,7 +910,7 @@ def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
         mean = _empty(rows, f32, where, stream)
         mp = mean.data_ptr()
     rstd = _empty(rows, f32, where, stream)
-    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, eps, yp, ld_y, hp, ld_h, mp, rstd.data_ptr(),
+    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, float(eps), yp, ld_y, hp, ld_h, mp, rstd.data_ptr(),
                                    _stream_handle(stream, device)))
     if given[0] is not None or given[1] is not None:
         _written(*given)
@@ -1000,7 +1000,7 @@ def embedding(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
         raise ValueError(f"out must be of {dtype}")
     out_kind = _kind(out, "out")
     op, ld_out = _matrix(out, out.dtype, (n, cols), device, "out")
-    _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, scale, op, out_kind, ld_out,
+    _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, float(scale), op, out_kind, ld_out,
                                   _stream_handle(stream, device)))
     if given is not None:
         _written(given)
@@ -1019,7 +1019,7 @@ def embedding_grad(grad, tokens, out, scale=1.0, accumulate=False, stream=None):
     vocab = out.shape[0]
     op, ld_out = _matrix(out, out.dtype, (vocab, cols), device, "out")
     work = _empty(lib.meq_embedding_work_floats(n, vocab, cols), torch.float32, grad.device, stream)
-    _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, scale, op, out_kind, ld_out, bool(accumulate),
+    _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, float(scale), op, out_kind, ld_out, bool(accumulate),
                                        work.data_ptr(), _stream_handle(stream, device)))
     _written(out)
     return out

@@ -5,6 +5,10 @@ that c tokens share, a term is added at most K = min(c, 48 + c / 32) times (32 i
 least 4 in one of 8 warps, 8 warps), and the sum is scaled, and where it accumulates added, in one rounding:
   T = (K + 1) u |scale| sum|g| + u |result|, and half a step of the type.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -113,7 +117,8 @@ def test_lookup_of_no_token(meq):
 # tokens, vocab, cols, pad, shift
 GRADS = [(1, 1, 1, 0, 0), (1, 1000, 768, 0, 0), (2, 3, 8, 0, 0), (24, 32000, 96, 0, 0), (31, 40, 7, 0, 1), (33, 511, 64, 8, 0), (100, 512, 100, 0, 0),
          (257, 513, 1025, 0, 0), (1000, 30, 256, 0, 8), (1000, 50001, 33, 1, 3), (3000, 1000, 768, 0, 0), (5000, 70, 512, 0, 0), (5000, 300001, 24, 0, 0),
-         (9000, 2000, 2048, 0, 0), (40000, 10000, 40, 0, 0), (70001, 3000, 136, 0, 0)]
+         (9000, 2000, 2048, 0, 0), (40000, 10000, 40, 0, 0), (70001, 3000, 136, 0, 0),
+         (128, 90, 24, 0, 0), (129, 90, 24, 0, 0), (16384, 700, 16, 0, 0), (16385, 700, 16, 0, 0), (200001, 5000, 8, 0, 0)]
 
 
 @pytest.mark.parametrize("out_type", ["fp32", "bf16", "fp16"])
@@ -126,6 +131,11 @@ def test_gradient(meq, out_type, dtype, n, vocab, cols, pad, shift):
     version = out._version
     assert meq.embedding_grad(grad, tokens, out, scale=scale) is out and out._version > version
     _check_grad(out, grad, tokens, scale, None, out_type)
+    padded = _matrix(vocab, cols, out_type, pad=5, shift=1, fill=7.0)
+    meq.embedding_grad(grad, tokens, padded, scale=scale)
+    assert torch.equal(padded, out)
+    if vocab > 1:
+        assert bool((padded.as_strided((vocab - 1, 5), (cols + 5, 1), padded.storage_offset() + cols) == 7.0).all())
     before = _matrix(vocab, cols, out_type, pad=3, shift=1, seed=5)
     got = _matrix(vocab, cols, out_type, pad=3, shift=1, fill=7.0)
     got.copy_(before)
@@ -214,6 +224,36 @@ def test_results_repeat_and_calls_overlap(meq, n, vocab, cols):
         for graph, o, r in zip(graphs, outs, results):
             graph.replay()
             assert torch.equal(o, want[i]) and torch.equal(r, looked[i])
+
+
+CAPTURED_FIRST = """
+import sys, torch
+sys.path.insert(0, {root!r})
+from paper_2609_35701_gb300 import meq
+t = torch.randint(0, 500, (3000,), device="cuda")
+table, w = torch.randn(500, 96, device="cuda"), torch.ones(96, device="cuda")
+out = torch.empty_like(table)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    x = meq.embedding(t, table)
+    r = meq.layer_norm(x, w)
+    g = meq.layer_norm_grad(r.y, x, w, r.mean, r.rstd)
+    meq.embedding_grad(g.dx, t, out)
+graph.replay()
+torch.cuda.synchronize()
+held = out.clone()
+x = meq.embedding(t, table)
+r = meq.layer_norm(x, w)
+meq.embedding_grad(meq.layer_norm_grad(r.y, x, w, r.mean, r.rstd).dx, t, out)
+assert torch.equal(held, out) and bool(out.any())
+"""
+
+
+def test_a_process_may_begin_with_a_capture(meq):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", CAPTURED_FIRST.format(root=root)], capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def test_gradient_is_the_lookups_transpose(meq):

@@ -324,6 +324,40 @@ def test_results_repeat_and_calls_overlap(meq, cols):
             assert all(torch.equal(p, q) for p, q in zip(out, want[i]))
 
 
+@pytest.mark.parametrize("cols", [96, 1025, 4096, 17000])
+def test_rms_norm_with_a_bias(meq, cols):
+    """The C call takes a bias, and its gradient, without a mean too."""
+    rows, lib = 40, meq.lib
+    x, dy = _random(rows, cols, "bf16", 1), _random(rows, cols, "bf16", 2)
+    w, b = _vector(cols, "fp32", 3, 1.0), _vector(cols, "fp32", 4, 0.5)
+    y, dx, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda")
+    dw, db, work = torch.empty_like(w), torch.empty_like(w), torch.empty(lib.meq_layer_norm_work_floats(rows, cols), device="cuda")
+    assert lib.meq_layer_norm(x.data_ptr(), cols, None, 0, 1, rows, cols, w.data_ptr(), b.data_ptr(), 0, EPS, y.data_ptr(), cols, None, 0, None,
+                              rstd.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    _check_forward(meq.RmsNorm(y, None, rstd), _np(x), _np(w), _np(b), False, "bf16")
+    assert lib.meq_layer_norm_grad(dy.data_ptr(), cols, x.data_ptr(), cols, None, 0, 1, rows, cols, w.data_ptr(), 0, None, rstd.data_ptr(), dx.data_ptr(),
+                                   cols, dw.data_ptr(), db.data_ptr(), 0, work.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    _check_backward(meq.LayerNormGrad(dx, dw, db), _np(dy), _np(x), _np(w), None, _np(rstd), 0.0, False, "bf16", "fp32")
+    want = _np(dy).sum(0)
+    _within(_np(db), want, _round(want, (96 + rows / 100 + 1) * U * np.abs(_np(dy)).sum(0), "fp32"))
+    # dbias alone, and neither
+    other = torch.empty_like(w)
+    for out in (other.data_ptr(), None):
+        assert lib.meq_layer_norm_grad(dy.data_ptr(), cols, x.data_ptr(), cols, None, 0, 1, rows, cols, w.data_ptr(), 0, None, rstd.data_ptr(),
+                                       dx.data_ptr(), cols, None, out, 0, work.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(other, db)
+
+
+def test_numbers_of_other_kinds(meq):
+    x, w = torch.randn(3, 8, device="cuda"), torch.ones(8, device="cuda")
+    assert torch.equal(meq.rms_norm(x, w, eps=np.float32(1e-6)).y, meq.rms_norm(x, w).y)
+    t = torch.tensor([1, 2], device="cuda")
+    assert torch.equal(meq.embedding(t, x, scale=np.float64(2)), meq.embedding(t, x, scale=2))
+
+
 def test_refusals(meq):
     x, w, v = torch.zeros(4, 8, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(4, device="cuda")
     half, wide = x.half(), torch.zeros(4, 16, device="cuda")
