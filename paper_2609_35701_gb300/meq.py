@@ -851,14 +851,29 @@ def _columns(t, cols, device, what, dtype=None):
     return t.data_ptr(), kind
 
 
-def _first(t, what):
-    """(meq_dtype, shape, row stride, device) of a call's first matrix, which has to be on the current device."""
+# What the calls below use of torch, bound by the first of them: an import in every call takes longer than the lookups.
+_f32 = _i64 = _new = _raw_stream = _device_now = _increment = None
+
+
+def _bind_torch():
+    global _f32, _i64, _new, _raw_stream, _device_now, _increment
     import torch
 
-    kind, shape, device = _kind(t, what), t.shape, t.get_device()
+    _i64, _new, _raw_stream, _device_now = torch.int64, torch.empty, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _increment = torch.autograd.graph.increment_version  # of tensors that a call has written through their pointers
+    _f32 = torch.float32
+
+
+def _first(t, what):
+    """(meq_dtype, shape, row stride, device) of a call's first matrix, which has to be on the current device."""
+    if _f32 is None:
+        _bind_torch()
+    kind, shape, device = _KINDS.get(t.dtype), t.shape, t.get_device()
+    if kind is None:
+        kind = _kind(t, what)
     if device < 0 or len(shape) != 2:
         _logits_args(t, what)
-    if device != torch._C._cuda_getDevice():
+    if device != _device_now():
         _current_device(t, what)
     ld, step = t.stride()
     if step != 1 or ld < shape[1]:
@@ -866,11 +881,12 @@ def _first(t, what):
     return kind, shape, ld, device
 
 
-def _written(*given):
-    """Tensors of the caller's that were written through their pointers, which autograd does not see."""
-    import torch
+def _memory(size, dtype, device, stream):
+    return _new(size, dtype=dtype, device=device) if stream is None else _empty(size, dtype, device, stream)
 
-    torch.autograd.graph.increment_version([t for t in given if t is not None])
+
+def _stream(stream, device):
+    return _raw_stream(device) if stream is None else _stream_handle(stream)
 
 
 @functools.lru_cache(maxsize=256)
@@ -879,20 +895,18 @@ def _norm_work(rows, cols):
 
 
 def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
-    import torch
-
     kind, shape, ld, device = _first(x, "x")
     rows, cols = shape
-    dtype, where, f32 = x.dtype, x.device, torch.float32
+    dtype, where, f32 = x.dtype, x.device, _f32
     r, ld_r = _matrix(residual, dtype, shape, device, "residual")
     w, weight_kind = _columns(weight, cols, device, "weight")
     if bias is None:
         b = None
     else:
         b, weight_kind = _columns(bias, cols, device, "bias", None if weight is None else weight.dtype)
-    given = y, h
+    given = [t for t in (y, h) if t is not None]
     if y is None:
-        y, ld_y = _empty(shape, dtype, where, stream), cols
+        y, ld_y = _memory(shape, dtype, where, stream), cols
         yp = y.data_ptr()
     else:
         yp, ld_y = _matrix(y, dtype, shape, device, "y")
@@ -901,19 +915,19 @@ def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
             raise ValueError("h is written with a residual only")
         h, hp, ld_h = x, None, 0
     elif h is None:
-        h, ld_h = _empty(shape, dtype, where, stream), cols
+        h, ld_h = _memory(shape, dtype, where, stream), cols
         hp = h.data_ptr()
     else:
         hp, ld_h = _matrix(h, dtype, shape, device, "h")
     mean = mp = None
     if centred:
-        mean = _empty(rows, f32, where, stream)
+        mean = _memory(rows, f32, where, stream)
         mp = mean.data_ptr()
-    rstd = _empty(rows, f32, where, stream)
+    rstd = _memory(rows, f32, where, stream)
     _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, float(eps), yp, ld_y, hp, ld_h, mp, rstd.data_ptr(),
-                                   _stream_handle(stream, device)))
-    if given[0] is not None or given[1] is not None:
-        _written(*given)
+                                   _stream(stream, device)))
+    if given:
+        _increment(given)
     return y, h, mean, rstd
 
 
@@ -933,18 +947,16 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, y=None, h=None, stream=Non
 
 
 def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
-    import torch
-
     kind, shape, ld, device = _first(dy, "dy")
     rows, cols = shape
-    dtype, where, f32 = dy.dtype, dy.device, torch.float32
+    dtype, where, f32 = dy.dtype, dy.device, _f32
     hp, ld_h = _matrix(h, dtype, shape, device, "h")
     sp, ld_s = _matrix(dh, dtype, shape, device, "dh")
     w, weight_kind = _columns(weight, cols, device, "weight")
     mp, rp = _vector(mean, f32, rows, device, "mean"), _vector(rstd, f32, rows, device, "rstd")
     given = [t for t in (dx, dweight, dbias) if t is not None]
     if dx is None:
-        dx, ld_x = _empty(shape, dtype, where, stream), cols
+        dx, ld_x = _memory(shape, dtype, where, stream), cols
         xp = dx.data_ptr()
     else:
         xp, ld_x = _matrix(dx, dtype, shape, device, "dx")
@@ -954,18 +966,18 @@ def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
     if dweight is not None:
         wp, _ = _columns(dweight, cols, device, "dweight")
     elif weight is not None:
-        dweight = _empty(size, grad_dtype, where, stream)
+        dweight = _memory(size, grad_dtype, where, stream)
         wp = dweight.data_ptr()
     if dbias is not None:
         bp, _ = _columns(dbias, cols, device, "dbias", grad_dtype)
     elif bias:
-        dbias = _empty(size, grad_dtype, where, stream)
+        dbias = _memory(size, grad_dtype, where, stream)
         bp = dbias.data_ptr()
-    work = _empty(_norm_work(rows, cols), f32, where, stream)
+    work = _memory(_norm_work(rows, cols), f32, where, stream)
     _check_call(lib.meq_layer_norm_grad(dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp,
-                                        grad_kind, work.data_ptr(), _stream_handle(stream, device)))
+                                        grad_kind, work.data_ptr(), _stream(stream, device)))
     if given:
-        _written(*given)
+        _increment(given)
     return dx, dweight, dbias
 
 
@@ -974,6 +986,8 @@ def layer_norm_grad(dy, h, weight, mean, rstd, dh=None, dx=None, dweight=None, d
     of y and the h, mean and rstd of its result. dh: a gradient of h to add; dx,
     dweight, dbias: tensors to write (dx may be dy, h or dh), else new ones, of the
     weight's type; bias False: no bias. dx is the gradient of x and of the residual."""
+    if mean is None:
+        raise ValueError("mean must be given: without it the norm is rms_norm's")
     return LayerNormGrad(*_norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream))
 
 
@@ -988,22 +1002,20 @@ def embedding(tokens, table, scale=1.0, out=None, dtype=None, stream=None):
     (meq_embedding). tokens: contiguous int64 CUDA tensor, negative for rows of
     zeros; table: CUDA matrix, fp32, bf16 or fp16; out: the matrix to write, else a
     new one of dtype (default: the table's)."""
-    import torch
-
     table_kind, (vocab, cols), ld, device = _first(table, "table")
     n = tokens.numel()
-    t = _vector(tokens, torch.int64, n, device, "tokens")
+    t = _vector(tokens, _i64, n, device, "tokens")
     given = out
     if out is None:
-        out = _empty((n, cols), table.dtype if dtype is None else dtype, table.device, stream)
+        out = _memory((n, cols), table.dtype if dtype is None else dtype, table.device, stream)
     elif dtype is not None and out.dtype is not dtype:
         raise ValueError(f"out must be of {dtype}")
     out_kind = _kind(out, "out")
     op, ld_out = _matrix(out, out.dtype, (n, cols), device, "out")
     _check_call(lib.meq_embedding(t, n, table.data_ptr(), table_kind, vocab, cols, ld, float(scale), op, out_kind, ld_out,
-                                  _stream_handle(stream, device)))
+                                  _stream(stream, device)))
     if given is not None:
-        _written(given)
+        _increment(given)
     return out
 
 
@@ -1011,15 +1023,13 @@ def embedding_grad(grad, tokens, out, scale=1.0, accumulate=False, stream=None):
     """The gradient of the table into out, a matrix of the table's shape
     (meq_embedding_grad), from the gradient of embedding's result. accumulate:
     added to what out holds. Returns out."""
-    import torch
-
     kind, (n, cols), ld, device = _first(grad, "grad")
-    t = _vector(tokens, torch.int64, n, device, "tokens")
+    t = _vector(tokens, _i64, n, device, "tokens")
     out_kind = _kind(out, "out")
     vocab = out.shape[0]
     op, ld_out = _matrix(out, out.dtype, (vocab, cols), device, "out")
-    work = _empty(lib.meq_embedding_work_floats(n, vocab, cols), torch.float32, grad.device, stream)
+    work = _memory(lib.meq_embedding_work_floats(n, vocab, cols), _f32, grad.device, stream)
     _check_call(lib.meq_embedding_grad(grad.data_ptr(), kind, n, cols, ld, t, vocab, float(scale), op, out_kind, ld_out, bool(accumulate),
-                                       work.data_ptr(), _stream_handle(stream, device)))
-    _written(out)
+                                       work.data_ptr(), _stream(stream, device)))
+    _increment(out)
     return out

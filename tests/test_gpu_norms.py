@@ -368,7 +368,7 @@ def test_refusals(meq):
            lambda: meq.layer_norm(wide[:, ::2], w), lambda: meq.layer_norm_grad(x, half, w, v, v), lambda: meq.layer_norm_grad(x, x, w, v[:2], v),
            lambda: meq.layer_norm_grad(x, x, w, v, v.double()), lambda: meq.layer_norm_grad(x, x, w, v, v, dh=x[:2]),
            lambda: meq.layer_norm_grad(x, x, w, v, v, dx=half), lambda: meq.layer_norm_grad(x, x, w, v, v, dweight=w.half()[:4]),
-           lambda: meq.layer_norm_grad(x, x, w, v, v, dweight=w.clone(), dbias=w.half())]
+           lambda: meq.layer_norm_grad(x, x, w, v, v, dweight=w.clone(), dbias=w.half()), lambda: meq.layer_norm_grad(x, x, w, None, v)]
     for i, call in enumerate(bad):
         with pytest.raises(ValueError):
             call()
