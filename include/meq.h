@@ -520,7 +520,9 @@ meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64
  * stream's later uses add to it.
  * x, residual, y, h, dy, dh, dx: device, rows x cols of meq_dtype `type`,
  *   consecutive columns, rows ld_* elements apart (>= cols); rows may start at
- *   any element. Fastest where all start at multiples of 16 bytes.
+ *   any element. Fastest where all start at multiples of 16 bytes, next where
+ *   the rows of all matrices lie in their 16 bytes alike (start and stride
+ *   leave the same rest), as they do when allocated alike.
  * weight, bias: device, cols elements of weight_type (NULL: 1 and 0).
  * mean, rstd: device, rows floats. mean NULL selects RMS norm, in both calls.
  * In place: y may be x or the residual, h may be x or the residual (not what y

@@ -118,7 +118,7 @@ def test_lookup_of_no_token(meq):
 GRADS = [(1, 1, 1, 0, 0), (1, 1000, 768, 0, 0), (2, 3, 8, 0, 0), (24, 32000, 96, 0, 0), (31, 40, 7, 0, 1), (33, 511, 64, 8, 0), (100, 512, 100, 0, 0),
          (257, 513, 1025, 0, 0), (1000, 30, 256, 0, 8), (1000, 50001, 33, 1, 3), (3000, 1000, 768, 0, 0), (5000, 70, 512, 0, 0), (5000, 300001, 24, 0, 0),
          (9000, 2000, 2048, 0, 0), (40000, 10000, 40, 0, 0), (70001, 3000, 136, 0, 0),
-         (128, 90, 24, 0, 0), (129, 90, 24, 0, 0), (16384, 700, 16, 0, 0), (16385, 700, 16, 0, 0), (200001, 5000, 8, 0, 0)]
+         (128, 90, 24, 0, 0), (129, 90, 24, 0, 0), (255, 400, 1032, 0, 0), (256, 60, 24, 0, 0), (257, 400, 24, 0, 0), (16384, 700, 16, 0, 0), (16385, 700, 16, 0, 0), (200001, 5000, 8, 0, 0)]
 
 
 @pytest.mark.parametrize("out_type", ["fp32", "bf16", "fp16"])
@@ -146,7 +146,7 @@ def test_gradient(meq, out_type, dtype, n, vocab, cols, pad, shift):
 
 
 @pytest.mark.parametrize("how", ["one", "distinct", "two", "none"])
-@pytest.mark.parametrize("n,cols", [(5, 16), (128, 96), (1000, 1025), (4096, 264), (30000, 64), (100000, 8)])
+@pytest.mark.parametrize("n,cols", [(5, 16), (128, 96), (256, 40), (250, 33), (257, 40), (1000, 1025), (4096, 264), (30000, 64), (100000, 8)])
 def test_gradient_of_runs(meq, how, n, cols):
     """One token everywhere, each once, two long runs, none at all."""
     vocab = max(n, 700)
