@@ -545,7 +545,8 @@ __device__ __forceinline__ void fill_rows(const RunArgs& a, int64_t block, F mar
   const int rows = static_cast<int>(min(static_cast<int64_t>(a.fill_rows), static_cast<int64_t>(a.vocab) - row0));
   const int threads = a.fill_rows >= kRunWarps ? 32 : kRunThreads;  // of a row
   for (int r = static_cast<int>(threadIdx.x) / threads; r < rows; r += kRunThreads / threads)
-    if (!marked(row0 + r, r)) zero_row(static_cast<uint8_t*>(a.out) + (row0 + r) * a.ld_bytes, a.row_bytes, static_cast<int>(threadIdx.x) % threads, threads);
+    if (!marked(row0 + r, r))
+      zero_row(static_cast<uint8_t*>(a.out) + (row0 + r) * a.ld_bytes, a.row_bytes, static_cast<int>(threadIdx.x) % threads, threads);
 }
 
 template <typename T, int kStep, int kPieces>
@@ -802,8 +803,8 @@ cudaError_t grid_of(int64_t units, int64_t per, dim3* grid) {
 template <typename Tin, typename Tout>
 cudaError_t launch_lookup(const LookupArgs& a, cudaStream_t st) {
   constexpr int kN = kTogether<Tout>, kPieces = kN * sizeof(Tin) == 32 ? 2 : 4;
-  const bool pieces = a.cols % kN == 0 && a.ld_table % kN == 0 && a.ld_out % kN == 0 && aligned_to(a.table, kN * sizeof(Tin) > 16 ? 16 : kN * sizeof(Tin)) &&
-                      aligned_to(a.out, 16);
+  const size_t in = kN * sizeof(Tin) > 16 ? 16 : kN * sizeof(Tin);
+  const bool pieces = a.cols % kN == 0 && a.ld_table % kN == 0 && a.ld_out % kN == 0 && aligned_to(a.table, in) && aligned_to(a.out, 16);
   int lanes = 32;
   if (pieces)
     while (lanes > 1 && a.cols / kN <= lanes / 2) lanes /= 2;
@@ -812,7 +813,8 @@ cudaError_t launch_lookup(const LookupArgs& a, cudaStream_t st) {
   dim3 grid;
   const cudaError_t e = grid_of((a.n + 32 / lanes - 1) / (32 / lanes) * segments, kLookupWarps, &grid);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pieces ? lookup_kernel<Tin, Tout, kPieces> : narrow ? lookup_kernel<Tin, Tout, -1> : lookup_kernel<Tin, Tout, 0>, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
+  auto* kernel = pieces ? lookup_kernel<Tin, Tout, kPieces> : narrow ? lookup_kernel<Tin, Tout, -1> : lookup_kernel<Tin, Tout, 0>;
+  return launch_pdl(kernel, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
 }
 template <typename Tin>
 cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
@@ -821,11 +823,14 @@ cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
   return launch_lookup<Tin, __half>(a, st);
 }
 
+// Tokens above which 16 blocks sort, not 8, us: 8192 16.7 with 8, 16.1 with 16, 16384 18.9 and 18.1, 32768 22.7 and 20.5,
+// 65536 32.6 and 25.3, 131072 74 and 36 (launch and event 6 of them); 16 leave fewer SMs that can hold a cluster to zero rows.
+constexpr int64_t kWideSort = 16384;
 // Rows of zeros are written beside the sort at some 6 TB/s for as long as it takes.
-constexpr int64_t kWideSort = 16384;  // tokens above which 16 blocks sort, not 8
 constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 6.0e6;
 
-// Pairs of a chunk: fewer where few tokens would leave warps without work.
+// Pairs of a chunk: fewer where few tokens would leave warps without work (6000 x 1001 accumulating 28 us, from 1216 units
+// on 36; larger calls within 5% from 1216 to 9728).
 int chunk_for(int64_t n, int64_t cols) {
   int chunk = 32;
   while (chunk > 4 && (n + chunk - 1) / chunk * ((cols + 255) / 256) < 4864) chunk /= 2;
@@ -889,8 +894,8 @@ cudaError_t launch_runs(RunArgs a, cudaStream_t st) {
   constexpr int kCols = Slice<T, kStep, kPieces>::kCols;
   const bool few = a.n <= kFewTokens;
   dim3 grid;
-  const cudaError_t e = grid_of((few ? a.n : a.chunks) * static_cast<int64_t>((a.cols + kCols - 1) / kCols) + static_cast<int64_t>(a.fills) * kRunWarps,
-                                kRunWarps, &grid);
+  const int64_t slices = (a.cols + kCols - 1) / kCols;
+  const cudaError_t e = grid_of((few ? a.n : a.chunks) * slices + static_cast<int64_t>(a.fills) * kRunWarps, kRunWarps, &grid);
   if (e != cudaSuccess) return e;
   const uint32_t others = grid.x - a.fills, fewer = others < a.fills ? others : a.fills;
   a.every = fewer > 0 ? grid.x / fewer : grid.x;
@@ -904,7 +909,8 @@ template <typename T>
 cudaError_t launch_runs_of(const RunArgs& a, cudaStream_t st) {
   constexpr int kN = Elem<T>::N;
   const size_t out = static_cast<size_t>(kN) * elem_bytes(a.out_type) < 16 ? 8 : 16;
-  const bool whole = a.cols % kN == 0 && a.ld % kN == 0 && aligned_to(a.grad, 16) && aligned_to(a.out, out) && a.ld_out * elem_bytes(a.out_type) % out == 0;
+  const bool whole = a.cols % kN == 0 && a.ld % kN == 0 && aligned_to(a.grad, 16) && aligned_to(a.out, out) &&
+                     a.ld_out * elem_bytes(a.out_type) % out == 0;
   if (!whole) return launch_runs<T, 1, 8>(a, st);
   return a.cols / kN > 32 ? launch_runs<T, kN, 2>(a, st) : launch_runs<T, kN, 1>(a, st);
 }
@@ -991,7 +997,8 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       if (!accumulate) {
         s.out = out, s.row_bytes = a.row_bytes, s.ld_bytes = a.ld_bytes;
         s.words = static_cast<uint32_t>((vocab + 31) / 32);
-        s.per_block = static_cast<uint32_t>(((uint64_t(1) << 32) + static_cast<unsigned>((clusters - 1) * ctas) - 1) / static_cast<unsigned>((clusters - 1) * ctas));
+        const uint64_t fill = static_cast<uint64_t>((clusters - 1) * ctas);
+        s.per_block = static_cast<uint32_t>(((uint64_t(1) << 32) + fill - 1) / fill);
         // what can be written while the tokens are sorted
         const double bytes = (kSortUs + kSortUsPerToken * static_cast<double>(n)) * kFillBytesPerUs;
         const double words = bytes / (32.0 * static_cast<double>(a.row_bytes));
@@ -1001,7 +1008,8 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       }
       e = launch_pdl(sort_kernel, dim3(static_cast<unsigned>(clusters * ctas)), dim3(kSortThreads), sizeof(SortShared), st, ctas, s);
       if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "sort launch");
-      a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint4*>(work + w.starts), a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
+      a.pairs = s.pairs[0], a.crossing = s.crossing, a.starts = reinterpret_cast<uint4*>(work + w.starts);
+      a.chunk = chunk_for(n, cols), a.chunks = static_cast<uint32_t>(w.chunks);
       a.parts = work + w.parts, a.ld_parts = w.ld_parts;
     } else {
       a.tokens = tokens;

@@ -4,12 +4,11 @@
 // row; then the block's groups are added up and leave one partial sum per column.
 //
 // Bound by HBM where rows are long and many, us (at the copy rate): RMS norm
-// 32768 x 4096 bf16 with dh 157 (161). The mean and the bias cost a quarter more
-// instructions (about 40 and 32 per element and thread of 8): layer norm 16384 x
-// 4096 76 (60), 16384 x 8192 169 (121), where only two groups share an SM and wait
-// for each other's barriers less than for their own. Small ones by the launch, the
-// first load, the groups' sums and the second launch: 8192 x 1024 17 (7.5), of
-// which 5 come after the last row.
+// 32768 x 4096 bf16 with dh 157 (161). The mean and the bias take 680 instructions
+// for 480 per warp and row of 1024 columns: layer norm 16384 x 4096 77 (60), 16384
+// x 8192 169 (121), where two groups of eight warps share an SM. Small ones by the
+// launch, the first load, the groups' sums and the second launch: 8192 x 1024 17
+// (7.5), of which 5 come after the last row.
 #include "norm_rows.cuh"
 
 namespace meq {
@@ -28,7 +27,8 @@ constexpr int threads_of() {
 }
 
 template <typename T, int kPieces, bool kOffset, bool kLayer>
-__global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1) row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
+__global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1)
+    row_backward_kernel(const __grid_constant__ BackwardArgs a, const RowShape s) {
   using P = Place<T, kPieces, kOffset>;
   constexpr int H = P::H, W = P::W;
   constexpr bool kShared = kWeightsShared<2 * H, kOffset, kLayer>;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1) row_bac
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
 #pragma unroll
-        for (int e = 0; e < W; e += 2) w_at[(k * W + e) / 2 * 32] = make_float4(v[k * W + e].x, v[k * W + e].y, v[k * W + e + 1].x, v[k * W + e + 1].y);
+        for (int e = k * W; e < (k + 1) * W; e += 2) w_at[e / 2 * 32] = make_float4(v[e].x, v[e].y, v[e + 1].x, v[e + 1].y);
     }
     __syncthreads();
   } else {
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1) row_bac
     if (!in) continue;
     T* dx = p.at(a.dx, row, a.ld_dx);
     // dx = rstd a - rstd mean(a) - (h - mu) rstd^2 mean(a xhat)
-    const float s1 = -now.y * now.y * (c[0] * per), s2 = kLayer && a.mean ? -now.y * (c[kLayer ? 1 : 0] * per) : 0.f;
+    // (rstd last: its square overflows where eps is tiny and the row constant)
+    const float s1 = -now.y * (now.y * (c[0] * per)), s2 = kLayer && a.mean ? -now.y * (c[kLayer ? 1 : 0] * per) : 0.f;
     const float2 m1 = make_float2(s1, s1), m2 = make_float2(s2, s2);
     // dy and h once more from shared memory: kept in registers they would leave no room for the sums.
 #pragma unroll

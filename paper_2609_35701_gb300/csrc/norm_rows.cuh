@@ -28,7 +28,6 @@ namespace norm {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kMostDepth = 4;
-constexpr int kMostWarps = 32;
 constexpr int kRingBudget = 220 * 1024;
 
 struct RowShape {
@@ -213,8 +212,7 @@ struct Place {
 };
 
 __device__ __forceinline__ void group_barrier(const RowShape& s, int group) {
-  if (s.warps == 1) __syncwarp();
-  else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * s.warps) : "memory");
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * s.warps) : "memory");
 }
 
 __device__ __forceinline__ void clear(Exchange& ex) {
@@ -268,7 +266,7 @@ __device__ __forceinline__ float2 round_pair(float2 x) {
 constexpr int kMostPieces = 4;  // per thread
 constexpr int kMostHeld = 16;   // elements of a thread that keeps two sums of each and the weights in registers
 
-// Whether the rows of the matrices (NULL: none) lie in their 16 bytes alike; *offset: they do not all start there.
+// Whether the rows of the matrices (NULL: none) lie in their 16 bytes alike; offset: they do not all start there.
 template <typename T>
 struct Starts {
   bool alike = true, offset = false;
@@ -312,7 +310,9 @@ inline bool row_shape(int64_t cols, int n, bool offset, int matrices, bool two_s
   s->slot_bytes = s->lanes * *pieces * 16;
   // the weights, where they lie beside the ring
   const int weight_bytes = two_sums && !offset && n * *pieces > kMostHeld ? s->warps * s->lanes * *pieces * n * 4 : 0;
-  auto fits = [&](int depth) { return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes + weight_bytes <= kRingBudget; };
+  auto fits = [&](int depth) {
+    return static_cast<int64_t>(s->groups) * s->warps * (32 / s->lanes) * depth * matrices * s->slot_bytes + weight_bytes <= kRingBudget;
+  };
   while (s->groups > 1 && !fits(2)) --s->groups;
   if (!fits(2)) return false;
   s->depth = kMostDepth;
@@ -324,7 +324,9 @@ inline unsigned blocks_for(int64_t sets, int sms, bool offset) {
   const int64_t n = sets < sms ? sets : sms;
   return static_cast<unsigned>(!offset ? n : n < sms || sms < 8 ? (n + 7) / 8 * 8 : n / 8 * 8);
 }
-__host__ __device__ inline int ring_bytes(const RowShape& s, int matrices) { return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes; }
+__host__ __device__ inline int ring_bytes(const RowShape& s, int matrices) {
+  return s.groups * s.warps * (32 / s.lanes) * s.depth * matrices * s.slot_bytes;
+}
 
 // Shapes and launches, in files of their own. False: the rows are too long, nothing was launched.
 bool launch_row_forward(const ForwardArgs& a, int type, int sms, cudaStream_t st, cudaError_t* e);

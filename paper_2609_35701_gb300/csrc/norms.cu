@@ -300,7 +300,8 @@ meq_status meq_layer_norm(const void* x, int64_t ld_x, const void* residual, int
     if (why.empty() && h && h == y) why = "y and h must not be the same";
     if (why.empty() && !(eps > 0.f && eps <= FLT_MAX)) why = "eps must be finite and > 0";
     if (why.empty() && rows > 0 && !rstd) why = "rstd must not be NULL";
-    if (why.empty() && !(aligned_to(weight, elem_bytes(weight_type)) && aligned_to(bias, elem_bytes(weight_type)) && aligned_to(mean, 4) && aligned_to(rstd, 4)))
+    if (why.empty() && !(aligned_to(weight, elem_bytes(weight_type)) && aligned_to(bias, elem_bytes(weight_type)) && aligned_to(mean, 4) &&
+                         aligned_to(rstd, 4)))
       why = "a pointer is not aligned to its type";
     if (!why.empty()) return fail(MEQ_ERR_INVALID_ARG, "meq_layer_norm: " + why);
     if (rows == 0) return MEQ_OK;

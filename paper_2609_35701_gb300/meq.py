@@ -924,8 +924,8 @@ def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
         mean = _memory(rows, f32, where, stream)
         mp = mean.data_ptr()
     rstd = _memory(rows, f32, where, stream)
-    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, float(eps), yp, ld_y, hp, ld_h, mp, rstd.data_ptr(),
-                                   _stream(stream, device)))
+    _check_call(lib.meq_layer_norm(x.data_ptr(), ld, r, ld_r, kind, rows, cols, w, b, weight_kind, float(eps), yp, ld_y, hp, ld_h, mp,
+                                   rstd.data_ptr(), _stream(stream, device)))
     if given:
         _increment(given)
     return y, h, mean, rstd

@@ -238,6 +238,17 @@ def test_unusual_rows(meq, cols):
     assert bool(g.dx[whole].isfinite().all()) and bool(g.dweight.isnan().all()) and bool(g.dbias.isfinite().all())
 
 
+def test_constant_rows_and_a_tiny_eps(meq):
+    """rstd up to 1e22: its square overflows, the gradient of a constant row, which is rstd (a - mean a), need not."""
+    for cols in (96, 1025, 17000):
+        x, dy, w = torch.full((4, cols), 2.0, device="cuda"), _random(4, cols, "fp32", 1), torch.ones(cols, device="cuda")
+        x[1] = 0.0
+        r = meq.layer_norm(x, w, eps=1e-44)
+        assert bool((r.y[1] == 0).all()) and bool(r.rstd[1].isfinite())
+        g = meq.layer_norm_grad(dy, x, w, r.mean, r.rstd)
+        assert bool(g.dx[1].isfinite().all()) and bool(g.dx[1].any())
+
+
 def test_options(meq):
     """No weight, no bias, given outputs of other types, no rows."""
     for cols in (96, 1025, 17000):
