@@ -96,51 +96,60 @@ __device__ __forceinline__ W load_words(const W* p) {
 constexpr int kLookupThreads = 256, kLookupWarps = kLookupThreads / 32;
 constexpr int kLookupCols = 512, kLookupFewCols = 128;  // of a warp, element by element: kPieces 0 and -1
 
-// A warp takes a segment of 32 kPieces pieces of a token's row, or of shorter rows several, `lanes` lanes each.
-template <typename Tin, typename Tout, int kPieces>
+// A warp takes a segment of 32 kPieces pieces of kTokens tokens' rows, or of shorter rows as many times 32 / lanes, `lanes`
+// lanes each.
+template <typename Tin, typename Tout, int kPieces, int kTokens>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a, const int lanes, const int segments) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
   const float nan = __int_as_float(0x7fc00000);
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kLookupWarps + (threadIdx.x >> 5);
-  const int lane = static_cast<int>(threadIdx.x & 31);
-  const int64_t group = divide(unit, segments), first = group * (32 / lanes);
-  const int64_t i = first + lane / lanes;
-  if (i >= a.n) return;
+  const int lane = static_cast<int>(threadIdx.x & 31), sets = 32 / lanes;
+  const int64_t group = divide(unit, segments), first = group * (sets * kTokens) + lane / lanes;
+  if (first >= a.n) return;
   const int segment = static_cast<int>(unit - group * segments), cols = static_cast<int>(a.cols);
-  const int64_t t = a.tokens[i];
-  const bool known = t >= 0 && t < a.vocab;
-  const Tin* row = static_cast<const Tin*>(a.table) + (known ? t : 0) * a.ld_table;
-  Tout* out = static_cast<Tout*>(a.out) + i * a.ld_out;
-  const float none = t < 0 ? 0.f : nan;
+  int64_t t[kTokens];
+#pragma unroll
+  for (int u = 0; u < kTokens; ++u) t[u] = first + u * sets < a.n ? a.tokens[first + u * sets] : -1;
+  auto known = [&](int u) { return t[u] >= 0 && t[u] < a.vocab; };
+  auto row = [&](int u) { return static_cast<const Tin*>(a.table) + (known(u) ? t[u] : 0) * a.ld_table; };
+  auto out = [&](int u) { return static_cast<Tout*>(a.out) + (first + u * sets) * a.ld_out; };
+  auto none = [&](int u) { return t[u] < 0 ? 0.f : nan; };
   if constexpr (kPieces > 0) {
     constexpr int kN = kTogether<Tout>;
     const int j0 = (segment * kPieces * 32 + (lane & (lanes - 1))) * kN;
-    Piece<Tin, kN> q[kPieces];
+    Piece<Tin, kN> q[kTokens][kPieces];
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {  // every load, before the first store; those beyond the row read its start
-      const int j = j0 + kN * lanes * k;
-      q[k] = load_words(reinterpret_cast<const Piece<Tin, kN>*>(row + (j < cols ? j : 0)));
+    for (int u = 0; u < kTokens; ++u) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {  // every load, before the first store; those beyond the row read its start
+        const int j = j0 + kN * lanes * k;
+        q[u][k] = load_words(reinterpret_cast<const Piece<Tin, kN>*>(row(u) + (j < cols ? j : 0)));
+      }
     }
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-      const int j = j0 + kN * lanes * k;
-      float2 x[kN / 2];
-      widen<Tin>(q[k], x);
+    for (int u = 0; u < kTokens; ++u) {
+      if (u > 0 && first + u * sets >= a.n) break;
 #pragma unroll
-      for (int e = 0; e < kN / 2; ++e) x[e] = known ? mul2(x[e], make_float2(a.scale, a.scale)) : make_float2(none, none);
-      if (j < cols) __stcs(reinterpret_cast<uint4*>(out + j), Elem<Tout>::pack(x));
+      for (int k = 0; k < kPieces; ++k) {
+        const int j = j0 + kN * lanes * k;
+        float2 x[kN / 2];
+        widen<Tin>(q[u][k], x);
+#pragma unroll
+        for (int e = 0; e < kN / 2; ++e) x[e] = known(u) ? mul2(x[e], make_float2(a.scale, a.scale)) : make_float2(none(u), none(u));
+        if (j < cols) __stcs(reinterpret_cast<uint4*>(out(u) + j), Elem<Tout>::pack(x));
+      }
     }
   } else {
     constexpr int kCols = kPieces == 0 ? kLookupCols : kLookupFewCols;
     const int j0 = segment * kCols + lane;
     typename Elem<Tin>::Bits q[kCols / 32];
 #pragma unroll
-    for (int k = 0; k < kCols / 32; ++k) q[k] = reinterpret_cast<const typename Elem<Tin>::Bits*>(row)[min(j0 + 32 * k, cols - 1)];
+    for (int k = 0; k < kCols / 32; ++k) q[k] = reinterpret_cast<const typename Elem<Tin>::Bits*>(row(0))[min(j0 + 32 * k, cols - 1)];
 #pragma unroll
     for (int k = 0; k < kCols / 32; ++k) {
       const float x = Elem<Tin>::get(reinterpret_cast<const Tin*>(&q[k])) * a.scale;
-      if (j0 + 32 * k < cols) out[j0 + 32 * k] = Elem<Tout>::make(known ? x : none);
+      if (j0 + 32 * k < cols) out(0)[j0 + 32 * k] = Elem<Tout>::make(known(0) ? x : none(0));
     }
   }
 }
@@ -802,18 +811,27 @@ cudaError_t grid_of(int64_t units, int64_t per, dim3* grid) {
 
 template <typename Tin, typename Tout>
 cudaError_t launch_lookup(const LookupArgs& a, cudaStream_t st) {
-  constexpr int kN = kTogether<Tout>, kPieces = kN * sizeof(Tin) == 32 ? 2 : 4;
+  constexpr int kN = kTogether<Tout>, kMost = kN * sizeof(Tin) == 32 ? 2 : 4;
   const size_t in = kN * sizeof(Tin) > 16 ? 16 : kN * sizeof(Tin);
   const bool pieces = a.cols % kN == 0 && a.ld_table % kN == 0 && a.ld_out % kN == 0 && aligned_to(a.table, in) && aligned_to(a.out, 16);
-  int lanes = 32;
-  if (pieces)
+  // A warp has kMost pieces per lane under way: of one token, or where a token needs fewer of two or four.
+  int lanes = 32, each = 1, segments = 1;
+  auto* kernel = lookup_kernel<Tin, Tout, kMost, 1>;
+  if (pieces) {
     while (lanes > 1 && a.cols / kN <= lanes / 2) lanes /= 2;
-  const bool narrow = a.cols <= kLookupFewCols;
-  const int each = pieces ? 32 * kPieces * kN : narrow ? kLookupFewCols : kLookupCols, segments = static_cast<int>((a.cols + each - 1) / each);
+    const int64_t need = (a.cols / kN + 31) / 32;
+    if (need == 1) kernel = lookup_kernel<Tin, Tout, 1, kMost>, each = kMost;
+    else if (need == 2 && kMost == 4) kernel = lookup_kernel<Tin, Tout, 2, 2>, each = 2;
+    else segments = static_cast<int>((need + kMost - 1) / kMost);
+  } else {
+    const bool narrow = a.cols <= kLookupFewCols;
+    kernel = narrow ? lookup_kernel<Tin, Tout, -1, 1> : lookup_kernel<Tin, Tout, 0, 1>;
+    segments = narrow ? 1 : static_cast<int>((a.cols + kLookupCols - 1) / kLookupCols);
+  }
+  const int64_t tokens = 32 / lanes * each;
   dim3 grid;
-  const cudaError_t e = grid_of((a.n + 32 / lanes - 1) / (32 / lanes) * segments, kLookupWarps, &grid);
+  const cudaError_t e = grid_of((a.n + tokens - 1) / tokens * segments, kLookupWarps, &grid);
   if (e != cudaSuccess) return e;
-  auto* kernel = pieces ? lookup_kernel<Tin, Tout, kPieces> : narrow ? lookup_kernel<Tin, Tout, -1> : lookup_kernel<Tin, Tout, 0>;
   return launch_pdl(kernel, grid, dim3(kLookupThreads), 0, st, 1, a, lanes, segments);
 }
 template <typename Tin>
