@@ -844,8 +844,9 @@ cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
 // Tokens above which 16 blocks sort, not 8, us: 8192 16.7 with 8, 16.1 with 16, 16384 18.9 and 18.1, 32768 22.7 and 20.5,
 // 65536 32.6 and 25.3, 131072 74 and 36 (launch and event 6 of them); 16 leave fewer SMs that can hold a cluster to zero rows.
 constexpr int64_t kWideSort = 16384;
-// Rows of zeros are written beside the sort at some 6 TB/s for as long as it takes.
-constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 6.0e6;
+// Rows are zeroed beside the sort for as long as it takes, at the rate here; the others beside the sums. At 0, 1.5, 3, 4.5
+// and 6 TB/s, us: 65536 tokens into 151936 x 4096 bf16 290, 286, 282, 282, 284, 8192 into 32000 x 768 fp32 37, 35, 33, 32, 31.
+constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 4.5e6;
 
 // Pairs of a chunk: fewer where few tokens would leave warps without work (6000 x 1001 accumulating 28 us, from 1216 units
 // on 36; larger calls within 5% from 1216 to 9728).
