@@ -540,7 +540,10 @@ int64_t meq_layer_norm_work_floats(int64_t rows, int64_t cols);
 /* dh: NULL, or added to dx. dweight, dbias: NULL, or device, cols elements of
  * grad_type, overwritten (zeros for no rows). work: device scratch of
  * meq_layer_norm_work_floats floats, 16-byte aligned, free again when the
- * enqueued kernels have run. */
+ * enqueued kernels have run. Up to 65536 elements it may be NULL: a call that
+ * needs it all the same (rows of the matrices that lie in their 16 bytes
+ * differently, or too long for a block) is MEQ_ERR_INVALID_ARG, and nothing is
+ * enqueued. */
 meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, const void* dh, int64_t ld_dh, int type,
                                int64_t rows, int64_t cols, const void* weight, int weight_type, const float* mean, const float* rstd,
                                void* dx, int64_t ld_dx, void* dweight, void* dbias, int grad_type, float* work, void* cuda_stream);

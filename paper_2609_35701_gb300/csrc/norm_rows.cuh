@@ -264,6 +264,7 @@ __device__ __forceinline__ float2 round_pair(float2 x) {
 
 // ------------------------------------------------------------------- host
 constexpr int kMostPieces = 4;  // per thread
+constexpr int kMostCluster = 8; // blocks that add up the sums over few rows among themselves
 constexpr int kMostHeld = 16;   // elements of a thread that keeps two sums of each and the weights in registers
 
 // Whether the rows of the matrices (NULL: none) lie in their 16 bytes alike; offset: they do not all start there.
@@ -331,6 +332,8 @@ __host__ __device__ inline int ring_bytes(const RowShape& s, int matrices) {
 // Shapes and launches, in files of their own. False: the rows are too long, nothing was launched.
 bool launch_row_forward(const ForwardArgs& a, int type, int sms, cudaStream_t st, cudaError_t* e);
 bool launch_row_backward(const BackwardArgs& a, int type, bool layer, int sms, int64_t* parts, cudaStream_t st, cudaError_t* e);
+// The same on few rows by one cluster, which writes dweight and dbias.
+bool launch_few_backward(const BackwardArgs& a, int type, bool layer, cudaStream_t st, cudaError_t* e);
 
 }  // namespace norm
 }  // namespace meq

@@ -25,6 +25,10 @@ constexpr int kTileThreads = 128;     // of a block of the wide rows' gradient
 constexpr int64_t kMostParts = 192;   // partial sums of a column, at most
 constexpr int64_t kPartFloats = kMostParts * 16384;
 constexpr int kFoldSlices = 32;
+// Up to so many elements one cluster takes the rows and adds up the sums over them itself: a launch less, which takes the
+// host as long as the rows take the GPU (24 x 768 fp32: 3.4 us on the GPU for 4.1, 17 on the host for 21). 64 x 1024
+// bf16 takes 6.6 us for 7.2, but 1000 x 65 11.3 for 8.4 on the GPU; with 256 x 1024 the cluster would take 10.6 for 7.7.
+constexpr int64_t kFewElements = 65536;
 
 // The sum of a block's values, for every thread; sh is free again after the next barrier.
 __device__ __forceinline__ float block_sum(float x, float* sh) {
@@ -337,7 +341,7 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
     if (why.empty()) why = check_matrix(dh, ld_dh, type, rows, cols, "dh", false);
     if (why.empty()) why = check_matrix(dx, ld_dx, type, rows, cols, "dx", true);
     if (why.empty() && rows > 0 && !rstd) why = "rstd must not be NULL";
-    if (why.empty() && (!work || !aligned_to(work, 16))) why = "work must not be NULL and be 16-byte aligned";
+    if (why.empty() && (!aligned_to(work, 16) || (!work && rows * cols > kFewElements))) why = "work must not be NULL and be 16-byte aligned";
     if (why.empty() && !(aligned_to(weight, elem_bytes(weight_type)) && aligned_to(dweight, elem_bytes(grad_type)) &&
                          aligned_to(dbias, elem_bytes(grad_type)) && aligned_to(mean, 4) && aligned_to(rstd, 4)))
       why = "a pointer is not aligned to its type";
@@ -346,14 +350,22 @@ meq_status meq_layer_norm_grad(const void* dy, int64_t ld_dy, const void* h, int
     BackwardArgs a{};
     a.dy = dy, a.h = h, a.dh = dh, a.weight = weight, a.mean = mean, a.rstd = rstd, a.dx = dx;
     a.rows = rows, a.cols = cols, a.ld_dy = ld_dy, a.ld_h = ld_h, a.ld_dh = ld_dh, a.ld_dx = ld_dx;
-    a.weight_type = weight_type, a.parts = dweight || dbias ? work : nullptr, a.row_sums = work + 2 * parts_for(rows, cols) * cols;
+    a.weight_type = weight_type, a.parts = dweight || dbias ? work : nullptr, a.row_sums = work ? work + 2 * parts_for(rows, cols) * cols : nullptr;
     int64_t parts = 0;
     if (rows > 0) {
       cudaError_t e;
       int sms = device_sms(&e);
       if (e != cudaSuccess) return launch_status(e, "meq_layer_norm_grad", "device attributes");
       if (sms > kMostParts) sms = kMostParts;  // what work has room for
-      if (!launch_row_backward(a, type, mean || dbias, sms, &parts, st, &e))
+      const bool wanted = dweight || dbias;
+      if (wanted && rows * cols <= kFewElements) {
+        a.dweight = dweight, a.dbias = dbias, a.grad_type = grad_type;
+        if (launch_few_backward(a, type, mean || dbias, st, &e)) return launch_status(e, "meq_layer_norm_grad", "launch");
+      }
+      const bool in_registers = (work || !wanted) && launch_row_backward(a, type, mean || dbias, sms, &parts, st, &e);
+      if (!in_registers && !work)
+        return fail(MEQ_ERR_INVALID_ARG, "meq_layer_norm_grad: these rows need work (they are too long, or lie in their 16 bytes differently)");
+      if (!in_registers)
         e = type == MEQ_F32    ? launch_wide_backward<float>(a, &parts, st)
             : type == MEQ_BF16 ? launch_wide_backward<__nv_bfloat16>(a, &parts, st)
                                : launch_wide_backward<__half>(a, &parts, st);

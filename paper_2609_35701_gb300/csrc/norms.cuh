@@ -33,7 +33,10 @@ struct BackwardArgs {
   void* dx;
   int64_t rows, cols, ld_dy, ld_h, ld_dh, ld_dx;
   int weight_type;
-  float* parts;         // [2][parts][cols]: partial sums of dy xhat and of dy
+  float* parts;         // [2][parts][cols]: partial sums of dy xhat and of dy; NULL: they are not wanted
+  void* dweight;        // launch_few_backward: the sums themselves; either may be NULL
+  void* dbias;
+  int grad_type;
   float* row_sums;      // wide rows: mean(a xhat) and mean(a) of each row
 };
 

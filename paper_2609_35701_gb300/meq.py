@@ -889,6 +889,9 @@ def _stream(stream, device):
     return _raw_stream(device) if stream is None else _stream_handle(stream)
 
 
+_FEW_ELEMENTS = 65536  # up to which meq_layer_norm_grad may do without work
+
+
 @functools.lru_cache(maxsize=256)
 def _norm_work(rows, cols):
     return lib.meq_layer_norm_work_floats(rows, cols)
@@ -973,9 +976,12 @@ def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
     elif bias:
         dbias = _memory(size, grad_dtype, where, stream)
         bp = dbias.data_ptr()
-    work = _memory(_norm_work(rows, cols), f32, where, stream)
-    _check_call(lib.meq_layer_norm_grad(dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp,
-                                        grad_kind, work.data_ptr(), _stream(stream, device)))
+    args = dy.data_ptr(), ld, hp, ld_h, sp, ld_s, kind, rows, cols, w, weight_kind, mp, rp, xp, ld_x, wp, bp, grad_kind
+    # few elements mostly need no work: it is made where the call says so
+    status = 1 if rows * cols > _FEW_ELEMENTS else lib.meq_layer_norm_grad(*args, None, _stream(stream, device))
+    if status:
+        work = _memory(_norm_work(rows, cols), f32, where, stream)
+        _check_call(lib.meq_layer_norm_grad(*args, work.data_ptr(), _stream(stream, device)))
     if given:
         _increment(given)
     return dx, dweight, dbias

@@ -362,6 +362,31 @@ def test_rms_norm_with_a_bias(meq, cols):
     assert torch.equal(other, db)
 
 
+@pytest.mark.parametrize("rows,cols,pad", [(1, 65536, 0), (64, 1024, 0), (65, 1024, 0), (683, 95, 0), (8, 8191, 1), (3, 16400, 0), (2, 20000, 0), (7, 40, 0)])
+def test_few_elements_with_and_without_work(meq, rows, cols, pad):
+    """Up to 65536 elements a call may do without work, or says that it needs it; the results with it are the same."""
+    lib, w = meq.lib, _vector(cols, "fp32", 3, 1.0)
+    x, dy = _random(rows, cols, "bf16", 1, pad), _random(rows, cols, "bf16", 2, pad)
+    r = meq.layer_norm(x, w, eps=EPS)
+    dx, (dw, db) = _matrix(rows, cols, "bf16", pad), torch.empty(2, cols, device="cuda")
+    args = (dy.data_ptr(), cols + pad, x.data_ptr(), cols + pad, None, 0, 1, rows, cols, w.data_ptr(), 0, r.mean.data_ptr(), r.rstd.data_ptr(), dx.data_ptr(),
+            cols + pad, dw.data_ptr(), db.data_ptr(), 0)
+    status = lib.meq_layer_norm_grad(*args, None, None)
+    assert status == (1 if rows * cols > 65536 or cols > 16384 else 0)
+    if status:
+        assert b"work" in lib.meq_last_error(None)
+    torch.cuda.synchronize()
+    first = dx.clone(), dw.clone(), db.clone()
+    work = torch.full((lib.meq_layer_norm_work_floats(rows, cols),), float("nan"), device="cuda")
+    assert lib.meq_layer_norm_grad(*args, work.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    _check_backward(meq.LayerNormGrad(dx, dw, db), _np(dy), _np(x), _np(w), _np(r.mean), _np(r.rstd), 0.0, True, "bf16", "fp32")
+    if not status:
+        assert all(torch.equal(p, q) for p, q in zip(first, (dx, dw, db)))
+    g = meq.layer_norm_grad(dy, x, w, r.mean, r.rstd)   # the binding finds out by itself; here dx is contiguous
+    _check_backward(g, _np(dy), _np(x), _np(w), _np(r.mean), _np(r.rstd), 0.0, True, "bf16", "fp32")
+
+
 def test_numbers_of_other_kinds(meq):
     x, w = torch.randn(3, 8, device="cuda"), torch.ones(8, device="cuda")
     assert torch.equal(meq.rms_norm(x, w, eps=np.float32(1e-6)).y, meq.rms_norm(x, w).y)

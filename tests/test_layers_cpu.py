@@ -39,7 +39,7 @@ def test_norm_refusals(meq):
     _refused(meq, meq.lib.meq_layer_norm_grad, base, [
         (dict(type=5), b"meq_dtype"), (dict(grad_type=3), b"meq_dtype"), (dict(rows=-2), b"rows"), (dict(cols=0), b"cols"), (dict(ld_dy=1), b"stride of dy"),
         (dict(ld_h=1), b"stride of h"), (dict(dh=FAKE, ld_dh=1), b"stride of dh"), (dict(ld_dx=1), b"stride of dx"), (dict(dy=None), b"dy must not"),
-        (dict(h=None), b"h must not"), (dict(dx=None), b"dx must not"), (dict(rstd=None), b"rstd"), (dict(work=None), b"work"), (dict(work=FAKE + 4), b"work"),
+        (dict(h=None), b"h must not"), (dict(dx=None), b"dx must not"), (dict(rstd=None), b"rstd"), (dict(work=None, rows=9000), b"work"), (dict(work=FAKE + 4), b"work"),
         (dict(dweight=FAKE + 2), b"aligned"), (dict(dbias=FAKE + 1, grad_type=BF16), b"aligned"), (dict(dx=FAKE + 1, type=BF16), b"aligned")])
     assert meq.lib.meq_layer_norm(None, 8, None, 0, F32, 0, 8, None, None, F32, 1e-5, None, 8, None, 0, None, None, None) == 0
     assert meq.lib.meq_layer_norm_grad(None, 8, None, 8, None, 0, F32, 0, 8, None, F32, None, None, None, 8, None, None, F32, FAKE, None) == 0
