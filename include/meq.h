@@ -527,7 +527,8 @@ meq_status meq_preference_loss(const void* logits, int type, int64_t rows, int64
  * mean, rstd: device, rows floats. mean NULL selects RMS norm, in both calls.
  * In place: y may be x or the residual, h may be x or the residual (not what y
  *   is), dx may be dy, h or dh: the same pointer and row stride. Otherwise
- *   outputs must not overlap inputs or one another.
+ *   outputs must not overlap inputs or one another. y over x without a residual
+ *   leaves no h for the backward pass.
  * Sums and statistics are fp32, in fixed orders: results repeat bit for bit. A
  * row whose sum of squares is not finite in fp32 gives NaN. rows may be 0.
  * Nothing is allocated, and the calls may come from several threads. Limits:

@@ -916,7 +916,8 @@ def _norm(x, weight, bias, residual, eps, y, h, stream, centred):
     if residual is None:
         if h is not None:
             raise ValueError("h is written with a residual only")
-        h, hp, ld_h = x, None, 0
+        # y over x leaves nothing that the backward pass could read
+        h, hp, ld_h = None if yp == x.data_ptr() and rows else x, None, 0
     elif h is None:
         h, ld_h = _memory(shape, dtype, where, stream), cols
         hp = h.data_ptr()
@@ -939,7 +940,8 @@ def layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5, y=None, h=Non
     CUDA matrix, fp32, bf16 or fp16, one row per token; weight, bias: vectors of
     one of these types; y, h: tensors to write (y may be x or residual, h the other
     or x: the stream's in-place update), else new ones. h of the result is what was
-    normalised; mean and rstd are for the backward pass."""
+    normalised (None where y has taken the place of x without a residual: there is
+    no backward pass then); mean and rstd are for the backward pass."""
     return LayerNorm(*_norm(x, weight, bias, residual, eps, y, h, stream, True))
 
 
@@ -951,6 +953,8 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, y=None, h=None, stream=Non
 
 def _norm_grad(dy, h, weight, mean, rstd, dh, dx, dweight, dbias, bias, stream):
     kind, shape, ld, device = _first(dy, "dy")
+    if h is None:
+        raise ValueError("h must be given: a norm whose y took the place of its x has none")
     rows, cols = shape
     dtype, where, f32 = dy.dtype, dy.device, _f32
     hp, ld_h = _matrix(h, dtype, shape, device, "h")

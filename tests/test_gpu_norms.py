@@ -414,3 +414,30 @@ def test_refusals(meq):
             meq.layer_norm(x, w, eps=eps)
     with pytest.raises(meq.MeqError):
         meq.layer_norm(x, w, residual=x, y=wide[:, :8], h=wide[:, :8])
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_a_norm_over_its_input_leaves_no_h(meq, cols):
+    """y = x without a residual: what was normalised is gone, so there is none to take a gradient from."""
+    rows, w, b = 37, _vector(cols, "fp32", 1, 1.0), _vector(cols, "fp32", 2, 0.0)
+    x, res, dy = (_random(rows, cols, "bf16", s) for s in (3, 4, 5))
+    want, rms = meq.layer_norm(x, w, b), meq.rms_norm(x, w)
+    assert want.h is x and rms.h is x
+    for same in (lambda t: t, lambda t: t.view(rows, cols)):  # the same tensor, and another of the same memory
+        a = x.clone()
+        got = meq.layer_norm(a, w, b, y=same(a))
+        assert torch.equal(got.y, want.y) and got.h is None
+        with pytest.raises(ValueError, match="h must be given"):
+            meq.layer_norm_grad(dy, got.h, w, got.mean, got.rstd)
+        a = x.clone()
+        got = meq.rms_norm(a, w, y=same(a))
+        assert torch.equal(got.y, rms.y) and got.h is None
+        with pytest.raises(ValueError, match="h must be given"):
+            meq.rms_norm_grad(dy, got.h, w, got.rstd)
+    assert meq.layer_norm(x, w, b, y=dy).h is x
+    # with a residual the sum is kept, whatever y takes the place of
+    kept = meq.layer_norm(x, w, b, residual=res).h
+    a, c = x.clone(), res.clone()
+    assert torch.equal(meq.layer_norm(a, w, b, residual=res, y=a).h, kept) and torch.equal(meq.layer_norm(x, w, b, residual=c, y=c).h, kept)
+    none = torch.empty(0, cols, dtype=torch.bfloat16, device="cuda")  # nothing is overwritten
+    assert meq.layer_norm(none, w, b, y=none).h is none
