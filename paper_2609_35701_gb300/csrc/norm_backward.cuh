@@ -160,9 +160,9 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1)
     row_sum<(kLayer ? 2 : 1), (kPieces > 1)>(c, s, p, ex, turn);
     if (!in) continue;
     T* dx = p.at(a.dx, row, a.ld_dx);
-    // dx = rstd a - rstd mean(a) - (h - mu) rstd^2 mean(a xhat)
-    // (rstd last: its square overflows where eps is tiny and the row constant)
-    const float s1 = -now.y * (now.y * (c[0] * per)), s2 = kLayer && a.mean ? -now.y * (c[kLayer ? 1 : 0] * per) : 0.f;
+    // dx = rstd (a - mean(a) - xhat mean(a xhat)), rstd last: with a tiny eps its square overflows, and so does its product
+    // with a mean that xhat would have made small.
+    const float s1 = -(c[0] * per), s2 = kLayer && a.mean ? -(c[kLayer ? 1 : 0] * per) : 0.f;
     const float2 m1 = make_float2(s1, s1), m2 = make_float2(s2, s2);
     // dy and h once more from shared memory: kept in registers they would leave no room for the sums.
 #pragma unroll
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(threads_of<Elem<T>::N * kPieces>(), 1)
 #pragma unroll
       for (int e = 0; e < W; ++e) {
         if (kLayer) x[e] = add2(x[e], mu);
-        x[e] = kLayer ? fma2(x[e], m1, m2) : mul2(x[e], m1);
-        d[e] = fma2(mul2(d[e], v[e]), rstd, x[e]);
+        d[e] = kLayer ? fma2(d[e], v[e], m2) : mul2(d[e], v[e]);
+        d[e] = mul2(fma2(mul2(x[e], rstd), m1, d[e]), rstd);
       }
       if (a.dh) {
         p.read(dh, k, in, x);

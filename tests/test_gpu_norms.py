@@ -441,3 +441,18 @@ def test_a_norm_over_its_input_leaves_no_h(meq, cols):
     assert torch.equal(meq.layer_norm(a, w, b, residual=res, y=a).h, kept) and torch.equal(meq.layer_norm(x, w, b, residual=c, y=c).h, kept)
     none = torch.empty(0, cols, dtype=torch.bfloat16, device="cuda")  # nothing is overwritten
     assert meq.layer_norm(none, w, b, y=none).h is none
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(5, 40), (5, 96), (4, 1025), (3, 4096), (700, 128), (300, 1025), (300, 4096), (40, 9000), (5, 17000)])
+def test_tiny_rows_that_vary(meq, kind, dtype, rows, cols):
+    """rstd near 3e20 and gradients as large: finite whatever the rows' length, though rstd's square is not."""
+    x = _random(rows, cols, dtype, 1, spread=3e-21)
+    dy, dh, w = _random(rows, cols, dtype, 2), _random(rows, cols, dtype, 3), _vector(cols, "fp32", 4, 1.0)
+    r = meq.layer_norm(x, w, eps=1e-44) if kind == "layer" else meq.rms_norm(x, w, eps=1e-44)
+    assert bool((r.rstd > 1e19).all()) and bool(r.rstd.isfinite().all())
+    for more in (None, dh):
+        g = _backward(meq, kind, dy, x, w, r, dh=more)
+        _check_backward(g, _np(dy), _np(x), _np(w), _np(r.mean) if kind == "layer" else None, _np(r.rstd), 0.0 if more is None else _np(dh),
+                        kind == "layer", dtype, "fp32")
