@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libmeq.so")
 SOURCES = ["ns_gemm.cu", "elementwise.cu", "meq_api.cu", "noalloc.cu", "adamw.cu", "losses.cu", "loss_stream.cu", "norms.cu",
            "norm_forward.cu", "norm_backward.cu", "norm_few.cu", "embedding.cu"]
 HEADERS = ["meq_internal.cuh", "meq_call.cuh", "meq_elem.cuh", "meq_elementwise.cuh", "meq_stats.cuh", "meq_mbar.cuh", "loss_rows.cuh",
-           "norms.cuh", "norm_rows.cuh", "norm_backward.cuh"]
+           "norms.cuh", "norm_rows.cuh", "norm_backward.cuh", "embedding_sort.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE]
 

@@ -22,6 +22,7 @@
 #include <mutex>
 #include <string>
 
+#include "embedding_sort.cuh"
 #include "meq_call.cuh"
 #include "meq_elem.cuh"
 #include "meq_elementwise.cuh"
@@ -383,7 +384,6 @@ struct RunArgs {
 };
 constexpr int kRunThreads = 256, kRunWarps = kRunThreads / 32;
 constexpr int kShortParts = 32;
-constexpr int kFewTokens = 256;
 constexpr uint32_t kFillBytes = 32768, kMostFillRows = 2048;  // of a block
 
 // kN sums to consecutive elements of a row of the gradient; kN > 1: 16 bytes of floats, or as many elements of 16 bits, at a time.
@@ -841,9 +841,6 @@ cudaError_t launch_lookup(const LookupArgs& a, int out_type, cudaStream_t st) {
   return launch_lookup<Tin, __half>(a, st);
 }
 
-// Tokens above which 16 blocks sort, not 8, us: 8192 16.7 with 8, 16.1 with 16, 16384 18.9 and 18.1, 32768 22.7 and 20.5,
-// 65536 32.6 and 25.3, 131072 74 and 36 (launch and event 6 of them); 16 leave fewer SMs that can hold a cluster to zero rows.
-constexpr int64_t kWideSort = 16384;
 // Rows are zeroed beside the sort for as long as it takes, at the rate here; the others beside the sums. At 0, 1.5, 3, 4.5
 // and 6 TB/s, us: 65536 tokens into 151936 x 4096 bf16 290, 286, 282, 282, 284, 8192 into 32000 x 768 fp32 37, 35, 33, 32, 31.
 constexpr double kSortUs = 9.0, kSortUsPerToken = 0.0002, kFillBytesPerUs = 4.5e6;
@@ -873,11 +870,11 @@ Work work_for(int64_t n, int64_t vocab, int64_t cols) {
   return w;
 }
 
-// Clusters of 8 or 16 blocks of the sort that the device holds at a time, asked once per device.
+// Clusters of 8 or 16 blocks of the sort that the device holds at a time (0: none), asked once per device.
 cudaError_t prepared_sort(int ctas, int* clusters) {
   constexpr int kMaxDevices = 64;
   static std::mutex mu;
-  static int known[kMaxDevices][2] = {};
+  static int known[kMaxDevices][2] = {};  // and one more, 0: not asked yet
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -886,7 +883,7 @@ cudaError_t prepared_sort(int ctas, int* clusters) {
   int& most = known[dev][ctas == 16];
   if (most == 0) {
     e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(sizeof(SortShared)));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && ctas == 16) e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(ctas));
@@ -901,10 +898,9 @@ cudaError_t prepared_sort(int ctas, int* clusters) {
     int n = 0;
     e = cudaOccupancyMaxActiveClusters(&n, sort_kernel, &cfg);
     if (e != cudaSuccess) return e;
-    if (n < 1) return cudaErrorInvalidConfiguration;
-    most = n;
+    most = 1 + (n > 0 ? n : 0);
   }
-  *clusters = most;
+  *clusters = most - 1;
   return cudaSuccess;
 }
 
@@ -985,11 +981,17 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       why = "a pointer is not aligned to its type";
     if (!why.empty()) return fail(MEQ_ERR_INVALID_ARG, "meq_embedding_grad: " + why);
     if (n == 0 && accumulate) return MEQ_OK;
-    cudaError_t e;
-    const int sms = device_sms(&e);
-    const int ctas = n > kWideSort ? 16 : 8;
-    int clusters = 0;
-    if (e == cudaSuccess) e = prepared_sort(ctas, &clusters);
+    cudaError_t e = cudaSuccess;
+    int clusters = 0, sms = 0;
+    auto clusters_of = [&](int blocks) {
+      if (e != cudaSuccess) cudaGetLastError();  // 16 blocks are not to be had, which 8 make good
+      int held = 0;
+      e = prepared_sort(blocks, &held);
+      return held;
+    };
+    const int ctas = sort_blocks(n, clusters_of, &clusters);
+    if (ctas > 0 && e == cudaSuccess && clusters < 1) e = cudaErrorInvalidConfiguration;
+    if (ctas > 0 && e == cudaSuccess) sms = device_sms(&e);
     if (e != cudaSuccess) return launch_status(e, "meq_embedding_grad", "device attributes");
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Work w = work_for(n, vocab, cols);
@@ -1001,7 +1003,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
       a.fill_rows = static_cast<uint32_t>(a.row_bytes >= kFillBytes ? 1 : kFillBytes / a.row_bytes);
       if (a.fill_rows > kMostFillRows) a.fill_rows = kMostFillRows;
     }
-    if (n > kFewTokens) {
+    if (ctas > 0) {
       SortArgs s{};
       s.tokens = tokens, s.n = a.n, s.vocab = a.vocab;
       int bits = 1;  // of the largest key, vocab
@@ -1036,7 +1038,7 @@ meq_status meq_embedding_grad(const void* grad, int type, int64_t n, int64_t col
     const int64_t rest = vocab - static_cast<int64_t>(a.first_word) * 32;
     if (!accumulate && rest > 0) a.fills = static_cast<uint32_t>((rest + a.fill_rows - 1) / a.fill_rows);
     e = type == MEQ_F32 ? launch_runs_of<float>(a, st) : type == MEQ_BF16 ? launch_runs_of<__nv_bfloat16>(a, st) : launch_runs_of<__half>(a, st);
-    if (e != cudaSuccess || n <= kFewTokens) return launch_status(e, "meq_embedding_grad", "sum launch");
+    if (e != cudaSuccess || ctas == 0) return launch_status(e, "meq_embedding_grad", "sum launch");
     const int64_t most = w.chunks * ((cols + 8 * kJoinCols - 1) / (8 * kJoinCols)), blocks = 2 * static_cast<int64_t>(sms);
     e = launch_pdl(joins_kernel, dim3(static_cast<unsigned>(most < blocks ? most : blocks)), dim3(kRunThreads), 0, st, 1, a);
     return launch_status(e, "meq_embedding_grad", "join launch");

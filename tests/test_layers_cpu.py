@@ -1,4 +1,7 @@
 """Norms and embedding on a host without a GPU: sizes, and refusals that come before any CUDA call."""
+import os
+import subprocess
+
 import pytest
 import torch
 
@@ -71,3 +74,31 @@ def test_binding_refuses_host_tensors(meq):
                  lambda: meq.embedding(t, x), lambda: meq.embedding_grad(x, t, x)):
         with pytest.raises(ValueError):
             call()
+
+
+SORT_BLOCKS = """
+#include <cstdio>
+#include "embedding_sort.cuh"
+int main() {
+  const long long tokens[] = {0, 256, 257, 16384, 16385, 1 << 27};
+  const int held[][2] = {{14, 7}, {1, 1}, {3, 0}, {0, 0}};  // clusters of 8 and of 16 blocks that a device holds
+  for (const auto& device : held)
+    for (long long n : tokens) {
+      int asked = 0, clusters = -1;
+      const int blocks = meq::sort_blocks(n, [&](int b) { ++asked; return device[b == 16]; }, &clusters);
+      std::printf("%d,%d,%d ", blocks, clusters, asked);
+    }
+}
+"""
+
+
+def test_the_sorts_cluster_is_one_that_the_device_holds(tmp_path):
+    """16 blocks sort many tokens where they can be had, else 8; few tokens ask for no cluster."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_35701_gb300", "csrc")
+    (tmp_path / "blocks.cpp").write_text(SORT_BLOCKS)
+    exe = str(tmp_path / "blocks")
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(tmp_path / "blocks.cpp"), "-o", exe], check=True)
+    none = ["0,0,0"] * 2
+    want = (none + ["8,14,1"] * 2 + ["16,7,1"] * 2) + (none + ["8,1,1"] * 2 + ["16,1,1"] * 2) + (none + ["8,3,1"] * 2 + ["8,3,2"] * 2)
+    want += none + ["8,0,1"] * 2 + ["8,0,2"] * 2
+    assert subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split() == want
