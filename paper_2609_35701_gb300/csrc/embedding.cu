@@ -442,7 +442,6 @@ __device__ __forceinline__ void put(const RunArgs& a, int64_t i, const float (&s
 template <typename T, int kStep, int kPieces>
 struct Slice {
   static constexpr int kCols = 32 * kStep * kPieces;
-  static constexpr int kAhead = kStep == 1 ? 4 : 8 / kPieces;  // rows loaded ahead
   int j0, cols;
   float acc[kPieces][kStep];
   __device__ __forceinline__ Slice(int slice, int lane, int cols_) : j0(slice * kCols + lane * kStep), cols(cols_) { clear(); }
@@ -457,14 +456,12 @@ struct Slice {
     uint4 q[kStep > 1 ? kPieces : 1];
     typename Elem<T>::Bits s[kStep > 1 ? 1 : kPieces];
   };
-  // Unconditional, so that the loads of several rows are on their way together: columns beyond the row read its start.
+  // Single elements (kStep 1), kAhead rows of them at a time. Unconditional, so that the loads of several rows are on their
+  // way together: columns beyond the row read its start.
+  static constexpr int kAhead = 4;
   __device__ __forceinline__ void load(Row& r, const T* row) const {
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-      const int j = col(k) < cols ? col(k) : 0;
-      if constexpr (kStep == 1) r.s[k] = reinterpret_cast<const typename Elem<T>::Bits*>(row)[j];
-      else r.q[k] = __ldcs(reinterpret_cast<const uint4*>(row + j));
-    }
+    for (int k = 0; k < kPieces; ++k) r.s[k] = reinterpret_cast<const typename Elem<T>::Bits*>(row)[col(k) < cols ? col(k) : 0];
   }
   __device__ __forceinline__ void add(const Row& r) {
 #pragma unroll
@@ -561,7 +558,6 @@ __device__ __forceinline__ void fill_rows(const RunArgs& a, int64_t block, F mar
 template <typename T, int kStep, int kPieces>
 __global__ void __launch_bounds__(kRunThreads, kStep > 1 ? 4 : 3) runs_kernel(const __grid_constant__ RunArgs a) {
   using S = Slice<T, kStep, kPieces>;
-  constexpr int kAhead = S::kAhead;
   pdl_allow_dependents();
   pdl_wait_predecessor();
   int64_t block;
@@ -649,6 +645,7 @@ __global__ void __launch_bounds__(kRunThreads, kStep > 1 ? 4 : 3) runs_kernel(co
       end_run(e);
     }
   } else {
+    constexpr int kAhead = S::kAhead;
 #pragma unroll 1
     for (int e0 = begin; e0 < end; e0 += kAhead) {
       typename S::Row r[kAhead];

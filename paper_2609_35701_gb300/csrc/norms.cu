@@ -72,7 +72,7 @@ template <typename T, int kStep>
 __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const ForwardArgs a) {
   pdl_allow_dependents();
   pdl_wait_predecessor();
-  __shared__ float sh[3][kWideWarps];
+  __shared__ float sh[2][kWideWarps];
   const int64_t first = threadIdx.x * kStep, step = kWideThreads * kStep;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
