@@ -281,3 +281,33 @@ def test_refusals(meq):
         with pytest.raises(ValueError):
             call()
             raise AssertionError(i)
+
+
+def test_results_that_a_32_bit_offset_does_not_reach(meq):
+    """Rows of the result 1.2e9 elements apart, of the lookup and of the table's gradient, written and added to."""
+    apart = 1200000000
+    far = torch.empty(2 * apart + 2000, dtype=torch.bfloat16, device="cuda")
+    for n, cols in ((5, 96), (300, 1025)):
+        tokens = torch.arange(n, device="cuda") % 4                # 3 is padding
+        tokens[tokens == 3] = -1
+        grad = _matrix(n, cols, "bf16", seed=1)
+        out = far.as_strided((3, cols), (apart, 1))
+        before = _matrix(3, cols, "bf16", seed=2)
+        for held in (None, before):
+            if held is not None:
+                out.copy_(held)
+            meq.embedding_grad(grad, tokens, out, accumulate=held is not None)
+            _check_grad(out, grad, tokens, 1.0, held, "bf16")
+        table = _matrix(4, cols, "bf16", seed=3)
+        t = torch.tensor([3, 0, 2], device="cuda")
+        assert torch.equal(meq.embedding(t, table, out=out), table[t])
+
+
+def test_one_token_in_up_to_256(meq):
+    """One warp adds up its rows in turn: each is added at most n times."""
+    for n in (97, 256):
+        grad, tokens = _matrix(n, 264, "fp32", seed=n), torch.full((n,), 5, device="cuda")
+        out = meq.embedding_grad(grad, tokens, torch.empty(9, 264, device="cuda"))
+        sizes, want = grad.double().abs().sum(0), grad.double().sum(0)
+        assert bool(((out[5].double() - want).abs() <= (n + 1) * U * sizes + U * want.abs()).all())
+        assert not out[[0, 1, 2, 3, 4, 6, 7, 8]].any()

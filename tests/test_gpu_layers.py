@@ -173,3 +173,56 @@ def test_other_streams_memory(meq):
         side.synchronize()
         assert torch.equal(y, want) and torch.equal(z.y, want)
         del y, z
+
+
+def test_calls_from_several_threads(meq):
+    """Four host threads, a stream each, norms and embedding of every path and refused calls among them: the results are
+    those of one thread, and a refusal's text is that of the thread's own call."""
+    import threading
+
+    shapes = [(200, 96, torch.float32), (900, 1025, torch.bfloat16), (20000, 768, torch.bfloat16), (300, 17000, torch.float16)]
+    data, want = [], []
+
+    def calls(i, stream=None):
+        x, res, w, t, table, out = data[i]
+        r = meq.layer_norm(x, w, w, residual=res, stream=stream)
+        g = meq.layer_norm_grad(res, r.h, w, r.mean, r.rstd, dh=x, stream=stream)
+        q = meq.rms_norm(x, w, stream=stream)
+        p = meq.rms_norm_grad(res, x, w, q.rstd, stream=stream)
+        e = meq.embedding(t, table, scale=2.0, dtype=x.dtype, stream=stream)
+        meq.embedding_grad(g.dx, t, out, stream=stream)
+        return list(r) + list(g) + [q.y, q.rstd] + list(p) + [e, out]
+
+    for i, (rows, cols, dtype) in enumerate(shapes):
+        g = torch.Generator().manual_seed(i)
+        x, res = (torch.randn(rows, cols, generator=g).cuda().to(dtype) for _ in range(2))
+        w, t = (1 + 0.1 * torch.randn(cols, generator=g)).cuda(), torch.randint(-5, 300, (rows,), generator=g).cuda()
+        data.append((x, res, w, t, torch.randn(300, cols, generator=g).cuda(), torch.empty(300, cols, device="cuda")))
+        want.append([v.clone() for v in calls(i)])
+    torch.cuda.synchronize()
+    failures, start = [], threading.Barrier(len(shapes))
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            start.wait()
+            for _ in range(15):
+                got = calls(i, stream)
+                x, w = data[i][0], data[i][2]
+                if i % 2:
+                    with pytest.raises(meq.MeqError, match="eps"):
+                        meq.rms_norm(x, w, eps=-1.0, stream=stream)
+                else:
+                    with pytest.raises(meq.MeqError, match="the same"):
+                        meq.rms_norm(x, w, residual=x, y=data[i][1], h=data[i][1], stream=stream)
+                stream.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want[i]))
+        except BaseException as e:  # noqa: BLE001 - reported by the main thread
+            failures.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(shapes))]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not failures, failures

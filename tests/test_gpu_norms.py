@@ -456,3 +456,63 @@ def test_tiny_rows_that_vary(meq, kind, dtype, rows, cols):
         g = _backward(meq, kind, dy, x, w, r, dh=more)
         _check_backward(g, _np(dy), _np(x), _np(w), _np(r.mean) if kind == "layer" else None, _np(r.rstd), 0.0 if more is None else _np(dh),
                         kind == "layer", dtype, "fp32")
+
+
+# The longest aligned rows that a group of warps holds, and the next, per type: backward with dh, layer norm's and RMS norm's.
+LIMITS = [("bf16", 13312), ("bf16", 13320), ("fp16", 14336), ("bf16", 16384), ("bf16", 16392), ("bf16", 16377), ("bf16", 16378),
+          ("fp32", 9216), ("fp32", 9220), ("fp32", 9213), ("fp32", 9214), ("fp32", 10240), ("fp32", 10244), ("fp32", 10237), ("fp32", 10238)]
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("rows", [3, 40])
+@pytest.mark.parametrize("dtype,cols", LIMITS)
+def test_either_side_of_the_longest_rows_in_registers(meq, kind, rows, dtype, cols):
+    x, res, dy, dh = (_random(rows, cols, dtype, s) for s in (1, 2, 3, 4))
+    w, b = _vector(cols, "fp32", 5, 1.0), _vector(cols, "fp32", 6, 0.0)
+    r = _forward(meq, kind, x, w, b if kind == "layer" else None, residual=res)
+    _check_forward(r, _np(r.h), _np(w), _np(b) if kind == "layer" else 0.0, kind == "layer", dtype)
+    for more in (None, dh):
+        g = _backward(meq, kind, dy, r.h, w, r, dh=more)
+        _check_backward(g, _np(dy), _np(r.h), _np(w), _np(r.mean) if kind == "layer" else None, _np(r.rstd), 0.0 if more is None else _np(dh),
+                        kind == "layer", dtype, "fp32")
+
+
+@pytest.mark.parametrize("weight_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cols", [40, 768, 1025, 4096, 17000])
+def test_weights_that_start_anywhere(meq, cols, dtype, weight_type):
+    """Weight, bias and their gradients as parts of one vector, each an element further: the bits of aligned ones."""
+    rows, held = 37, torch.zeros(4 * cols + 16, dtype=DT[weight_type], device="cuda")
+    x, dy = _random(rows, cols, dtype, 1), _random(rows, cols, dtype, 2)
+    w, b = _vector(cols, weight_type, 3, 1.0), _vector(cols, weight_type, 4, 0.0)
+    w1, b1, dw1, db1 = (held[i * (cols + 1) + 1:][:cols] for i in range(4))
+    w1.copy_(w)
+    b1.copy_(b)
+    want, got = meq.layer_norm(x, w, b), meq.layer_norm(x, w1, b1)
+    assert torch.equal(got.y, want.y) and torch.equal(got.mean, want.mean) and torch.equal(got.rstd, want.rstd)
+    want, got = (meq.layer_norm_grad(dy, x, a, got.mean, got.rstd, dweight=p, dbias=q) for a, p, q in ((w, None, None), (w1, dw1, db1)))
+    assert got.dweight is dw1 and all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_rows_that_a_32_bit_offset_does_not_reach(meq):
+    """Three rows 1.2e9 elements apart, read and written in buffers of their own."""
+    rows, apart = 3, 1200000000
+
+    def far():
+        return torch.empty(2 * apart + 20000, dtype=torch.bfloat16, device="cuda")
+
+    buffers = [far() for _ in range(4)]
+    for cols in (96, 1025, 4096, 17000):
+        def view(t, like=None):
+            v = t.as_strided((rows, cols), (apart, 1))
+            return v if like is None else v.copy_(like)
+
+        x, res, dy = (_random(rows, cols, "bf16", s) for s in (1, 2, 3))
+        w, b = _vector(cols, "fp32", 4, 1.0), _vector(cols, "fp32", 5, 0.0)
+        want = meq.layer_norm(x, w, b, residual=res)
+        held = view(buffers[1], res)
+        got = meq.layer_norm(view(buffers[0], x), w, b, residual=held, y=view(buffers[2]), h=view(buffers[3]))
+        assert torch.equal(got.h, want.h)
+        _check_forward(got, _np(got.h), _np(w), _np(b), True, "bf16")
+        g = meq.layer_norm_grad(view(buffers[0], dy), got.h, w, want.mean, want.rstd, dh=held, dx=view(buffers[2]))
+        _check_backward(g, _np(dy), _np(want.h), _np(w), _np(want.mean), _np(want.rstd), _np(res), True, "bf16", "fp32")
