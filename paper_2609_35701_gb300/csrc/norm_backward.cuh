@@ -4,11 +4,14 @@
 // row; then the block's groups are added up and leave one partial sum per column.
 //
 // Bound by HBM where rows are long and many, us (at the copy rate): RMS norm
-// 32768 x 4096 bf16 with dh 157 (161). The mean and the bias take 680 instructions
-// for 480 per warp and row of 1024 columns: layer norm 16384 x 4096 77 (60), 16384
-// x 8192 169 (121), where two groups of eight warps share an SM. Small ones by the
-// launch, the first load, the groups' sums and the second launch: 8192 x 1024 17
-// (7.5), of which 5 come after the last row.
+// 32768 x 4096 bf16 with dh 157 (161). Layer norms of long rows by latency: of 32
+// elements a thread an SM holds 16 warps, which issue in 0.53 of its slots (670
+// instructions per warp and row of 1024 columns; RMS norm with dh 540, 0.39) and
+// else wait for loads and for their group's barriers: 16384 x 4096 77 (60), 16384 x
+// 8192 161 (121), where an SM has two groups of eight warps and rings of two rows.
+// Rows off 16 bytes alike: 16384 x 2047 67 (30). Small ones by the launch, the first
+// load, the groups' sums and the second launch: 8192 x 1024 17.5 (7.5), of which 5
+// come after the last row.
 //
 // Few rows (kFew): one cluster of at most eight blocks, which reads the partial
 // sums in its shared memory and writes the sums themselves, without a second
@@ -22,8 +25,8 @@ namespace norm {
 namespace {
 
 // The weights' place: with two sums over rows per element, 32 elements of a thread leave no registers for them (as
-// compiled with them, 92 bytes per thread were spilled and 16384 x 8192 bf16 took 226 us; 169 with them in shared
-// memory). Rows that start at different places would need copies at each offset: theirs stay in registers.
+// compiled with them, 92 bytes per thread were spilled and 16384 x 8192 bf16 took 226 us; with them in shared memory 169,
+// now 161). Rows that start at different places would need copies at each offset: theirs stay in registers.
 template <int kElements, bool kOffset, bool kLayer>
 constexpr bool kWeightsShared = kElements > kMostHeld && kLayer && !kOffset;
 

@@ -3,9 +3,11 @@
 //
 // Bound by HBM where rows are long and many, us (at the copy rate): RMS norm
 // 32768 x 4096 bf16 with a residual 172 (161), layer norm 8192 x 2048 fp32 22.7
-// (20.1), 16384 x 2048 bf16 24 (20). Else by instructions, some 300 per warp and
-// row beside 45 per piece: 16384 x 2047, whose rows take three warps instead of
-// two, 39 (20); 6001 x 1025 with a residual 17 (7.4).
+// (20.1), 16384 x 2048 bf16 24 (20). Rows that start elsewhere in their 16 bytes
+// by latency: 24 elements, weights and biases in a thread's registers leave an SM
+// 15 or 16 warps, which issue in half of its slots (0.51) and else wait, each for
+// its own last result or for shared memory: 16384 x 2047 40 (20), 6001 x 1025 with
+// a residual 17 (7.4). A warp and row take some 300 instructions, and 45 a piece.
 #include "norm_rows.cuh"
 
 namespace meq {

@@ -16,7 +16,7 @@
 // pieces are cut at 16-byte boundaries once for all rows. Only a row's first and
 // last piece may be a part, which is stored element by element. (Pieces cut from
 // the row's start, shifted into place on the way in and out, took 2 to 3 times the
-// time: 16384 x 2047 bf16 forward 52 us, 39 so; backward 151 and 73.)
+// time: 16384 x 2047 bf16 forward 52 us, 40 so; backward 151 and 67.)
 #pragma once
 
 #include "meq_call.cuh"

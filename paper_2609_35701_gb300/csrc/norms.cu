@@ -67,7 +67,9 @@ __device__ __forceinline__ void store(T* p, int64_t j, const float (&x)[kStep]) 
 }
 
 // Rows that no group of warps holds: a block per row, which it reads again for each step (from L2, but for very long
-// ones). 2000 x 16384 fp32 84 us (39 at the copy rate), its backward pass, which reads dy and h twice, 119 (59).
+// ones). 2000 x 16384 fp32 84 us (39 at the copy rate), its backward pass, which reads dy and h twice, 126 (59). Matrices
+// whose rows lie in their 16 bytes differently come here too, an element per lane and load: 16384 x 2047 bf16 into rows of
+// 2048 125 us (40 into rows of 2047; 20 at the copy rate), backward 231 (67; 30).
 template <typename T, int kStep>
 __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const ForwardArgs a) {
   pdl_allow_dependents();
